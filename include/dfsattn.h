@@ -4,7 +4,9 @@
  * The library runs the sparse 3D self-attention of a video diffusion transformer as the
  * paper's Algorithm 1 states it: a 3D Hilbert-curve token reorder, hierarchical block
  * scoring, top-k / adaptive block-mask selection, block-sparse attention over the
- * reordered sequence, and the inverse reorder.
+ * reordered sequence, and the inverse reorder.  In front of it stand the norms and position
+ * rotation of queries and keys, beside it attention over a window and a few first keys, both
+ * with their backward passes.
  *
  * Conventions shared by every entry point
  *   - `g` points to HOST memory.  Every other pointer is DEVICE memory owned by the caller;
@@ -287,6 +289,103 @@ int dfs_recall(const dfs_geom* g, const float* lse_sparse, const float* lse_dens
  */
 int dfs_schedule(int32_t total_steps, int32_t t, int32_t delta, double cached_keep, int32_t* dense, int32_t* refresh,
                  double* sparsity);
+
+/*
+ * A tensor [batch, heads, rows, d] wherever it lies: the address of its first element (device memory) and how many elements it is
+ * from one entry, head and row to the next.  The d channels of a row are adjacent; rows start on 16-byte boundaries, so `data` must
+ * be 16-byte aligned and the stride of every axis with more than one entry a multiple of 16 bytes, and not negative.  A stride of
+ * zero repeats an input.  An output's rows must not overlap one another (DFS_EINVAL) nor, unless an entry point says so, an input's.
+ * Structs are HOST memory.  A tensor without elements may have data NULL.
+ */
+typedef struct {
+  void* data;
+  int64_t batch, head, row;
+} dfs_view;
+
+/* Queries and keys of every head in front of attention: their norm and the rotation by position. */
+typedef struct {
+  int32_t batch, tokens;     /* sequences and tokens of each; either may be 0 */
+  int32_t heads, heads_kv;   /* query heads; key and value heads; at most 65 535 each */
+  int32_t d;                 /* head dimension: 64 or 128 */
+  int32_t interleaved;       /* 1: channels 2i and 2i + 1 of an axis's share turn together; 0: i and i + half the share */
+  int32_t axes;              /* 1 to 3 numbers a position has */
+  int32_t rot[3];            /* channels that each axis turns, from channel 0 on, axis by axis; the rest are not turned.  Even
+                                (interleaved) or multiples of 16, positive up to `axes`, together at most d */
+  double theta;              /* pair i of an axis of n channels turns by position * theta^(-2i/n); > 0 */
+  float eps;                 /* of the norm; >= 0 */
+} dfs_qk_geom;
+
+/*
+ * For every row x of q and k: y = x / sqrt(mean(x^2) + eps) * w, then each pair (a, b) of y turned by its angle t,
+ * (a cos t - b sin t, a sin t + b cos t).  Norm and rotation are fp32 and rounded once; angles are reduced in fp64, so any int32
+ * position is as good as a small one.  A position of zeros turns nothing (text tokens).  Rows of v are copied.
+ *   q [batch, heads, tokens, d], k, v [batch, heads_kv, tokens, d] in, of `dtype` (DFS_F32, DFS_BF16); v may be NULL
+ *   positions  int32, tokens x axes numbers, row by row, `pos_batch` numbers from one sequence to the next (0: all share them)
+ *   w_q, w_k   [d] fp32 in, or NULL (ones)
+ *   q_out, k_out, v_out  out, v_out NULL like v.  Without kv_start each may be its own input, with the same strides.
+ *   kv_start   NULL, or [batch] int32: token i of sequence b goes to row kv_start[b] + i of k_out and v_out, which have kv_rows rows
+ *              (a cache); a row outside [0, kv_rows) is dropped, all other rows are left as they are.  Without it kv_rows is not read.
+ * A row of zeros with eps 0 gives NaN.
+ */
+int dfs_qk_norm_rope(const dfs_qk_geom* g, int dtype, const dfs_view* q, const dfs_view* k, const dfs_view* v, const int32_t* positions,
+                     int64_t pos_batch, const float* w_q, const float* w_k, const dfs_view* q_out, const dfs_view* k_out,
+                     const dfs_view* v_out, const int32_t* kv_start, int32_t kv_rows, void* stream);
+
+/*
+ * Its backward pass, from the inputs of the forward call and the gradients of its outputs (all [batch, heads or heads_kv, tokens, d]):
+ * with g the gradient turned back, n = x / sqrt(mean(x^2) + eps) and gw = g * w,
+ *   dx = (gw - n mean(gw n)) / sqrt(mean(x^2) + eps),   dw = sum of g n over batch, heads and tokens.
+ * dv is a copy of dv_out (both NULL: nothing).  dq, dk, dv may each be the gradient they come from, with the same strides.
+ *   dw_q, dw_k [d] fp32 out, each may be NULL.  Sums in fp32 in an order that follows from the sizes alone: same call, same bits.
+ * ws: dfs_qk_workspace_bytes() if dw_q or dw_k is given, else none.
+ */
+int dfs_qk_norm_rope_bwd(const dfs_qk_geom* g, int dtype, const dfs_view* q, const dfs_view* k, const int32_t* positions, int64_t pos_batch,
+                         const float* w_q, const float* w_k, const dfs_view* dq_out, const dfs_view* dk_out, const dfs_view* dv_out,
+                         const dfs_view* dq, const dfs_view* dk, const dfs_view* dv, float* dw_q, float* dw_k, void* ws, size_t ws_bytes,
+                         void* stream);
+
+/* Bytes of scratch of dfs_qk_norm_rope_bwd (0 if the geometry is invalid).  Host only. */
+size_t dfs_qk_workspace_bytes(const dfs_qk_geom* g);
+
+/* Attention over the keys around a query's position and a few first ones. */
+typedef struct {
+  int32_t batch, heads, heads_kv, d;   /* heads a multiple of heads_kv: query heads g*j .. g*j + g - 1 share key head j; d 64 or 128 */
+  int32_t n_q, n_k;                    /* rows of the query and of the key tensors, of every sequence; at most 2^28, either may be 0 */
+  int32_t left, right;                 /* how far a query sees back and ahead; negative: without limit */
+  int32_t sinks;                       /* the first keys that every query sees which may see so far ahead; 0 if none */
+} dfs_window;
+
+/*
+ * Row i of a sequence with q_len query rows and k_len keys stands at position p = k_len - q_len + i (its last query is at its last
+ * key) and sees key j if j < k_len, j <= p + right, and j >= p - left or j < sinks:
+ *   o = sum_j softmax_j(scale <q, k_j>) v_j,   lse = ln sum_j exp(scale <q, k_j>).
+ * A row that sees nothing has o = 0 and lse = -inf.  bf16: matrix products with fp32 sums, softmax in fp32, its weights rounded to
+ * bf16 for the product with v; f32: fp32 throughout.
+ *   q [batch, heads, n_q, d], k, v [batch, heads_kv, n_k, d] in, o like q out
+ *   q_len, k_len  NULL (n_q, n_k) or [batch] int32 in; values outside [0, n_q], [0, n_k] are cut to that range
+ *   lse [batch, heads, n_q] fp32 out, dense, or NULL
+ *   scale > 0
+ * Rows of q at or behind q_len are not read and their o and lse are left as they are.  Keys and values that no row of a sequence sees
+ * may hold anything.  A value that is not finite makes the rows that see it, and possibly up to 127 rows beside those, NaN or infinite.
+ * The same call gives the same bits every time; with other sizes a row may differ by rounding.
+ * ws: dfs_window_workspace_bytes(w, dtype, 0), which may be 0 (then NULL will do).
+ */
+int dfs_window_attn_fwd(const dfs_window* w, int dtype, const dfs_view* q, const dfs_view* k, const dfs_view* v, const int32_t* q_len,
+                        const int32_t* k_len, float scale, const dfs_view* o, float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Its backward pass: dq, dk and dv from the forward call's inputs, its o and lse, and do, the gradient of o:
+ *   P = exp(scale <q, k_j> - lse),  dv_j = sum P do,  dS = P (<do, v_j> - <do, o>),  dq = scale sum dS k_j,  dk_j = scale sum dS q,
+ * dk and dv summed over the query heads that share a key head.  No atomics: same call, same bits.  bf16: P and dS are rounded to bf16
+ * for the products, sums are fp32; f32: fp32 throughout.  dq rows at or behind q_len, dk and dv rows at or behind k_len are left as they
+ * are; rows that nothing sees, or that see nothing, get zeros.  ws: dfs_window_workspace_bytes(w, dtype, 1).
+ */
+int dfs_window_attn_bwd(const dfs_window* w, int dtype, const dfs_view* q, const dfs_view* k, const dfs_view* v, const dfs_view* o,
+                        const float* lse, const dfs_view* d_o, const int32_t* q_len, const int32_t* k_len, float scale, const dfs_view* dq,
+                        const dfs_view* dk, const dfs_view* dv, void* ws, size_t ws_bytes, void* stream);
+
+/* Bytes of scratch of dfs_window_attn_fwd (backward = 0) or dfs_window_attn_bwd (1); 0 also if `w` is invalid.  Host only. */
+size_t dfs_window_workspace_bytes(const dfs_window* w, int dtype, int backward);
 
 /*
  * Diagnostic for measurements, not part of the method: while `counters` (device memory, 3 x uint64, zeroed by

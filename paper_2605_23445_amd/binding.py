@@ -39,6 +39,22 @@ class _MaskStateC(C.Structure):
                 ("K_max", C.c_int32)]
 
 
+class QkGeom(C.Structure):
+    """Mirror of dfs_qk_geom; its rot[3] are rot0, rot1 and rot2 here."""
+    _fields_ = [(n, C.c_int32) for n in ("batch", "tokens", "heads", "heads_kv", "d", "interleaved", "axes", "rot0", "rot1", "rot2")] + \
+        [("theta", C.c_double), ("eps", C.c_float)]
+
+
+class Window(C.Structure):
+    """Mirror of dfs_window."""
+    _fields_ = [(n, C.c_int32) for n in ("batch", "heads", "heads_kv", "d", "n_q", "n_k", "left", "right", "sinks")]
+
+
+class _View(C.Structure):
+    """Mirror of dfs_view."""
+    _fields_ = [("data", C.c_void_p), ("batch", C.c_int64), ("head", C.c_int64), ("row", C.c_int64)]
+
+
 @dataclass
 class MaskState:
     """Caller-owned mask buffers of one attention layer (kept across diffusion steps)."""
@@ -59,7 +75,7 @@ def _load():
                           "(or python paper_2605_23445_amd/build.py) first - there is no fallback path")
     lib = C.CDLL(_LIB_PATH)
     vp, i32, i64, dbl, f32, sz = C.c_void_p, C.c_int32, C.c_int64, C.c_double, C.c_float, C.c_size_t
-    gp = C.POINTER(Geom)
+    gp, qp, wp, tp = C.POINTER(Geom), C.POINTER(QkGeom), C.POINTER(Window), C.POINTER(_View)
     sig = {
         "dfs_geom_sizes": (C.c_int, [gp, C.POINTER(Sizes)]),
         "dfs_workspace_bytes": (sz, [gp, C.c_int]),
@@ -84,6 +100,12 @@ def _load():
         "dfs_probe_read": (C.c_int, [vp, sz, C.c_int32, C.c_int32, vp, vp]),
         "dfs_forward": (C.c_int, [gp, C.c_int, vp, vp, vp, vp, vp, C.c_int, C.c_int, dbl, dbl,
                                   C.POINTER(_MaskStateC), f32, vp, vp, sz, vp]),
+        "dfs_qk_norm_rope": (C.c_int, [qp, C.c_int, tp, tp, tp, vp, i64, vp, vp, tp, tp, tp, vp, i32, vp]),
+        "dfs_qk_norm_rope_bwd": (C.c_int, [qp, C.c_int, tp, tp, vp, i64, vp, vp, tp, tp, tp, tp, tp, tp, vp, vp, vp, sz, vp]),
+        "dfs_qk_workspace_bytes": (sz, [qp]),
+        "dfs_window_attn_fwd": (C.c_int, [wp, C.c_int, tp, tp, tp, vp, vp, f32, tp, vp, vp, sz, vp]),
+        "dfs_window_attn_bwd": (C.c_int, [wp, C.c_int, tp, tp, tp, tp, vp, tp, vp, vp, f32, tp, tp, tp, vp, sz, vp]),
+        "dfs_window_workspace_bytes": (sz, [wp, C.c_int, C.c_int]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -117,7 +139,8 @@ _lib = _load()
 EXPORTS = ("dfs_geom_sizes", "dfs_workspace_bytes", "dfs_last_error", "dfs_keep_count", "dfs_hilbert_perm", "dfs_permute",
            "dfs_block_score", "dfs_select_mask", "dfs_sparse_attn_fwd", "dfs_unperm", "dfs_forward", "dfs_token_order", "dfs_recall",
            "dfs_schedule", "dfs_block_score_src", "dfs_sparse_attn_fwd_src", "dfs_attn_clock_probe", "dfs_block_score_fused", "dfs_probe_mfma", "dfs_probe_copy", "dfs_probe_read",
-           "dfs_select_mask_static")
+           "dfs_select_mask_static", "dfs_qk_norm_rope", "dfs_qk_norm_rope_bwd", "dfs_qk_workspace_bytes", "dfs_window_attn_fwd",
+           "dfs_window_attn_bwd", "dfs_window_workspace_bytes")
 DFS_ORDER_HILBERT3D, DFS_ORDER_RASTER, DFS_ORDER_HILBERT2D, DFS_ORDER_BLOCK3D = 0, 1, 2, 3
 
 
@@ -385,3 +408,103 @@ def dfs_forward(g: Geom, dtype: int, q, k, v, perm_pad, inv, refresh: bool, mode
                             _ptr(perm_pad, torch.int32, s.N_pad, "perm_pad"), _ptr(inv, torch.int32, s.N, "inv"),
                             int(bool(refresh)), mode, float(sparsity), float(mass), cst, float(scale),
                             _ptr(o, td, n, "o"), wp, wb, _stream()))
+
+
+# Norm and rotation of queries and keys, and windowed attention.  Their tensors are [batch, heads, rows, d] with any strides whose rows are
+# dense: slices of a fused projection, transposed views, rows of a cache.
+
+
+def _here(t: torch.Tensor, name: str):
+    if not t.is_cuda or t.device.index != _current_device():
+        raise ValueError(f"{name} must be a tensor on the current device")
+
+
+def _view(t: torch.Tensor | None, dtype: int, batch: int, heads: int, rows: int, d: int, name: str):
+    """dfs_view of a tensor (None -> NULL)."""
+    if t is None:
+        return None
+    _here(t, name)
+    td = _torch_dtype(dtype)
+    if t.dtype is not td:
+        raise ValueError(f"{name} must be {td}, got {t.dtype}")
+    if tuple(t.shape) != (batch, heads, rows, d):
+        raise ValueError(f"{name} must be {[batch, heads, rows, d]}, got {list(t.shape)}")
+    b, h, r, one = t.stride()
+    if one != 1 and t.numel():
+        raise ValueError(f"the channels of a row of {name} must be adjacent")
+    return _View(t.data_ptr(), b, h, r)
+
+
+def _flat(t: torch.Tensor | None, dtype, numel: int, name: str):
+    if t is None:
+        return None
+    _here(t, name)
+    return _ptr(t, dtype, numel, name)
+
+
+def _positions(g: QkGeom, positions: torch.Tensor):
+    """Address of the positions and how many numbers they are from one sequence to the next."""
+    shape = (g.tokens, g.axes)
+    if tuple(positions.shape) not in (shape, (1, *shape), (g.batch, *shape)):
+        raise ValueError(f"positions must be {list(shape)} or one of these for each sequence, got {list(positions.shape)}")
+    each = positions.dim() == 3 and positions.shape[0] == g.batch and g.batch > 1
+    return _flat(positions, torch.int32, 0, "positions"), g.tokens * g.axes if each else 0
+
+
+def _scratch(ws: torch.Tensor | None):
+    if ws is not None:
+        _here(ws, "ws")
+    return _ws_args(ws)
+
+
+def dfs_qk_workspace_bytes(g: QkGeom) -> int:
+    return int(_lib.dfs_qk_workspace_bytes(g))
+
+
+def dfs_qk_norm_rope(g: QkGeom, dtype: int, q, k, v, positions, w_q, w_k, q_out, k_out, v_out, kv_start=None):
+    """Norm and rotation of q and k, a copy of v (v and v_out may be None).  With kv_start ([batch] int32) k_out and v_out are the rows of a
+    cache, [batch, heads_kv, rows, d], and token i of sequence b goes to its row kv_start[b] + i."""
+    shape = (g.batch, g.heads_kv, g.tokens, g.d)
+    rows = g.tokens if kv_start is None else k_out.shape[2]
+    pos, pos_batch = _positions(g, positions)
+    _check(_lib.dfs_qk_norm_rope(g, dtype, _view(q, dtype, g.batch, g.heads, g.tokens, g.d, "q"), _view(k, dtype, *shape, "k"),
+                                 _view(v, dtype, *shape, "v"), pos, pos_batch, _flat(w_q, torch.float32, g.d, "w_q"),
+                                 _flat(w_k, torch.float32, g.d, "w_k"), _view(q_out, dtype, g.batch, g.heads, g.tokens, g.d, "q_out"),
+                                 _view(k_out, dtype, g.batch, g.heads_kv, rows, g.d, "k_out"),
+                                 _view(v_out, dtype, g.batch, g.heads_kv, rows, g.d, "v_out"),
+                                 _flat(kv_start, torch.int32, g.batch, "kv_start"), rows, _stream()))
+
+
+def dfs_qk_norm_rope_bwd(g: QkGeom, dtype: int, q, k, positions, w_q, w_k, dq_out, dk_out, dv_out, dq, dk, dv, dw_q=None, dw_k=None, ws=None):
+    """Gradients of dfs_qk_norm_rope: dq, dk, dv (dv_out and dv may be None) and those of the weights (each may be None)."""
+    qs, ks = (g.batch, g.heads, g.tokens, g.d), (g.batch, g.heads_kv, g.tokens, g.d)
+    pos, pos_batch = _positions(g, positions)
+    wsp, wb = _scratch(ws)
+    _check(_lib.dfs_qk_norm_rope_bwd(g, dtype, _view(q, dtype, *qs, "q"), _view(k, dtype, *ks, "k"), pos, pos_batch,
+                                     _flat(w_q, torch.float32, g.d, "w_q"), _flat(w_k, torch.float32, g.d, "w_k"),
+                                     _view(dq_out, dtype, *qs, "dq_out"), _view(dk_out, dtype, *ks, "dk_out"), _view(dv_out, dtype, *ks, "dv_out"),
+                                     _view(dq, dtype, *qs, "dq"), _view(dk, dtype, *ks, "dk"), _view(dv, dtype, *ks, "dv"),
+                                     _flat(dw_q, torch.float32, g.d, "dw_q"), _flat(dw_k, torch.float32, g.d, "dw_k"), wsp, wb, _stream()))
+
+
+def dfs_window_workspace_bytes(w: Window, dtype: int, backward: bool) -> int:
+    return int(_lib.dfs_window_workspace_bytes(w, dtype, int(bool(backward))))
+
+
+def dfs_window_attn_fwd(w: Window, dtype: int, q, k, v, q_len, k_len, scale: float, o, lse=None, ws=None):
+    """Attention over a window and a few first keys; q_len and k_len ([batch] int32) may be None, ws where it takes none."""
+    qs, ks = (w.batch, w.heads, w.n_q, w.d), (w.batch, w.heads_kv, w.n_k, w.d)
+    wsp, wb = _scratch(ws)
+    _check(_lib.dfs_window_attn_fwd(w, dtype, _view(q, dtype, *qs, "q"), _view(k, dtype, *ks, "k"), _view(v, dtype, *ks, "v"),
+                                    _flat(q_len, torch.int32, w.batch, "q_len"), _flat(k_len, torch.int32, w.batch, "k_len"), float(scale),
+                                    _view(o, dtype, *qs, "o"), _flat(lse, torch.float32, w.batch * w.heads * w.n_q, "lse"), wsp, wb, _stream()))
+
+
+def dfs_window_attn_bwd(w: Window, dtype: int, q, k, v, o, lse, d_o, q_len, k_len, scale: float, dq, dk, dv, ws):
+    """Gradients of dfs_window_attn_fwd from its inputs, its o and lse, and d_o, the gradient of o."""
+    qs, ks = (w.batch, w.heads, w.n_q, w.d), (w.batch, w.heads_kv, w.n_k, w.d)
+    wsp, wb = _scratch(ws)
+    _check(_lib.dfs_window_attn_bwd(w, dtype, _view(q, dtype, *qs, "q"), _view(k, dtype, *ks, "k"), _view(v, dtype, *ks, "v"),
+                                    _view(o, dtype, *qs, "o"), _flat(lse, torch.float32, w.batch * w.heads * w.n_q, "lse"), _view(d_o, dtype, *qs, "d_o"),
+                                    _flat(q_len, torch.int32, w.batch, "q_len"), _flat(k_len, torch.int32, w.batch, "k_len"), float(scale),
+                                    _view(dq, dtype, *qs, "dq"), _view(dk, dtype, *ks, "dk"), _view(dv, dtype, *ks, "dv"), wsp, wb, _stream()))

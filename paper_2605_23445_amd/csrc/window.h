@@ -1,0 +1,228 @@
+// What the kernels of windowed attention share: their arguments, the tiles of rows in LDS and the operands of the matrix cores.
+//
+// All kernels work on tiles of rows of d channels.  A tile is loaded from global memory straight into LDS; rows behind its last real one are
+// zeros.  An operand "by rows" (rows of the tile are rows of the matrix, contracted over channels) is a 16-byte chunk per lane; an operand "by columns"
+// (channels are rows of the matrix, contracted over the tile's rows) comes through the transposing LDS read in bf16 and element by element in fp32.
+// With 32x32 products a lane holds, of the result, column lane % 32 and rows 8 (i / 4) + 4 (lane / 32) + i % 4 in register i: as B operand of a product
+// contracted over those rows the registers serve as they are.
+#pragma once
+#include "view.h"
+
+namespace dfs {
+
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+#define LDS_PTR(T) __attribute__((address_space(3))) T*
+
+constexpr int NO_LIMIT = 1 << 29;                    // of left and right: further than any two positions are apart
+constexpr float LOG2E = 1.4426950408889634f;
+
+struct WindowArgs {
+  View q, k, v, o, d_o, dq, dk, dv;
+  float *lse, *delta;                                // [batch, heads, n_q]
+  const int32_t *q_len, *k_len;
+  int32_t batch, heads, heads_kv, group, n_q, n_k, left, right, sinks;
+  int32_t blocks;                                    // work-groups of a sequence's key head
+  float scale;
+};
+
+// A sequence's lengths, and the position of its first query.
+struct Lengths {
+  int q, k, shift;
+  __device__ __forceinline__ Lengths(const WindowArgs& a, int b) {
+    q = a.q_len ? a.q_len[b] : a.n_q;
+    k = a.k_len ? a.k_len[b] : a.n_k;
+    q = q < 0 ? 0 : q > a.n_q ? a.n_q : q;
+    k = k < 0 ? 0 : k > a.n_k ? a.n_k : k;
+    shift = k - q;
+  }
+};
+
+__device__ __forceinline__ int min_of(int a, int b) { return a < b ? a : b; }
+__device__ __forceinline__ int max_of(int a, int b) { return a > b ? a : b; }
+
+// The tiles of KN keys that a run of queries needs.
+template <int KN>
+struct Span {
+  int lo, hi, first, n_first, n;                     // window [lo, hi); first keys [0, first) in front of it; tiles of these, and of all
+  __device__ __forceinline__ Span(const WindowArgs& a, int p0, int p1, int k_len) {       // positions p0 .. p1 (none if p1 < p0)
+    lo = max_of(0, p0 - a.left);
+    hi = min_of(k_len, p1 + a.right + 1);
+    if (p1 < p0 || hi < 0) hi = 0;
+    first = min_of(min_of(a.sinks, lo), hi);
+    if (lo > hi) lo = hi;
+    n_first = (first + KN - 1) / KN;
+    n = n_first + (hi - lo + KN - 1) / KN;
+  }
+  __device__ __forceinline__ int begin(int t) const { return t < n_first ? t * KN : lo + (t - n_first) * KN; }
+  __device__ __forceinline__ int end(int t) const { return t < n_first ? first : hi; }
+};
+
+// Whether a query that sees [lo, hi] and the first keys sees `key`, of those in front of `end`.  Without branches: written with && and || and an assignment
+// under `if`, the compiler (ROCm 7.2) made branches of it and lost the assignment to the first register of an accumulator in one of them.
+__device__ __forceinline__ bool sees(int key, int end, int lo, int hi, int sinks) { return (key < end) & (key <= hi) & ((key >= lo) | (key < sinks)); }
+
+// Work-group of the linear order in which each XCD takes a run of its own (consecutive work-groups go to the XCDs in turn), so that those that read
+// the same rows share an L2.
+__device__ __forceinline__ int xcd_order(int id, int n) {
+  const int xcd = id % 8, slot = id / 8, per = n / 8, more = n % 8;
+  return xcd * per + (xcd < more ? xcd : more) + slot;
+}
+
+template <typename T> struct Mat;
+template <> struct Mat<uint16_t> {
+  typedef bf16x8 Frag;
+  // 16 bytes of every row: 16 channels in all
+  static __device__ __forceinline__ f32x16 mma(Frag a, Frag b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+};
+template <> struct Mat<float> {
+  typedef f32x4 Frag;
+  // 8 channels in all
+  static __device__ __forceinline__ f32x16 mma(Frag a, Frag b, f32x16 c) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[i], b[i], c, 0, 0, 0);
+    return c;
+  }
+};
+
+// A result of 32 x 32 as B operand of a product contracted over its rows.
+template <typename T> struct Weights;
+template <> struct Weights<uint16_t> {
+  u32x4 p[2];
+  __device__ __forceinline__ void set(const f32x16& x) {
+#pragma unroll
+    for (int i = 0; i < 16; i += 2) {
+      const bf16x2 b = {(__bf16)x[i], (__bf16)x[i + 1]};
+      p[i / 8][(i % 8) / 2] = __builtin_bit_cast(uint32_t, b);
+    }
+  }
+};
+template <> struct Weights<float> {
+  f32x16 p;
+  __device__ __forceinline__ void set(const f32x16& x) { p = x; }
+};
+
+// Tiles of ROWS rows of D elements, loaded by NW waves.  COLUMNS: the swizzle that suits reads by columns alone.
+template <typename T, int D, int ROWS, int NW, bool COLUMNS>
+struct Tile {
+  static constexpr int RB = D * int(sizeof(T)), CH = RB / 16, BYTES = ROWS * RB, STEPS = CH / 2;   // STEPS: products of a contraction over channels
+  static constexpr int LOADS = ROWS * CH / (64 * NW);
+  static constexpr int FOLD = CH < 16 ? 16 / CH : 1;
+  static_assert(ROWS * CH % (64 * NW) == 0, "a load fills 64 chunks");
+  // XOR of the 16-byte chunks of a row, so that the rows which a wave reads at once lie in different banks
+  static __device__ __forceinline__ int swizzle(int row) {
+    return COLUMNS ? 4 * ((row / FOLD) % (CH < 16 ? CH / 4 : 4)) : (row / FOLD) % (CH < 16 ? CH : 16);
+  }
+  // Loads: byte offset of this lane's chunk of load j in a tensor whose rows are `stride` bytes apart.
+  struct Loader {
+    uint32_t off[LOADS];
+    __device__ __forceinline__ Loader(int64_t stride, int wave, int lane) {
+#pragma unroll
+      for (int j = 0; j < LOADS; ++j) {
+        const int p = (j * NW + wave) * 64 + lane, row = p / CH, pc = p % CH;
+        off[j] = uint32_t(row) * uint32_t(stride) + uint32_t((pc ^ swizzle(row)) * 16);
+      }
+    }
+    // Asks for the tile whose first row is at `src`; `rows` of it are real.  lds: byte address of the tile.  The loads are asm so that the compiler does
+    // not wait for them in front of every LDS read; wait_loads() below does, in front of a barrier.
+    __device__ __forceinline__ void issue(const char* src, int rows, int64_t stride, uint32_t lds, int wave) const {
+      const uint64_t at = reinterpret_cast<uint64_t>(src);
+      const uint32_t bytes = rows > 0 ? uint32_t((rows < ROWS ? rows : ROWS) - 1) * uint32_t(stride) + RB : 0;
+      const u32x4 desc = {uint32_t(__builtin_amdgcn_readfirstlane(uint32_t(at))), uint32_t(__builtin_amdgcn_readfirstlane(uint32_t(at >> 32))) & 0xFFFFu,
+                          uint32_t(__builtin_amdgcn_readfirstlane(bytes)), 0x00020000u};
+      const uint32_t to = __builtin_amdgcn_readfirstlane(lds + uint32_t(wave) * 1024);
+#pragma unroll
+      for (int j = 0; j < LOADS; ++j)
+        asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                     ::"s"(to), "v"(off[j]), "s"(desc), "i"(j * NW * 1024) : "memory", "m0", "scc");
+    }
+  };
+  // Operand by rows: chunk 2 step + h of row 32 half + n.
+  struct RowReader {
+    uint32_t at, sw;
+    int h;
+    __device__ __forceinline__ RowReader(int lane) : at(uint32_t((lane & 31) * RB)), sw(uint32_t(swizzle(lane & 31))), h(lane >> 5) {}
+    __device__ __forceinline__ typename Mat<T>::Frag get(uint32_t lds, int half, int step) const {
+      return __builtin_bit_cast(typename Mat<T>::Frag,
+                                *reinterpret_cast<LDS_PTR(const u32x4)>(lds + at + uint32_t(half * 32 * RB) + ((uint32_t(2 * step + h) ^ sw) * 16)));
+    }
+  };
+  // acc[c] += (32 channels from 32 c on) x (rows of half `half`, contracted with w)
+  struct ColumnReader {
+    uint32_t at[D / 32][2];
+    __device__ __forceinline__ ColumnReader(int lane) {
+      const int h = lane >> 5;
+      if constexpr (sizeof(T) == 2) {
+        // the 16 lanes of a group hand in four rows of 16 channels and get four rows of one channel each
+        const int row = 4 * h + ((lane & 15) >> 2), chunk = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1), byte = (lane & 1) * 8;
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c) {
+          at[c][0] = uint32_t(row * RB + ((4 * c + chunk) ^ swizzle(row)) * 16 + byte);
+          at[c][1] = uint32_t((row + 8) * RB + ((4 * c + chunk) ^ swizzle(row + 8)) * 16 + byte);
+        }
+      } else {
+        at[0][0] = uint32_t(lane & 31);
+        at[0][1] = uint32_t(h);
+      }
+    }
+    __device__ __forceinline__ void mma(uint32_t lds, int half, const Weights<T>& w, f32x16 (&acc)[D / 32]) const {
+      if constexpr (sizeof(T) == 2) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+          for (int c = 0; c < D / 32; ++c) {
+            const uint32_t p = lds + uint32_t((half * 32 + s * 16) * RB);
+            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<LDS_PTR(s16x4)>(p + at[c][0]));
+            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<LDS_PTR(s16x4)>(p + at[c][1]));
+            const bf16x8 a = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+            acc[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, __builtin_bit_cast(bf16x8, w.p[s]), acc[c], 0, 0, 0);
+          }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int row = half * 32 + 8 * (i / 4) + 4 * int(at[0][1]) + i % 4;
+          const uint32_t p = lds + uint32_t(row * RB), sw = uint32_t(swizzle(row));
+#pragma unroll
+          for (int c = 0; c < D / 32; ++c) {
+            const uint32_t ch = uint32_t(32 * c) + at[0][0];
+            const float a = *reinterpret_cast<LDS_PTR(const float)>(p + ((ch / 4) ^ sw) * 16 + (ch % 4) * 4);
+            acc[c] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, w.p[i], acc[c], 0, 0, 0);
+          }
+        }
+      }
+    }
+  };
+};
+
+__device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0F70); }          // vmcnt(0)
+
+template <int N> __device__ __forceinline__ void clear(f32x16 (&x)[N]) {
+#pragma unroll
+  for (int c = 0; c < N; ++c)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[c][i] = 0.f;
+}
+
+// Row `row` of accumulators by columns (column = lane % 32 of the row's 32 channels per c), times f, to a row of T.
+template <typename T, int N> __device__ __forceinline__ void store_row(char* row, const f32x16 (&x)[N], float f, int h) {
+#pragma unroll
+  for (int c = 0; c < N; ++c)
+#pragma unroll
+    for (int i = 0; i < 16; i += 4) {
+      const int ch = 32 * c + 2 * i + 4 * h;
+      if constexpr (sizeof(T) == 2) {
+        const bf16x2 a = {(__bf16)(x[c][i] * f), (__bf16)(x[c][i + 1] * f)}, b = {(__bf16)(x[c][i + 2] * f), (__bf16)(x[c][i + 3] * f)};
+        *reinterpret_cast<uint2*>(row + ch * 2) = make_uint2(__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b));
+      } else {
+        *reinterpret_cast<float4*>(row + ch * 4) = make_float4(x[c][i] * f, x[c][i + 1] * f, x[c][i + 2] * f, x[c][i + 3] * f);
+      }
+    }
+}
+
+int run_window_bwd(const WindowArgs& a, int d, int dtype, hipStream_t st);
+
+}  // namespace dfs

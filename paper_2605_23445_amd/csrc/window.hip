@@ -1,0 +1,215 @@
+// Attention over a window around each query's position and a few first keys.
+//
+// The rows of a work-group are queries of ALL heads that share a key head, query by query (row r is head r % group of query r / group): a tile of
+// keys and values is brought in once for the group, and a block of rows spans fewer positions, so that it meets fewer tiles of which it
+// sees only a part.  Keys come in tiles of 64 rows: first those of the first keys that lie in front of the block's window, then the window's, from its
+// first key on.
+#include <float.h>
+#include <math.h>
+
+#include "window.h"
+
+namespace dfs {
+
+constexpr int KN = 64;                               // keys of a tile
+
+template <typename T, int D>
+__global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) window_fwd_kernel(WindowArgs a) {
+  constexpr int NW = 4, BM = 32 * NW;
+  using KTile = Tile<T, D, KN, NW, false>;
+  using VTile = Tile<T, D, KN, NW, true>;
+  constexpr int STEPS = KTile::STEPS;
+  __shared__ __attribute__((aligned(1024))) char tiles[4 * KTile::BYTES];
+  const uint32_t lds = uint32_t(reinterpret_cast<uintptr_t>((LDS_PTR(void))(tiles)));
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 31, h = lane >> 5;
+
+  const int id = xcd_order(blockIdx.x, gridDim.x), blk = id % a.blocks, bh = id / a.blocks, b = bh / a.heads_kv, kvh = bh % a.heads_kv;
+  const Lengths len(a, b);
+  const int64_t r0 = int64_t(blk) * BM, left = int64_t(len.q) * a.group - r0;
+  const int rows = left < BM ? int(left) : BM;
+  if (rows <= 0) return;
+  const int i0 = int(r0 / a.group), i1 = int((r0 + rows - 1) / a.group);
+  const Span<KN> span(a, i0 + len.shift, i1 + len.shift, len.k);
+
+  const int64_t r = r0 + wave * 32 + n;
+  const bool real = wave * 32 + n < rows;
+  const int qi = real ? int(r / a.group) : i0, qh = kvh * a.group + (real ? int(r % a.group) : 0), p = qi + len.shift;
+  typename Mat<T>::Frag qf[STEPS];
+  {
+    const char* qp = a.q.at(b, qh, qi);
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) qf[s] = *reinterpret_cast<const typename Mat<T>::Frag*>(qp + (2 * s + h) * 16);
+  }
+  const char *kh = a.k.at(b, kvh, 0), *vh = a.v.at(b, kvh, 0);
+  const typename KTile::Loader k_load(a.k.row, wave, lane);
+  const typename VTile::Loader v_load(a.v.row, wave, lane);
+  const typename KTile::RowReader k_read(lane);
+  const typename VTile::ColumnReader v_read(lane);
+  auto issue = [&](int t) {
+    const int begin = span.begin(t), rest = span.end(t) - begin;
+    const uint32_t buf = lds + uint32_t((t & 1) * 2 * KTile::BYTES);
+    k_load.issue(kh + int64_t(begin) * a.k.row, rest, a.k.row, buf, wave);
+    v_load.issue(vh + int64_t(begin) * a.v.row, rest, a.v.row, buf + KTile::BYTES, wave);
+  };
+
+  f32x16 acc[D / 32];
+  clear(acc);
+  float m = -INFINITY, l = 0.f;                      // row maximum in the base-2 exponent's units, this lane's share of the row sum
+  const float c2 = a.scale * LOG2E;
+  const int key_lo = p - a.left, key_hi = p + a.right;
+  if (span.n > 0) issue(0);
+  for (int t = 0; t < span.n; ++t) {
+    wait_loads();
+    __syncthreads();                                 // tile t is there, and the buffers of tile t - 1 are free
+    if (t + 1 < span.n) issue(t + 1);
+    const uint32_t buf = lds + uint32_t((t & 1) * 2 * KTile::BYTES);
+    const int begin = span.begin(t), end = span.end(t);
+    const bool whole = begin + KN <= end && begin + KN - 1 <= i0 + len.shift + a.right && (t < span.n_first || begin >= i1 + len.shift - a.left);
+    f32x16 s[2];
+    clear(s);
+#pragma unroll
+    for (int half = 0; half < 2; ++half)
+#pragma unroll
+      for (int st = 0; st < STEPS; ++st) s[half] = Mat<T>::mma(k_read.get(buf, half, st), qf[st], s[half]);
+    if (!whole) {
+#pragma unroll
+      for (int half = 0; half < 2; ++half)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int key = begin + 32 * half + 8 * (i / 4) + 4 * h + i % 4;
+          s[half][i] = sees(key, end, key_lo, key_hi, a.sinks) ? s[half][i] : -INFINITY;
+        }
+    }
+    float mx = s[0][0];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) mx = fmaxf(mx, fmaxf(s[0][i], s[1][i]));
+    const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+    mx = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * c2;
+    const float m_new = fmaxf(m, mx), ref = m_new == -INFINITY ? 0.f : m_new;
+    if (__builtin_amdgcn_ballot_w64(m_new > m)) {
+      const float alpha = __builtin_amdgcn_exp2f(m - ref);
+      m = m_new;
+      l *= alpha;
+#pragma unroll
+      for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[c][i] *= alpha;
+    }
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        s[half][i] = __builtin_amdgcn_exp2f(fmaf(s[half][i], c2, -ref));
+        l += s[half][i];
+      }
+      Weights<T> w;
+      w.set(s[half]);
+      v_read.mma(buf + KTile::BYTES, half, w, acc);
+    }
+  }
+  const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
+  l = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+  if (!real) return;
+  store_row<T>(a.o.at(b, qh, qi), acc, l == 0.f ? 0.f : 1.f / l, h);
+  if (a.lse && h == 0) a.lse[(int64_t(b) * a.heads + qh) * a.n_q + qi] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * (1.f / LOG2E);
+}
+
+static int check_window(const char* call, const dfs_window* w, int dtype) {
+  if (!w) return fail(DFS_EINVAL, "%s: window pointer is NULL", call);
+  if (dtype != DFS_F32 && dtype != DFS_BF16) return fail(DFS_EDTYPE, "%s: dtype %d is not DFS_F32 or DFS_BF16", call, dtype);
+  if (w->batch < 0 || w->n_q < 0 || w->n_k < 0 || w->n_q > 1 << 28 || w->n_k > 1 << 28)
+    return fail(DFS_ESHAPE, "%s: batch=%d must not be negative, n_q=%d and n_k=%d be in [0, 2^28]", call, w->batch, w->n_q, w->n_k);
+  if (w->heads < 1 || w->heads_kv < 1 || w->heads > 65535 || w->heads % w->heads_kv)
+    return fail(DFS_ESHAPE, "%s: heads=%d must be in [1, 65535] and a multiple of heads_kv=%d", call, w->heads, w->heads_kv);
+  if (w->d != 64 && w->d != 128) return fail(DFS_ESHAPE, "%s: d=%d: head dimension must be 64 or 128", call, w->d);
+  if (w->sinks < 0) return fail(DFS_ESHAPE, "%s: sinks=%d is negative", call, w->sinks);
+  // a sequence's rows and the grids' work-groups are counted in 31 bits
+  const int64_t rows = int64_t(w->heads / w->heads_kv) * w->n_q, most = rows > w->n_k ? rows : w->n_k;
+  if (rows >= int64_t(1) << 31 || (most / 32 + 2) * w->batch * int64_t(w->heads_kv) >= int64_t(1) << 31 || int64_t(w->batch) * w->heads >= int64_t(1) << 31)
+    return fail(DFS_ESHAPE, "%s: batch x heads x rows too large", call);
+  return DFS_OK;
+}
+
+// Rows of tiles are addressed by 32 bits within a tile.
+static int check_tiles(const char* call, const char* name, const View& v) {
+  if (v.row > (int64_t(1) << 24)) return fail(DFS_ESHAPE, "%s: rows of %s are more than 2^24 bytes apart", call, name);
+  return DFS_OK;
+}
+
+static int fill_window(const char* call, const dfs_window* w, int dtype, const dfs_view* q, const dfs_view* k, const dfs_view* v, const dfs_view* o, bool o_out,
+                       const float* lse, const int32_t* q_len, const int32_t* k_len, float scale, WindowArgs* a) {
+  int rc = check_window(call, w, dtype);
+  if (rc) return rc;
+  if (!(scale > 0.f) || !isfinite(scale)) return fail(DFS_EINVAL, "%s: scale must be positive and finite", call);
+  if (misaligned(4, {lse, q_len, k_len})) return fail(DFS_EINVAL, "%s: lse and lengths must be 4-byte aligned", call);
+  if ((rc = check_view(call, "q", q, dtype, w->batch, w->heads, w->n_q, w->d, false, &a->q))) return rc;
+  if ((rc = check_view(call, "k", k, dtype, w->batch, w->heads_kv, w->n_k, w->d, false, &a->k))) return rc;
+  if ((rc = check_view(call, "v", v, dtype, w->batch, w->heads_kv, w->n_k, w->d, false, &a->v))) return rc;
+  if ((rc = check_view(call, "o", o, dtype, w->batch, w->heads, w->n_q, w->d, o_out, &a->o))) return rc;
+  if ((rc = check_tiles(call, "k", a->k)) || (rc = check_tiles(call, "v", a->v))) return rc;
+  a->lse = const_cast<float*>(lse);
+  a->q_len = q_len;
+  a->k_len = k_len;
+  a->batch = w->batch;
+  a->heads = w->heads;
+  a->heads_kv = w->heads_kv;
+  a->group = w->heads / w->heads_kv;
+  a->n_q = w->n_q;
+  a->n_k = w->n_k;
+  a->left = w->left < 0 || w->left > NO_LIMIT ? NO_LIMIT : w->left;
+  a->right = w->right < 0 || w->right > NO_LIMIT ? NO_LIMIT : w->right;
+  a->sinks = w->sinks;
+  a->scale = scale;
+  return DFS_OK;
+}
+
+}  // namespace dfs
+
+using namespace dfs;
+
+extern "C" {
+
+size_t dfs_window_workspace_bytes(const dfs_window* w, int dtype, int backward) {
+  if (check_window("dfs_window_workspace_bytes", w, dtype) != DFS_OK) return 0;
+  return backward ? align256(size_t(w->batch) * w->heads * w->n_q * sizeof(float)) : 0;
+}
+
+int dfs_window_attn_fwd(const dfs_window* w, int dtype, const dfs_view* q, const dfs_view* k, const dfs_view* v, const int32_t* q_len,
+                        const int32_t* k_len, float scale, const dfs_view* o, float* lse, void* ws, size_t ws_bytes, void* stream) {
+  const char* call = "dfs_window_attn_fwd";
+  WindowArgs a = {};
+  int rc = fill_window(call, w, dtype, q, k, v, o, true, lse, q_len, k_len, scale, &a);
+  if (rc) return rc;
+  if (w->batch == 0 || w->n_q == 0) return DFS_OK;
+  a.blocks = int((int64_t(a.group) * a.n_q + 127) / 128);
+  const unsigned grid = unsigned(int64_t(a.blocks) * a.batch * a.heads_kv);
+  const hipStream_t st = as_stream(stream);
+  if (dtype == DFS_BF16)
+    w->d == 64 ? window_fwd_kernel<uint16_t, 64><<<grid, 256, 0, st>>>(a) : window_fwd_kernel<uint16_t, 128><<<grid, 256, 0, st>>>(a);
+  else
+    w->d == 64 ? window_fwd_kernel<float, 64><<<grid, 256, 0, st>>>(a) : window_fwd_kernel<float, 128><<<grid, 256, 0, st>>>(a);
+  return launch_status(call);
+}
+
+int dfs_window_attn_bwd(const dfs_window* w, int dtype, const dfs_view* q, const dfs_view* k, const dfs_view* v, const dfs_view* o,
+                        const float* lse, const dfs_view* d_o, const int32_t* q_len, const int32_t* k_len, float scale, const dfs_view* dq,
+                        const dfs_view* dk, const dfs_view* dv, void* ws, size_t ws_bytes, void* stream) {
+  const char* call = "dfs_window_attn_bwd";
+  WindowArgs a = {};
+  int rc = fill_window(call, w, dtype, q, k, v, o, false, lse, q_len, k_len, scale, &a);
+  if (rc) return rc;
+  if ((rc = check_view(call, "d_o", d_o, dtype, w->batch, w->heads, w->n_q, w->d, false, &a.d_o))) return rc;
+  if ((rc = check_view(call, "dq", dq, dtype, w->batch, w->heads, w->n_q, w->d, true, &a.dq))) return rc;
+  if ((rc = check_view(call, "dk", dk, dtype, w->batch, w->heads_kv, w->n_k, w->d, true, &a.dk))) return rc;
+  if ((rc = check_view(call, "dv", dv, dtype, w->batch, w->heads_kv, w->n_k, w->d, true, &a.dv))) return rc;
+  if ((rc = check_tiles(call, "q", a.q)) || (rc = check_tiles(call, "d_o", a.d_o))) return rc;
+  if (!lse && w->batch && w->n_q) return fail(DFS_EINVAL, "%s: lse is NULL", call);
+  const size_t need = dfs_window_workspace_bytes(w, dtype, 1);
+  if (need && (!ws || (uintptr_t(ws) & 255) || ws_bytes < need))
+    return fail(DFS_EWORKSPACE, "%s: workspace of %zu bytes needed (256-byte aligned), got %zu", call, need, ws_bytes);
+  if (w->batch == 0) return DFS_OK;
+  a.delta = static_cast<float*>(ws);
+  return run_window_bwd(a, w->d, dtype, as_stream(stream));
+}
+
+}  // extern "C"
