@@ -24,9 +24,11 @@ constexpr float LOG2E = 1.4426950408889634f;
 struct WindowArgs {
   View q, k, v, o, d_o, dq, dk, dv;
   float *lse, *delta;                                // [batch, heads, n_q]
+  float* part;                                       // backward: sums of the first keys' gradients
   const int32_t *q_len, *k_len;
   int32_t batch, heads, heads_kv, group, n_q, n_k, left, right, sinks;
   int32_t blocks;                                    // work-groups of a sequence's key head
+  int32_t first_tiles, first_splits;                 // backward: tiles of 32 first keys, and work-groups that share one's queries
   float scale;
 };
 
@@ -60,6 +62,10 @@ struct Span {
   }
   __device__ __forceinline__ int begin(int t) const { return t < n_first ? t * KN : lo + (t - n_first) * KN; }
   __device__ __forceinline__ int end(int t) const { return t < n_first ? first : hi; }
+  // Whether queries at positions p0 .. p1 see none of the 32 keys from `key` on of tile t, which ends at `end`.
+  __device__ __forceinline__ bool unseen(const WindowArgs& a, int t, int key, int end, int p0, int p1) const {
+    return key >= end || key > p1 + a.right || (t >= n_first && key >= a.sinks && key + 31 < p0 - a.left);
+  }
 };
 
 // Whether a query that sees [lo, hi] and the first keys sees `key`, of those in front of `end`.  Without branches: written with && and || and an assignment

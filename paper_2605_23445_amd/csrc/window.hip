@@ -130,6 +130,27 @@ static int check_window(const char* call, const dfs_window* w, int dtype) {
   return DFS_OK;
 }
 
+// First keys that count: none where every window reaches back to them.
+static int first_keys(const dfs_window* w) {
+  if (w->left < 0 || w->left >= w->n_k) return 0;
+  return w->sinks < w->n_k ? w->sinks : w->n_k;
+}
+
+// Scratch of the backward pass: delta of every row, then the parts of the first keys' gradients.  The queries of 32 first keys go to as many work-groups
+// as make 512 in all, of which each of four waves has two tiles of 32 at least.
+struct BwdLayout { size_t part, total; int tiles, splits; };
+static BwdLayout bwd_layout(const dfs_window* w) {
+  BwdLayout L;
+  const int64_t seqs = int64_t(w->batch) * w->heads_kv, rows = int64_t(w->n_q) * (w->heads / w->heads_kv);
+  L.part = align256(size_t(w->batch) * w->heads * w->n_q * sizeof(float));
+  L.tiles = (first_keys(w) + 31) / 32;
+  int64_t splits = seqs && L.tiles ? 512 / (seqs * L.tiles) : 1;
+  if (splits > rows / 256) splits = rows / 256;
+  L.splits = splits < 1 ? 1 : int(splits);
+  L.total = L.part + size_t(seqs) * L.tiles * (L.splits + 1) * 64 * w->d * sizeof(float);
+  return L;
+}
+
 // Rows of tiles are addressed by 32 bits within a tile.
 static int check_tiles(const char* call, const char* name, const View& v) {
   if (v.row > (int64_t(1) << 24)) return fail(DFS_ESHAPE, "%s: rows of %s are more than 2^24 bytes apart", call, name);
@@ -158,7 +179,7 @@ static int fill_window(const char* call, const dfs_window* w, int dtype, const d
   a->n_k = w->n_k;
   a->left = w->left < 0 || w->left > NO_LIMIT ? NO_LIMIT : w->left;
   a->right = w->right < 0 || w->right > NO_LIMIT ? NO_LIMIT : w->right;
-  a->sinks = w->sinks;
+  a->sinks = first_keys(w);
   a->scale = scale;
   return DFS_OK;
 }
@@ -171,7 +192,7 @@ extern "C" {
 
 size_t dfs_window_workspace_bytes(const dfs_window* w, int dtype, int backward) {
   if (check_window("dfs_window_workspace_bytes", w, dtype) != DFS_OK) return 0;
-  return backward ? align256(size_t(w->batch) * w->heads * w->n_q * sizeof(float)) : 0;
+  return backward ? bwd_layout(w).total : 0;
 }
 
 int dfs_window_attn_fwd(const dfs_window* w, int dtype, const dfs_view* q, const dfs_view* k, const dfs_view* v, const int32_t* q_len,
@@ -208,7 +229,11 @@ int dfs_window_attn_bwd(const dfs_window* w, int dtype, const dfs_view* q, const
   if (need && (!ws || (uintptr_t(ws) & 255) || ws_bytes < need))
     return fail(DFS_EWORKSPACE, "%s: workspace of %zu bytes needed (256-byte aligned), got %zu", call, need, ws_bytes);
   if (w->batch == 0) return DFS_OK;
+  const BwdLayout L = bwd_layout(w);
   a.delta = static_cast<float*>(ws);
+  a.part = reinterpret_cast<float*>(static_cast<char*>(ws) + L.part);
+  a.first_tiles = L.tiles;
+  a.first_splits = L.splits;
   return run_window_bwd(a, w->d, dtype, as_stream(stream));
 }
 
