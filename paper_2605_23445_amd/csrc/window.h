@@ -24,11 +24,13 @@ constexpr float LOG2E = 1.4426950408889634f;
 struct WindowArgs {
   View q, k, v, o, d_o, dq, dk, dv;
   float *lse, *delta;                                // [batch, heads, n_q]
-  float* part;                                       // backward: sums of the first keys' gradients
+  float* part;                                       // sums of a part: of the first keys' gradients, or of a row's output
+  float2* part_sums;                                 // maximum and sum of a row's part
   const int32_t *q_len, *k_len;
   int32_t batch, heads, heads_kv, group, n_q, n_k, left, right, sinks;
   int32_t blocks;                                    // work-groups of a sequence's key head
   int32_t first_tiles, first_splits;                 // backward: tiles of 32 first keys, and work-groups that share one's queries
+  int32_t splits;                                    // forward: work-groups that share the keys of 32 rows
   float scale;
 };
 
@@ -213,19 +215,24 @@ template <int N> __device__ __forceinline__ void clear(f32x16 (&x)[N]) {
     for (int i = 0; i < 16; ++i) x[c][i] = 0.f;
 }
 
+// Four channels of a row from `ch` on, times f.
+template <typename T> __device__ __forceinline__ void store_four(char* row, int ch, const float (&x)[4], float f) {
+  if constexpr (sizeof(T) == 2) {
+    const bf16x2 a = {(__bf16)(x[0] * f), (__bf16)(x[1] * f)}, b = {(__bf16)(x[2] * f), (__bf16)(x[3] * f)};
+    *reinterpret_cast<uint2*>(row + ch * 2) = make_uint2(__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b));
+  } else {
+    *reinterpret_cast<float4*>(row + ch * 4) = make_float4(x[0] * f, x[1] * f, x[2] * f, x[3] * f);
+  }
+}
+
 // Row `row` of accumulators by columns (column = lane % 32 of the row's 32 channels per c), times f, to a row of T.
 template <typename T, int N> __device__ __forceinline__ void store_row(char* row, const f32x16 (&x)[N], float f, int h) {
 #pragma unroll
   for (int c = 0; c < N; ++c)
 #pragma unroll
     for (int i = 0; i < 16; i += 4) {
-      const int ch = 32 * c + 2 * i + 4 * h;
-      if constexpr (sizeof(T) == 2) {
-        const bf16x2 a = {(__bf16)(x[c][i] * f), (__bf16)(x[c][i + 1] * f)}, b = {(__bf16)(x[c][i + 2] * f), (__bf16)(x[c][i + 3] * f)};
-        *reinterpret_cast<uint2*>(row + ch * 2) = make_uint2(__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b));
-      } else {
-        *reinterpret_cast<float4*>(row + ch * 4) = make_float4(x[c][i] * f, x[c][i + 1] * f, x[c][i + 2] * f, x[c][i + 3] * f);
-      }
+      const float four[4] = {x[c][i], x[c][i + 1], x[c][i + 2], x[c][i + 3]};
+      store_four<T>(row, 32 * c + 2 * i + 4 * h, four, f);
     }
 }
 

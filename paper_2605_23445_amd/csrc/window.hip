@@ -12,6 +12,7 @@
 namespace dfs {
 
 constexpr int KN = 64;                               // keys of a tile
+constexpr int SPLIT_GROUPS = 768;                    // work-groups that a call over few rows is split into, at most
 
 template <typename T, int D>
 __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) window_fwd_kernel(WindowArgs a) {
@@ -114,6 +115,173 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) window_fwd_kernel
   if (a.lse && h == 0) a.lse[(int64_t(b) * a.heads + qh) * a.n_q + qi] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * (1.f / LOG2E);
 }
 
+// Few queries: the keys of 32 rows are split over the waves of a work-group and over `splits` work-groups, and what they find is joined.  A wave's tiles of 32
+// keys are its own, so that none waits for another before the end, and one is on its way while another is worked on: 64 KB a CU.
+template <typename T, int D> constexpr int split_waves() { return sizeof(T) == 4 && D == 128 ? 2 : 4; }
+template <typename T, int D>
+__global__ void __launch_bounds__((64 * split_waves<T, D>()), 1) window_split_kernel(WindowArgs a) {
+  constexpr int NW = split_waves<T, D>(), SN = 32, REGS = D / 2;
+  using KTile = Tile<T, D, SN, 1, false>;
+  using VTile = Tile<T, D, SN, 1, true>;
+  constexpr int STEPS = KTile::STEPS;
+  static_assert(REGS * 64 * 4 <= 4 * KTile::BYTES, "a wave's sums fit where its tiles were");
+  __shared__ __attribute__((aligned(1024))) char tiles[NW * 4 * KTile::BYTES];
+  __shared__ float s_m[NW][32], s_l[NW][32];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 31, h = lane >> 5;
+  const uint32_t lds = uint32_t(reinterpret_cast<uintptr_t>((LDS_PTR(void))(tiles))) + uint32_t(wave * 4 * KTile::BYTES);
+
+  const int split = blockIdx.x % a.splits, at = blockIdx.x / a.splits, blk = at % a.blocks, bh = at / a.blocks, b = bh / a.heads_kv, kvh = bh % a.heads_kv;
+  const Lengths len(a, b);
+  const int64_t r0 = int64_t(blk) * 32, left = int64_t(len.q) * a.group - r0;
+  const int rows = left < 32 ? int(left) : 32;
+  if (rows <= 0) return;
+  const int i0 = int(r0 / a.group), i1 = int((r0 + rows - 1) / a.group);
+  const Span<SN> span(a, i0 + len.shift, i1 + len.shift, len.k);
+  const int per = (span.n + a.splits - 1) / a.splits, t_end = min_of(span.n, (split + 1) * per);
+
+  const bool real = n < rows;
+  const int qi = real ? int((r0 + n) / a.group) : i0, qh = kvh * a.group + (real ? int((r0 + n) % a.group) : 0), p = qi + len.shift;
+  const char *kh = a.k.at(b, kvh, 0), *vh = a.v.at(b, kvh, 0);
+  const typename KTile::Loader k_load(a.k.row, 0, lane);
+  const typename VTile::Loader v_load(a.v.row, 0, lane);
+  auto issue = [&](int t, int buf) {
+    const int begin = span.begin(t), rest = span.end(t) - begin;
+    const uint32_t to = lds + uint32_t(buf * 2 * KTile::BYTES);
+    k_load.issue(kh + int64_t(begin) * a.k.row, rest, a.k.row, to, 0);
+    v_load.issue(vh + int64_t(begin) * a.v.row, rest, a.v.row, to + KTile::BYTES, 0);
+  };
+  int t = split * per + wave, parity = 0;
+  if (t < t_end) issue(t, 0);
+  typename Mat<T>::Frag qf[STEPS];
+  {
+    const char* qp = a.q.at(b, qh, qi);
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) qf[s] = *reinterpret_cast<const typename Mat<T>::Frag*>(qp + (2 * s + h) * 16);
+  }
+  const typename KTile::RowReader k_read(lane);
+  const typename VTile::ColumnReader v_read(lane);
+  f32x16 acc[D / 32];
+  clear(acc);
+  float m = -INFINITY, l = 0.f;
+  const float c2 = a.scale * LOG2E;
+  for (; t < t_end; t += NW, parity ^= 1) {
+    wait_loads();
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    if (t + NW < t_end) issue(t + NW, parity ^ 1);
+    const uint32_t buf = lds + uint32_t(parity * 2 * KTile::BYTES);
+    const int begin = span.begin(t), end = span.end(t);
+    f32x16 s;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] = 0.f;
+#pragma unroll
+    for (int st = 0; st < STEPS; ++st) s = Mat<T>::mma(k_read.get(buf, 0, st), qf[st], s);
+    const bool whole = begin + SN <= end && begin + SN - 1 <= i0 + len.shift + a.right && (t < span.n_first || begin >= i1 + len.shift - a.left);
+    if (!whole) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int key = begin + 8 * (i / 4) + 4 * h + i % 4;
+        s[i] = sees(key, end, p - a.left, p + a.right, a.sinks) ? s[i] : -INFINITY;
+      }
+    }
+    float mx = s[0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
+    const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+    const float m_new = fmaxf(m, fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * c2), ref = m_new == -INFINITY ? 0.f : m_new;
+    if (__builtin_amdgcn_ballot_w64(m_new > m)) {
+      const float alpha = __builtin_amdgcn_exp2f(m - ref);
+      m = m_new;
+      l *= alpha;
+#pragma unroll
+      for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[c][i] *= alpha;
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c2, -ref));
+      l += s[i];
+    }
+    Weights<T> w;
+    w.set(s);
+    v_read.mma(buf + KTile::BYTES, 0, w, acc);
+  }
+  const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
+  l = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+  // The waves' sums meet where the tiles were; each wave joins a share of the channels.
+  float* all = reinterpret_cast<float*>(tiles);
+  __syncthreads();
+#pragma unroll
+  for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) all[(wave * REGS + c * 16 + i) * 64 + lane] = acc[c][i];
+  if (h == 0) {
+    s_m[wave][n] = m;
+    s_l[wave][n] = l;
+  }
+  __syncthreads();
+  float top = s_m[0][n], total = 0.f, share[NW];
+#pragma unroll
+  for (int w = 1; w < NW; ++w) top = fmaxf(top, s_m[w][n]);
+  const float ref = top == -INFINITY ? 0.f : top;
+#pragma unroll
+  for (int w = 0; w < NW; ++w) {
+    share[w] = __builtin_amdgcn_exp2f(s_m[w][n] - ref);
+    total += share[w] * s_l[w][n];
+  }
+  if (!real) return;
+  const bool alone = a.splits == 1;
+  const float f = !alone ? 1.f : total == 0.f ? 0.f : 1.f / total;
+  const int64_t slot = (int64_t(at) * a.splits + split) * 32 + n;
+  char* out = alone ? a.o.at(b, qh, qi) : reinterpret_cast<char*>(a.part + slot * D);
+#pragma unroll
+  for (int g = 0; g < REGS / NW; g += 4) {
+    const int reg = wave * (REGS / NW) + g, ch = reg / 16 * 32 + reg % 16 * 2 + 4 * h;
+    float x[4] = {};
+#pragma unroll
+    for (int w = 0; w < NW; ++w)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[j] = fmaf(share[w], all[(w * REGS + reg + j) * 64 + lane], x[j]);
+    if (alone) store_four<T>(out, ch, x, f);
+    else store_four<float>(out, ch, x, f);
+  }
+  if (wave == 0 && h == 0) {
+    if (!alone) a.part_sums[slot] = make_float2(top, total);
+    else if (a.lse) a.lse[(int64_t(b) * a.heads + qh) * a.n_q + qi] = total == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * (1.f / LOG2E);
+  }
+}
+
+// Joins the splits of a row: a thread takes four channels.
+template <typename T, int D>
+__global__ void __launch_bounds__(256) window_join_kernel(WindowArgs a) {
+  constexpr int TR = D / 4, RB = 256 / TR;           // threads of a row, rows of a work-group
+  const int at = blockIdx.x / (32 / RB), n = blockIdx.x % (32 / RB) * RB + threadIdx.x / TR, ch = threadIdx.x % TR * 4;
+  const int blk = at % a.blocks, bh = at / a.blocks, b = bh / a.heads_kv, kvh = bh % a.heads_kv;
+  const Lengths len(a, b);
+  const int64_t r = int64_t(blk) * 32 + n;
+  if (r >= int64_t(len.q) * a.group) return;
+  const int qi = int(r / a.group), qh = kvh * a.group + int(r % a.group);
+  const int64_t slot = int64_t(at) * a.splits * 32 + n;
+  float top = -INFINITY, total = 0.f, x[4] = {};
+#pragma unroll 8
+  for (int s = 0; s < a.splits; ++s) top = fmaxf(top, a.part_sums[slot + s * 32].x);
+  const float ref = top == -INFINITY ? 0.f : top;
+#pragma unroll 4
+  for (int s = 0; s < a.splits; ++s) {
+    const float2 ml = a.part_sums[slot + s * 32];
+    const float4 y = *reinterpret_cast<const float4*>(a.part + (slot + s * 32) * D + ch);
+    const float share = __builtin_amdgcn_exp2f(ml.x - ref);
+    total = fmaf(share, ml.y, total);
+    x[0] = fmaf(share, y.x, x[0]);
+    x[1] = fmaf(share, y.y, x[1]);
+    x[2] = fmaf(share, y.z, x[2]);
+    x[3] = fmaf(share, y.w, x[3]);
+  }
+  store_four<T>(a.o.at(b, qh, qi), ch, x, total == 0.f ? 0.f : 1.f / total);
+  if (ch == 0 && a.lse) a.lse[(int64_t(b) * a.heads + qh) * a.n_q + qi] = total == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * (1.f / LOG2E);
+}
+
 static int check_window(const char* call, const dfs_window* w, int dtype) {
   if (!w) return fail(DFS_EINVAL, "%s: window pointer is NULL", call);
   if (dtype != DFS_F32 && dtype != DFS_BF16) return fail(DFS_EDTYPE, "%s: dtype %d is not DFS_F32 or DFS_BF16", call, dtype);
@@ -148,6 +316,28 @@ static BwdLayout bwd_layout(const dfs_window* w) {
   if (splits > rows / 256) splits = rows / 256;
   L.splits = splits < 1 ? 1 : int(splits);
   L.total = L.part + size_t(seqs) * L.tiles * (L.splits + 1) * 64 * w->d * sizeof(float);
+  return L;
+}
+
+// The forward pass over few rows: into how many work-groups the keys of 32 rows are split; 0: not split, blocks of 128 rows.  Scratch: a row of fp32
+// sums, its maximum and sum for each split.
+struct FwdLayout { size_t sums, total; int64_t blocks; int splits; };
+static FwdLayout fwd_layout(const dfs_window* w, int dtype) {
+  const int64_t seqs = int64_t(w->batch) * w->heads_kv, group = w->heads / w->heads_kv, rows = group * w->n_q;
+  FwdLayout L = {0, 0, (rows + 31) / 32 * seqs, 0};
+  if (rows > 32 && (rows + 127) / 128 * seqs >= 256) return L;
+  const int waves = dtype == DFS_F32 && w->d == 128 ? 2 : 4;
+  // keys that 32 rows see, at most
+  int64_t keys = w->n_k, reach = int64_t(w->left) + w->right + 32 / group + 1;
+  if (w->left >= 0 && w->right >= 0 && reach < keys) keys = reach + first_keys(w) < keys ? reach + first_keys(w) : keys;
+  const int64_t tiles = (keys + 31) / 32 + (first_keys(w) > 0);
+  int64_t splits = L.blocks ? SPLIT_GROUPS / L.blocks : 1, most = (tiles + waves - 1) / waves;
+  if (splits > most) splits = most;
+  L.splits = splits < 1 ? 1 : int(splits);
+  if (L.splits > 1) {
+    L.sums = align256(size_t(L.blocks) * L.splits * 32 * w->d * sizeof(float));
+    L.total = L.sums + size_t(L.blocks) * L.splits * 32 * sizeof(float2);
+  }
   return L;
 }
 
@@ -192,7 +382,7 @@ extern "C" {
 
 size_t dfs_window_workspace_bytes(const dfs_window* w, int dtype, int backward) {
   if (check_window("dfs_window_workspace_bytes", w, dtype) != DFS_OK) return 0;
-  return backward ? bwd_layout(w).total : 0;
+  return backward ? bwd_layout(w).total : fwd_layout(w, dtype).total;
 }
 
 int dfs_window_attn_fwd(const dfs_window* w, int dtype, const dfs_view* q, const dfs_view* k, const dfs_view* v, const int32_t* q_len,
@@ -202,13 +392,35 @@ int dfs_window_attn_fwd(const dfs_window* w, int dtype, const dfs_view* q, const
   int rc = fill_window(call, w, dtype, q, k, v, o, true, lse, q_len, k_len, scale, &a);
   if (rc) return rc;
   if (w->batch == 0 || w->n_q == 0) return DFS_OK;
+  const FwdLayout L = fwd_layout(w, dtype);
+  const hipStream_t st = as_stream(stream);
+  if (L.total && (!ws || (uintptr_t(ws) & 255) || ws_bytes < L.total))
+    return fail(DFS_EWORKSPACE, "%s: workspace of %zu bytes needed (256-byte aligned), got %zu", call, L.total, ws_bytes);
+  auto by_type = [&](auto f) {
+    auto d = [&](auto t) { w->d == 64 ? f(t, std::integral_constant<int, 64>{}) : f(t, std::integral_constant<int, 128>{}); };
+    dtype == DFS_BF16 ? d(uint16_t{}) : d(float{});
+  };
+  if (L.splits) {
+    a.blocks = int((int64_t(a.group) * a.n_q + 31) / 32);
+    a.splits = L.splits;
+    a.part = static_cast<float*>(ws);
+    a.part_sums = reinterpret_cast<float2*>(static_cast<char*>(ws) + L.sums);
+    by_type([&](auto t, auto d) {
+      using T = decltype(t);
+      constexpr int D = decltype(d)::value;
+      window_split_kernel<T, D><<<unsigned(L.blocks * L.splits), 64 * split_waves<T, D>(), 0, st>>>(a);
+    });
+    if (L.splits == 1) return launch_status(call);
+    if ((rc = launch_status(call))) return rc;
+    by_type([&](auto t, auto d) {
+      constexpr int D = decltype(d)::value;
+      window_join_kernel<decltype(t), D><<<unsigned(L.blocks * (D / 32)), 256, 0, st>>>(a);
+    });
+    return launch_status(call);
+  }
   a.blocks = int((int64_t(a.group) * a.n_q + 127) / 128);
   const unsigned grid = unsigned(int64_t(a.blocks) * a.batch * a.heads_kv);
-  const hipStream_t st = as_stream(stream);
-  if (dtype == DFS_BF16)
-    w->d == 64 ? window_fwd_kernel<uint16_t, 64><<<grid, 256, 0, st>>>(a) : window_fwd_kernel<uint16_t, 128><<<grid, 256, 0, st>>>(a);
-  else
-    w->d == 64 ? window_fwd_kernel<float, 64><<<grid, 256, 0, st>>>(a) : window_fwd_kernel<float, 128><<<grid, 256, 0, st>>>(a);
+  by_type([&](auto t, auto d) { window_fwd_kernel<decltype(t), decltype(d)::value><<<grid, 256, 0, st>>>(a); });
   return launch_status(call);
 }
 

@@ -361,14 +361,7 @@ __global__ void __launch_bounds__(256) window_first_sum_kernel(WindowArgs a) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) x[j] += p[j * 64];
   }
-  const float f = which ? 1.f : a.scale;
-  char* row = (which ? a.dv : a.dk).at(b, kvh, key) + ch * sizeof(T);
-  if constexpr (sizeof(T) == 2) {
-    const bf16x2 lo = {(__bf16)(x[0] * f), (__bf16)(x[1] * f)}, hi = {(__bf16)(x[2] * f), (__bf16)(x[3] * f)};
-    *reinterpret_cast<uint2*>(row) = make_uint2(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi));
-  } else {
-    *reinterpret_cast<float4*>(row) = make_float4(x[0] * f, x[1] * f, x[2] * f, x[3] * f);
-  }
+  store_four<T>((which ? a.dv : a.dk).at(b, kvh, key), ch, x, which ? 1.f : a.scale);
 }
 
 template <typename T, int D>
