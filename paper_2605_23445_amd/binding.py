@@ -113,7 +113,8 @@ def _load():
     return lib
 
 
-def _load_calls(names=("forward", "token_order", "permute", "unperm", "block_score", "select_mask", "sparse_attn", "recall")):
+def _load_calls(names=("forward", "token_order", "permute", "unperm", "block_score", "select_mask", "sparse_attn", "recall",
+                       "qk_norm_rope", "qk_norm_rope_bwd", "window_attn_fwd", "window_attn_bwd")):
     """The calls of the _calls module.  They do in native code what those of the same names do below, for plain
     arguments, and return None for what they leave to these: as the stand-ins do for every call where the module is not there or
     was built against another torch, whose classes it reads (another Python does not find it: its name holds the version)."""
@@ -125,6 +126,7 @@ def _load_calls(names=("forward", "token_order", "permute", "unperm", "block_sco
             why = "older than this file"
         else:
             _calls.set_geom_type(Geom)
+            _calls.set_layer_types(QkGeom, Window)
             return [getattr(_calls, name) for name in names]
     except ImportError as e:
         why = str(e)
@@ -135,7 +137,7 @@ def _load_calls(names=("forward", "token_order", "permute", "unperm", "block_sco
 
 _lib = _load()
 (_plain_forward, _plain_token_order, _plain_permute, _plain_unperm, _plain_block_score, _plain_select_mask, _plain_sparse_attn,
- _plain_recall) = _load_calls()
+ _plain_recall, _plain_qk_norm_rope, _plain_qk_norm_rope_bwd, _plain_window_attn_fwd, _plain_window_attn_bwd) = _load_calls()
 EXPORTS = ("dfs_geom_sizes", "dfs_workspace_bytes", "dfs_last_error", "dfs_keep_count", "dfs_hilbert_perm", "dfs_permute",
            "dfs_block_score", "dfs_select_mask", "dfs_sparse_attn_fwd", "dfs_unperm", "dfs_forward", "dfs_token_order", "dfs_recall",
            "dfs_schedule", "dfs_block_score_src", "dfs_sparse_attn_fwd_src", "dfs_attn_clock_probe", "dfs_block_score_fused", "dfs_probe_mfma", "dfs_probe_copy", "dfs_probe_read",
@@ -464,6 +466,11 @@ def dfs_qk_workspace_bytes(g: QkGeom) -> int:
 def dfs_qk_norm_rope(g: QkGeom, dtype: int, q, k, v, positions, w_q, w_k, q_out, k_out, v_out, kv_start=None):
     """Norm and rotation of q and k, a copy of v (v and v_out may be None).  With kv_start ([batch] int32) k_out and v_out are the rows of a
     cache, [batch, heads_kv, rows, d], and token i of sequence b goes to its row kv_start[b] + i."""
+    rc = _plain_qk_norm_rope(g, dtype, q, k, v, positions, w_q, w_k, q_out, k_out, v_out, kv_start)
+    if rc == 0:
+        return
+    if rc is not None:
+        _check(rc)
     shape = (g.batch, g.heads_kv, g.tokens, g.d)
     rows = g.tokens if kv_start is None else k_out.shape[2]
     pos, pos_batch = _positions(g, positions)
@@ -477,6 +484,11 @@ def dfs_qk_norm_rope(g: QkGeom, dtype: int, q, k, v, positions, w_q, w_k, q_out,
 
 def dfs_qk_norm_rope_bwd(g: QkGeom, dtype: int, q, k, positions, w_q, w_k, dq_out, dk_out, dv_out, dq, dk, dv, dw_q=None, dw_k=None, ws=None):
     """Gradients of dfs_qk_norm_rope: dq, dk, dv (dv_out and dv may be None) and those of the weights (each may be None)."""
+    rc = _plain_qk_norm_rope_bwd(g, dtype, q, k, positions, w_q, w_k, dq_out, dk_out, dv_out, dq, dk, dv, dw_q, dw_k, ws)
+    if rc == 0:
+        return
+    if rc is not None:
+        _check(rc)
     qs, ks = (g.batch, g.heads, g.tokens, g.d), (g.batch, g.heads_kv, g.tokens, g.d)
     pos, pos_batch = _positions(g, positions)
     wsp, wb = _scratch(ws)
@@ -493,6 +505,11 @@ def dfs_window_workspace_bytes(w: Window, dtype: int, backward: bool) -> int:
 
 def dfs_window_attn_fwd(w: Window, dtype: int, q, k, v, q_len, k_len, scale: float, o, lse=None, ws=None):
     """Attention over a window and a few first keys; q_len and k_len ([batch] int32) may be None, ws where it takes none."""
+    rc = _plain_window_attn_fwd(w, dtype, q, k, v, q_len, k_len, scale, o, lse, ws)
+    if rc == 0:
+        return
+    if rc is not None:
+        _check(rc)
     qs, ks = (w.batch, w.heads, w.n_q, w.d), (w.batch, w.heads_kv, w.n_k, w.d)
     wsp, wb = _scratch(ws)
     _check(_lib.dfs_window_attn_fwd(w, dtype, _view(q, dtype, *qs, "q"), _view(k, dtype, *ks, "k"), _view(v, dtype, *ks, "v"),
@@ -502,6 +519,11 @@ def dfs_window_attn_fwd(w: Window, dtype: int, q, k, v, q_len, k_len, scale: flo
 
 def dfs_window_attn_bwd(w: Window, dtype: int, q, k, v, o, lse, d_o, q_len, k_len, scale: float, dq, dk, dv, ws):
     """Gradients of dfs_window_attn_fwd from its inputs, its o and lse, and d_o, the gradient of o."""
+    rc = _plain_window_attn_bwd(w, dtype, q, k, v, o, lse, d_o, q_len, k_len, scale, dq, dk, dv, ws)
+    if rc == 0:
+        return
+    if rc is not None:
+        _check(rc)
     qs, ks = (w.batch, w.heads, w.n_q, w.d), (w.batch, w.heads_kv, w.n_k, w.d)
     wsp, wb = _scratch(ws)
     _check(_lib.dfs_window_attn_bwd(w, dtype, _view(q, dtype, *qs, "q"), _view(k, dtype, *ks, "k"), _view(v, dtype, *ks, "v"),

@@ -19,7 +19,8 @@
 
 namespace {
 
-PyObject* g_geom_type = nullptr;                    // binding.Geom, a ctypes structure with the layout of dfs_geom
+// binding.Geom, QkGeom and Window, ctypes structures with the layouts of dfs_geom, dfs_qk_geom and dfs_window
+PyObject *g_geom_type = nullptr, *g_qk_type = nullptr, *g_window_type = nullptr;
 PyObject *s_kv_idx, *s_kv_cnt, *s_mask, *s_k_head, *s_K_max;
 
 struct NotPlain {};                                 // thrown where binding.py has to look at an argument
@@ -41,17 +42,19 @@ double to_double(PyObject* x) {
   return double(to_int(x));
 }
 
-dfs_geom to_geom(PyObject* x) {
-  need(reinterpret_cast<PyObject*>(Py_TYPE(x)) == g_geom_type);
-  dfs_geom g;
+template <class S>
+S to_struct(PyObject* x, PyObject* type) {
+  need(reinterpret_cast<PyObject*>(Py_TYPE(x)) == type);
+  S s;
   Py_buffer b;
   need(PyObject_GetBuffer(x, &b, PyBUF_SIMPLE) == 0);
-  const bool fits = b.len == Py_ssize_t(sizeof(g));
-  if (fits) std::memcpy(&g, b.buf, sizeof(g));
+  const bool fits = b.len == Py_ssize_t(sizeof(s));
+  if (fits) std::memcpy(&s, b.buf, sizeof(s));
   PyBuffer_Release(&b);
   need(fits);
-  return g;
+  return s;
 }
+dfs_geom to_geom(PyObject* x) { return to_struct<dfs_geom>(x, g_geom_type); }
 
 // A contiguous device tensor of at least `numel` elements (of `type`, if one is given): its address.
 void* to_ptr(PyObject* x, at::ScalarType type, int64_t numel, int64_t* bytes = nullptr) {
@@ -233,6 +236,137 @@ PyObject* recall(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// Norm and rotation of queries and keys, and windowed attention.  As binding.py has them: tensors of given shapes on the current device, whose rows are
+// dense, None where it takes None.
+struct Here {
+  int device;
+  Here() : device(int(c10::hip::current_device())) {}
+
+  const at::Tensor& tensor(PyObject* x, at::ScalarType type) const {
+    need(THPVariable_CheckExact(x));
+    const at::Tensor& t = THPVariable_Unpack(x);
+    need(t.is_cuda() && t.get_device() == device && (type == at::ScalarType::Undefined || t.scalar_type() == type));
+    return t;
+  }
+  struct MaybeView {
+    dfs_view v;
+    bool there;
+    const dfs_view* get() const { return there ? &v : nullptr; }
+  };
+  MaybeView view(PyObject* x, int dtype, int64_t batch, int64_t heads, int64_t rows, int64_t d) const {
+    MaybeView r = {};
+    if (x == Py_None) return r;
+    const at::Tensor& t = tensor(x, tensor_type(dtype));
+    need(t.dim() == 4);
+    const auto n = t.sizes(), s = t.strides();
+    need(n[0] == batch && n[1] == heads && n[2] == rows && n[3] == d && (s[3] == 1 || t.numel() == 0));
+    r.v = dfs_view{t.data_ptr(), s[0], s[1], s[2]};
+    r.there = true;
+    return r;
+  }
+  template <class T> T* flat(PyObject* x, at::ScalarType type, int64_t numel, int64_t* bytes = nullptr) const {
+    if (x == Py_None) return nullptr;
+    const at::Tensor& t = tensor(x, type);
+    need(t.is_contiguous() && t.numel() >= numel);
+    if (bytes) *bytes = t.numel() * int64_t(t.element_size());
+    return static_cast<T*>(t.data_ptr());
+  }
+  const int32_t* positions(const dfs_qk_geom& g, PyObject* x, int64_t* pos_batch) const {
+    const at::Tensor& t = tensor(x, at::kInt);
+    const auto n = t.sizes();
+    const int64_t dim = t.dim();
+    need(t.is_contiguous() && (dim == 2 || (dim == 3 && (n[0] == 1 || n[0] == g.batch))) && n[dim - 2] == g.tokens && n[dim - 1] == g.axes);
+    *pos_batch = dim == 3 && n[0] == g.batch && g.batch > 1 ? int64_t(g.tokens) * g.axes : 0;
+    return static_cast<const int32_t*>(t.data_ptr());
+  }
+};
+
+PyObject* qk_norm_rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> int {
+    need(n == 12);
+    const auto g = to_struct<dfs_qk_geom>(a[0], g_qk_type);
+    const int dtype = to_int(a[1]);
+    const Here here;
+    const auto type = tensor_type(dtype);
+    int64_t pos_batch = 0;
+    const int32_t* pos = here.positions(g, a[5], &pos_batch);
+    const auto* start = here.flat<const int32_t>(a[11], at::kInt, g.batch);
+    int64_t rows = g.tokens;
+    if (start) {
+      const at::Tensor& cache = here.tensor(a[9], type);
+      need(cache.dim() == 4);
+      rows = cache.size(2);
+      need(rows == int64_t(int32_t(rows)));
+    }
+    const auto q = here.view(a[2], dtype, g.batch, g.heads, g.tokens, g.d), k = here.view(a[3], dtype, g.batch, g.heads_kv, g.tokens, g.d),
+               v = here.view(a[4], dtype, g.batch, g.heads_kv, g.tokens, g.d), q_out = here.view(a[8], dtype, g.batch, g.heads, g.tokens, g.d),
+               k_out = here.view(a[9], dtype, g.batch, g.heads_kv, rows, g.d), v_out = here.view(a[10], dtype, g.batch, g.heads_kv, rows, g.d);
+    const auto *w_q = here.flat<const float>(a[6], at::kFloat, g.d), *w_k = here.flat<const float>(a[7], at::kFloat, g.d);
+    void* st = stream();
+    return without_gil([&] {
+      return dfs_qk_norm_rope(&g, dtype, q.get(), k.get(), v.get(), pos, pos_batch, w_q, w_k, q_out.get(), k_out.get(), v_out.get(), start, int32_t(rows), st);
+    });
+  });
+}
+
+PyObject* qk_norm_rope_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> int {
+    need(n == 16);
+    const auto g = to_struct<dfs_qk_geom>(a[0], g_qk_type);
+    const int dtype = to_int(a[1]);
+    const Here here;
+    int64_t pos_batch = 0, ws_bytes = 0;
+    const int32_t* pos = here.positions(g, a[4], &pos_batch);
+    const auto heads = [&](PyObject* x) { return here.view(x, dtype, g.batch, g.heads, g.tokens, g.d); };
+    const auto heads_kv = [&](PyObject* x) { return here.view(x, dtype, g.batch, g.heads_kv, g.tokens, g.d); };
+    const auto q = heads(a[2]), k = heads_kv(a[3]), dq_out = heads(a[7]), dk_out = heads_kv(a[8]), dv_out = heads_kv(a[9]), dq = heads(a[10]),
+               dk = heads_kv(a[11]), dv = heads_kv(a[12]);
+    const auto *w_q = here.flat<const float>(a[5], at::kFloat, g.d), *w_k = here.flat<const float>(a[6], at::kFloat, g.d);
+    auto *dw_q = here.flat<float>(a[13], at::kFloat, g.d), *dw_k = here.flat<float>(a[14], at::kFloat, g.d);
+    void *ws = here.flat<void>(a[15], at::ScalarType::Undefined, 0, &ws_bytes), *st = stream();
+    return without_gil([&] {
+      return dfs_qk_norm_rope_bwd(&g, dtype, q.get(), k.get(), pos, pos_batch, w_q, w_k, dq_out.get(), dk_out.get(), dv_out.get(), dq.get(), dk.get(),
+                                  dv.get(), dw_q, dw_k, ws, size_t(ws_bytes), st);
+    });
+  });
+}
+
+template <bool BACK>
+PyObject* window_attn(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> int {
+    need(n == (BACK ? 15 : 11));
+    const auto w = to_struct<dfs_window>(a[0], g_window_type);
+    const int dtype = to_int(a[1]);
+    const Here here;
+    int64_t ws_bytes = 0;
+    const auto of_q = [&](PyObject* x) { return here.view(x, dtype, w.batch, w.heads, w.n_q, w.d); };
+    const auto of_k = [&](PyObject* x) { return here.view(x, dtype, w.batch, w.heads_kv, w.n_k, w.d); };
+    const auto q = of_q(a[2]), k = of_k(a[3]), v = of_k(a[4]), o = of_q(a[BACK ? 5 : 8]);
+    auto* lse = here.flat<float>(a[BACK ? 6 : 9], at::kFloat, int64_t(w.batch) * w.heads * w.n_q);
+    PyObject* const* len = a + (BACK ? 8 : 5);
+    const auto *q_len = here.flat<const int32_t>(len[0], at::kInt, w.batch), *k_len = here.flat<const int32_t>(len[1], at::kInt, w.batch);
+    const float scale = float(to_double(len[2]));
+    void *ws = here.flat<void>(a[n - 1], at::ScalarType::Undefined, 0, &ws_bytes), *st = stream();
+    if (!BACK)
+      return without_gil([&] { return dfs_window_attn_fwd(&w, dtype, q.get(), k.get(), v.get(), q_len, k_len, scale, o.get(), lse, ws, size_t(ws_bytes), st); });
+    const auto d_o = of_q(a[7]), dq = of_q(a[BACK ? 11 : 0]), dk = of_k(a[BACK ? 12 : 0]), dv = of_k(a[BACK ? 13 : 0]);
+    return without_gil([&] {
+      return dfs_window_attn_bwd(&w, dtype, q.get(), k.get(), v.get(), o.get(), lse, d_o.get(), q_len, k_len, scale, dq.get(), dk.get(), dv.get(), ws,
+                                 size_t(ws_bytes), st);
+    });
+  });
+}
+
+PyObject* set_layer_types(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n == 2) {
+    Py_INCREF(a[0]);
+    Py_INCREF(a[1]);
+    g_qk_type = a[0];
+    g_window_type = a[1];
+  }
+  Py_RETURN_NONE;
+}
+
 PyObject* set_geom_type(PyObject*, PyObject* type) {
   Py_INCREF(type);
   g_geom_type = type;
@@ -248,7 +382,12 @@ PyMethodDef methods[] = {
     {"select_mask", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(select_mask)), METH_FASTCALL, nullptr},
     {"sparse_attn", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(sparse_attn)), METH_FASTCALL, nullptr},
     {"recall", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(recall)), METH_FASTCALL, nullptr},
+    {"qk_norm_rope", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(qk_norm_rope)), METH_FASTCALL, nullptr},
+    {"qk_norm_rope_bwd", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(qk_norm_rope_bwd)), METH_FASTCALL, nullptr},
+    {"window_attn_fwd", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(window_attn<false>)), METH_FASTCALL, nullptr},
+    {"window_attn_bwd", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(window_attn<true>)), METH_FASTCALL, nullptr},
     {"set_geom_type", set_geom_type, METH_O, nullptr},
+    {"set_layer_types", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(set_layer_types)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
