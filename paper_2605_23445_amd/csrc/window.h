@@ -49,37 +49,86 @@ struct Lengths {
 __device__ __forceinline__ int min_of(int a, int b) { return a < b ? a : b; }
 __device__ __forceinline__ int max_of(int a, int b) { return a > b ? a : b; }
 
-// The tiles of KN keys that a run of queries needs.
-template <int KN>
+// Puts `none` where register i of a lane's 32 x 32 result stands for a row outside [lo, hi] (and at or behind `more`) of those from 4 (lane / 32) on.  By
+// selects and whole conditions: written with && and an assignment under `if`, the compiler (ROCm 7.2) made branches of it and lost the assignment to
+// the first register of an accumulator in one of them.
+__device__ __forceinline__ void keep(f32x16& x, int lo, int hi, float none) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i) x[i] = ((8 * (i / 4) + i % 4 >= lo) & (8 * (i / 4) + i % 4 <= hi)) ? x[i] : none;
+}
+__device__ __forceinline__ void keep(f32x16& x, int lo, int hi, int more, float none) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i)
+    x[i] = ((8 * (i / 4) + i % 4 <= hi) & ((8 * (i / 4) + i % 4 >= lo) | (8 * (i / 4) + i % 4 < more))) ? x[i] : none;
+}
+
+// The keys that a run of queries needs, in pieces of 32: the first keys that lie in front of the run's window, then the window from its first key on.
 struct Span {
-  int lo, hi, first, n_first, n;                     // window [lo, hi); first keys [0, first) in front of it; tiles of these, and of all
-  __device__ __forceinline__ Span(const WindowArgs& a, int p0, int p1, int k_len) {       // positions p0 .. p1 (none if p1 < p0)
+  int p0, p1, lo, hi, first, n_first, n;             // positions; window [lo, hi); first keys [0, first) in front of it; pieces of these, and of all
+  __device__ __forceinline__ Span(const WindowArgs& a, int p0_, int p1_, int k_len) : p0(p0_), p1(p1_) {
     lo = max_of(0, p0 - a.left);
     hi = min_of(k_len, p1 + a.right + 1);
-    if (p1 < p0 || hi < 0) hi = 0;
+    if (hi < 0) hi = 0;
     first = min_of(min_of(a.sinks, lo), hi);
     if (lo > hi) lo = hi;
-    n_first = (first + KN - 1) / KN;
-    n = n_first + (hi - lo + KN - 1) / KN;
+    n_first = (first + 31) / 32;
+    n = n_first + (hi - lo + 31) / 32;
   }
-  __device__ __forceinline__ int begin(int t) const { return t < n_first ? t * KN : lo + (t - n_first) * KN; }
-  __device__ __forceinline__ int end(int t) const { return t < n_first ? first : hi; }
-  // Whether queries at positions p0 .. p1 see none of the 32 keys from `key` on of tile t, which ends at `end`.
-  __device__ __forceinline__ bool unseen(const WindowArgs& a, int t, int key, int end, int p0, int p1) const {
-    return key >= end || key > p1 + a.right || (t >= n_first && key >= a.sinks && key + 31 < p0 - a.left);
+  __device__ __forceinline__ int begin(int i) const { return i < n_first ? i * 32 : lo + (i - n_first) * 32; }
+  __device__ __forceinline__ int end(int i) const { return i < n_first ? first : hi; }
+  // Whether every query of the run sees all 32 keys of piece i.
+  __device__ __forceinline__ bool whole(const WindowArgs& a, int i) const {
+    const int key = begin(i);
+    return key + 32 <= end(i) && key + 31 <= p0 + a.right && (i < n_first || key >= p1 - a.left);
+  }
+  // Whether queries at positions q0 .. q1 see none of piece i's keys.
+  __device__ __forceinline__ bool unseen(const WindowArgs& a, int i, int q0, int q1) const {
+    const int key = begin(i);
+    return key >= end(i) || key > q1 + a.right || (i >= n_first && key >= a.sinks && key + 31 < q0 - a.left);
+  }
+  // Puts `none` where the query at position p of this lane (half h of the wave) does not see a key of piece i; x holds keys as rows.
+  __device__ __forceinline__ void mask(const WindowArgs& a, int i, int p, int h, f32x16& x, float none) const {
+    const int key = begin(i) + 4 * h, top = min_of(end(i) - 1, p + a.right) - key;
+    if (i >= n_first && key < a.sinks) keep(x, p - a.left - key, top, a.sinks - key, none);          // the window reaches back to first keys
+    else keep(x, i < n_first ? 0 : p - a.left - key, top, none);
   }
 };
 
-// Whether a query that sees [lo, hi] and the first keys sees `key`, of those in front of `end`.  Without branches: written with && and || and an assignment
-// under `if`, the compiler (ROCm 7.2) made branches of it and lost the assignment to the first register of an accumulator in one of them.
-__device__ __forceinline__ bool sees(int key, int end, int lo, int hi, int sinks) { return (key < end) & (key <= hi) & ((key >= lo) | (key < sinks)); }
+// Which sequence's key head and which of its `blocks` work-groups a work-group is.  Consecutive work-groups go to the eight XCDs in turn: each XCD takes
+// key heads of its own, whole ones, so that those who read the same rows share an L2; with a multiple of eight the XCDs take them in turn, so that sequences
+// of different lengths spread over all.
+struct Place {
+  int blk, bh, b, kvh;
+  __device__ __forceinline__ Place(const WindowArgs& a, int id, int n) {
+    const int xcd = id % 8, slot = id / 8, seqs = n / a.blocks;
+    if (seqs % 8 == 0) {
+      blk = slot % a.blocks;
+      bh = slot / a.blocks * 8 + xcd;
+    } else {
+      const int per = n / 8, more = n % 8, at = xcd * per + (xcd < more ? xcd : more) + slot;
+      blk = at % a.blocks;
+      bh = at / a.blocks;
+    }
+    b = bh / a.heads_kv;
+    kvh = bh % a.heads_kv;
+  }
+};
 
-// Work-group of the linear order in which each XCD takes a run of its own (consecutive work-groups go to the XCDs in turn), so that those that read
-// the same rows share an L2.
-__device__ __forceinline__ int xcd_order(int id, int n) {
-  const int xcd = id % 8, slot = id / 8, per = n / 8, more = n % 8;
-  return xcd * per + (xcd < more ? xcd : more) + slot;
-}
+// What a lane of a block of rows knows of its row.
+struct Row {
+  int n, h, i0, i1, qi, qh, p;                       // column and half of the wave; first and last query of the block; query, head, position
+  bool real;
+  __device__ __forceinline__ Row(const WindowArgs& a, const Place& at, const Lengths& len, int64_t r0, int rows, int mine, int lane) {
+    n = lane & 31;
+    h = lane >> 5;
+    i0 = int(r0 / a.group);
+    i1 = int((r0 + rows - 1) / a.group);
+    real = mine < rows;
+    qi = real ? int((r0 + mine) / a.group) : i0;
+    qh = at.kvh * a.group + (real ? int((r0 + mine) % a.group) : 0);
+    p = qi + len.shift;
+  }
+};
 
 template <typename T> struct Mat;
 template <> struct Mat<uint16_t> {
@@ -122,7 +171,7 @@ struct Tile {
   static constexpr int FOLD = CH < 16 ? 16 / CH : 1;
   static_assert(ROWS * CH % (64 * NW) == 0, "a load fills 64 chunks");
   // XOR of the 16-byte chunks of a row, so that the rows which a wave reads at once lie in different banks
-  static __device__ __forceinline__ int swizzle(int row) {
+  static constexpr __host__ __device__ __forceinline__ int swizzle(int row) {
     return COLUMNS ? 4 * ((row / FOLD) % (CH < 16 ? CH / 4 : 4)) : (row / FOLD) % (CH < 16 ? CH : 16);
   }
   // Loads: byte offset of this lane's chunk of load j in a tensor whose rows are `stride` bytes apart.
@@ -135,18 +184,31 @@ struct Tile {
         off[j] = uint32_t(row) * uint32_t(stride) + uint32_t((pc ^ swizzle(row)) * 16);
       }
     }
-    // Asks for the tile whose first row is at `src`; `rows` of it are real.  lds: byte address of the tile.  The loads are asm so that the compiler does
-    // not wait for them in front of every LDS read; wait_loads() below does, in front of a barrier.
-    __device__ __forceinline__ void issue(const char* src, int rows, int64_t stride, uint32_t lds, int wave) const {
+    // `rows` real rows from `src` on, as a descriptor that gives zeros behind them.
+    static __device__ __forceinline__ u32x4 source(const char* src, int rows, int64_t stride) {
       const uint64_t at = reinterpret_cast<uint64_t>(src);
       const uint32_t bytes = rows > 0 ? uint32_t((rows < ROWS ? rows : ROWS) - 1) * uint32_t(stride) + RB : 0;
-      const u32x4 desc = {uint32_t(__builtin_amdgcn_readfirstlane(uint32_t(at))), uint32_t(__builtin_amdgcn_readfirstlane(uint32_t(at >> 32))) & 0xFFFFu,
-                          uint32_t(__builtin_amdgcn_readfirstlane(bytes)), 0x00020000u};
+      return u32x4{uint32_t(__builtin_amdgcn_readfirstlane(uint32_t(at))), uint32_t(__builtin_amdgcn_readfirstlane(uint32_t(at >> 32))) & 0xFFFFu,
+                   uint32_t(__builtin_amdgcn_readfirstlane(bytes)), 0x00020000u};
+    }
+    // Load j of a tile to `to`, where this wave's first chunk goes.  Asm, so that the compiler does not wait for it in front of every LDS read; wait_loads()
+    // below does, in front of a barrier.
+    __device__ __forceinline__ void issue_one(u32x4 desc, uint32_t to, int j) const {
+      asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                   ::"s"(to), "v"(off[j]), "s"(desc), "i"(j * NW * 1024) : "memory", "m0", "scc");
+    }
+    // Asks for a tile of two pieces of 32 rows, from src0 and src1 on.
+    struct Pair { u32x4 desc[2]; };
+    static __device__ __forceinline__ Pair pair(const char* src0, int rows0, const char* src1, int rows1, int64_t stride) {
+      return Pair{{source(src0, rows0 < 32 ? rows0 : 32, stride), source(src1 - 32 * stride, rows1 > 0 ? (rows1 < 32 ? rows1 : 32) + 32 : 0, stride)}};
+    }
+    __device__ __forceinline__ void issue_one(const Pair& p, uint32_t to, int j) const { issue_one(p.desc[j * 2 / LOADS], to, j); }
+    // Asks for the tile whose first row is at `src`; `rows` of it are real.  lds: byte address of the tile.
+    __device__ __forceinline__ void issue(const char* src, int rows, int64_t stride, uint32_t lds, int wave) const {
+      const u32x4 desc = source(src, rows, stride);
       const uint32_t to = __builtin_amdgcn_readfirstlane(lds + uint32_t(wave) * 1024);
 #pragma unroll
-      for (int j = 0; j < LOADS; ++j)
-        asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
-                     ::"s"(to), "v"(off[j]), "s"(desc), "i"(j * NW * 1024) : "memory", "m0", "scc");
+      for (int j = 0; j < LOADS; ++j) issue_one(desc, to, j);
     }
   };
   // Operand by rows: chunk 2 step + h of row 32 half + n.
@@ -177,18 +239,20 @@ struct Tile {
         at[0][1] = uint32_t(h);
       }
     }
+    // bf16: rows 16 s .. 16 s + 15 of half `half`, channels 32 c .. 32 c + 31
+    __device__ __forceinline__ bf16x8 get(uint32_t lds, int half, int s, int c) const {
+      const uint32_t p = lds + uint32_t((half * 32 + s * 16) * RB);
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<LDS_PTR(s16x4)>(p + at[c][0]));
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<LDS_PTR(s16x4)>(p + at[c][1]));
+      return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
     __device__ __forceinline__ void mma(uint32_t lds, int half, const Weights<T>& w, f32x16 (&acc)[D / 32]) const {
       if constexpr (sizeof(T) == 2) {
 #pragma unroll
         for (int s = 0; s < 2; ++s)
 #pragma unroll
-          for (int c = 0; c < D / 32; ++c) {
-            const uint32_t p = lds + uint32_t((half * 32 + s * 16) * RB);
-            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<LDS_PTR(s16x4)>(p + at[c][0]));
-            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<LDS_PTR(s16x4)>(p + at[c][1]));
-            const bf16x8 a = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-            acc[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, __builtin_bit_cast(bf16x8, w.p[s]), acc[c], 0, 0, 0);
-          }
+          for (int c = 0; c < D / 32; ++c)
+            acc[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(get(lds, half, s, c), __builtin_bit_cast(bf16x8, w.p[s]), acc[c], 0, 0, 0);
       } else {
 #pragma unroll
         for (int i = 0; i < 16; ++i) {

@@ -2,7 +2,7 @@
 //
 // The rows of a work-group are queries of ALL heads that share a key head, query by query (row r is head r % group of query r / group): a tile of
 // keys and values is brought in once for the group, and a block of rows spans fewer positions, so that it meets fewer tiles of which it
-// sees only a part.  Keys come in tiles of 64 rows: first those of the first keys that lie in front of the block's window, then the window's, from its
+// sees only a part.  Keys come in pieces of 32 rows: first those of the first keys that lie in front of the block's window, then the window's, from its
 // first key on.
 #include <float.h>
 #include <math.h>
@@ -14,72 +14,66 @@ namespace dfs {
 constexpr int KN = 64;                               // keys of a tile
 constexpr int SPLIT_GROUPS = 768;                    // work-groups that a call over few rows is split into, at most
 
-template <typename T, int D>
-__global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) window_fwd_kernel(WindowArgs a) {
+// f32: one step per tile of 64 keys, bound by the fp32 matrix instructions.
+template <int D>
+__global__ void __launch_bounds__(256, 1) window_f32_kernel(WindowArgs a) {
+  typedef float T;
   constexpr int NW = 4, BM = 32 * NW;
   using KTile = Tile<T, D, KN, NW, false>;
   using VTile = Tile<T, D, KN, NW, true>;
   constexpr int STEPS = KTile::STEPS;
   __shared__ __attribute__((aligned(1024))) char tiles[4 * KTile::BYTES];
   const uint32_t lds = uint32_t(reinterpret_cast<uintptr_t>((LDS_PTR(void))(tiles)));
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 31, h = lane >> 5;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
-  const int id = xcd_order(blockIdx.x, gridDim.x), blk = id % a.blocks, bh = id / a.blocks, b = bh / a.heads_kv, kvh = bh % a.heads_kv;
-  const Lengths len(a, b);
-  const int64_t r0 = int64_t(blk) * BM, left = int64_t(len.q) * a.group - r0;
+  const Place at(a, blockIdx.x, gridDim.x);
+  const Lengths len(a, at.b);
+  const int64_t r0 = int64_t(at.blk) * BM, left = int64_t(len.q) * a.group - r0;
   const int rows = left < BM ? int(left) : BM;
   if (rows <= 0) return;
-  const int i0 = int(r0 / a.group), i1 = int((r0 + rows - 1) / a.group);
-  const Span<KN> span(a, i0 + len.shift, i1 + len.shift, len.k);
-
-  const int64_t r = r0 + wave * 32 + n;
-  const bool real = wave * 32 + n < rows;
-  const int qi = real ? int(r / a.group) : i0, qh = kvh * a.group + (real ? int(r % a.group) : 0), p = qi + len.shift;
-  typename Mat<T>::Frag qf[STEPS];
+  const Row row(a, at, len, r0, rows, wave * 32 + (lane & 31), lane);
+  const Span span(a, row.i0 + len.shift, row.i1 + len.shift, len.k);
+  const int n_tiles = (span.n + 1) / 2;
+  Mat<T>::Frag qf[STEPS];
   {
-    const char* qp = a.q.at(b, qh, qi);
+    const char* qp = a.q.at(at.b, row.qh, row.qi);
 #pragma unroll
-    for (int s = 0; s < STEPS; ++s) qf[s] = *reinterpret_cast<const typename Mat<T>::Frag*>(qp + (2 * s + h) * 16);
+    for (int s = 0; s < STEPS; ++s) qf[s] = *reinterpret_cast<const Mat<T>::Frag*>(qp + (2 * s + row.h) * 16);
   }
-  const char *kh = a.k.at(b, kvh, 0), *vh = a.v.at(b, kvh, 0);
+  const char *kh = a.k.at(at.b, at.kvh, 0), *vh = a.v.at(at.b, at.kvh, 0);
   const typename KTile::Loader k_load(a.k.row, wave, lane);
   const typename VTile::Loader v_load(a.v.row, wave, lane);
   const typename KTile::RowReader k_read(lane);
   const typename VTile::ColumnReader v_read(lane);
+  const uint32_t to = __builtin_amdgcn_readfirstlane(lds + uint32_t(wave) * 1024);
   auto issue = [&](int t) {
-    const int begin = span.begin(t), rest = span.end(t) - begin;
-    const uint32_t buf = lds + uint32_t((t & 1) * 2 * KTile::BYTES);
-    k_load.issue(kh + int64_t(begin) * a.k.row, rest, a.k.row, buf, wave);
-    v_load.issue(vh + int64_t(begin) * a.v.row, rest, a.v.row, buf + KTile::BYTES, wave);
+    const int x = span.begin(2 * t), nx = span.end(2 * t) - x, y = span.begin(2 * t + 1), ny = span.end(2 * t + 1) - y;
+    const uint32_t buf = to + uint32_t((t & 1) * 2 * KTile::BYTES);
+    const auto ks = k_load.pair(kh + x * a.k.row, nx, kh + y * a.k.row, ny, a.k.row);
+    const auto vs = v_load.pair(vh + x * a.v.row, nx, vh + y * a.v.row, ny, a.v.row);
+#pragma unroll
+    for (int j = 0; j < KTile::LOADS; ++j) k_load.issue_one(ks, buf, j);
+#pragma unroll
+    for (int j = 0; j < KTile::LOADS; ++j) v_load.issue_one(vs, buf + KTile::BYTES, j);
   };
 
   f32x16 acc[D / 32];
   clear(acc);
   float m = -INFINITY, l = 0.f;                      // row maximum in the base-2 exponent's units, this lane's share of the row sum
   const float c2 = a.scale * LOG2E;
-  const int key_lo = p - a.left, key_hi = p + a.right;
-  if (span.n > 0) issue(0);
-  for (int t = 0; t < span.n; ++t) {
+  if (n_tiles > 0) issue(0);
+  for (int t = 0; t < n_tiles; ++t) {
     wait_loads();
     __syncthreads();                                 // tile t is there, and the buffers of tile t - 1 are free
-    if (t + 1 < span.n) issue(t + 1);
+    if (t + 1 < n_tiles) issue(t + 1);
     const uint32_t buf = lds + uint32_t((t & 1) * 2 * KTile::BYTES);
-    const int begin = span.begin(t), end = span.end(t);
-    const bool whole = begin + KN <= end && begin + KN - 1 <= i0 + len.shift + a.right && (t < span.n_first || begin >= i1 + len.shift - a.left);
     f32x16 s[2];
     clear(s);
 #pragma unroll
-    for (int half = 0; half < 2; ++half)
+    for (int half = 0; half < 2; ++half) {
 #pragma unroll
       for (int st = 0; st < STEPS; ++st) s[half] = Mat<T>::mma(k_read.get(buf, half, st), qf[st], s[half]);
-    if (!whole) {
-#pragma unroll
-      for (int half = 0; half < 2; ++half)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int key = begin + 32 * half + 8 * (i / 4) + 4 * h + i % 4;
-          s[half][i] = sees(key, end, key_lo, key_hi, a.sinks) ? s[half][i] : -INFINITY;
-        }
+      if (!span.whole(a, 2 * t + half)) span.mask(a, 2 * t + half, row.p, row.h, s[half], -INFINITY);
     }
     float mx = s[0][0];
 #pragma unroll
@@ -110,9 +104,229 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) window_fwd_kernel
   }
   const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
   l = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
-  if (!real) return;
-  store_row<T>(a.o.at(b, qh, qi), acc, l == 0.f ? 0.f : 1.f / l, h);
-  if (a.lse && h == 0) a.lse[(int64_t(b) * a.heads + qh) * a.n_q + qi] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * (1.f / LOG2E);
+  if (!row.real) return;
+  store_row<T>(a.o.at(at.b, row.qh, row.qi), acc, l == 0.f ? 0.f : 1.f / l, row.h);
+  if (a.lse && row.h == 0) a.lse[(int64_t(at.b) * a.heads + row.qh) * a.n_q + row.qi] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * (1.f / LOG2E);
+}
+
+// bf16: a pipeline over pieces of 32 keys, two to a tile.  In one stage the matrix cores form the logits of the piece two ahead and the product of the previous
+// one's weights with its values, while the vector units turn the logits of the piece between them into weights; scheduling fences keep matrix and vector
+// instructions side by side.  K(t + 2) and V(t + 1) are asked for in tile t's first stage and have a whole tile to come.
+//
+// A row's weights are taken against a reference that follows its maximum in whole numbers of the base-2 exponent and only where a logit is more than
+// HEADROOM above it, so that most pieces cost a maximum and a comparison; weights that wait for their product are then scaled by an exact power of two.
+template <int D>
+__global__ void __launch_bounds__(256, 2) window_pipe_kernel(WindowArgs a) {
+  constexpr int NW = 4, BM = 32 * NW;
+  using KTile = Tile<uint16_t, D, KN, NW, false>;
+  using VTile = Tile<uint16_t, D, KN, NW, true>;
+  constexpr int STEPS = KTile::STEPS, CS = D / 32, LOADS = KTile::LOADS, BYTES = KTile::BYTES;
+  constexpr float HEADROOM = 4.f;
+  // K of even tiles, of odd ones, V of even ones, of odd ones
+  __shared__ __attribute__((aligned(1024))) char tiles[4 * BYTES];
+  const uint32_t lds = uint32_t(reinterpret_cast<uintptr_t>((LDS_PTR(void))(tiles)));
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+
+  const Place at(a, blockIdx.x, gridDim.x);
+  const Lengths len(a, at.b);
+  const int64_t r0 = int64_t(at.blk) * BM, left = int64_t(len.q) * a.group - r0;
+  const int rows = left < BM ? int(left) : BM;
+  if (rows <= 0) return;
+  const Row row(a, at, len, r0, rows, wave * 32 + (lane & 31), lane);
+  const Span span(a, row.i0 + len.shift, row.i1 + len.shift, len.k);
+  const int n_tiles = (span.n + 1) / 2;
+
+  const char *kh = a.k.at(at.b, at.kvh, 0), *vh = a.v.at(at.b, at.kvh, 0);
+  const typename KTile::Loader k_load(a.k.row, wave, lane);
+  const typename VTile::Loader v_load(a.v.row, wave, lane);
+  const uint32_t to = __builtin_amdgcn_readfirstlane(lds + uint32_t(wave) * 1024);
+  auto source = [&](auto load, const char* base, int64_t stride, int t) {
+    const int x = span.begin(2 * t), y = span.begin(2 * t + 1);
+    return load.pair(base + x * stride, span.end(2 * t) - x, base + y * stride, span.end(2 * t + 1) - y, stride);
+  };
+  if (n_tiles > 0) {
+    const auto ks = source(k_load, kh, a.k.row, 0);
+#pragma unroll
+    for (int j = 0; j < LOADS; ++j) k_load.issue_one(ks, to, j);
+  }
+  bf16x8 qf[STEPS];
+  {
+    const char* qp = a.q.at(at.b, row.qh, row.qi);
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) qf[s] = *reinterpret_cast<const bf16x8*>(qp + (2 * s + row.h) * 16);
+  }
+  // LDS addresses of the operand reads, in the buffers of this tile's keys and values; the half tile is in the instructions' offsets
+  const typename KTile::RowReader k_read(lane);
+  typename VTile::ColumnReader v_read(lane);
+  uint32_t k_at[STEPS];
+#pragma unroll
+  for (int s = 0; s < STEPS; ++s) k_at[s] = lds + k_read.at + ((uint32_t(2 * s + row.h) ^ k_read.sw) * 16);
+#pragma unroll
+  for (int c = 0; c < CS; ++c)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) v_read.at[c][i] += lds + 2 * BYTES;
+  auto k_frag = [&](int half, int s) {
+    return __builtin_bit_cast(bf16x8, *reinterpret_cast<LDS_PTR(const u32x4)>(k_at[s] + uint32_t(half * 32 * KTile::RB)));
+  };
+
+  f32x16 acc[CS], s0, s1;
+  Weights<uint16_t> w0 = {}, w1 = {};
+  clear(acc);
+  float ref = -FLT_MAX, l = 0.f;                     // reference in the base-2 exponent's units, this lane's share of the row sum
+  const float c2 = a.scale * LOG2E;
+  auto mask = [&](int i, f32x16& s) __attribute__((always_inline)) {
+    if (__builtin_expect(span.whole(a, i), 1)) return;
+    asm volatile("");                                // keeps this a branch
+    span.mask(a, i, row.p, row.h, s, -INFINITY);
+  };
+  // In front of the weights of logits s: raises the reference of rows that outgrow it.  `wait`: weights without their product yet.
+  auto settle = [&](const f32x16& s, Weights<uint16_t>& wait) __attribute__((always_inline)) {
+    float mx = s[0];
+#pragma unroll
+    for (int i = 1; i < 15; i += 2) mx = fmaxf(mx, fmaxf(s[i], s[i + 1]));
+    mx = fmaxf(mx, s[15]);
+    const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+    mx = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * c2;
+    const bool more = mx > ref + HEADROOM;
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(more) != 0, 0)) {
+      const float top = more ? ceilf(mx) : ref;
+      float f = __builtin_amdgcn_exp2f(ref - top);
+      // The accumulators are scaled in place, by statements of their own, so that they keep one home across the branch.  The compiler does not see
+      // what these read: the waits for matrix instructions in flight (19 states at most) stand in front.
+      asm volatile("s_nop 15\n\ts_nop 3" : "+v"(f));
+      ref = top;
+      l *= f;
+#pragma unroll
+      for (int c = 0; c < CS; ++c)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          float y = acc[c][i];
+          asm volatile("v_mul_f32 %0, %1, %0" : "+v"(y) : "v"(f));
+          acc[c][i] = y;
+        }
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const bf16x2 b2 = {(__bf16)(__uint_as_float(wait.p[i][j] << 16) * f), (__bf16)(__uint_as_float(wait.p[i][j] & 0xFFFF0000u) * f)};
+          wait.p[i][j] = __builtin_bit_cast(uint32_t, b2);
+        }
+    }
+  };
+  auto weigh = [&](const f32x16& s, float (&e)[16], Weights<uint16_t>& w, int from, int to_) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = from; i < to_; ++i) {
+      l += e[i];
+      if (i % 2 == 1) {
+        const bf16x2 b2 = {(__bf16)e[i - 1], (__bf16)e[i]};
+        w.p[i / 8][i % 8 / 2] = __builtin_bit_cast(uint32_t, b2);
+      }
+    }
+  };
+  // One stage, in issue order: products of `pw` with half `half` of V, logits `sn` of half `half` of K, weights `w` of logits `s`.
+  auto stage = [&](auto half_, const Weights<uint16_t>& pw, f32x16& sn, const f32x16& s, Weights<uint16_t>& w, auto mem) __attribute__((always_inline)) {
+    constexpr int half = decltype(half_)::value, v_half = half;
+    constexpr int NF = 2 * STEPS, AHEAD = 3;         // operands: logits' and products' in turn
+    bf16x8 frag[NF];
+    auto load = [&](int f) { frag[f] = f % 2 == 0 ? k_frag(half, f / 2) : v_read.get(0, v_half, f / 2 / CS, f / 2 % CS); };
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sn[i] = 0.f;
+    float e[16];
+#pragma unroll
+    for (int f = 0; f < AHEAD; ++f) load(f);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int f = 0; f < NF; ++f) {
+      if (f + AHEAD < NF) load(f + AHEAD);
+      mem(f);
+      if (f % 2 == 0) sn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[f], qf[f / 2], sn, 0, 0, 0);
+      else acc[f / 2 % CS] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[f], __builtin_bit_cast(bf16x8, pw.p[f / 2 / CS]), acc[f / 2 % CS], 0, 0, 0);
+#pragma unroll
+      for (int i = f * 16 / NF; i < (f + 1) * 16 / NF; ++i) {
+        e[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c2, -ref));
+        asm volatile("" : "+v"(e[i]));
+      }
+      if (f > 0) weigh(s, e, w, (f - 1) * 16 / NF, f * 16 / NF);
+      if (f == NF - 1) weigh(s, e, w, f * 16 / NF, 16);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  auto all_weights = [&](const f32x16& s, Weights<uint16_t>& w) __attribute__((always_inline)) {
+    float e[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) e[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c2, -ref));
+    weigh(s, e, w, 0, 16);
+  };
+  int k_step = BYTES, v_step = BYTES;                // to the other buffer of keys, of values
+  if (n_tiles > 0) {
+    // the logits of tile 0 and the weights of its first half
+    wait_loads();
+    __syncthreads();
+    {
+      const auto vs = source(v_load, vh, a.v.row, 0);
+#pragma unroll
+      for (int j = 0; j < LOADS; ++j) v_load.issue_one(vs, to + 2 * BYTES, j);
+      if (n_tiles > 1) {
+        const auto ks = source(k_load, kh, a.k.row, 1);
+#pragma unroll
+        for (int j = 0; j < LOADS; ++j) k_load.issue_one(ks, to + BYTES, j);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s0[i] = s1[i] = 0.f;
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) {
+      s0 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_frag(0, s), qf[s], s0, 0, 0, 0);
+      s1 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k_frag(1, s), qf[s], s1, 0, 0, 0);
+    }
+    mask(0, s0);
+    mask(1, s1);
+    settle(s0, w1);
+    all_weights(s0, w0);
+    settle(s1, w0);
+  }
+  // Tile t's values and tile t + 1's keys: s1 holds the logits of tile t's second half, w0 the weights of its first.
+  for (int t = 0; t + 1 < n_tiles; ++t) {
+    wait_loads();                                    // this wave's parts of K(t + 1) and V(t) are there
+    __syncthreads();                                 // all parts are, and every wave has left K(t) and V(t - 1)
+    const int t2 = t + 2 < n_tiles ? t + 2 : t + 1;  // behind the last tile that once more, into a buffer that nothing reads
+    const auto ks = source(k_load, kh, a.k.row, t2);
+    const auto vs = source(v_load, vh, a.v.row, t + 1);
+    const uint32_t k_to = to + (t & 1 ? BYTES : 0), v_to = to + (t & 1 ? 2 : 3) * BYTES;
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) k_at[s] += k_step;
+    k_step = -k_step;
+    stage(std::integral_constant<int, 0>{}, w0, s0, s1, w1, [&](int f) {
+      constexpr int NF = 2 * STEPS;
+#pragma unroll
+      for (int j = f * 2 * LOADS / NF; j < (f + 1) * 2 * LOADS / NF; ++j) {
+        if (j < LOADS) v_load.issue_one(vs, v_to, j);
+        else k_load.issue_one(ks, k_to, j - LOADS);
+      }
+    });
+    mask(2 * t + 2, s0);
+    settle(s0, w1);
+    stage(std::integral_constant<int, 1>{}, w1, s1, s0, w0, [](int) {});
+    mask(2 * t + 3, s1);
+    settle(s1, w0);
+#pragma unroll
+    for (int c = 0; c < CS; ++c)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) v_read.at[c][i] += v_step;
+    v_step = -v_step;
+  }
+  if (n_tiles > 0) {
+    wait_loads();
+    __syncthreads();
+    v_read.mma(0, 0, w0, acc);
+    all_weights(s1, w1);
+    v_read.mma(0, 1, w1, acc);
+  }
+  const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
+  l = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+  if (!row.real) return;
+  store_row<uint16_t>(a.o.at(at.b, row.qh, row.qi), acc, l == 0.f ? 0.f : 1.f / l, row.h);
+  if (a.lse && row.h == 0) a.lse[(int64_t(at.b) * a.heads + row.qh) * a.n_q + row.qi] = l == 0.f ? -INFINITY : (ref + __builtin_amdgcn_logf(l)) * (1.f / LOG2E);
 }
 
 // Few queries: the keys of 32 rows are split over the waves of a work-group and over `splits` work-groups, and what they find is joined.  A wave's tiles of 32
@@ -136,7 +350,7 @@ __global__ void __launch_bounds__((64 * split_waves<T, D>()), 1) window_split_ke
   const int rows = left < 32 ? int(left) : 32;
   if (rows <= 0) return;
   const int i0 = int(r0 / a.group), i1 = int((r0 + rows - 1) / a.group);
-  const Span<SN> span(a, i0 + len.shift, i1 + len.shift, len.k);
+  const Span span(a, i0 + len.shift, i1 + len.shift, len.k);
   const int per = (span.n + a.splits - 1) / a.splits, t_end = min_of(span.n, (split + 1) * per);
 
   const bool real = n < rows;
@@ -170,20 +384,12 @@ __global__ void __launch_bounds__((64 * split_waves<T, D>()), 1) window_split_ke
     __builtin_amdgcn_wave_barrier();
     if (t + NW < t_end) issue(t + NW, parity ^ 1);
     const uint32_t buf = lds + uint32_t(parity * 2 * KTile::BYTES);
-    const int begin = span.begin(t), end = span.end(t);
     f32x16 s;
 #pragma unroll
     for (int i = 0; i < 16; ++i) s[i] = 0.f;
 #pragma unroll
     for (int st = 0; st < STEPS; ++st) s = Mat<T>::mma(k_read.get(buf, 0, st), qf[st], s);
-    const bool whole = begin + SN <= end && begin + SN - 1 <= i0 + len.shift + a.right && (t < span.n_first || begin >= i1 + len.shift - a.left);
-    if (!whole) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int key = begin + 8 * (i / 4) + 4 * h + i % 4;
-        s[i] = sees(key, end, p - a.left, p + a.right, a.sinks) ? s[i] : -INFINITY;
-      }
-    }
+    if (!span.whole(a, t)) span.mask(a, t, p, h, s, -INFINITY);
     float mx = s[0];
 #pragma unroll
     for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
@@ -420,7 +626,10 @@ int dfs_window_attn_fwd(const dfs_window* w, int dtype, const dfs_view* q, const
   }
   a.blocks = int((int64_t(a.group) * a.n_q + 127) / 128);
   const unsigned grid = unsigned(int64_t(a.blocks) * a.batch * a.heads_kv);
-  by_type([&](auto t, auto d) { window_fwd_kernel<decltype(t), decltype(d)::value><<<grid, 256, 0, st>>>(a); });
+  if (dtype == DFS_BF16)
+    w->d == 64 ? window_pipe_kernel<64><<<grid, 256, 0, st>>>(a) : window_pipe_kernel<128><<<grid, 256, 0, st>>>(a);
+  else
+    w->d == 64 ? window_f32_kernel<64><<<grid, 256, 0, st>>>(a) : window_f32_kernel<128><<<grid, 256, 0, st>>>(a);
   return launch_status(call);
 }
 

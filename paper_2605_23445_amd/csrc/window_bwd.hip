@@ -23,63 +23,65 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) window_dq_kernel(
   constexpr int STEPS = KTile::STEPS;
   __shared__ __attribute__((aligned(1024))) char tiles[4 * KTile::BYTES];
   const uint32_t lds = uint32_t(reinterpret_cast<uintptr_t>((LDS_PTR(void))(tiles)));
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 31, h = lane >> 5;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
-  const int id = xcd_order(blockIdx.x, gridDim.x), blk = id % a.blocks, bh = id / a.blocks, b = bh / a.heads_kv, kvh = bh % a.heads_kv;
-  const Lengths len(a, b);
-  const int64_t r0 = int64_t(blk) * BM, left = int64_t(len.q) * a.group - r0;
+  const Place at(a, blockIdx.x, gridDim.x);
+  const Lengths len(a, at.b);
+  const int64_t r0 = int64_t(at.blk) * BM, left = int64_t(len.q) * a.group - r0;
   const int rows = left < BM ? int(left) : BM;
   if (rows <= 0) return;
-  const int i0 = int(r0 / a.group), i1 = int((r0 + rows - 1) / a.group);
-  const Span<KN> span(a, i0 + len.shift, i1 + len.shift, len.k);
+  const Row row(a, at, len, r0, rows, wave * 32 + (lane & 31), lane);
+  const Span span(a, row.i0 + len.shift, row.i1 + len.shift, len.k);
+  const int n_tiles = (span.n + 1) / 2;
+  // this wave's positions
+  const int first = min_of(wave * 32, rows - 1), last = min_of(wave * 32 + 31, rows - 1);
+  const int q0 = int((r0 + first) / a.group) + len.shift, q1 = int((r0 + last) / a.group) + len.shift;
 
-  const int64_t r = r0 + wave * 32 + n;
-  const bool real = wave * 32 + n < rows;
-  const int qi = real ? int(r / a.group) : i0, qh = kvh * a.group + (real ? int(r % a.group) : 0), p = qi + len.shift;
   typename Mat<T>::Frag qf[STEPS], gf[STEPS];
-  const int64_t at = (int64_t(b) * a.heads + qh) * a.n_q + qi;
+  const int64_t sums = (int64_t(at.b) * a.heads + row.qh) * a.n_q + row.qi;
   float delta = 0.f;
   {
-    const char *qp = a.q.at(b, qh, qi), *gp = a.d_o.at(b, qh, qi), *op = a.o.at(b, qh, qi);
+    const char *qp = a.q.at(at.b, row.qh, row.qi), *gp = a.d_o.at(at.b, row.qh, row.qi), *op = a.o.at(at.b, row.qh, row.qi);
 #pragma unroll
     for (int s = 0; s < STEPS; ++s) {
-      qf[s] = *reinterpret_cast<const typename Mat<T>::Frag*>(qp + (2 * s + h) * 16);
-      gf[s] = *reinterpret_cast<const typename Mat<T>::Frag*>(gp + (2 * s + h) * 16);
-      const auto of = *reinterpret_cast<const typename Mat<T>::Frag*>(op + (2 * s + h) * 16);
+      qf[s] = *reinterpret_cast<const typename Mat<T>::Frag*>(qp + (2 * s + row.h) * 16);
+      gf[s] = *reinterpret_cast<const typename Mat<T>::Frag*>(gp + (2 * s + row.h) * 16);
+      const auto of = *reinterpret_cast<const typename Mat<T>::Frag*>(op + (2 * s + row.h) * 16);
 #pragma unroll
       for (int i = 0; i < int(16 / sizeof(T)); ++i) delta = fmaf(float(gf[s][i]), float(of[i]), delta);
     }
     const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(delta), __float_as_uint(delta), false, false);
     delta = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
-    if (real && h == 0) a.delta[at] = delta;
+    if (row.real && row.h == 0) a.delta[sums] = delta;
   }
-  const float lse = a.lse[at], ref = lse == -INFINITY ? INFINITY : lse * LOG2E;        // a row that sees nothing has weights of zero
-  const char *kh = a.k.at(b, kvh, 0), *vh = a.v.at(b, kvh, 0);
+  const float lse = a.lse[sums], ref = lse == -INFINITY ? INFINITY : lse * LOG2E;      // a row that sees nothing has weights of zero
+  const char *kh = a.k.at(at.b, at.kvh, 0), *vh = a.v.at(at.b, at.kvh, 0);
   const typename KTile::Loader k_load(a.k.row, wave, lane), v_load(a.v.row, wave, lane);
   const typename KTile::RowReader read(lane);
   const typename KTile::ColumnReader k_cols(lane);
+  const uint32_t to = __builtin_amdgcn_readfirstlane(lds + uint32_t(wave) * 1024);
   auto issue = [&](int t) {
-    const int begin = span.begin(t), rest = span.end(t) - begin;
-    const uint32_t buf = lds + uint32_t((t & 1) * 2 * KTile::BYTES);
-    k_load.issue(kh + int64_t(begin) * a.k.row, rest, a.k.row, buf, wave);
-    v_load.issue(vh + int64_t(begin) * a.v.row, rest, a.v.row, buf + KTile::BYTES, wave);
+    const int x = span.begin(2 * t), nx = span.end(2 * t) - x, y = span.begin(2 * t + 1), ny = span.end(2 * t + 1) - y;
+    const uint32_t buf = to + uint32_t((t & 1) * 2 * KTile::BYTES);
+    const auto ks = k_load.pair(kh + x * a.k.row, nx, kh + y * a.k.row, ny, a.k.row);
+    const auto vs = v_load.pair(vh + x * a.v.row, nx, vh + y * a.v.row, ny, a.v.row);
+#pragma unroll
+    for (int j = 0; j < KTile::LOADS; ++j) k_load.issue_one(ks, buf, j);
+#pragma unroll
+    for (int j = 0; j < KTile::LOADS; ++j) v_load.issue_one(vs, buf + KTile::BYTES, j);
   };
   f32x16 acc[D / 32];
   clear(acc);
   const float c2 = a.scale * LOG2E;
-  const int key_lo = p - a.left, key_hi = p + a.right;
-  const int pw0 = int((r0 + wave * 32) / a.group) + len.shift, pw1 = int((r0 + min_of(rows, wave * 32 + 32) - 1) / a.group) + len.shift;    // this wave's positions
-  if (span.n > 0) issue(0);
-  for (int t = 0; t < span.n; ++t) {
+  if (n_tiles > 0) issue(0);
+  for (int t = 0; t < n_tiles; ++t) {
     wait_loads();
     __syncthreads();
-    if (t + 1 < span.n) issue(t + 1);
+    if (t + 1 < n_tiles) issue(t + 1);
     const uint32_t buf = lds + uint32_t((t & 1) * 2 * KTile::BYTES);
-    const int begin = span.begin(t), end = span.end(t);
-    const bool whole = begin + KN <= end && begin + KN - 1 <= i0 + len.shift + a.right && (t < span.n_first || begin >= i1 + len.shift - a.left);
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
-      if (span.unseen(a, t, begin + 32 * half, end, pw0, pw1)) continue;
+      if (span.unseen(a, 2 * t + half, q0, q1)) continue;
       f32x16 s[1], g[1];
       clear(s);
       clear(g);
@@ -93,19 +95,13 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) window_dq_kernel(
         const float w = __builtin_amdgcn_exp2f(fmaf(s[0][i], c2, -ref));
         s[0][i] = w * (g[0][i] - delta);
       }
-      if (!whole) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int key = begin + 32 * half + 8 * (i / 4) + 4 * h + i % 4;
-          s[0][i] = sees(key, end, key_lo, key_hi, a.sinks) ? s[0][i] : 0.f;
-        }
-      }
+      if (!span.whole(a, 2 * t + half)) span.mask(a, 2 * t + half, row.p, row.h, s[0], 0.f);
       Weights<T> w;
       w.set(s[0]);
       k_cols.mma(buf, half, w, acc);
     }
   }
-  if (real) store_row<T>(a.dq.at(b, qh, qi), acc, a.scale, h);
+  if (row.real) store_row<T>(a.dq.at(at.b, row.qh, row.qi), acc, a.scale, row.h);
 }
 
 // Keys as columns: register i of a lane holds query row 8 (i / 4) + 4 h + i % 4 of a tile of 32, against the lane's key.  A lone wave a SIMD issues a vector
@@ -123,7 +119,8 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) window_dkv_kernel
   const uint32_t lds = uint32_t(reinterpret_cast<uintptr_t>((LDS_PTR(void))(tiles))), lds_v = lds + 4 * QTile::BYTES;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 31, h = lane >> 5;
 
-  const int id = xcd_order(blockIdx.x, gridDim.x), blk = id % a.blocks, bh = id / a.blocks, b = bh / a.heads_kv, kvh = bh % a.heads_kv;
+  const Place at(a, blockIdx.x, gridDim.x);
+  const int blk = at.blk, bh = at.bh, b = at.b, kvh = at.kvh;
   const Lengths len(a, b);
   const int j0 = blk * BN, keys = min_of(len.k - j0, BN);
   if (keys <= 0) return;
@@ -136,24 +133,36 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) window_dkv_kernel
   const typename QTile::RowReader read(lane);
   const typename QTile::ColumnReader cols(lane);
   // The tile to ask for next, and the sums of the one behind it: asked for in front of a tile's rows, which nothing waits for before the next barrier.
-  int head = kvh * a.group, begin = lo, sum_head = head, sum_begin = lo;
+  int begin = lo, sum_begin = lo;
+  const char *q_at = a.q.at(b, kvh * a.group, lo), *g_at = a.d_o.at(b, kvh * a.group, lo);
+  const int64_t q_step = QN * a.q.row, g_step = QN * a.d_o.row, q_back = a.q.head - per_head * q_step, g_back = a.d_o.head - per_head * g_step;
+  const float *lse_at = a.lse + (int64_t(b) * a.heads + kvh * a.group) * a.n_q, *delta_at = a.delta + (lse_at - a.lse);
   float ref = 0.f, delta = 0.f;
   auto issue = [&](int buf) {
     const uint32_t to = lds + uint32_t(buf * 2 * QTile::BYTES);
-    q_load.issue(a.q.at(b, head, begin), hi - begin, a.q.row, to, wave);
-    g_load.issue(a.d_o.at(b, head, begin), hi - begin, a.d_o.row, to + QTile::BYTES, wave);
+    q_load.issue(q_at, hi - begin, a.q.row, to, wave);
+    g_load.issue(g_at, hi - begin, a.d_o.row, to + QTile::BYTES, wave);
     begin += QN;
-    if (begin >= hi) { begin = lo; ++head; }
+    q_at += q_step;
+    g_at += g_step;
+    if (begin >= hi) {                               // the next head's first
+      begin = lo;
+      q_at += q_back;
+      g_at += g_back;
+    }
   };
   auto ask_sums = [&](bool more) {
     if (more && threadIdx.x < QN) {
       const int row = min_of(sum_begin + int(threadIdx.x), hi - 1);
-      const int64_t at = (int64_t(b) * a.heads + sum_head) * a.n_q + row;
-      ref = a.lse[at];
-      delta = a.delta[at];
+      ref = lse_at[row];
+      delta = delta_at[row];
     }
     sum_begin += QN;
-    if (sum_begin >= hi) { sum_begin = lo; ++sum_head; }
+    if (sum_begin >= hi) {
+      sum_begin = lo;
+      lse_at += a.n_q;
+      delta_at += a.n_q;
+    }
   };
   auto keep_sums = [&](int buf) {
     if (threadIdx.x < QN) {
@@ -185,6 +194,10 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) window_dkv_kernel
   clear(dv);
   const float c2 = a.scale * LOG2E;
   int row0 = lo;                                     // first query of this tile
+  // bf16: LDS addresses of a lane's operands by rows and by columns in this tile's queries, by rows in the values; the others follow by XOR of the chunk, so that
+  // three registers do for forty.
+  uint32_t row_at = lds + read.at + ((uint32_t(h) ^ read.sw) * 16), col_at = lds + cols.at[0][0], val_at = lds_v + uint32_t(wave * 32 * QTile::RB) + read.at + ((uint32_t(h) ^ read.sw) * 16);
+  int to_other = 2 * QTile::BYTES;
   for (int t = 0; t < tiles_n; ++t) {
     wait_loads();
     __syncthreads();
@@ -196,41 +209,119 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) window_dkv_kernel
     }
     const int p0 = row0 + len.shift;
     const bool whole = row0 + QN <= hi && keys == BN && j0 + BN - 1 <= p0 + a.right && j0 >= p0 + QN - 1 - a.left;
+    auto mask = [&](f32x16& s) __attribute__((always_inline)) {
+      if (whole) return;
+      asm volatile("");                              // keeps this a branch
+      const int p = p0 + 4 * h;
+      keep(s, key - a.right - p, min_of(key + a.left - p, hi - 1 - row0 - 4 * h), -INFINITY);
+    };
     f32x16 s, g;
 #pragma unroll
     for (int i = 0; i < 16; ++i) s[i] = g[i] = 0.f;
+    if constexpr (sizeof(T) == 2) {
+      // The four products in issue order, operands asked for AHEAD of their instruction, the weights worked out beside the second product and dS beside the
+      // third; scheduling fences keep it so, and keep operands that are asked for early from driving the accumulators to scratch.
+      constexpr int CS2 = 2 * (D / 32), NF = 2 * STEPS + 2 * CS2, AHEAD = 3;
+      bf16x8 frag[NF], vfrag[STEPS];
+      f32x4 ref4[4], delta4[4];
+      Weights<T> w, ws;
+      auto by_rows = [](uint32_t at) { return __builtin_bit_cast(bf16x8, *reinterpret_cast<LDS_PTR(const u32x4)>(at)); };
+      auto by_columns = [&](uint32_t at, int s, int c) {
+        constexpr uint32_t FAR = uint32_t(QTile::swizzle(8)) * 16;        // rows 8 further on: their chunks are swapped by this
+        const uint32_t lo = (at ^ uint32_t(64 * c)) + uint32_t(16 * s * QTile::RB), hi = (at ^ (uint32_t(64 * c) ^ FAR)) + uint32_t((16 * s + 8) * QTile::RB);
+        const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<LDS_PTR(s16x4)>(lo));
+        const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<LDS_PTR(s16x4)>(hi));
+        return __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+      };
+      auto load = [&](int f) {
+        constexpr int C = D / 32;
+        if (f < STEPS) frag[f] = by_rows(row_at ^ uint32_t(32 * f));
+        else if (f < 2 * STEPS) {
+          frag[f] = by_rows((row_at ^ uint32_t(32 * (f - STEPS))) + QTile::BYTES);
+          if (V_LDS) vfrag[f - STEPS] = by_rows(val_at ^ uint32_t(32 * (f - STEPS)));
+        } else if (f < 2 * STEPS + CS2) frag[f] = by_columns(col_at + QTile::BYTES, (f - 2 * STEPS) / C, (f - 2 * STEPS) % C);
+        else frag[f] = by_columns(col_at, (f - 2 * STEPS - CS2) / C, (f - 2 * STEPS - CS2) % C);
+      };
+      asm volatile("" : "+v"(row_at), "+v"(col_at), "+v"(val_at));
 #pragma unroll
-    for (int st = 0; st < STEPS; ++st) s = Mat<T>::mma(read.get(buf, 0, st), kf[st], s);
-    __builtin_amdgcn_sched_barrier(0);
+      for (int f = 0; f < AHEAD; ++f) load(f);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c2, -row_ref[t & 1][8 * (i / 4) + 4 * h + i % 4]));
-    if (!whole) {
+      for (int f = 0; f < NF; ++f) {
+        if (f == STEPS) {
+          mask(s);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        if (f + AHEAD < NF) load(f + AHEAD);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {                // a row's sums two slots ahead of theirs
+          if (f == STEPS + i * STEPS / 4 - 2) ref4[i] = *reinterpret_cast<const f32x4*>(&row_ref[t & 1][8 * i + 4 * h]);
+          if (f == 2 * STEPS + i * CS2 / 4 - 2) delta4[i] = *reinterpret_cast<const f32x4*>(&row_delta[t & 1][8 * i + 4 * h]);
+        }
+        if (f < STEPS) s = Mat<T>::mma(frag[f], kf[f], s);
+        else if (f < 2 * STEPS) g = Mat<T>::mma(frag[f], V_LDS ? vfrag[f - STEPS] : vf[V_LDS ? 0 : f - STEPS], g);
+        else if (f < 2 * STEPS + CS2) {
+          const int j = f - 2 * STEPS;
+          dv[j % (D / 32)] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[f], __builtin_bit_cast(bf16x8, w.p[j / (D / 32)]), dv[j % (D / 32)], 0, 0, 0);
+        } else {
+          const int j = f - 2 * STEPS - CS2;
+          dk[j % (D / 32)] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[f], __builtin_bit_cast(bf16x8, ws.p[j / (D / 32)]), dk[j % (D / 32)], 0, 0, 0);
+        }
+        if (f >= STEPS && f < 2 * STEPS) {           // 16 weights over STEPS slots
+          constexpr int E = 16 / STEPS;
+          const int j = f - STEPS;
+#pragma unroll
+          for (int i = E * j; i < E * j + E; ++i) {
+            s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c2, -ref4[i / 4][i % 4]));
+            if (i % 2) {
+              const bf16x2 pair = {(__bf16)s[i - 1], (__bf16)s[i]};
+              w.p[i / 8][i % 8 / 2] = __builtin_bit_cast(uint32_t, pair);
+            }
+          }
+        }
+        if (f >= 2 * STEPS && f < 2 * STEPS + CS2) {
+          constexpr int E = 16 / CS2;
+          const int j = f - 2 * STEPS;
+#pragma unroll
+          for (int i = E * j; i < E * j + E; ++i) {
+            g[i] = s[i] * (g[i] - delta4[i / 4][i % 4]);
+            if (i % 2) {
+              const bf16x2 pair = {(__bf16)g[i - 1], (__bf16)g[i]};
+              ws.p[i / 8][i % 8 / 2] = __builtin_bit_cast(uint32_t, pair);
+            }
+          }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    } else {
+#pragma unroll
+      for (int st = 0; st < STEPS; ++st) {
+        s = Mat<T>::mma(read.get(buf, 0, st), kf[st], s);
+        g = Mat<T>::mma(read.get(buf + QTile::BYTES, 0, st), vf[V_LDS ? 0 : st], g);
+      }
+      mask(s);
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        const int row = 8 * (i / 4) + 4 * h + i % 4, p = p0 + row;
-        s[i] = sees(key, row0 + row < hi ? NO_LIMIT : 0, p - a.left, p + a.right, 0) ? s[i] : 0.f;
+        const int row = 8 * (i / 4) + 4 * h + i % 4;
+        s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c2, -row_ref[t & 1][row]));
+        g[i] = s[i] * (g[i] - row_delta[t & 1][row]);
       }
+      Weights<T> w;
+      w.set(s);
+      cols.mma(buf + QTile::BYTES, 0, w, dv);
+      w.set(g);
+      cols.mma(buf, 0, w, dk);
     }
-    Weights<T> w;
-    w.set(s);
-    __builtin_amdgcn_sched_barrier(0);
-    cols.mma(buf + QTile::BYTES, 0, w, dv);
-    // Phases that the compiler does not mix: with operands asked for across them 64 registers went to scratch.
-    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int st = 0; st < STEPS; ++st)
-      g = Mat<T>::mma(read.get(buf + QTile::BYTES, 0, st), V_LDS ? read.get(lds_v, wave, st) : vf[V_LDS ? 0 : st], g);
-    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const float d = s[i] * (g[i] - row_delta[t & 1][8 * (i / 4) + 4 * h + i % 4]);
-      g[i] = whole ? d : s[i] == 0.f ? 0.f : d;      // where nothing is seen <do, v> may be anything
-    }
-    w.set(g);
-    __builtin_amdgcn_sched_barrier(0);
-    cols.mma(buf, 0, w, dk);
     row0 += QN;
     if (row0 >= hi) row0 = lo;
+    row_at += to_other;
+    col_at += to_other;
+    to_other = -to_other;
+  }
+  // A key that no window has in it may hold anything: its products may be too.
+  if (!(key <= len.k - 1 + a.right && key >= len.shift - a.left)) {
+    clear(dk);
+    clear(dv);
   }
   if (blk * NW + wave < a.first_tiles) {             // the first keys' part is added by window_first_sum_kernel
     float* mine = first_part(a, D, bh, blk * NW + wave, a.first_splits) + lane;

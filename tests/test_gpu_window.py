@@ -37,6 +37,15 @@ CASES = {
     "later_piece": (6, 2, 128, 70, 700, 129, 0, 4, None, [700, 390]),
     "lengths_cut": (1, 1, 64, 40, 40, 9, 0, 1, [1 << 30, -5], [41, 40]),
     "wide_group": (24, 2, 64, 33, 100, 40, 0, 2, None, None),
+    # enough blocks of 128 rows that keys are not split: the kernels of long calls
+    "blocks_causal": (64, 64, 64, 250, 250, 100, 0, 4, None, None),
+    "blocks_group_of_3": (48, 16, 128, 340, 340, 70, 0, 40, None, None),
+    "blocks_both_sides": (22, 22, 128, 700, 700, 97, 33, 5, None, None),
+    "blocks_both_sides_d64": (30, 15, 64, 600, 600, 64, 127, 70, None, None),
+    "blocks_ragged": (66, 22, 64, 470, 470, 129, 0, 4, [470, 0, 131], [470, 0, 131]),
+    "blocks_no_limits": (32, 32, 128, 480, 510, -1, -1, 0, None, None),
+    "blocks_later_piece": (60, 20, 128, 300, 900, 200, 0, 33, None, [900, 555]),
+    "blocks_more_queries_than_keys": (128, 128, 64, 140, 70, 30, 0, 2, None, [70, 3]),
 }
 
 
@@ -141,7 +150,7 @@ def test_against_the_oracle(name, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("name", ["few_tokens_group_of_3", "both_sides", "ragged", "one_token_ragged", "many_first_keys"])
+@pytest.mark.parametrize("name", ["few_tokens_group_of_3", "both_sides", "ragged", "one_token_ragged", "many_first_keys", "blocks_group_of_3"])
 def test_token_major_tensors(name, dtype):
     w, q, k, v, d_o, q_len, k_len, q_lens, k_lens = _make(name, dtype, 1, True)
     scale = 0.2
@@ -152,7 +161,8 @@ def test_token_major_tensors(name, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("name", ["one_token_ragged", "ragged", "more_queries_than_keys", "later_piece", "few_tokens_group_of_3"])
+@pytest.mark.parametrize("name", ["one_token_ragged", "ragged", "more_queries_than_keys", "later_piece", "few_tokens_group_of_3", "blocks_ragged",
+                                  "blocks_later_piece"])
 def test_what_nothing_sees_may_hold_anything(name, dtype):
     """Queries behind the last, keys and values behind the last and in front of every window: NaN and infinities there change nothing."""
     w, q, k, v, d_o, q_len, k_len, q_lens, k_lens = _make(name, dtype, 2)
