@@ -114,18 +114,23 @@ struct Place {
   }
 };
 
+// Query of row r of a sequence's key head.  Rows are counted in 31 bits.
+__device__ __forceinline__ int query_of(const WindowArgs& a, int r) { return int(uint32_t(r) / uint32_t(a.group)); }
+// Rows of a block of `most` from r0 on that are there.
+__device__ __forceinline__ int rows_of(const WindowArgs& a, const Lengths& len, int r0, int most) { return min_of(len.q * a.group - r0, most); }
+
 // What a lane of a block of rows knows of its row.
 struct Row {
   int n, h, i0, i1, qi, qh, p;                       // column and half of the wave; first and last query of the block; query, head, position
   bool real;
-  __device__ __forceinline__ Row(const WindowArgs& a, const Place& at, const Lengths& len, int64_t r0, int rows, int mine, int lane) {
+  __device__ __forceinline__ Row(const WindowArgs& a, const Place& at, const Lengths& len, int r0, int rows, int mine, int lane) {
     n = lane & 31;
     h = lane >> 5;
-    i0 = int(r0 / a.group);
-    i1 = int((r0 + rows - 1) / a.group);
+    i0 = query_of(a, r0);
+    i1 = query_of(a, r0 + rows - 1);
     real = mine < rows;
-    qi = real ? int((r0 + mine) / a.group) : i0;
-    qh = at.kvh * a.group + (real ? int((r0 + mine) % a.group) : 0);
+    qi = real ? query_of(a, r0 + mine) : i0;
+    qh = at.kvh * a.group + (real ? r0 + mine - qi * a.group : 0);
     p = qi + len.shift;
   }
 };
@@ -191,11 +196,15 @@ struct Tile {
       return u32x4{uint32_t(__builtin_amdgcn_readfirstlane(uint32_t(at))), uint32_t(__builtin_amdgcn_readfirstlane(uint32_t(at >> 32))) & 0xFFFFu,
                    uint32_t(__builtin_amdgcn_readfirstlane(bytes)), 0x00020000u};
     }
-    // Load j of a tile to `to`, where this wave's first chunk goes.  Asm, so that the compiler does not wait for it in front of every LDS read; wait_loads()
-    // below does, in front of a barrier.
-    __device__ __forceinline__ void issue_one(u32x4 desc, uint32_t to, int j) const {
-      asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
-                   ::"s"(to), "v"(off[j]), "s"(desc), "i"(j * NW * 1024) : "memory", "m0", "scc");
+    // Load j of a tile to `to`, where this wave's first chunk goes; ONCE: of rows that nothing else reads.  Asm, so that the compiler does not wait for it in
+    // front of every LDS read; wait_loads() below does, in front of a barrier.
+    template <bool ONCE = false> __device__ __forceinline__ void issue_one(u32x4 desc, uint32_t to, int j) const {
+      if (ONCE)
+        asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen nt lds"
+                     ::"s"(to), "v"(off[j]), "s"(desc), "i"(j * NW * 1024) : "memory", "m0", "scc");
+      else
+        asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                     ::"s"(to), "v"(off[j]), "s"(desc), "i"(j * NW * 1024) : "memory", "m0", "scc");
     }
     // Asks for a tile of two pieces of 32 rows, from src0 and src1 on.
     struct Pair { u32x4 desc[2]; };
@@ -204,11 +213,11 @@ struct Tile {
     }
     __device__ __forceinline__ void issue_one(const Pair& p, uint32_t to, int j) const { issue_one(p.desc[j * 2 / LOADS], to, j); }
     // Asks for the tile whose first row is at `src`; `rows` of it are real.  lds: byte address of the tile.
-    __device__ __forceinline__ void issue(const char* src, int rows, int64_t stride, uint32_t lds, int wave) const {
+    template <bool ONCE = false> __device__ __forceinline__ void issue(const char* src, int rows, int64_t stride, uint32_t lds, int wave) const {
       const u32x4 desc = source(src, rows, stride);
       const uint32_t to = __builtin_amdgcn_readfirstlane(lds + uint32_t(wave) * 1024);
 #pragma unroll
-      for (int j = 0; j < LOADS; ++j) issue_one(desc, to, j);
+      for (int j = 0; j < LOADS; ++j) issue_one<ONCE>(desc, to, j);
     }
   };
   // Operand by rows: chunk 2 step + h of row 32 half + n.
@@ -271,6 +280,18 @@ struct Tile {
 };
 
 __device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0F70); }          // vmcnt(0)
+// Until at most N of this wave's loads are on their way (they come in order), in front of reads of what the others brought.
+template <int N> __device__ __forceinline__ void wait_loads_but() {
+  __builtin_amdgcn_s_waitcnt(0x0F70 | (N & 15) | (N >> 4) << 14);
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+// Until this wave's LDS reads are done, in front of loads that overwrite what they read.
+__device__ __forceinline__ void wait_reads() {
+  __builtin_amdgcn_s_waitcnt(0xC07F);                // lgkmcnt(0)
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
 
 template <int N> __device__ __forceinline__ void clear(f32x16 (&x)[N]) {
 #pragma unroll

@@ -12,7 +12,6 @@
 namespace dfs {
 
 constexpr int KN = 64;                               // keys of a tile
-constexpr int SPLIT_GROUPS = 768;                    // work-groups that a call over few rows is split into, at most
 
 // f32: one step per tile of 64 keys, bound by the fp32 matrix instructions.
 template <int D>
@@ -28,8 +27,7 @@ __global__ void __launch_bounds__(256, 1) window_f32_kernel(WindowArgs a) {
 
   const Place at(a, blockIdx.x, gridDim.x);
   const Lengths len(a, at.b);
-  const int64_t r0 = int64_t(at.blk) * BM, left = int64_t(len.q) * a.group - r0;
-  const int rows = left < BM ? int(left) : BM;
+  const int r0 = at.blk * BM, rows = rows_of(a, len, r0, BM);
   if (rows <= 0) return;
   const Row row(a, at, len, r0, rows, wave * 32 + (lane & 31), lane);
   const Span span(a, row.i0 + len.shift, row.i1 + len.shift, len.k);
@@ -129,8 +127,7 @@ __global__ void __launch_bounds__(256, 2) window_pipe_kernel(WindowArgs a) {
 
   const Place at(a, blockIdx.x, gridDim.x);
   const Lengths len(a, at.b);
-  const int64_t r0 = int64_t(at.blk) * BM, left = int64_t(len.q) * a.group - r0;
-  const int rows = left < BM ? int(left) : BM;
+  const int r0 = at.blk * BM, rows = rows_of(a, len, r0, BM);
   if (rows <= 0) return;
   const Row row(a, at, len, r0, rows, wave * 32 + (lane & 31), lane);
   const Span span(a, row.i0 + len.shift, row.i1 + len.shift, len.k);
@@ -330,9 +327,10 @@ __global__ void __launch_bounds__(256, 2) window_pipe_kernel(WindowArgs a) {
 }
 
 // Few queries: the keys of 32 rows are split over the waves of a work-group and over `splits` work-groups, and what they find is joined.  A wave's tiles of 32
-// keys are its own, so that none waits for another before the end, and one is on its way while another is worked on: 64 KB a CU.
+// keys are its own, so that none waits for another before the end, and but for the keys or values
+// that are worked on the LDS is full of loads on their way.
 template <typename T, int D> constexpr int split_waves() { return sizeof(T) == 4 && D == 128 ? 2 : 4; }
-template <typename T, int D>
+template <typename T, int D, bool ONCE>
 __global__ void __launch_bounds__((64 * split_waves<T, D>()), 1) window_split_kernel(WindowArgs a) {
   constexpr int NW = split_waves<T, D>(), SN = 32, REGS = D / 2;
   using KTile = Tile<T, D, SN, 1, false>;
@@ -346,32 +344,43 @@ __global__ void __launch_bounds__((64 * split_waves<T, D>()), 1) window_split_ke
 
   const int split = blockIdx.x % a.splits, at = blockIdx.x / a.splits, blk = at % a.blocks, bh = at / a.blocks, b = bh / a.heads_kv, kvh = bh % a.heads_kv;
   const Lengths len(a, b);
-  const int64_t r0 = int64_t(blk) * 32, left = int64_t(len.q) * a.group - r0;
-  const int rows = left < 32 ? int(left) : 32;
+  const int r0 = blk * 32, rows = rows_of(a, len, r0, 32);
   if (rows <= 0) return;
-  const int i0 = int(r0 / a.group), i1 = int((r0 + rows - 1) / a.group);
+  const int i0 = query_of(a, r0), i1 = query_of(a, r0 + rows - 1);
   const Span span(a, i0 + len.shift, i1 + len.shift, len.k);
   const int per = (span.n + a.splits - 1) / a.splits, t_end = min_of(span.n, (split + 1) * per);
 
   const bool real = n < rows;
-  const int qi = real ? int((r0 + n) / a.group) : i0, qh = kvh * a.group + (real ? int((r0 + n) % a.group) : 0), p = qi + len.shift;
+  const int qi = real ? query_of(a, r0 + n) : i0, qh = kvh * a.group + (real ? r0 + n - qi * a.group : 0), p = qi + len.shift;
   const char *kh = a.k.at(b, kvh, 0), *vh = a.v.at(b, kvh, 0);
   const typename KTile::Loader k_load(a.k.row, 0, lane);
   const typename VTile::Loader v_load(a.v.row, 0, lane);
-  auto issue = [&](int t, int buf) {
-    const int begin = span.begin(t), rest = span.end(t) - begin;
-    const uint32_t to = lds + uint32_t(buf * 2 * KTile::BYTES);
-    k_load.issue(kh + int64_t(begin) * a.k.row, rest, a.k.row, to, 0);
-    v_load.issue(vh + int64_t(begin) * a.v.row, rest, a.v.row, to + KTile::BYTES, 0);
-  };
-  int t = split * per + wave, parity = 0;
-  if (t < t_end) issue(t, 0);
   typename Mat<T>::Frag qf[STEPS];
   {
     const char* qp = a.q.at(b, qh, qi);
 #pragma unroll
     for (int s = 0; s < STEPS; ++s) qf[s] = *reinterpret_cast<const typename Mat<T>::Frag*>(qp + (2 * s + h) * 16);
   }
+  // Two tiles' keys and values are on their way but for what is being read.  Behind the last tile nothing is asked for, by as many loads, so that the
+  // waits count the same.
+  auto ask_keys = [&](int t, int buf) {
+    const int begin = span.begin(t), rest = t < t_end ? span.end(t) - begin : 0;
+    k_load.template issue<ONCE>(kh + int64_t(begin) * a.k.row, rest, a.k.row, lds + uint32_t(buf * 2 * KTile::BYTES), 0);
+  };
+  auto ask_values = [&](int t, int buf) {
+    const int begin = span.begin(t), rest = t < t_end ? span.end(t) - begin : 0;
+    v_load.template issue<ONCE>(vh + int64_t(begin) * a.v.row, rest, a.v.row, lds + uint32_t(buf * 2 * KTile::BYTES + KTile::BYTES), 0);
+  };
+  int t = split * per + wave, parity = 0;
+  if (t < t_end) {
+    ask_keys(t, 0);
+    ask_values(t, 0);
+    ask_keys(t + NW, 1);
+    ask_values(t + NW, 1);
+  }
+  // The queries are waited for here, with what was asked for behind them, or the compiler does it in every tile and for all loads.
+#pragma unroll
+  for (int s = 0; s < STEPS; ++s) asm volatile("" : "+v"(qf[s]));
   const typename KTile::RowReader k_read(lane);
   const typename VTile::ColumnReader v_read(lane);
   f32x16 acc[D / 32];
@@ -379,16 +388,15 @@ __global__ void __launch_bounds__((64 * split_waves<T, D>()), 1) window_split_ke
   float m = -INFINITY, l = 0.f;
   const float c2 = a.scale * LOG2E;
   for (; t < t_end; t += NW, parity ^= 1) {
-    wait_loads();
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    if (t + NW < t_end) issue(t + NW, parity ^ 1);
     const uint32_t buf = lds + uint32_t(parity * 2 * KTile::BYTES);
+    wait_loads_but<3 * KTile::LOADS>();
     f32x16 s;
 #pragma unroll
     for (int i = 0; i < 16; ++i) s[i] = 0.f;
 #pragma unroll
     for (int st = 0; st < STEPS; ++st) s = Mat<T>::mma(k_read.get(buf, 0, st), qf[st], s);
+    wait_reads();
+    ask_keys(t + 2 * NW, parity);
     if (!span.whole(a, t)) span.mask(a, t, p, h, s, -INFINITY);
     float mx = s[0];
 #pragma unroll
@@ -411,8 +419,12 @@ __global__ void __launch_bounds__((64 * split_waves<T, D>()), 1) window_split_ke
     }
     Weights<T> w;
     w.set(s);
+    wait_loads_but<3 * KTile::LOADS>();
     v_read.mma(buf + KTile::BYTES, 0, w, acc);
+    wait_reads();
+    ask_values(t + 2 * NW, parity);
   }
+  wait_loads();                                      // the last ones, of nothing, still write zeros where the sums go
   const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
   l = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
   // The waves' sums meet where the tiles were; each wave joins a share of the channels.
@@ -465,9 +477,9 @@ __global__ void __launch_bounds__(256) window_join_kernel(WindowArgs a) {
   const int at = blockIdx.x / (32 / RB), n = blockIdx.x % (32 / RB) * RB + threadIdx.x / TR, ch = threadIdx.x % TR * 4;
   const int blk = at % a.blocks, bh = at / a.blocks, b = bh / a.heads_kv, kvh = bh % a.heads_kv;
   const Lengths len(a, b);
-  const int64_t r = int64_t(blk) * 32 + n;
-  if (r >= int64_t(len.q) * a.group) return;
-  const int qi = int(r / a.group), qh = kvh * a.group + int(r % a.group);
+  const int r = blk * 32 + n;
+  if (r >= len.q * a.group) return;
+  const int qi = query_of(a, r), qh = kvh * a.group + r - qi * a.group;
   const int64_t slot = int64_t(at) * a.splits * 32 + n;
   float top = -INFINITY, total = 0.f, x[4] = {};
 #pragma unroll 8
@@ -497,9 +509,9 @@ static int check_window(const char* call, const dfs_window* w, int dtype) {
     return fail(DFS_ESHAPE, "%s: heads=%d must be in [1, 65535] and a multiple of heads_kv=%d", call, w->heads, w->heads_kv);
   if (w->d != 64 && w->d != 128) return fail(DFS_ESHAPE, "%s: d=%d: head dimension must be 64 or 128", call, w->d);
   if (w->sinks < 0) return fail(DFS_ESHAPE, "%s: sinks=%d is negative", call, w->sinks);
-  // a sequence's rows and the grids' work-groups are counted in 31 bits
+  // a sequence's rows, which blocks of 128 may pass, and the grids' work-groups are counted in 31 bits
   const int64_t rows = int64_t(w->heads / w->heads_kv) * w->n_q, most = rows > w->n_k ? rows : w->n_k;
-  if (rows >= int64_t(1) << 31 || (most / 32 + 2) * w->batch * int64_t(w->heads_kv) >= int64_t(1) << 31 || int64_t(w->batch) * w->heads >= int64_t(1) << 31)
+  if (rows > int64_t(1) << 30 || (most / 32 + 2) * w->batch * int64_t(w->heads_kv) >= int64_t(1) << 31 || int64_t(w->batch) * w->heads >= int64_t(1) << 31)
     return fail(DFS_ESHAPE, "%s: batch x heads x rows too large", call);
   return DFS_OK;
 }
@@ -511,14 +523,14 @@ static int first_keys(const dfs_window* w) {
 }
 
 // Scratch of the backward pass: delta of every row, then the parts of the first keys' gradients.  The queries of 32 first keys go to as many work-groups
-// as make 512 in all, of which each of four waves has two tiles of 32 at least.
+// as make 256 in all, one a CU, of which each of four waves has two tiles of 32 at least.
 struct BwdLayout { size_t part, total; int tiles, splits; };
 static BwdLayout bwd_layout(const dfs_window* w) {
   BwdLayout L;
   const int64_t seqs = int64_t(w->batch) * w->heads_kv, rows = int64_t(w->n_q) * (w->heads / w->heads_kv);
   L.part = align256(size_t(w->batch) * w->heads * w->n_q * sizeof(float));
   L.tiles = (first_keys(w) + 31) / 32;
-  int64_t splits = seqs && L.tiles ? 512 / (seqs * L.tiles) : 1;
+  int64_t splits = seqs && L.tiles ? 256 / (seqs * L.tiles) : 1;
   if (splits > rows / 256) splits = rows / 256;
   L.splits = splits < 1 ? 1 : int(splits);
   L.total = L.part + size_t(seqs) * L.tiles * (L.splits + 1) * 64 * w->d * sizeof(float);
@@ -527,18 +539,26 @@ static BwdLayout bwd_layout(const dfs_window* w) {
 
 // The forward pass over few rows: into how many work-groups the keys of 32 rows are split; 0: not split, blocks of 128 rows.  Scratch: a row of fp32
 // sums, its maximum and sum for each split.
-struct FwdLayout { size_t sums, total; int64_t blocks; int splits; };
+struct FwdLayout { size_t sums, total; int64_t blocks; int splits; bool once; };
 static FwdLayout fwd_layout(const dfs_window* w, int dtype) {
   const int64_t seqs = int64_t(w->batch) * w->heads_kv, group = w->heads / w->heads_kv, rows = group * w->n_q;
-  FwdLayout L = {0, 0, (rows + 31) / 32 * seqs, 0};
-  if (rows > 32 && (rows + 127) / 128 * seqs >= 256) return L;
+  FwdLayout L = {0, 0, (rows + 31) / 32 * seqs, 0, false};
+  // Blocks of 128 rows need enough of them: 32 rows a work-group run four times as many, each in a quarter of the time, for as long as all run at once
+  // (us, blocks of 128 against split: 2 048 tokens x 8 heads, d = 64, 20.5 / 11.4; 1 024 x 16 heads of 4 key heads, d = 128, 14.5 / 18.3; 30 000 x 1, d = 128,
+  // 95 / 154; fp32, 1 000 x 12, d = 64, 47 / 31).
+  if (rows > 32 && (rows + 127) / 128 * seqs > (w->d == 64 ? 128 : 64)) return L;
   const int waves = dtype == DFS_F32 && w->d == 128 ? 2 : 4;
   // keys that 32 rows see, at most
   int64_t keys = w->n_k, reach = int64_t(w->left) + w->right + 32 / group + 1;
   if (w->left >= 0 && w->right >= 0 && reach < keys) keys = reach + first_keys(w) < keys ? reach + first_keys(w) : keys;
   const int64_t tiles = (keys + 31) / 32 + (first_keys(w) > 0);
-  int64_t splits = L.blocks ? SPLIT_GROUPS / L.blocks : 1, most = (tiles + waves - 1) / waves;
-  if (splits > most) splits = most;
+  // What is more than the memory-side cache holds from one step to the next passes it by (48 x 8 key heads over 4 100 keys, 0.8 GB: 156 -> 141 us).
+  L.once = rows <= 32 && tiles * 32 * seqs * w->d * 2 * elem_size(dtype) > int64_t(256) << 20;
+  // 128 work-groups draw all that memory gives (one token of 16 x 8 key heads over 4 100 keys: 6.2 TB/s); more of them cost each its start and its part, some
+  // 5 us, which only long lists are worth, where they even out lengths (4 x 8 key heads over 32 768 to 65 536 keys: 128 take 187 us, 512 131).
+  const int64_t some = 128 / (L.blocks ? L.blocks : 1), all = 512 / (L.blocks ? L.blocks : 1), own = tiles / (waves * 32);
+  int64_t splits = some < (tiles + waves - 1) / waves ? some : (tiles + waves - 1) / waves;
+  if (splits < all && splits < own) splits = all < own ? all : own;
   L.splits = splits < 1 ? 1 : int(splits);
   if (L.splits > 1) {
     L.sums = align256(size_t(L.blocks) * L.splits * 32 * w->d * sizeof(float));
@@ -614,7 +634,9 @@ int dfs_window_attn_fwd(const dfs_window* w, int dtype, const dfs_view* q, const
     by_type([&](auto t, auto d) {
       using T = decltype(t);
       constexpr int D = decltype(d)::value;
-      window_split_kernel<T, D><<<unsigned(L.blocks * L.splits), 64 * split_waves<T, D>(), 0, st>>>(a);
+      const unsigned grid = unsigned(L.blocks * L.splits);
+      if (L.once) window_split_kernel<T, D, true><<<grid, 64 * split_waves<T, D>(), 0, st>>>(a);
+      else window_split_kernel<T, D, false><<<grid, 64 * split_waves<T, D>(), 0, st>>>(a);
     });
     if (L.splits == 1) return launch_status(call);
     if ((rc = launch_status(call))) return rc;

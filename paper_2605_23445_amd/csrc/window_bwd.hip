@@ -27,15 +27,14 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) window_dq_kernel(
 
   const Place at(a, blockIdx.x, gridDim.x);
   const Lengths len(a, at.b);
-  const int64_t r0 = int64_t(at.blk) * BM, left = int64_t(len.q) * a.group - r0;
-  const int rows = left < BM ? int(left) : BM;
+  const int r0 = at.blk * BM, rows = rows_of(a, len, r0, BM);
   if (rows <= 0) return;
   const Row row(a, at, len, r0, rows, wave * 32 + (lane & 31), lane);
   const Span span(a, row.i0 + len.shift, row.i1 + len.shift, len.k);
   const int n_tiles = (span.n + 1) / 2;
   // this wave's positions
   const int first = min_of(wave * 32, rows - 1), last = min_of(wave * 32 + 31, rows - 1);
-  const int q0 = int((r0 + first) / a.group) + len.shift, q1 = int((r0 + last) / a.group) + len.shift;
+  const int q0 = query_of(a, r0 + first) + len.shift, q1 = query_of(a, r0 + last) + len.shift;
 
   typename Mat<T>::Frag qf[STEPS], gf[STEPS];
   const int64_t sums = (int64_t(at.b) * a.heads + row.qh) * a.n_q + row.qi;
@@ -447,6 +446,7 @@ __global__ void __launch_bounds__(256) window_first_sum_kernel(WindowArgs a) {
   const int key = tile * 32 + lane % 32, ch = i / 16 * 32 + i % 16 * 2 + lane / 32 * 4;
   if (key >= len.k) return;
   float x[4] = {};
+#pragma unroll 8
   for (int s = 0; s <= a.first_splits; ++s) {
     const float* p = first_part(a, D, bh, tile, s) + (which * (D / 2) + i) * 64 + lane;
 #pragma unroll
