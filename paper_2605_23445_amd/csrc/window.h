@@ -25,11 +25,13 @@ struct WindowArgs {
   View q, k, v, o, d_o, dq, dk, dv;
   float *lse, *delta;                                // [batch, heads, n_q]
   float* part;                                       // sums of a part: of the first keys' gradients, or of a row's output
+  float *key_part, *row_part;                        // backward: sums of a split's part of 32 keys' gradients, of 32 rows'
   float2* part_sums;                                 // maximum and sum of a row's part
   const int32_t *q_len, *k_len;
   int32_t batch, heads, heads_kv, group, n_q, n_k, left, right, sinks;
   int32_t blocks;                                    // work-groups of a sequence's key head
   int32_t first_tiles, first_splits;                 // backward: tiles of 32 first keys, and work-groups that share one's queries
+  int32_t key_splits, row_splits;                    // backward: work-groups that share a block of keys, a block of rows
   int32_t splits;                                    // forward: work-groups that share the keys of 32 rows
   float scale;
 };

@@ -522,18 +522,28 @@ static int first_keys(const dfs_window* w) {
   return w->sinks < w->n_k ? w->sinks : w->n_k;
 }
 
-// Scratch of the backward pass: delta of every row, then the parts of the first keys' gradients.  The queries of 32 first keys go to as many work-groups
-// as make 256 in all, one a CU, of which each of four waves has two tiles of 32 at least.
-struct BwdLayout { size_t part, total; int tiles, splits; };
+// Scratch of the backward pass: delta of every row, then parts of gradients.  The queries of 32 first keys go to as many work-groups as make 256 in all, one a
+// CU, of which each of four waves has two tiles of 32 at least.  Where blocks of 128 keys, or rows, are fewer than CUs, work-groups share one's queries,
+// or keys, four tiles each at least: 4 000 fp32 rows of one key head would else have 32 work-groups, for milliseconds.
+struct BwdLayout { size_t first, keys, rows, total; int tiles, splits, key_splits, row_splits; };
+static int share(int64_t blocks, int64_t tiles) {
+  int64_t n = blocks ? 256 / blocks : 1;
+  if (n > tiles / 4) n = tiles / 4;
+  return n < 1 ? 1 : int(n);
+}
 static BwdLayout bwd_layout(const dfs_window* w) {
   BwdLayout L;
-  const int64_t seqs = int64_t(w->batch) * w->heads_kv, rows = int64_t(w->n_q) * (w->heads / w->heads_kv);
-  L.part = align256(size_t(w->batch) * w->heads * w->n_q * sizeof(float));
+  const int64_t seqs = int64_t(w->batch) * w->heads_kv, group = w->heads / w->heads_kv, rows = group * w->n_q;
+  const int64_t reach = w->left < 0 || w->right < 0 ? int64_t(1) << 40 : int64_t(w->left) + w->right + 128;
+  const int64_t key_blocks = (int64_t(w->n_k) + 127) / 128 * seqs, row_blocks = (rows + 127) / 128 * seqs, part = 64 * w->d * sizeof(float);
   L.tiles = (first_keys(w) + 31) / 32;
-  int64_t splits = seqs && L.tiles ? 256 / (seqs * L.tiles) : 1;
-  if (splits > rows / 256) splits = rows / 256;
-  L.splits = splits < 1 ? 1 : int(splits);
-  L.total = L.part + size_t(seqs) * L.tiles * (L.splits + 1) * 64 * w->d * sizeof(float);
+  L.splits = share(seqs * L.tiles, rows / 64);
+  L.key_splits = share(key_blocks, ((reach < w->n_q ? reach : w->n_q) + 31) / 32 * group);
+  L.row_splits = share(row_blocks, ((reach < w->n_k ? reach : w->n_k) + 63) / 64);
+  L.first = align256(size_t(w->batch) * w->heads * w->n_q * sizeof(float));
+  L.keys = L.first + size_t(seqs) * L.tiles * L.splits * part;
+  L.rows = L.keys + (L.key_splits > 1 ? size_t(key_blocks) * 4 * L.key_splits : size_t(seqs) * L.tiles) * part;
+  L.total = L.rows + (L.row_splits > 1 ? size_t(row_blocks) * 4 * L.row_splits * (part / 2) : 0);
   return L;
 }
 
@@ -674,9 +684,13 @@ int dfs_window_attn_bwd(const dfs_window* w, int dtype, const dfs_view* q, const
   if (w->batch == 0) return DFS_OK;
   const BwdLayout L = bwd_layout(w);
   a.delta = static_cast<float*>(ws);
-  a.part = reinterpret_cast<float*>(static_cast<char*>(ws) + L.part);
+  a.part = reinterpret_cast<float*>(static_cast<char*>(ws) + L.first);
+  a.key_part = reinterpret_cast<float*>(static_cast<char*>(ws) + L.keys);
+  a.row_part = reinterpret_cast<float*>(static_cast<char*>(ws) + L.rows);
   a.first_tiles = L.tiles;
   a.first_splits = L.splits;
+  a.key_splits = L.key_splits;
+  a.row_splits = L.row_splits;
   return run_window_bwd(a, w->d, dtype, as_stream(stream));
 }
 

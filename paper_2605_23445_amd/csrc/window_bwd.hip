@@ -11,10 +11,17 @@
 
 namespace dfs {
 
-// Sums of dk and dv of the 32 first keys of `tile`, as a wave holds them: split `split`, the last one's place is the key blocks'.
+// Parts, as a wave holds them.  Of dk and dv of the 32 first keys of `tile`, from the queries that see them as first ones:
 __device__ __forceinline__ float* first_part(const WindowArgs& a, int d, int bh, int tile, int split) {
-  return a.part + ((int64_t(bh) * a.first_tiles + tile) * (a.first_splits + 1) + split) * 64 * d;
+  return a.part + ((int64_t(bh) * a.first_tiles + tile) * a.first_splits + split) * 64 * d;
 }
+// of dk and dv of the 32 keys of `tile`, from their windows: of all tiles where blocks of keys are shared, else of those of first keys;
+__device__ __forceinline__ float* key_part(const WindowArgs& a, int d, int bh, int tile, int split) {
+  const int tiles = a.key_splits > 1 ? (a.n_k + 127) / 128 * 4 : a.first_tiles;
+  return a.key_part + ((int64_t(bh) * tiles + tile) * a.key_splits + split) * 64 * d;
+}
+// of dq of the 32 rows of `tile`.
+__device__ __forceinline__ float* row_part(const WindowArgs& a, int d, int64_t tile, int split) { return a.row_part + (tile * a.row_splits + split) * 32 * d; }
 
 template <typename T, int D>
 __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) window_dq_kernel(WindowArgs a) {
@@ -27,11 +34,11 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) window_dq_kernel(
 
   const Place at(a, blockIdx.x, gridDim.x);
   const Lengths len(a, at.b);
-  const int r0 = at.blk * BM, rows = rows_of(a, len, r0, BM);
+  const int blk = at.blk / a.row_splits, split = at.blk - blk * a.row_splits, r0 = blk * BM, rows = rows_of(a, len, r0, BM);
   if (rows <= 0) return;
   const Row row(a, at, len, r0, rows, wave * 32 + (lane & 31), lane);
   const Span span(a, row.i0 + len.shift, row.i1 + len.shift, len.k);
-  const int n_tiles = (span.n + 1) / 2;
+  const int all_tiles = (span.n + 1) / 2, per = (all_tiles + a.row_splits - 1) / a.row_splits, t0 = split * per, n_tiles = min_of(all_tiles, t0 + per);
   // this wave's positions
   const int first = min_of(wave * 32, rows - 1), last = min_of(wave * 32 + 31, rows - 1);
   const int q0 = query_of(a, r0 + first) + len.shift, q1 = query_of(a, r0 + last) + len.shift;
@@ -51,7 +58,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) window_dq_kernel(
     }
     const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(delta), __float_as_uint(delta), false, false);
     delta = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
-    if (row.real && row.h == 0) a.delta[sums] = delta;
+    if (row.real && row.h == 0 && split == 0) a.delta[sums] = delta;
   }
   const float lse = a.lse[sums], ref = lse == -INFINITY ? INFINITY : lse * LOG2E;      // a row that sees nothing has weights of zero
   const char *kh = a.k.at(at.b, at.kvh, 0), *vh = a.v.at(at.b, at.kvh, 0);
@@ -72,8 +79,8 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) window_dq_kernel(
   f32x16 acc[D / 32];
   clear(acc);
   const float c2 = a.scale * LOG2E;
-  if (n_tiles > 0) issue(0);
-  for (int t = 0; t < n_tiles; ++t) {
+  if (t0 < n_tiles) issue(t0);
+  for (int t = t0; t < n_tiles; ++t) {
     wait_loads();
     __syncthreads();
     if (t + 1 < n_tiles) issue(t + 1);
@@ -100,7 +107,36 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) window_dq_kernel(
       k_cols.mma(buf, half, w, acc);
     }
   }
-  if (row.real) store_row<T>(a.dq.at(at.b, row.qh, row.qi), acc, a.scale, row.h);
+  if (a.row_splits > 1) {
+    float* mine = row_part(a, D, (int64_t(at.bh) * (a.blocks / a.row_splits) + blk) * NW + wave, split) + lane;
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) mine[(c * 16 + i) * 64] = acc[c][i];
+  } else if (row.real) {
+    store_row<T>(a.dq.at(at.b, row.qh, row.qi), acc, a.scale, row.h);
+  }
+}
+
+// Four channels of what a lane holds of 32 rows: register i, row lane % 32.
+__device__ __forceinline__ int channel_of(int i, int lane) { return i / 16 * 32 + i % 16 * 2 + lane / 32 * 4; }
+__device__ __forceinline__ void add_four(float (&x)[4], const float* p) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) x[j] += p[j * 64];
+}
+
+// Adds up what the work-groups that share a block of rows left.  A thread takes four channels of a row.
+template <typename T, int D>
+__global__ void __launch_bounds__(256) window_dq_sum_kernel(WindowArgs a) {
+  const int tiles = a.blocks / a.row_splits * 4, tile = blockIdx.x % tiles, bh = blockIdx.x / tiles, b = bh / a.heads_kv, kvh = bh % a.heads_kv;
+  const Lengths len(a, b);
+  const int at = blockIdx.y * 256 + threadIdx.x, lane = at % 64, i = at / 64 * 4, r = tile * 32 + lane % 32;
+  if (r >= len.q * a.group) return;
+  const int qi = query_of(a, r), qh = kvh * a.group + r - qi * a.group;
+  float x[4] = {};
+#pragma unroll 8
+  for (int s = 0; s < a.row_splits; ++s) add_four(x, row_part(a, D, blockIdx.x, s) + i * 64 + lane);
+  store_four<T>(a.dq.at(b, qh, qi), channel_of(i, lane), x, a.scale);
 }
 
 // Keys as columns: register i of a lane holds query row 8 (i / 4) + 4 h + i % 4 of a tile of 32, against the lane's key.  A lone wave a SIMD issues a vector
@@ -119,7 +155,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) window_dkv_kernel
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 31, h = lane >> 5;
 
   const Place at(a, blockIdx.x, gridDim.x);
-  const int blk = at.blk, bh = at.bh, b = at.b, kvh = at.kvh;
+  const int blk = at.blk / a.key_splits, split = at.blk - blk * a.key_splits, bh = at.bh, b = at.b, kvh = at.kvh;
   const Lengths len(a, b);
   const int j0 = blk * BN, keys = min_of(len.k - j0, BN);
   if (keys <= 0) return;
@@ -127,15 +163,18 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) window_dkv_kernel
   const bool real = wave * 32 + n < keys;
   // queries [lo, hi) see a key of this block in their window
   const int lo = max_of(0, j0 - a.right - len.shift), hi = min_of(len.q, max_of(0, j0 + keys + a.left - len.shift));
-  const int per_head = hi > lo ? (hi - lo + QN - 1) / QN : 0, tiles_n = per_head * a.group;
+  // this work-group's run of their tiles, head by head
+  const int per_head = hi > lo ? (hi - lo + QN - 1) / QN : 0, per = (per_head * a.group + a.key_splits - 1) / a.key_splits;
+  const int tiles_n = max_of(0, min_of(per, per_head * a.group - split * per)), head = per_head ? split * per / per_head : 0;
+  const int start = lo + (split * per - head * per_head) * QN;
   const typename QTile::Loader q_load(a.q.row, wave, lane), g_load(a.d_o.row, wave, lane);
   const typename QTile::RowReader read(lane);
   const typename QTile::ColumnReader cols(lane);
   // The tile to ask for next, and the sums of the one behind it: asked for in front of a tile's rows, which nothing waits for before the next barrier.
-  int begin = lo, sum_begin = lo;
-  const char *q_at = a.q.at(b, kvh * a.group, lo), *g_at = a.d_o.at(b, kvh * a.group, lo);
+  int begin = start, sum_begin = start;
+  const char *q_at = a.q.at(b, kvh * a.group + head, start), *g_at = a.d_o.at(b, kvh * a.group + head, start);
   const int64_t q_step = QN * a.q.row, g_step = QN * a.d_o.row, q_back = a.q.head - per_head * q_step, g_back = a.d_o.head - per_head * g_step;
-  const float *lse_at = a.lse + (int64_t(b) * a.heads + kvh * a.group) * a.n_q, *delta_at = a.delta + (lse_at - a.lse);
+  const float *lse_at = a.lse + (int64_t(b) * a.heads + kvh * a.group + head) * a.n_q, *delta_at = a.delta + (lse_at - a.lse);
   float ref = 0.f, delta = 0.f;
   auto issue = [&](int buf) {
     const uint32_t to = lds + uint32_t(buf * 2 * QTile::BYTES);
@@ -192,7 +231,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) window_dkv_kernel
   clear(dk);
   clear(dv);
   const float c2 = a.scale * LOG2E;
-  int row0 = lo;                                     // first query of this tile
+  int row0 = start;                                  // first query of this tile
   // bf16: LDS addresses of a lane's operands by rows and by columns in this tile's queries, by rows in the values; the others follow by XOR of the chunk, so that
   // three registers do for forty.
   uint32_t row_at = lds + read.at + ((uint32_t(h) ^ read.sw) * 16), col_at = lds + cols.at[0][0], val_at = lds_v + uint32_t(wave * 32 * QTile::RB) + read.at + ((uint32_t(h) ^ read.sw) * 16);
@@ -322,8 +361,8 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) window_dkv_kernel
     clear(dk);
     clear(dv);
   }
-  if (blk * NW + wave < a.first_tiles) {             // the first keys' part is added by window_first_sum_kernel
-    float* mine = first_part(a, D, bh, blk * NW + wave, a.first_splits) + lane;
+  if (a.key_splits > 1 || blk * NW + wave < a.first_tiles) {           // window_dkv_sum_kernel adds the parts
+    float* mine = key_part(a, D, bh, blk * NW + wave, split) + lane;
 #pragma unroll
     for (int c = 0; c < D / 32; ++c)
 #pragma unroll
@@ -437,43 +476,48 @@ __global__ void __launch_bounds__((64 * first_waves<T, D>()), 1) window_first_ke
   }
 }
 
-// Adds up what the blocks of keys and the splits left of the first keys' gradients.  A thread takes four channels of a key.
+// Adds up what the work-groups that share a block of keys left, and those of the first keys.  A thread takes four channels of a key.
 template <typename T, int D>
-__global__ void __launch_bounds__(256) window_first_sum_kernel(WindowArgs a) {
-  const int tile = blockIdx.x % a.first_tiles, bh = blockIdx.x / a.first_tiles, b = bh / a.heads_kv, kvh = bh % a.heads_kv;
+__global__ void __launch_bounds__(256) window_dkv_sum_kernel(WindowArgs a, int tiles) {
+  const int tile = blockIdx.x % tiles, bh = blockIdx.x / tiles, b = bh / a.heads_kv, kvh = bh % a.heads_kv;
   const Lengths len(a, b);
-  const int at = blockIdx.y * 256 + threadIdx.x, lane = at % 64, i = at / 64 * 4 % (D / 2), which = at / 64 * 4 / (D / 2);
-  const int key = tile * 32 + lane % 32, ch = i / 16 * 32 + i % 16 * 2 + lane / 32 * 4;
+  const int at = blockIdx.y * 256 + threadIdx.x, lane = at % 64, j = at / 64 * 4, which = j / (D / 2), key = tile * 32 + lane % 32;
   if (key >= len.k) return;
   float x[4] = {};
 #pragma unroll 8
-  for (int s = 0; s <= a.first_splits; ++s) {
-    const float* p = first_part(a, D, bh, tile, s) + (which * (D / 2) + i) * 64 + lane;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) x[j] += p[j * 64];
+  for (int s = 0; s < a.key_splits; ++s) add_four(x, key_part(a, D, bh, tile, s) + j * 64 + lane);
+  if (tile < a.first_tiles) {
+#pragma unroll 8
+    for (int s = 0; s < a.first_splits; ++s) add_four(x, first_part(a, D, bh, tile, s) + j * 64 + lane);
   }
-  store_four<T>((which ? a.dv : a.dk).at(b, kvh, key), ch, x, which ? 1.f : a.scale);
+  store_four<T>((which ? a.dv : a.dk).at(b, kvh, key), channel_of(j % (D / 2), lane), x, which ? 1.f : a.scale);
 }
 
 template <typename T, int D>
 static int launch(const WindowArgs& args, hipStream_t st) {
   WindowArgs a = args;
   const int64_t seqs = int64_t(a.batch) * a.heads_kv;
+  const char* call = "dfs_window_attn_bwd";
   if (a.n_q > 0) {
-    a.blocks = int((int64_t(a.group) * a.n_q + 127) / 128);
+    a.blocks = (a.group * a.n_q + 127) / 128 * a.row_splits;
     window_dq_kernel<T, D><<<unsigned(a.blocks * seqs), 256, 0, st>>>(a);
-    if (int rc = launch_status("dfs_window_attn_bwd")) return rc;
+    if (int rc = launch_status(call)) return rc;
+    if (a.row_splits > 1) {
+      window_dq_sum_kernel<T, D><<<dim3(unsigned(a.blocks / a.row_splits * 4 * seqs), D / 32), 256, 0, st>>>(a);
+      if (int rc = launch_status(call)) return rc;
+    }
   }
   if (a.n_k == 0) return DFS_OK;
-  a.blocks = (a.n_k + 127) / 128;
+  const int key_blocks = (a.n_k + 127) / 128, tiles = a.key_splits > 1 ? key_blocks * 4 : a.first_tiles;
+  a.blocks = key_blocks * a.key_splits;
   window_dkv_kernel<T, D><<<unsigned(a.blocks * seqs), 256, 0, st>>>(a);
-  if (int rc = launch_status("dfs_window_attn_bwd")) return rc;
+  if (int rc = launch_status(call)) return rc;
   if (a.first_tiles > 0) {
     window_first_kernel<T, D><<<unsigned(seqs * a.first_tiles * a.first_splits), 64 * first_waves<T, D>(), 0, st>>>(a);
-    if (int rc = launch_status("dfs_window_attn_bwd")) return rc;
-    window_first_sum_kernel<T, D><<<dim3(unsigned(seqs * a.first_tiles), D / 16), 256, 0, st>>>(a);
+    if (int rc = launch_status(call)) return rc;
   }
-  return launch_status("dfs_window_attn_bwd");
+  if (tiles > 0) window_dkv_sum_kernel<T, D><<<dim3(unsigned(seqs * tiles), D / 16), 256, 0, st>>>(a, tiles);
+  return launch_status(call);
 }
 
 int run_window_bwd(const WindowArgs& a, int d, int dtype, hipStream_t st) {

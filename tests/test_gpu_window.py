@@ -37,6 +37,9 @@ CASES = {
     "later_piece": (6, 2, 128, 70, 700, 129, 0, 4, None, [700, 390]),
     "lengths_cut": (1, 1, 64, 40, 40, 9, 0, 1, [1 << 30, -5], [41, 40]),
     "wide_group": (24, 2, 64, 33, 100, 40, 0, 2, None, None),
+    # long lists for few work-groups: their parts are added up
+    "long_one_head": (1, 1, 64, 1500, 1500, 700, 0, 4, None, None),
+    "long_group_of_5": (5, 1, 128, 700, 1100, 600, 50, 40, [700, 333], [1100, 1024]),
     # enough blocks of 128 rows that keys are not split: the kernels of long calls
     "blocks_causal": (64, 64, 64, 250, 250, 100, 0, 4, None, None),
     "blocks_group_of_3": (48, 16, 128, 340, 340, 70, 0, 40, None, None),
@@ -150,7 +153,7 @@ def test_against_the_oracle(name, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("name", ["few_tokens_group_of_3", "both_sides", "ragged", "one_token_ragged", "many_first_keys", "blocks_group_of_3"])
+@pytest.mark.parametrize("name", ["few_tokens_group_of_3", "both_sides", "ragged", "one_token_ragged", "many_first_keys", "blocks_group_of_3", "long_group_of_5"])
 def test_token_major_tensors(name, dtype):
     w, q, k, v, d_o, q_len, k_len, q_lens, k_lens = _make(name, dtype, 1, True)
     scale = 0.2
@@ -162,7 +165,7 @@ def test_token_major_tensors(name, dtype):
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("name", ["one_token_ragged", "ragged", "more_queries_than_keys", "later_piece", "few_tokens_group_of_3", "blocks_ragged",
-                                  "blocks_later_piece"])
+                                  "blocks_later_piece", "long_group_of_5"])
 def test_what_nothing_sees_may_hold_anything(name, dtype):
     """Queries behind the last, keys and values behind the last and in front of every window: NaN and infinities there change nothing."""
     w, q, k, v, d_o, q_len, k_len, q_lens, k_lens = _make(name, dtype, 2)
