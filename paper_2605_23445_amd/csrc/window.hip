@@ -14,9 +14,8 @@ namespace dfs {
 constexpr int KN = 64;                               // keys of a tile
 
 // f32: one step per tile of 64 keys, bound by the fp32 matrix instructions.
-template <int D>
-__global__ void __launch_bounds__(256, 1) window_f32_kernel(WindowArgs a) {
-  typedef float T;
+template <typename T, int D>
+__global__ void __launch_bounds__(256, sizeof(T) == 2 ? 4 : 1) window_plain_kernel(WindowArgs a) {
   constexpr int NW = 4, BM = 32 * NW;
   using KTile = Tile<T, D, KN, NW, false>;
   using VTile = Tile<T, D, KN, NW, true>;
@@ -32,11 +31,11 @@ __global__ void __launch_bounds__(256, 1) window_f32_kernel(WindowArgs a) {
   const Row row(a, at, len, r0, rows, wave * 32 + (lane & 31), lane);
   const Span span(a, row.i0 + len.shift, row.i1 + len.shift, len.k);
   const int n_tiles = (span.n + 1) / 2;
-  Mat<T>::Frag qf[STEPS];
+  typename Mat<T>::Frag qf[STEPS];
   {
     const char* qp = a.q.at(at.b, row.qh, row.qi);
 #pragma unroll
-    for (int s = 0; s < STEPS; ++s) qf[s] = *reinterpret_cast<const Mat<T>::Frag*>(qp + (2 * s + row.h) * 16);
+    for (int s = 0; s < STEPS; ++s) qf[s] = *reinterpret_cast<const typename Mat<T>::Frag*>(qp + (2 * s + row.h) * 16);
   }
   const char *kh = a.k.at(at.b, at.kvh, 0), *vh = a.v.at(at.b, at.kvh, 0);
   const typename KTile::Loader k_load(a.k.row, wave, lane);
@@ -111,15 +110,15 @@ __global__ void __launch_bounds__(256, 1) window_f32_kernel(WindowArgs a) {
 // one's weights with its values, while the vector units turn the logits of the piece between them into weights; scheduling fences keep matrix and vector
 // instructions side by side.  K(t + 2) and V(t + 1) are asked for in tile t's first stage and have a whole tile to come.
 //
-// A row's weights are taken against a reference that follows its maximum in whole numbers of the base-2 exponent and only where a logit is more than
-// HEADROOM above it, so that most pieces cost a maximum and a comparison; weights that wait for their product are then scaled by an exact power of two.
+// A row's weights are taken against a reference that is its largest logit's so far to start with and moves where weights have become large: the sums of a
+// lane's weights, which are needed anyway, tell at the cost of a comparison.
 template <int D>
 __global__ void __launch_bounds__(256, 2) window_pipe_kernel(WindowArgs a) {
   constexpr int NW = 4, BM = 32 * NW;
   using KTile = Tile<uint16_t, D, KN, NW, false>;
   using VTile = Tile<uint16_t, D, KN, NW, true>;
   constexpr int STEPS = KTile::STEPS, CS = D / 32, LOADS = KTile::LOADS, BYTES = KTile::BYTES;
-  constexpr float HEADROOM = 4.f;
+  constexpr float SUM_LIMIT = 64.f;                  // of the sixteen weights of a piece that a lane works out
   // K of even tiles, of odd ones, V of even ones, of odd ones
   __shared__ __attribute__((aligned(1024))) char tiles[4 * BYTES];
   const uint32_t lds = uint32_t(reinterpret_cast<uintptr_t>((LDS_PTR(void))(tiles)));
@@ -176,17 +175,34 @@ __global__ void __launch_bounds__(256, 2) window_pipe_kernel(WindowArgs a) {
     asm volatile("");                                // keeps this a branch
     span.mask(a, i, row.p, row.h, s, -INFINITY);
   };
-  // In front of the weights of logits s: raises the reference of rows that outgrow it.  `wait`: weights without their product yet.
-  auto settle = [&](const f32x16& s, Weights<uint16_t>& wait) __attribute__((always_inline)) {
-    float mx = s[0];
+  // The weights of logits s as they are packed, `from` .. `to_` of a lane's 16, and their sum.
+  auto weigh = [&](float (&e)[16], Weights<uint16_t>& w, float& sum, int from, int to_) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 1; i < 15; i += 2) mx = fmaxf(mx, fmaxf(s[i], s[i + 1]));
-    mx = fmaxf(mx, s[15]);
-    const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
-    mx = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * c2;
-    const bool more = mx > ref + HEADROOM;
-    if (__builtin_expect(__builtin_amdgcn_ballot_w64(more) != 0, 0)) {
-      const float top = more ? ceilf(mx) : ref;
+    for (int i = from; i < to_; ++i) {
+      sum += e[i];
+      if (i % 2 == 1) {
+        const bf16x2 b2 = {(__bf16)e[i - 1], (__bf16)e[i]};
+        w.p[i / 8][i % 8 / 2] = __builtin_bit_cast(uint32_t, b2);
+      }
+    }
+  };
+  auto all_weights = [&](const f32x16& s, Weights<uint16_t>& w, float& sum) __attribute__((always_inline)) {
+    float e[16];
+    sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) e[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c2, -ref));
+    weigh(e, w, sum, 0, 16);
+  };
+  // Behind the weights `w` of logits s, whose sum is `sum`: where a lane's are too large, rows that have grown raise their reference and the weights are
+  // worked out again.  (A NaN does not pass the comparison.)
+  auto settle = [&](const f32x16& s, Weights<uint16_t>& w, float sum) __attribute__((always_inline)) {
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(sum <= SUM_LIMIT)) != 0, 0)) {
+      float mx = s[0];
+#pragma unroll
+      for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
+      const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+      mx = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * c2;
+      const float top = mx > ref ? mx : ref;         // not fmaxf: a NaN leaves the reference where it is
       float f = __builtin_amdgcn_exp2f(ref - top);
       // The accumulators are scaled in place, by statements of their own, so that they keep one home across the branch.  The compiler does not see
       // what these read: the waits for matrix instructions in flight (19 states at most) stand in front.
@@ -201,27 +217,12 @@ __global__ void __launch_bounds__(256, 2) window_pipe_kernel(WindowArgs a) {
           asm volatile("v_mul_f32 %0, %1, %0" : "+v"(y) : "v"(f));
           acc[c][i] = y;
         }
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const bf16x2 b2 = {(__bf16)(__uint_as_float(wait.p[i][j] << 16) * f), (__bf16)(__uint_as_float(wait.p[i][j] & 0xFFFF0000u) * f)};
-          wait.p[i][j] = __builtin_bit_cast(uint32_t, b2);
-        }
+      all_weights(s, w, sum);
     }
-  };
-  auto weigh = [&](const f32x16& s, float (&e)[16], Weights<uint16_t>& w, int from, int to_) __attribute__((always_inline)) {
-#pragma unroll
-    for (int i = from; i < to_; ++i) {
-      l += e[i];
-      if (i % 2 == 1) {
-        const bf16x2 b2 = {(__bf16)e[i - 1], (__bf16)e[i]};
-        w.p[i / 8][i % 8 / 2] = __builtin_bit_cast(uint32_t, b2);
-      }
-    }
+    l += sum;
   };
   // One stage, in issue order: products of `pw` with half `half` of V, logits `sn` of half `half` of K, weights `w` of logits `s`.
-  auto stage = [&](auto half_, const Weights<uint16_t>& pw, f32x16& sn, const f32x16& s, Weights<uint16_t>& w, auto mem) __attribute__((always_inline)) {
+  auto stage = [&](auto half_, const Weights<uint16_t>& pw, f32x16& sn, const f32x16& s, Weights<uint16_t>& w, float& sum, auto mem) __attribute__((always_inline)) {
     constexpr int half = decltype(half_)::value, v_half = half;
     constexpr int NF = 2 * STEPS, AHEAD = 3;         // operands: logits' and products' in turn
     bf16x8 frag[NF];
@@ -229,6 +230,7 @@ __global__ void __launch_bounds__(256, 2) window_pipe_kernel(WindowArgs a) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) sn[i] = 0.f;
     float e[16];
+    sum = 0.f;
 #pragma unroll
     for (int f = 0; f < AHEAD; ++f) load(f);
     __builtin_amdgcn_sched_barrier(0);
@@ -243,16 +245,10 @@ __global__ void __launch_bounds__(256, 2) window_pipe_kernel(WindowArgs a) {
         e[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c2, -ref));
         asm volatile("" : "+v"(e[i]));
       }
-      if (f > 0) weigh(s, e, w, (f - 1) * 16 / NF, f * 16 / NF);
-      if (f == NF - 1) weigh(s, e, w, f * 16 / NF, 16);
+      if (f > 0) weigh(e, w, sum, (f - 1) * 16 / NF, f * 16 / NF);
+      if (f == NF - 1) weigh(e, w, sum, f * 16 / NF, 16);
       __builtin_amdgcn_sched_barrier(0);
     }
-  };
-  auto all_weights = [&](const f32x16& s, Weights<uint16_t>& w) __attribute__((always_inline)) {
-    float e[16];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) e[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c2, -ref));
-    weigh(s, e, w, 0, 16);
   };
   int k_step = BYTES, v_step = BYTES;                // to the other buffer of keys, of values
   if (n_tiles > 0) {
@@ -278,9 +274,9 @@ __global__ void __launch_bounds__(256, 2) window_pipe_kernel(WindowArgs a) {
     }
     mask(0, s0);
     mask(1, s1);
-    settle(s0, w1);
-    all_weights(s0, w0);
-    settle(s1, w0);
+    float sum;
+    all_weights(s0, w0, sum);
+    settle(s0, w0, sum);
   }
   // Tile t's values and tile t + 1's keys: s1 holds the logits of tile t's second half, w0 the weights of its first.
   for (int t = 0; t + 1 < n_tiles; ++t) {
@@ -293,7 +289,8 @@ __global__ void __launch_bounds__(256, 2) window_pipe_kernel(WindowArgs a) {
 #pragma unroll
     for (int s = 0; s < STEPS; ++s) k_at[s] += k_step;
     k_step = -k_step;
-    stage(std::integral_constant<int, 0>{}, w0, s0, s1, w1, [&](int f) {
+    float sum;
+    stage(std::integral_constant<int, 0>{}, w0, s0, s1, w1, sum, [&](int f) {
       constexpr int NF = 2 * STEPS;
 #pragma unroll
       for (int j = f * 2 * LOADS / NF; j < (f + 1) * 2 * LOADS / NF; ++j) {
@@ -301,11 +298,11 @@ __global__ void __launch_bounds__(256, 2) window_pipe_kernel(WindowArgs a) {
         else k_load.issue_one(ks, k_to, j - LOADS);
       }
     });
+    settle(s1, w1, sum);
     mask(2 * t + 2, s0);
-    settle(s0, w1);
-    stage(std::integral_constant<int, 1>{}, w1, s1, s0, w0, [](int) {});
+    stage(std::integral_constant<int, 1>{}, w1, s1, s0, w0, sum, [](int) {});
+    settle(s0, w0, sum);
     mask(2 * t + 3, s1);
-    settle(s1, w0);
 #pragma unroll
     for (int c = 0; c < CS; ++c)
 #pragma unroll
@@ -316,7 +313,9 @@ __global__ void __launch_bounds__(256, 2) window_pipe_kernel(WindowArgs a) {
     wait_loads();
     __syncthreads();
     v_read.mma(0, 0, w0, acc);
-    all_weights(s1, w1);
+    float sum;
+    all_weights(s1, w1, sum);
+    settle(s1, w1, sum);
     v_read.mma(0, 1, w1, acc);
   }
   const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
@@ -661,7 +660,7 @@ int dfs_window_attn_fwd(const dfs_window* w, int dtype, const dfs_view* q, const
   if (dtype == DFS_BF16)
     w->d == 64 ? window_pipe_kernel<64><<<grid, 256, 0, st>>>(a) : window_pipe_kernel<128><<<grid, 256, 0, st>>>(a);
   else
-    w->d == 64 ? window_f32_kernel<64><<<grid, 256, 0, st>>>(a) : window_f32_kernel<128><<<grid, 256, 0, st>>>(a);
+    w->d == 64 ? window_plain_kernel<float, 64><<<grid, 256, 0, st>>>(a) : window_plain_kernel<float, 128><<<grid, 256, 0, st>>>(a);
   return launch_status(call);
 }
 
