@@ -23,8 +23,10 @@ __device__ __forceinline__ float* key_part(const WindowArgs& a, int d, int bh, i
 // of dq of the 32 rows of `tile`.
 __device__ __forceinline__ float* row_part(const WindowArgs& a, int d, int64_t tile, int split) { return a.row_part + (tile * a.row_splits + split) * 32 * d; }
 
-template <typename T, int D>
-__global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) window_dq_kernel(WindowArgs a) {
+// f32: one step per tile of 64 keys, bound by the fp32 matrix instructions.
+template <int D>
+__global__ void __launch_bounds__(256, 1) window_dq_f32_kernel(WindowArgs a) {
+  typedef float T;
   constexpr int NW = 4, BM = 32 * NW, KN = 64;
   using KTile = Tile<T, D, KN, NW, false>;
   constexpr int STEPS = KTile::STEPS;
@@ -43,16 +45,16 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) window_dq_kernel(
   const int first = min_of(wave * 32, rows - 1), last = min_of(wave * 32 + 31, rows - 1);
   const int q0 = query_of(a, r0 + first) + len.shift, q1 = query_of(a, r0 + last) + len.shift;
 
-  typename Mat<T>::Frag qf[STEPS], gf[STEPS];
+  Mat<T>::Frag qf[STEPS], gf[STEPS];
   const int64_t sums = (int64_t(at.b) * a.heads + row.qh) * a.n_q + row.qi;
   float delta = 0.f;
   {
     const char *qp = a.q.at(at.b, row.qh, row.qi), *gp = a.d_o.at(at.b, row.qh, row.qi), *op = a.o.at(at.b, row.qh, row.qi);
 #pragma unroll
     for (int s = 0; s < STEPS; ++s) {
-      qf[s] = *reinterpret_cast<const typename Mat<T>::Frag*>(qp + (2 * s + row.h) * 16);
-      gf[s] = *reinterpret_cast<const typename Mat<T>::Frag*>(gp + (2 * s + row.h) * 16);
-      const auto of = *reinterpret_cast<const typename Mat<T>::Frag*>(op + (2 * s + row.h) * 16);
+      qf[s] = *reinterpret_cast<const Mat<T>::Frag*>(qp + (2 * s + row.h) * 16);
+      gf[s] = *reinterpret_cast<const Mat<T>::Frag*>(gp + (2 * s + row.h) * 16);
+      const auto of = *reinterpret_cast<const Mat<T>::Frag*>(op + (2 * s + row.h) * 16);
 #pragma unroll
       for (int i = 0; i < int(16 / sizeof(T)); ++i) delta = fmaf(float(gf[s][i]), float(of[i]), delta);
     }
@@ -111,6 +113,169 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) window_dq_kernel(
     float* mine = row_part(a, D, (int64_t(at.bh) * (a.blocks / a.row_splits) + blk) * NW + wave, split) + lane;
 #pragma unroll
     for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) mine[(c * 16 + i) * 64] = acc[c][i];
+  } else if (row.real) {
+    store_row<T>(a.dq.at(at.b, row.qh, row.qi), acc, a.scale, row.h);
+  }
+}
+
+// bf16: per piece of 32 keys three runs of products, <do, v>, the next piece's logits and dS k, with the weights worked out beside the first and dS beside the
+// second; operands are asked for AHEAD of their instruction, scheduling fences keep it so.  The logits that a piece starts with are the piece's before.  Keys
+// have three buffers, as the next tile's are read while this one's still are; two work-groups fill the LDS of a CU.
+template <int D>
+__global__ void __launch_bounds__(256, 2) window_dq_kernel(WindowArgs a) {
+  typedef uint16_t T;
+  constexpr int NW = 4, BM = 32 * NW, KN = 64;
+  using KTile = Tile<T, D, KN, NW, false>;
+  constexpr int STEPS = KTile::STEPS, CS = D / 32, LOADS = KTile::LOADS, BYTES = KTile::BYTES, RB = KTile::RB;
+  __shared__ __attribute__((aligned(1024))) char tiles[5 * BYTES];                    // three of keys, two of values
+  const uint32_t lds = uint32_t(reinterpret_cast<uintptr_t>((LDS_PTR(void))(tiles)));
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+
+  const Place at(a, blockIdx.x, gridDim.x);
+  const Lengths len(a, at.b);
+  const int blk = at.blk / a.row_splits, split = at.blk - blk * a.row_splits, r0 = blk * BM, rows = rows_of(a, len, r0, BM);
+  if (rows <= 0) return;
+  const Row row(a, at, len, r0, rows, wave * 32 + (lane & 31), lane);
+  const Span span(a, row.i0 + len.shift, row.i1 + len.shift, len.k);
+  const int all_tiles = (span.n + 1) / 2, per = (all_tiles + a.row_splits - 1) / a.row_splits, t0 = split * per, n_tiles = min_of(all_tiles, t0 + per);
+  const char *kh = a.k.at(at.b, at.kvh, 0), *vh = a.v.at(at.b, at.kvh, 0);
+  const typename KTile::Loader k_load(a.k.row, wave, lane), v_load(a.v.row, wave, lane);
+  const uint32_t to = __builtin_amdgcn_readfirstlane(lds + uint32_t(wave) * 1024);
+  auto issue = [&](int t, uint32_t k_buf, uint32_t v_buf) {
+    const int x = span.begin(2 * t), nx = t < n_tiles ? span.end(2 * t) - x : 0, y = span.begin(2 * t + 1), ny = t < n_tiles ? span.end(2 * t + 1) - y : 0;
+    const auto ks = k_load.pair(kh + x * a.k.row, nx, kh + y * a.k.row, ny, a.k.row);
+    const auto vs = v_load.pair(vh + x * a.v.row, nx, vh + y * a.v.row, ny, a.v.row);
+#pragma unroll
+    for (int j = 0; j < LOADS; ++j) k_load.issue_one(ks, to + k_buf, j);
+#pragma unroll
+    for (int j = 0; j < LOADS; ++j) v_load.issue_one(vs, to + v_buf, j);
+  };
+  if (t0 < n_tiles) issue(t0, 0, 3 * BYTES);
+
+  bf16x8 qf[STEPS], gf[STEPS];
+  const int64_t sums = (int64_t(at.b) * a.heads + row.qh) * a.n_q + row.qi;
+  float delta = 0.f;
+  {
+    const char *qp = a.q.at(at.b, row.qh, row.qi), *gp = a.d_o.at(at.b, row.qh, row.qi), *op = a.o.at(at.b, row.qh, row.qi);
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) {
+      qf[s] = *reinterpret_cast<const bf16x8*>(qp + (2 * s + row.h) * 16);
+      gf[s] = *reinterpret_cast<const bf16x8*>(gp + (2 * s + row.h) * 16);
+      const auto of = *reinterpret_cast<const bf16x8*>(op + (2 * s + row.h) * 16);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) delta = fmaf(float(gf[s][i]), float(of[i]), delta);
+    }
+    const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(delta), __float_as_uint(delta), false, false);
+    delta = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+    if (row.real && row.h == 0 && split == 0) a.delta[sums] = delta;
+  }
+  const float lse = a.lse[sums], ref = lse == -INFINITY ? INFINITY : lse * LOG2E;      // a row that sees nothing has weights of zero
+  // LDS addresses of a lane's operands: this tile's keys by columns, by rows the keys whose logits come next and this tile's values; chunks by XOR
+  const typename KTile::RowReader read(lane);
+  const typename KTile::ColumnReader cols(lane);
+  uint32_t next_at = lds + read.at + ((uint32_t(row.h) ^ read.sw) * 16), val_at = next_at + 3 * BYTES, col_at = lds + cols.at[0][0];
+  auto by_rows = [](uint32_t x) { return __builtin_bit_cast(bf16x8, *reinterpret_cast<LDS_PTR(const u32x4)>(x)); };
+  auto by_columns = [](uint32_t x, int s, int c) {
+    constexpr uint32_t FAR = uint32_t(KTile::swizzle(8)) * 16;           // rows 8 further on: their chunks are swapped by this
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<LDS_PTR(s16x4)>((x ^ uint32_t(64 * c)) + uint32_t(16 * s * RB)));
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<LDS_PTR(s16x4)>((x ^ (uint32_t(64 * c) ^ FAR)) + uint32_t((16 * s + 8) * RB)));
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+  };
+  f32x16 acc[CS], s;
+  clear(acc);
+  const float c2 = a.scale * LOG2E;
+  auto mask = [&](int i) __attribute__((always_inline)) {
+    if (__builtin_expect(span.whole(a, i), 1)) return;
+    asm volatile("");                                // keeps this a branch
+    span.mask(a, i, row.p, row.h, s, -INFINITY);
+  };
+  // A piece, half `half` of this tile.  `between`: in front of the next piece's logits, which are those of half `next` at next_at.
+  auto piece = [&](auto half_, auto between) __attribute__((always_inline)) {
+    constexpr int half = decltype(half_)::value, NF = 2 * STEPS + 2 * CS, AHEAD = 3;
+    constexpr bool APART = half == 1;                // nothing is asked for across `between`
+    bf16x8 frag[NF];
+    f32x16 g, sn;
+    Weights<T> w;
+    auto load = [&](int f) {
+      if (f < STEPS) frag[f] = by_rows((val_at ^ uint32_t(32 * f)) + uint32_t(half * 32 * RB));
+      else if (f < 2 * STEPS) frag[f] = by_rows((next_at ^ uint32_t(32 * (f - STEPS))) + uint32_t((1 - half) * 32 * RB));
+      else frag[f] = by_columns(col_at + uint32_t(half * 32 * RB), (f - 2 * STEPS) / CS, (f - 2 * STEPS) % CS);
+    };
+#pragma unroll
+    for (int i = 0; i < 16; ++i) g[i] = sn[i] = 0.f;
+#pragma unroll
+    for (int f = 0; f < AHEAD; ++f) load(f);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int f = 0; f < NF; ++f) {
+      if (f == STEPS) {
+        between();
+        if (APART) {
+#pragma unroll
+          for (int i = 0; i < AHEAD; ++i) load(f + i);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      if (f + AHEAD < NF && !(APART && f < STEPS && f + AHEAD >= STEPS)) load(f + AHEAD);
+      if (f < STEPS) g = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[f], gf[f], g, 0, 0, 0);
+      else if (f < 2 * STEPS) sn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[f], qf[f - STEPS], sn, 0, 0, 0);
+      else {
+        const int j = f - 2 * STEPS;
+        acc[j % CS] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[f], __builtin_bit_cast(bf16x8, w.p[j / CS]), acc[j % CS], 0, 0, 0);
+      }
+      constexpr int E = 16 / STEPS;
+      if (f < STEPS) {
+#pragma unroll
+        for (int i = E * f; i < E * f + E; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c2, -ref));
+      } else if (f < 2 * STEPS) {
+#pragma unroll
+        for (int i = E * (f - STEPS); i < E * (f - STEPS) + E; ++i) {
+          g[i] = s[i] * (g[i] - delta);
+          if (i % 2) {
+            const bf16x2 pair = {(__bf16)g[i - 1], (__bf16)g[i]};
+            w.p[i / 8][i % 8 / 2] = __builtin_bit_cast(uint32_t, pair);
+          }
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    s = sn;
+  };
+  if (t0 < n_tiles) {
+    wait_loads();
+    __syncthreads();
+    issue(t0 + 1, BYTES, 4 * BYTES);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] = 0.f;
+#pragma unroll
+    for (int f = 0; f < STEPS; ++f) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(by_rows(next_at ^ uint32_t(32 * f)), qf[f], s, 0, 0, 0);
+    mask(2 * t0);
+  }
+  int k_now = 0, v_step = BYTES;                     // buffer of this tile's keys; to the other buffer of values
+  for (int t = t0; t < n_tiles; ++t) {
+    asm volatile("" : "+v"(next_at), "+v"(val_at), "+v"(col_at));
+    piece(std::integral_constant<int, 0>{}, [] {});
+    mask(2 * t + 1);
+    const int k_next = k_now == 2 * BYTES ? 0 : k_now + BYTES, k_far = k_next == 2 * BYTES ? 0 : k_next + BYTES;
+    next_at += k_next - k_now;
+    piece(std::integral_constant<int, 1>{}, [&] {
+      wait_loads();                                  // this wave's parts of the next tile are there
+      __syncthreads();                               // all parts are, and every wave has left this tile's values and the keys of the tile before
+      issue(t + 2, k_far, v_step > 0 ? 3 * BYTES : 4 * BYTES);
+    });
+    mask(2 * t + 2);
+    col_at += k_next - k_now;
+    val_at += v_step;
+    k_now = k_next;
+    v_step = -v_step;
+  }
+  wait_loads();                                      // nothing of this work-group's is on its way when its LDS is another's
+  if (a.row_splits > 1) {
+    float* mine = row_part(a, D, (int64_t(at.bh) * (a.blocks / a.row_splits) + blk) * NW + wave, split) + lane;
+#pragma unroll
+    for (int c = 0; c < CS; ++c)
 #pragma unroll
       for (int i = 0; i < 16; ++i) mine[(c * 16 + i) * 64] = acc[c][i];
   } else if (row.real) {
@@ -500,7 +665,8 @@ static int launch(const WindowArgs& args, hipStream_t st) {
   const char* call = "dfs_window_attn_bwd";
   if (a.n_q > 0) {
     a.blocks = (a.group * a.n_q + 127) / 128 * a.row_splits;
-    window_dq_kernel<T, D><<<unsigned(a.blocks * seqs), 256, 0, st>>>(a);
+    if constexpr (sizeof(T) == 2) window_dq_kernel<D><<<unsigned(a.blocks * seqs), 256, 0, st>>>(a);
+    else window_dq_f32_kernel<D><<<unsigned(a.blocks * seqs), 256, 0, st>>>(a);
     if (int rc = launch_status(call)) return rc;
     if (a.row_splits > 1) {
       window_dq_sum_kernel<T, D><<<dim3(unsigned(a.blocks / a.row_splits * 4 * seqs), D / 32), 256, 0, st>>>(a);
