@@ -309,8 +309,8 @@ __global__ void __launch_bounds__(256) window_dq_sum_kernel(WindowArgs a) {
 // alone take 128 registers, the keys' rows stay in registers and the values' come from LDS in every tile.
 template <typename T, int D>
 __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) window_dkv_kernel(WindowArgs a) {
-  constexpr int NW = 4, BN = 32 * NW, QN = 32;
-  constexpr bool V_LDS = sizeof(T) == 2 && D == 128;
+  constexpr bool BF16 = sizeof(T) == 2, V_LDS = BF16;
+  constexpr int NW = 4, BN = 32 * NW, QN = BF16 && D == 64 ? 64 : 32, HALVES = QN / 32;
   using QTile = Tile<T, D, QN, NW, false>;
   using VTile = Tile<T, D, BN, NW, false>;
   constexpr int STEPS = QTile::STEPS;
@@ -410,13 +410,15 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) window_dkv_kernel
       ask_sums(t + 2 < tiles_n);
       issue((t + 1) & 1);
     }
-    const int p0 = row0 + len.shift;
-    const bool whole = row0 + QN <= hi && keys == BN && j0 + BN - 1 <= p0 + a.right && j0 >= p0 + QN - 1 - a.left;
+    auto part = [&](auto half_) __attribute__((always_inline)) {
+    constexpr int half = decltype(half_)::value;
+    const int first = row0 + 32 * half, p0 = first + len.shift;          // first query of the 32
+    const bool whole = first + 32 <= hi && keys == BN && j0 + BN - 1 <= p0 + a.right && j0 >= p0 + 31 - a.left;
     auto mask = [&](f32x16& s) __attribute__((always_inline)) {
       if (whole) return;
       asm volatile("");                              // keeps this a branch
       const int p = p0 + 4 * h;
-      keep(s, key - a.right - p, min_of(key + a.left - p, hi - 1 - row0 - 4 * h), -INFINITY);
+      keep(s, key - a.right - p, min_of(key + a.left - p, hi - 1 - first - 4 * h), -INFINITY);
     };
     f32x16 s, g;
 #pragma unroll
@@ -424,6 +426,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) window_dkv_kernel
     if constexpr (sizeof(T) == 2) {
       // The four products in issue order, operands asked for AHEAD of their instruction, the weights worked out beside the second product and dS beside the
       // third; scheduling fences keep it so, and keep operands that are asked for early from driving the accumulators to scratch.
+      constexpr uint32_t AT = half * 32 * QTile::RB;
       constexpr int CS2 = 2 * (D / 32), NF = 2 * STEPS + 2 * CS2, AHEAD = 3;
       bf16x8 frag[NF], vfrag[STEPS];
       f32x4 ref4[4], delta4[4];
@@ -438,12 +441,12 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) window_dkv_kernel
       };
       auto load = [&](int f) {
         constexpr int C = D / 32;
-        if (f < STEPS) frag[f] = by_rows(row_at ^ uint32_t(32 * f));
+        if (f < STEPS) frag[f] = by_rows((row_at ^ uint32_t(32 * f)) + AT);
         else if (f < 2 * STEPS) {
-          frag[f] = by_rows((row_at ^ uint32_t(32 * (f - STEPS))) + QTile::BYTES);
+          frag[f] = by_rows((row_at ^ uint32_t(32 * (f - STEPS))) + QTile::BYTES + AT);
           if (V_LDS) vfrag[f - STEPS] = by_rows(val_at ^ uint32_t(32 * (f - STEPS)));
-        } else if (f < 2 * STEPS + CS2) frag[f] = by_columns(col_at + QTile::BYTES, (f - 2 * STEPS) / C, (f - 2 * STEPS) % C);
-        else frag[f] = by_columns(col_at, (f - 2 * STEPS - CS2) / C, (f - 2 * STEPS - CS2) % C);
+        } else if (f < 2 * STEPS + CS2) frag[f] = by_columns(col_at + QTile::BYTES + AT, (f - 2 * STEPS) / C, (f - 2 * STEPS) % C);
+        else frag[f] = by_columns(col_at + AT, (f - 2 * STEPS - CS2) / C, (f - 2 * STEPS - CS2) % C);
       };
       asm volatile("" : "+v"(row_at), "+v"(col_at), "+v"(val_at));
 #pragma unroll
@@ -458,8 +461,8 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) window_dkv_kernel
         if (f + AHEAD < NF) load(f + AHEAD);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {                // a row's sums two slots ahead of theirs
-          if (f == STEPS + i * STEPS / 4 - 2) ref4[i] = *reinterpret_cast<const f32x4*>(&row_ref[t & 1][8 * i + 4 * h]);
-          if (f == 2 * STEPS + i * CS2 / 4 - 2) delta4[i] = *reinterpret_cast<const f32x4*>(&row_delta[t & 1][8 * i + 4 * h]);
+          if (f == STEPS + i * STEPS / 4 - 2) ref4[i] = *reinterpret_cast<const f32x4*>(&row_ref[t & 1][32 * half + 8 * i + 4 * h]);
+          if (f == 2 * STEPS + i * CS2 / 4 - 2) delta4[i] = *reinterpret_cast<const f32x4*>(&row_delta[t & 1][32 * half + 8 * i + 4 * h]);
         }
         if (f < STEPS) s = Mat<T>::mma(frag[f], kf[f], s);
         else if (f < 2 * STEPS) g = Mat<T>::mma(frag[f], V_LDS ? vfrag[f - STEPS] : vf[V_LDS ? 0 : f - STEPS], g);
@@ -515,6 +518,9 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) window_dkv_kernel
       w.set(g);
       cols.mma(buf, 0, w, dk);
     }
+    };
+    part(std::integral_constant<int, 0>{});
+    if constexpr (HALVES == 2) part(std::integral_constant<int, 1>{});
     row0 += QN;
     if (row0 >= hi) row0 = lo;
     row_at += to_other;
