@@ -136,15 +136,21 @@ template <typename T, int D, bool PAIRS> struct Token {
   }
 };
 
+// ONCE: past the memory-side cache, which cannot hold what is read.
+template <bool ONCE> __device__ __forceinline__ u32x4 load_chunk(const char* p) {
+  const u32x4* q = reinterpret_cast<const u32x4*>(p);
+  return ONCE ? __builtin_nontemporal_load(q) : *q;
+}
+
 template <int N> __device__ __forceinline__ void weights(const float* w, int c, float (&x)[N]) {
 #pragma unroll
   for (int i = 0; i < N; ++i) x[i] = w ? w[c * N + i] : 1.f;
 }
 
-template <typename T, int D, bool PAIRS>
+template <typename T, int D, bool PAIRS, bool ONCE>
 __global__ void __launch_bounds__(256) rope_kernel(RopeArgs a) {
   using Tok = Token<T, D, PAIRS>;
-  constexpr int N = Tok::N, L = Tok::L, U = 4;       // U: rows in flight
+  constexpr int N = Tok::N, L = Tok::L, U = 2;       // U: rows in flight
   const int lane = threadIdx.x & 63;
   const Tok tok(a, (int64_t(blockIdx.x) * blockDim.x + threadIdx.x) / L, lane);
   const int h0 = blockIdx.y * a.per, h1 = h0 + a.per;
@@ -156,14 +162,14 @@ __global__ void __launch_bounds__(256) rope_kernel(RopeArgs a) {
     constexpr int X = decltype(which)::value;
     const int from = h0 > base ? h0 - base : 0, to = h1 - base < heads ? h1 - base : heads;
     if (from >= to) return;
-    if (X < 2) weights<N>(a.w[X], tok.c, w);
+    if constexpr (X < 2) weights<N>(a.w[X], tok.c, w);
     const char* src = a.in[X].at(tok.b, 0, tok.t) + tok.c * 16;
     char* dst = a.out[X].at(tok.b, 0, X ? (in_room ? at : 0) : tok.t) + tok.c * 16;
     const bool store = X ? in_room : tok.real;
     for (int h = from; h < to; h += U) {
       u32x4 raw[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u) raw[u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(src + (h + u < to ? h + u : h) * a.in[X].head));
+      for (int u = 0; u < U; ++u) raw[u] = load_chunk<ONCE>(src + (h + u < to ? h + u : h) * a.in[X].head);
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         if (X < 2) {
@@ -277,7 +283,11 @@ __global__ void __launch_bounds__(1024) rope_sum_kernel(const float* __restrict_
   if (t == 0 && out) out[col % d] = sums[0][c];
 }
 
-constexpr int BWD_GROUPS = 1024;                     // at most, of rope_bwd_kernel
+// Rows of all heads' that a work-group walks over, at most: all tokens go through one run of heads before the next begins, so that memory is written in few
+// streams (75 600 tokens x 40 heads of q, k and v: 10 rows 840 us, 5.5 TB/s, all 120 900).  Fewer cost the angles again, and more for shared key heads
+// (4 x 16 384 tokens, 32 + 2 x 8 rows: 8 339, 10 315, 14 312).
+constexpr int RUN = 10;
+constexpr int BWD_GROUPS = 1024;                     // at most, of rope_bwd_kernel: rows that rope_sum_kernel adds up
 
 static int check_qk(const char* call, const dfs_qk_geom* g) {
   if (!g) return fail(DFS_EINVAL, "%s: geometry pointer is NULL", call);
@@ -342,10 +352,13 @@ static BwdGrid bwd_grid(const dfs_qk_geom* g, int e) {
   const int slots = 256 / (g->d * e / 16), all = g->heads + 2 * g->heads_kv;
   BwdGrid r;
   r.x = (int64_t(g->batch) * g->tokens + slots - 1) / slots;
-  if (r.x > BWD_GROUPS) r.x = BWD_GROUPS;
-  int64_t y = r.x ? BWD_GROUPS / r.x : 1;
-  r.per = int((all + (y < all ? y : all) - 1) / (y < all ? y : all));
+  int64_t y = r.x ? BWD_GROUPS / r.x : 1, runs = (all + RUN - 1) / RUN;
+  if (y < runs) y = runs < BWD_GROUPS ? runs : BWD_GROUPS;
+  if (y > all) y = all;
+  r.per = int((all + y - 1) / y);
   r.y = (all + r.per - 1) / r.per;
+  const int64_t most = BWD_GROUPS / r.y > 1 ? BWD_GROUPS / r.y : 1;
+  if (r.x > most) r.x = most;
   return r;
 }
 
@@ -380,14 +393,20 @@ int dfs_qk_norm_rope(const dfs_qk_geom* g, int dtype, const dfs_view* q, const d
   if (n == 0) return DFS_OK;
   const int L = g->d * elem_size(dtype) / 16, all = g->heads + (1 + a.copy_v) * g->heads_kv;
   // Work-groups of one wave and runs of heads until there are eight waves a SIMD, or a row a lane.
-  const int64_t waves = (n * L + 63) / 64;
+  const int64_t waves = (n * L + 63) / 64, bytes = n * all * L * 16;
   const int threads = waves * 4 >= 8192 ? 256 : 64;
-  int64_t y = (8192 + waves - 1) / waves;
+  const bool once = bytes > int64_t(256) << 20;
+  int64_t y = (8192 + waves - 1) / waves, runs = (all + RUN - 1) / RUN;
+  if (y < runs) y = runs;
   if (y > all) y = all;
   a.per = int((all + y - 1) / y);
   const dim3 grid(unsigned((n * L + threads - 1) / threads), unsigned((all + a.per - 1) / a.per));
   by_type(g, dtype, [&](auto t, auto d, auto p) {
-    rope_kernel<decltype(t), decltype(d)::value, decltype(p)::value><<<grid, threads, 0, as_stream(stream)>>>(a);
+    using T = decltype(t);
+    constexpr int D = decltype(d)::value;
+    constexpr bool PAIRS = decltype(p)::value;
+    if (once) rope_kernel<T, D, PAIRS, true><<<grid, threads, 0, as_stream(stream)>>>(a);
+    else rope_kernel<T, D, PAIRS, false><<<grid, threads, 0, as_stream(stream)>>>(a);
   });
   return launch_status(call);
 }

@@ -44,10 +44,9 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 4 : 1) window_plain_kern
   const typename VTile::ColumnReader v_read(lane);
   const uint32_t to = __builtin_amdgcn_readfirstlane(lds + uint32_t(wave) * 1024);
   auto issue = [&](int t) {
-    const int x = span.begin(2 * t), nx = span.end(2 * t) - x, y = span.begin(2 * t + 1), ny = span.end(2 * t + 1) - y;
     const uint32_t buf = to + uint32_t((t & 1) * 2 * KTile::BYTES);
-    const auto ks = k_load.pair(kh + x * a.k.row, nx, kh + y * a.k.row, ny, a.k.row);
-    const auto vs = v_load.pair(vh + x * a.v.row, nx, vh + y * a.v.row, ny, a.v.row);
+    const auto ks = k_load.of(span, kh, a.k.row, t);
+    const auto vs = v_load.of(span, vh, a.v.row, t);
 #pragma unroll
     for (int j = 0; j < KTile::LOADS; ++j) k_load.issue_one(ks, buf, j);
 #pragma unroll
@@ -136,12 +135,8 @@ __global__ void __launch_bounds__(256, 2) window_pipe_kernel(WindowArgs a) {
   const typename KTile::Loader k_load(a.k.row, wave, lane);
   const typename VTile::Loader v_load(a.v.row, wave, lane);
   const uint32_t to = __builtin_amdgcn_readfirstlane(lds + uint32_t(wave) * 1024);
-  auto source = [&](auto load, const char* base, int64_t stride, int t) {
-    const int x = span.begin(2 * t), y = span.begin(2 * t + 1);
-    return load.pair(base + x * stride, span.end(2 * t) - x, base + y * stride, span.end(2 * t + 1) - y, stride);
-  };
   if (n_tiles > 0) {
-    const auto ks = source(k_load, kh, a.k.row, 0);
+    const auto ks = k_load.of(span, kh, a.k.row, 0);
 #pragma unroll
     for (int j = 0; j < LOADS; ++j) k_load.issue_one(ks, to, j);
   }
@@ -256,11 +251,11 @@ __global__ void __launch_bounds__(256, 2) window_pipe_kernel(WindowArgs a) {
     wait_loads();
     __syncthreads();
     {
-      const auto vs = source(v_load, vh, a.v.row, 0);
+      const auto vs = v_load.of(span, vh, a.v.row, 0);
 #pragma unroll
       for (int j = 0; j < LOADS; ++j) v_load.issue_one(vs, to + 2 * BYTES, j);
       if (n_tiles > 1) {
-        const auto ks = source(k_load, kh, a.k.row, 1);
+        const auto ks = k_load.of(span, kh, a.k.row, 1);
 #pragma unroll
         for (int j = 0; j < LOADS; ++j) k_load.issue_one(ks, to + BYTES, j);
       }
@@ -283,8 +278,8 @@ __global__ void __launch_bounds__(256, 2) window_pipe_kernel(WindowArgs a) {
     wait_loads();                                    // this wave's parts of K(t + 1) and V(t) are there
     __syncthreads();                                 // all parts are, and every wave has left K(t) and V(t - 1)
     const int t2 = t + 2 < n_tiles ? t + 2 : t + 1;  // behind the last tile that once more, into a buffer that nothing reads
-    const auto ks = source(k_load, kh, a.k.row, t2);
-    const auto vs = source(v_load, vh, a.v.row, t + 1);
+    const auto ks = k_load.of(span, kh, a.k.row, t2);
+    const auto vs = v_load.of(span, vh, a.v.row, t + 1);
     const uint32_t k_to = to + (t & 1 ? BYTES : 0), v_to = to + (t & 1 ? 2 : 3) * BYTES;
 #pragma unroll
     for (int s = 0; s < STEPS; ++s) k_at[s] += k_step;

@@ -69,10 +69,9 @@ __global__ void __launch_bounds__(256, 1) window_dq_f32_kernel(WindowArgs a) {
   const typename KTile::ColumnReader k_cols(lane);
   const uint32_t to = __builtin_amdgcn_readfirstlane(lds + uint32_t(wave) * 1024);
   auto issue = [&](int t) {
-    const int x = span.begin(2 * t), nx = span.end(2 * t) - x, y = span.begin(2 * t + 1), ny = span.end(2 * t + 1) - y;
     const uint32_t buf = to + uint32_t((t & 1) * 2 * KTile::BYTES);
-    const auto ks = k_load.pair(kh + x * a.k.row, nx, kh + y * a.k.row, ny, a.k.row);
-    const auto vs = v_load.pair(vh + x * a.v.row, nx, vh + y * a.v.row, ny, a.v.row);
+    const auto ks = k_load.of(span, kh, a.k.row, t);
+    const auto vs = v_load.of(span, vh, a.v.row, t);
 #pragma unroll
     for (int j = 0; j < KTile::LOADS; ++j) k_load.issue_one(ks, buf, j);
 #pragma unroll
@@ -144,9 +143,9 @@ __global__ void __launch_bounds__(256, 2) window_dq_kernel(WindowArgs a) {
   const typename KTile::Loader k_load(a.k.row, wave, lane), v_load(a.v.row, wave, lane);
   const uint32_t to = __builtin_amdgcn_readfirstlane(lds + uint32_t(wave) * 1024);
   auto issue = [&](int t, uint32_t k_buf, uint32_t v_buf) {
-    const int x = span.begin(2 * t), nx = t < n_tiles ? span.end(2 * t) - x : 0, y = span.begin(2 * t + 1), ny = t < n_tiles ? span.end(2 * t + 1) - y : 0;
-    const auto ks = k_load.pair(kh + x * a.k.row, nx, kh + y * a.k.row, ny, a.k.row);
-    const auto vs = v_load.pair(vh + x * a.v.row, nx, vh + y * a.v.row, ny, a.v.row);
+    // behind the last tile pieces without rows, or another's tile, which nothing reads
+    const auto ks = k_load.of(span, kh, a.k.row, t);
+    const auto vs = v_load.of(span, vh, a.v.row, t);
 #pragma unroll
     for (int j = 0; j < LOADS; ++j) k_load.issue_one(ks, to + k_buf, j);
 #pragma unroll
