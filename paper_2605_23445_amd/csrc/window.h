@@ -67,6 +67,7 @@ __device__ __forceinline__ void keep(f32x16& x, int lo, int hi, int more, float 
 // The keys that a run of queries needs, in pieces of 32: the first keys that lie in front of the run's window, then the window from its first key on.
 struct Span {
   int p0, p1, lo, hi, first, n_first, n;             // positions; window [lo, hi); first keys [0, first) in front of it; pieces of these, and of all
+  int first_whole, w0, w1;                           // pieces that every query sees whole: of first keys those in front of first_whole, [w0, w1)
   __device__ __forceinline__ Span(const WindowArgs& a, int p0_, int p1_, int k_len) : p0(p0_), p1(p1_) {
     lo = max_of(0, p0 - a.left);
     hi = min_of(k_len, p1 + a.right + 1);
@@ -75,14 +76,15 @@ struct Span {
     if (lo > hi) lo = hi;
     n_first = (first + 31) / 32;
     n = n_first + (hi - lo + 31) / 32;
+    const int ahead = p0 + a.right + 1;              // keys in front of it are not too far ahead of any
+    first_whole = max_of(0, min_of(first, ahead)) / 32;
+    w0 = n_first + max_of(0, p1 - a.left - lo + 31) / 32;
+    w1 = n_first + max_of(0, min_of(hi, ahead) - lo) / 32;
   }
   __device__ __forceinline__ int begin(int i) const { return i < n_first ? i * 32 : lo + (i - n_first) * 32; }
   __device__ __forceinline__ int end(int i) const { return i < n_first ? first : hi; }
   // Whether every query of the run sees all 32 keys of piece i.
-  __device__ __forceinline__ bool whole(const WindowArgs& a, int i) const {
-    const int key = begin(i);
-    return key + 32 <= end(i) && key + 31 <= p0 + a.right && (i < n_first || key >= p1 - a.left);
-  }
+  __device__ __forceinline__ bool whole(int i) const { return (i >= w0 && i < w1) || i < first_whole; }
   // Whether queries at positions q0 .. q1 see none of piece i's keys.
   __device__ __forceinline__ bool unseen(const WindowArgs& a, int i, int q0, int q1) const {
     const int key = begin(i);
@@ -322,14 +324,29 @@ template <typename T> __device__ __forceinline__ void store_four(char* row, int 
   }
 }
 
-// Row `row` of accumulators by columns (column = lane % 32 of the row's 32 channels per c), times f, to a row of T.
-template <typename T, int N> __device__ __forceinline__ void store_row(char* row, const f32x16 (&x)[N], float f, int h) {
+// Row `row` of accumulators by columns (column = lane % 32 of the row's 32 channels per c), times f, to a row of T: 16 bytes a lane, in bf16 after the lanes that
+// hold a row's other halves have exchanged four channels of eight.
+template <typename T, int N> __device__ __forceinline__ void store_row(bool real, char* row, const f32x16 (&x)[N], float f, int h) {
 #pragma unroll
   for (int c = 0; c < N; ++c)
+    if constexpr (sizeof(T) == 2) {
 #pragma unroll
-    for (int i = 0; i < 16; i += 4) {
-      const float four[4] = {x[c][i], x[c][i + 1], x[c][i + 2], x[c][i + 3]};
-      store_four<T>(row, 32 * c + 2 * i + 4 * h, four, f);
+      for (int i = 0; i < 16; i += 8) {
+        uint32_t p[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const bf16x2 b = {(__bf16)(x[c][i + 2 * j] * f), (__bf16)(x[c][i + 2 * j + 1] * f)};
+          p[j] = __builtin_bit_cast(uint32_t, b);
+        }
+        const auto lo = __builtin_amdgcn_permlane32_swap(p[0], p[2], false, false), hi = __builtin_amdgcn_permlane32_swap(p[1], p[3], false, false);
+        if (real) *reinterpret_cast<u32x4*>(row + (32 * c + 2 * i + 8 * h) * 2) = u32x4{lo[0], hi[0], lo[1], hi[1]};
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; i += 4) {
+        const float four[4] = {x[c][i], x[c][i + 1], x[c][i + 2], x[c][i + 3]};
+        if (real) store_four<T>(row, 32 * c + 2 * i + 4 * h, four, f);
+      }
     }
 }
 

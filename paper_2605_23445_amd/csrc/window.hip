@@ -69,7 +69,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 4 : 1) window_plain_kern
     for (int half = 0; half < 2; ++half) {
 #pragma unroll
       for (int st = 0; st < STEPS; ++st) s[half] = Mat<T>::mma(k_read.get(buf, half, st), qf[st], s[half]);
-      if (!span.whole(a, 2 * t + half)) span.mask(a, 2 * t + half, row.p, row.h, s[half], -INFINITY);
+      if (!span.whole(2 * t + half)) span.mask(a, 2 * t + half, row.p, row.h, s[half], -INFINITY);
     }
     float mx = s[0][0];
 #pragma unroll
@@ -100,9 +100,8 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 4 : 1) window_plain_kern
   }
   const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
   l = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
-  if (!row.real) return;
-  store_row<T>(a.o.at(at.b, row.qh, row.qi), acc, l == 0.f ? 0.f : 1.f / l, row.h);
-  if (a.lse && row.h == 0) a.lse[(int64_t(at.b) * a.heads + row.qh) * a.n_q + row.qi] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * (1.f / LOG2E);
+  store_row<T>(row.real, a.o.at(at.b, row.qh, row.qi), acc, l == 0.f ? 0.f : 1.f / l, row.h);
+  if (row.real && a.lse && row.h == 0) a.lse[(int64_t(at.b) * a.heads + row.qh) * a.n_q + row.qi] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * (1.f / LOG2E);
 }
 
 // bf16: a pipeline over pieces of 32 keys, two to a tile.  In one stage the matrix cores form the logits of the piece two ahead and the product of the previous
@@ -136,9 +135,14 @@ __global__ void __launch_bounds__(256, 2) window_pipe_kernel(WindowArgs a) {
   const typename VTile::Loader v_load(a.v.row, wave, lane);
   const uint32_t to = __builtin_amdgcn_readfirstlane(lds + uint32_t(wave) * 1024);
   if (n_tiles > 0) {
-    const auto ks = k_load.of(span, kh, a.k.row, 0);
+    const auto k0 = k_load.of(span, kh, a.k.row, 0), k1 = k_load.of(span, kh, a.k.row, 1);
+    const auto v0 = v_load.of(span, vh, a.v.row, 0);
 #pragma unroll
-    for (int j = 0; j < LOADS; ++j) k_load.issue_one(ks, to, j);
+    for (int j = 0; j < LOADS; ++j) k_load.issue_one(k0, to, j);
+#pragma unroll
+    for (int j = 0; j < LOADS; ++j) v_load.issue_one(v0, to + 2 * BYTES, j);
+#pragma unroll
+    for (int j = 0; j < LOADS; ++j) k_load.issue_one(k1, to + BYTES, j);
   }
   bf16x8 qf[STEPS];
   {
@@ -166,7 +170,7 @@ __global__ void __launch_bounds__(256, 2) window_pipe_kernel(WindowArgs a) {
   float ref = -FLT_MAX, l = 0.f;                     // reference in the base-2 exponent's units, this lane's share of the row sum
   const float c2 = a.scale * LOG2E;
   auto mask = [&](int i, f32x16& s) __attribute__((always_inline)) {
-    if (__builtin_expect(span.whole(a, i), 1)) return;
+    if (__builtin_expect(span.whole(i), 1)) return;
     asm volatile("");                                // keeps this a branch
     span.mask(a, i, row.p, row.h, s, -INFINITY);
   };
@@ -250,16 +254,6 @@ __global__ void __launch_bounds__(256, 2) window_pipe_kernel(WindowArgs a) {
     // the logits of tile 0 and the weights of its first half
     wait_loads();
     __syncthreads();
-    {
-      const auto vs = v_load.of(span, vh, a.v.row, 0);
-#pragma unroll
-      for (int j = 0; j < LOADS; ++j) v_load.issue_one(vs, to + 2 * BYTES, j);
-      if (n_tiles > 1) {
-        const auto ks = k_load.of(span, kh, a.k.row, 1);
-#pragma unroll
-        for (int j = 0; j < LOADS; ++j) k_load.issue_one(ks, to + BYTES, j);
-      }
-    }
 #pragma unroll
     for (int i = 0; i < 16; ++i) s0[i] = s1[i] = 0.f;
 #pragma unroll
@@ -315,9 +309,8 @@ __global__ void __launch_bounds__(256, 2) window_pipe_kernel(WindowArgs a) {
   }
   const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
   l = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
-  if (!row.real) return;
-  store_row<uint16_t>(a.o.at(at.b, row.qh, row.qi), acc, l == 0.f ? 0.f : 1.f / l, row.h);
-  if (a.lse && row.h == 0) a.lse[(int64_t(at.b) * a.heads + row.qh) * a.n_q + row.qi] = l == 0.f ? -INFINITY : (ref + __builtin_amdgcn_logf(l)) * (1.f / LOG2E);
+  store_row<uint16_t>(row.real, a.o.at(at.b, row.qh, row.qi), acc, l == 0.f ? 0.f : 1.f / l, row.h);
+  if (row.real && a.lse && row.h == 0) a.lse[(int64_t(at.b) * a.heads + row.qh) * a.n_q + row.qi] = l == 0.f ? -INFINITY : (ref + __builtin_amdgcn_logf(l)) * (1.f / LOG2E);
 }
 
 // Few queries: the keys of 32 rows are split over the waves of a work-group and over `splits` work-groups, and what they find is joined.  A wave's tiles of 32
@@ -391,7 +384,7 @@ __global__ void __launch_bounds__((64 * split_waves<T, D>()), 1) window_split_ke
     for (int st = 0; st < STEPS; ++st) s = Mat<T>::mma(k_read.get(buf, 0, st), qf[st], s);
     wait_reads();
     ask_keys(t + 2 * NW, parity);
-    if (!span.whole(a, t)) span.mask(a, t, p, h, s, -INFINITY);
+    if (!span.whole(t)) span.mask(a, t, p, h, s, -INFINITY);
     float mx = s[0];
 #pragma unroll
     for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);

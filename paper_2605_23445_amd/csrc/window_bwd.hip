@@ -102,7 +102,7 @@ __global__ void __launch_bounds__(256, 1) window_dq_f32_kernel(WindowArgs a) {
         const float w = __builtin_amdgcn_exp2f(fmaf(s[0][i], c2, -ref));
         s[0][i] = w * (g[0][i] - delta);
       }
-      if (!span.whole(a, 2 * t + half)) span.mask(a, 2 * t + half, row.p, row.h, s[0], 0.f);
+      if (!span.whole(2 * t + half)) span.mask(a, 2 * t + half, row.p, row.h, s[0], 0.f);
       Weights<T> w;
       w.set(s[0]);
       k_cols.mma(buf, half, w, acc);
@@ -114,8 +114,8 @@ __global__ void __launch_bounds__(256, 1) window_dq_f32_kernel(WindowArgs a) {
     for (int c = 0; c < D / 32; ++c)
 #pragma unroll
       for (int i = 0; i < 16; ++i) mine[(c * 16 + i) * 64] = acc[c][i];
-  } else if (row.real) {
-    store_row<T>(a.dq.at(at.b, row.qh, row.qi), acc, a.scale, row.h);
+  } else {
+    store_row<T>(row.real, a.dq.at(at.b, row.qh, row.qi), acc, a.scale, row.h);
   }
 }
 
@@ -186,7 +186,7 @@ __global__ void __launch_bounds__(256, 2) window_dq_kernel(WindowArgs a) {
   clear(acc);
   const float c2 = a.scale * LOG2E;
   auto mask = [&](int i) __attribute__((always_inline)) {
-    if (__builtin_expect(span.whole(a, i), 1)) return;
+    if (__builtin_expect(span.whole(i), 1)) return;
     asm volatile("");                                // keeps this a branch
     span.mask(a, i, row.p, row.h, s, -INFINITY);
   };
@@ -277,8 +277,8 @@ __global__ void __launch_bounds__(256, 2) window_dq_kernel(WindowArgs a) {
     for (int c = 0; c < CS; ++c)
 #pragma unroll
       for (int i = 0; i < 16; ++i) mine[(c * 16 + i) * 64] = acc[c][i];
-  } else if (row.real) {
-    store_row<T>(a.dq.at(at.b, row.qh, row.qi), acc, a.scale, row.h);
+  } else {
+    store_row<T>(row.real, a.dq.at(at.b, row.qh, row.qi), acc, a.scale, row.h);
   }
 }
 
@@ -542,9 +542,8 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) window_dkv_kernel
       }
     return;
   }
-  if (!real) return;
-  store_row<T>(a.dk.at(b, kvh, key), dk, a.scale, h);
-  store_row<T>(a.dv.at(b, kvh, key), dv, 1.f, h);
+  store_row<T>(real, a.dk.at(b, kvh, key), dk, a.scale, h);
+  store_row<T>(real, a.dv.at(b, kvh, key), dv, 1.f, h);
 }
 
 // The first keys against the queries that see them only because they are first.  Every query is one, so the queries are split over work-groups, and
