@@ -23,7 +23,8 @@ constexpr float LOG2E = 1.4426950408889634f;
 
 struct WindowArgs {
   View q, k, v, o, d_o, dq, dk, dv;
-  float *lse, *delta;                                // [batch, heads, n_q]
+  float* lse;                                        // [batch, heads, n_q]
+  float2* sums;                                      // backward, alike: a row's log-sum-exp in base 2 and <do, o>
   float* part;                                       // sums of a part: of the first keys' gradients, or of a row's output
   float *key_part, *row_part;                        // backward: sums of a split's part of 32 keys' gradients, of 32 rows'
   float2* part_sums;                                 // maximum and sum of a row's part

@@ -509,7 +509,7 @@ static int first_keys(const dfs_window* w) {
   return w->sinks < w->n_k ? w->sinks : w->n_k;
 }
 
-// Scratch of the backward pass: delta of every row, then parts of gradients.  The queries of 32 first keys go to as many work-groups as make 256 in all, one a
+// Scratch of the backward pass: two sums of every row, then parts of gradients.  The queries of 32 first keys go to as many work-groups as make 256 in all, one a
 // CU, of which each of four waves has two tiles of 32 at least.  Where blocks of 128 keys, or rows, are fewer than CUs, work-groups share one's queries,
 // or keys, four tiles each at least: 4 000 fp32 rows of one key head would else have 32 work-groups, for milliseconds.
 struct BwdLayout { size_t first, keys, rows, total; int tiles, splits, key_splits, row_splits; };
@@ -527,7 +527,7 @@ static BwdLayout bwd_layout(const dfs_window* w) {
   L.splits = share(seqs * L.tiles, rows / 64);
   L.key_splits = share(key_blocks, ((reach < w->n_q ? reach : w->n_q) + 31) / 32 * group);
   L.row_splits = share(row_blocks, ((reach < w->n_k ? reach : w->n_k) + 63) / 64);
-  L.first = align256(size_t(w->batch) * w->heads * w->n_q * sizeof(float));
+  L.first = align256(size_t(w->batch) * w->heads * w->n_q * sizeof(float2));
   L.keys = L.first + size_t(seqs) * L.tiles * L.splits * part;
   L.rows = L.keys + (L.key_splits > 1 ? size_t(key_blocks) * 4 * L.key_splits : size_t(seqs) * L.tiles) * part;
   L.total = L.rows + (L.row_splits > 1 ? size_t(row_blocks) * 4 * L.row_splits * (part / 2) : 0);
@@ -670,7 +670,7 @@ int dfs_window_attn_bwd(const dfs_window* w, int dtype, const dfs_view* q, const
     return fail(DFS_EWORKSPACE, "%s: workspace of %zu bytes needed (256-byte aligned), got %zu", call, need, ws_bytes);
   if (w->batch == 0) return DFS_OK;
   const BwdLayout L = bwd_layout(w);
-  a.delta = static_cast<float*>(ws);
+  a.sums = static_cast<float2*>(ws);
   a.part = reinterpret_cast<float*>(static_cast<char*>(ws) + L.first);
   a.key_part = reinterpret_cast<float*>(static_cast<char*>(ws) + L.keys);
   a.row_part = reinterpret_cast<float*>(static_cast<char*>(ws) + L.rows);

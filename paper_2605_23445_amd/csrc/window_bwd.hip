@@ -1,6 +1,6 @@
 // Backward pass of attention over a window and a few first keys: the queries' gradient, then those of keys and values.
 //
-// The first kernel goes over keys for a block of queries, as the forward pass does, and leaves delta = <do, o> of every row; the second goes over queries
+// The first kernel goes over keys for a block of queries, as the forward pass does, and leaves <do, o> of every row beside its log-sum-exp; the second goes over queries
 // for a block of keys, head by head of those that share it, so that every sum is one work-group's and no atomics are needed.  Both work the weights
 // out anew from the log-sum-exp.  The second takes the pairs of the windows alone: the first keys, which every query sees, would keep a work-group
 // for as long as all others take together.  Their other pairs are dealt to work-groups of a third kernel, and a fourth adds the parts up.
@@ -60,9 +60,9 @@ __global__ void __launch_bounds__(256, 1) window_dq_f32_kernel(WindowArgs a) {
     }
     const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(delta), __float_as_uint(delta), false, false);
     delta = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
-    if (row.real && row.h == 0 && split == 0) a.delta[sums] = delta;
   }
   const float lse = a.lse[sums], ref = lse == -INFINITY ? INFINITY : lse * LOG2E;      // a row that sees nothing has weights of zero
+  if (row.real && row.h == 0 && split == 0) a.sums[sums] = make_float2(ref, delta);
   const char *kh = a.k.at(at.b, at.kvh, 0), *vh = a.v.at(at.b, at.kvh, 0);
   const typename KTile::Loader k_load(a.k.row, wave, lane), v_load(a.v.row, wave, lane);
   const typename KTile::RowReader read(lane);
@@ -168,9 +168,9 @@ __global__ void __launch_bounds__(256, 2) window_dq_kernel(WindowArgs a) {
     }
     const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(delta), __float_as_uint(delta), false, false);
     delta = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
-    if (row.real && row.h == 0 && split == 0) a.delta[sums] = delta;
   }
   const float lse = a.lse[sums], ref = lse == -INFINITY ? INFINITY : lse * LOG2E;      // a row that sees nothing has weights of zero
+  if (row.real && row.h == 0 && split == 0) a.sums[sums] = make_float2(ref, delta);
   // LDS addresses of a lane's operands: this tile's keys by columns, by rows the keys whose logits come next and this tile's values; chunks by XOR
   const typename KTile::RowReader read(lane);
   const typename KTile::ColumnReader cols(lane);
@@ -303,6 +303,18 @@ __global__ void __launch_bounds__(256) window_dq_sum_kernel(WindowArgs a) {
   store_four<T>(a.dq.at(b, qh, qi), channel_of(i, lane), x, a.scale);
 }
 
+// Two sums of N query rows (32 or 64) to LDS, a row after the other; zeros for those behind `rows`.
+template <int N> __device__ __forceinline__ void load_sums(const float2* from, int rows, uint32_t lds, int lane) {
+  const uint64_t at = reinterpret_cast<uint64_t>(from);
+  const u32x4 desc = {uint32_t(__builtin_amdgcn_readfirstlane(uint32_t(at))), uint32_t(__builtin_amdgcn_readfirstlane(uint32_t(at >> 32))) & 0xFFFFu,
+                      uint32_t(__builtin_amdgcn_readfirstlane(min_of(rows, N) * 8)), 0x00020000u};
+  const uint32_t to = __builtin_amdgcn_readfirstlane(lds);
+#pragma unroll
+  for (int j = 0; j < N / 32; ++j)
+    asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds"
+                 ::"s"(to), "v"(lane * 4 + j * 256), "s"(desc), "i"(j * 256) : "memory", "m0", "scc");
+}
+
 // Keys as columns: register i of a lane holds query row 8 (i / 4) + 4 h + i % 4 of a tile of 32, against the lane's key.  A lone wave a SIMD issues a vector
 // instruction every eight to ten cycles and cannot keep the matrix cores busy, so two work-groups share a CU: in bf16 at d = 128, where the accumulators
 // alone take 128 registers, the keys' rows stay in registers and the values' come from LDS in every tile.
@@ -314,8 +326,9 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) window_dkv_kernel
   using VTile = Tile<T, D, BN, NW, false>;
   constexpr int STEPS = QTile::STEPS;
   __shared__ __attribute__((aligned(1024))) char tiles[4 * QTile::BYTES + (V_LDS ? VTile::BYTES : 0)];
-  __shared__ __attribute__((aligned(16))) float row_ref[2][QN], row_delta[2][QN];
+  __shared__ __attribute__((aligned(1024))) float2 row_sums[2][QN];
   const uint32_t lds = uint32_t(reinterpret_cast<uintptr_t>((LDS_PTR(void))(tiles))), lds_v = lds + 4 * QTile::BYTES;
+  const uint32_t lds_sums = uint32_t(reinterpret_cast<uintptr_t>((LDS_PTR(void))(row_sums)));
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 31, h = lane >> 5;
 
   const Place at(a, blockIdx.x, gridDim.x);
@@ -334,52 +347,32 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) window_dkv_kernel
   const typename QTile::Loader q_load(a.q.row, wave, lane), g_load(a.d_o.row, wave, lane);
   const typename QTile::RowReader read(lane);
   const typename QTile::ColumnReader cols(lane);
-  // The tile to ask for next, and the sums of the one behind it: asked for in front of a tile's rows, which nothing waits for before the next barrier.
-  int begin = start, sum_begin = start;
+  // The tile to ask for next, with its rows' sums.
+  int begin = start;
   const char *q_at = a.q.at(b, kvh * a.group + head, start), *g_at = a.d_o.at(b, kvh * a.group + head, start);
   const int64_t q_step = QN * a.q.row, g_step = QN * a.d_o.row, q_back = a.q.head - per_head * q_step, g_back = a.d_o.head - per_head * g_step;
-  const float *lse_at = a.lse + (int64_t(b) * a.heads + kvh * a.group + head) * a.n_q, *delta_at = a.delta + (lse_at - a.lse);
-  float ref = 0.f, delta = 0.f;
+  const float2* sums_at = a.sums + (int64_t(b) * a.heads + kvh * a.group + head) * a.n_q + start;
   auto issue = [&](int buf) {
     const uint32_t to = lds + uint32_t(buf * 2 * QTile::BYTES);
     q_load.issue(q_at, hi - begin, a.q.row, to, wave);
     g_load.issue(g_at, hi - begin, a.d_o.row, to + QTile::BYTES, wave);
+    if (wave == 0) load_sums<QN>(sums_at, hi - begin, lds_sums + uint32_t(buf * QN * 8), lane);
     begin += QN;
     q_at += q_step;
     g_at += g_step;
+    sums_at += QN;
     if (begin >= hi) {                               // the next head's first
       begin = lo;
       q_at += q_back;
       g_at += g_back;
-    }
-  };
-  auto ask_sums = [&](bool more) {
-    if (more && threadIdx.x < QN) {
-      const int row = min_of(sum_begin + int(threadIdx.x), hi - 1);
-      ref = lse_at[row];
-      delta = delta_at[row];
-    }
-    sum_begin += QN;
-    if (sum_begin >= hi) {
-      sum_begin = lo;
-      lse_at += a.n_q;
-      delta_at += a.n_q;
-    }
-  };
-  auto keep_sums = [&](int buf) {
-    if (threadIdx.x < QN) {
-      row_ref[buf][threadIdx.x] = ref == -INFINITY ? INFINITY : ref * LOG2E;            // a row that sees nothing has weights of zero
-      row_delta[buf][threadIdx.x] = delta;
+      sums_at += a.n_q - per_head * QN;
     }
   };
   if (tiles_n > 0) {
-    ask_sums(true);
     if (V_LDS) {
       const typename VTile::Loader v_load(a.v.row, wave, lane);
       v_load.issue(a.v.at(b, kvh, j0), keys, a.v.row, lds_v, wave);
     }
-    keep_sums(0);
-    ask_sums(tiles_n > 1);
     issue(0);
   }
   typename Mat<T>::Frag kf[STEPS], vf[V_LDS ? 1 : STEPS];
@@ -404,11 +397,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) window_dkv_kernel
     wait_loads();
     __syncthreads();
     const uint32_t buf = lds + uint32_t((t & 1) * 2 * QTile::BYTES);
-    if (t + 1 < tiles_n) {
-      keep_sums((t + 1) & 1);
-      ask_sums(t + 2 < tiles_n);
-      issue((t + 1) & 1);
-    }
+    if (t + 1 < tiles_n) issue((t + 1) & 1);
     auto part = [&](auto half_) __attribute__((always_inline)) {
     constexpr int half = decltype(half_)::value;
     const int first = row0 + 32 * half, p0 = first + len.shift;          // first query of the 32
@@ -426,9 +415,9 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) window_dkv_kernel
       // The four products in issue order, operands asked for AHEAD of their instruction, the weights worked out beside the second product and dS beside the
       // third; scheduling fences keep it so, and keep operands that are asked for early from driving the accumulators to scratch.
       constexpr uint32_t AT = half * 32 * QTile::RB;
-      constexpr int CS2 = 2 * (D / 32), NF = 2 * STEPS + 2 * CS2, AHEAD = 3;
+      constexpr int CS2 = 2 * (D / 32), NF = 2 * STEPS + 2 * CS2, AHEAD = D == 64 ? 3 : 2;
       bf16x8 frag[NF], vfrag[STEPS];
-      f32x4 ref4[4], delta4[4];
+      f32x4 sums4[16 / 2];
       Weights<T> w, ws;
       auto by_rows = [](uint32_t at) { return __builtin_bit_cast(bf16x8, *reinterpret_cast<LDS_PTR(const u32x4)>(at)); };
       auto by_columns = [&](uint32_t at, int s, int c) {
@@ -459,10 +448,9 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) window_dkv_kernel
         }
         if (f + AHEAD < NF) load(f + AHEAD);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {                // a row's sums two slots ahead of theirs
-          if (f == STEPS + i * STEPS / 4 - 2) ref4[i] = *reinterpret_cast<const f32x4*>(&row_ref[t & 1][32 * half + 8 * i + 4 * h]);
-          if (f == 2 * STEPS + i * CS2 / 4 - 2) delta4[i] = *reinterpret_cast<const f32x4*>(&row_delta[t & 1][32 * half + 8 * i + 4 * h]);
-        }
+        for (int i = 0; i < 8; ++i)                  // two rows' sums two slots ahead of theirs, for the weights and, without room for them, again for dS
+          if (f == STEPS + i * STEPS / 8 - 2 || (D == 128 && f == 2 * STEPS + i * CS2 / 8 - 2))
+            sums4[i] = *reinterpret_cast<const f32x4*>(&row_sums[t & 1][32 * half + 8 * (i / 2) + 4 * h + i % 2 * 2]);
         if (f < STEPS) s = Mat<T>::mma(frag[f], kf[f], s);
         else if (f < 2 * STEPS) g = Mat<T>::mma(frag[f], V_LDS ? vfrag[f - STEPS] : vf[V_LDS ? 0 : f - STEPS], g);
         else if (f < 2 * STEPS + CS2) {
@@ -477,7 +465,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) window_dkv_kernel
           const int j = f - STEPS;
 #pragma unroll
           for (int i = E * j; i < E * j + E; ++i) {
-            s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c2, -ref4[i / 4][i % 4]));
+            s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c2, -sums4[i / 2][i % 2 * 2]));
             if (i % 2) {
               const bf16x2 pair = {(__bf16)s[i - 1], (__bf16)s[i]};
               w.p[i / 8][i % 8 / 2] = __builtin_bit_cast(uint32_t, pair);
@@ -489,7 +477,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) window_dkv_kernel
           const int j = f - 2 * STEPS;
 #pragma unroll
           for (int i = E * j; i < E * j + E; ++i) {
-            g[i] = s[i] * (g[i] - delta4[i / 4][i % 4]);
+            g[i] = s[i] * (g[i] - sums4[i / 2][i % 2 * 2 + 1]);
             if (i % 2) {
               const bf16x2 pair = {(__bf16)g[i - 1], (__bf16)g[i]};
               ws.p[i / 8][i % 8 / 2] = __builtin_bit_cast(uint32_t, pair);
@@ -508,8 +496,8 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) window_dkv_kernel
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         const int row = 8 * (i / 4) + 4 * h + i % 4;
-        s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c2, -row_ref[t & 1][row]));
-        g[i] = s[i] * (g[i] - row_delta[t & 1][row]);
+        s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c2, -row_sums[t & 1][row].x));
+        g[i] = s[i] * (g[i] - row_sums[t & 1][row].y);
       }
       Weights<T> w;
       w.set(s);
@@ -542,8 +530,15 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) window_dkv_kernel
       }
     return;
   }
-  store_row<T>(real, a.dk.at(b, kvh, key), dk, a.scale, h);
-  store_row<T>(real, a.dv.at(b, kvh, key), dv, 1.f, h);
+  if (!real) return;
+#pragma unroll
+  for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+    for (int i = 0; i < 16; i += 4) {
+      const float x[4] = {dk[c][i], dk[c][i + 1], dk[c][i + 2], dk[c][i + 3]}, y[4] = {dv[c][i], dv[c][i + 1], dv[c][i + 2], dv[c][i + 3]};
+      store_four<T>(a.dk.at(b, kvh, key), 32 * c + 2 * i + 4 * h, x, a.scale);
+      store_four<T>(a.dv.at(b, kvh, key), 32 * c + 2 * i + 4 * h, y, 1.f);
+    }
 }
 
 // The first keys against the queries that see them only because they are first.  Every query is one, so the queries are split over work-groups, and
@@ -556,7 +551,7 @@ __global__ void __launch_bounds__((64 * first_waves<T, D>()), 1) window_first_ke
   constexpr int STEPS = QTile::STEPS, ACC = D / 2;   // ACC: accumulators of a lane for one of the two gradients
   static_assert(2 * ACC * 64 * 4 <= 4 * QTile::BYTES, "a wave's sums fit where its tiles were");
   __shared__ __attribute__((aligned(1024))) char tiles[NW * 4 * QTile::BYTES];
-  __shared__ __attribute__((aligned(16))) float row_ref[NW][QN], row_delta[NW][QN];
+  __shared__ __attribute__((aligned(1024))) float2 row_sums[NW][2][QN];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 31, h = lane >> 5;
   const uint32_t lds = uint32_t(reinterpret_cast<uintptr_t>((LDS_PTR(void))(tiles))) + uint32_t(wave * 4 * QTile::BYTES);
 
@@ -574,6 +569,8 @@ __global__ void __launch_bounds__((64 * first_waves<T, D>()), 1) window_first_ke
     const uint32_t to = lds + uint32_t(buf * 2 * QTile::BYTES);
     q_load.issue(a.q.at(b, head, begin), hi - begin, a.q.row, to, 0);
     g_load.issue(a.d_o.at(b, head, begin), hi - begin, a.d_o.row, to + QTile::BYTES, 0);
+    load_sums<QN>(a.sums + (int64_t(b) * a.heads + head) * a.n_q + begin, hi - begin,
+                  uint32_t(reinterpret_cast<uintptr_t>((LDS_PTR(void))(row_sums))) + uint32_t((wave * 2 + buf) * QN * 8), lane);
   };
   f32x16 dk[D / 32], dv[D / 32];
   clear(dk);
@@ -592,13 +589,7 @@ __global__ void __launch_bounds__((64 * first_waves<T, D>()), 1) window_first_ke
     int parity = 0;
     for (int t = t0; t < tiles_n; t += step, parity ^= 1) {
       const int row0 = lo + t % per_head * QN, p0 = row0 + len.shift;
-      const int64_t at = (int64_t(b) * a.heads + kvh * a.group + t / per_head) * a.n_q + min_of(row0 + n, hi - 1);
-      const float ref = a.lse[at], delta = a.delta[at];
-      row_ref[wave][n] = ref == -INFINITY ? INFINITY : ref * LOG2E;
-      row_delta[wave][n] = delta;
-      wait_loads();
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      __builtin_amdgcn_wave_barrier();
+      wait_loads_but<0>();
       if (t + step < tiles_n) issue(t + step, parity ^ 1);
       const uint32_t buf = lds + uint32_t(parity * 2 * QTile::BYTES);
       f32x16 s, g;
@@ -613,7 +604,8 @@ __global__ void __launch_bounds__((64 * first_waves<T, D>()), 1) window_first_ke
       for (int i = 0; i < 16; ++i) {
         const int row = 8 * (i / 4) + 4 * h + i % 4;
         const bool see = (key < last) & (key < p0 + row - a.left) & (row0 + row < hi);
-        const float x = __builtin_amdgcn_exp2f(fmaf(s[i], c2, -row_ref[wave][row])), d = x * (g[i] - row_delta[wave][row]);
+        const float2 sums = row_sums[wave][parity][row];
+        const float x = __builtin_amdgcn_exp2f(fmaf(s[i], c2, -sums.x)), d = x * (g[i] - sums.y);
         s[i] = see ? x : 0.f;
         g[i] = see ? d : 0.f;
       }
@@ -622,8 +614,6 @@ __global__ void __launch_bounds__((64 * first_waves<T, D>()), 1) window_first_ke
       cols.mma(buf + QTile::BYTES, 0, w, dv);
       w.set(g);
       cols.mma(buf, 0, w, dk);
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      __builtin_amdgcn_wave_barrier();               // the next round's sums stay behind this one's reads
     }
   }
   __syncthreads();
