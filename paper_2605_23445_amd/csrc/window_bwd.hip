@@ -20,8 +20,8 @@ __device__ __forceinline__ float* key_part(const WindowArgs& a, int d, int bh, i
   const int tiles = a.key_splits > 1 ? (a.n_k + 127) / 128 * 4 : a.first_tiles;
   return a.key_part + ((int64_t(bh) * tiles + tile) * a.key_splits + split) * 64 * d;
 }
-// of dq of the 32 rows of `tile`.
-__device__ __forceinline__ float* row_part(const WindowArgs& a, int d, int64_t tile, int split) { return a.row_part + (tile * a.row_splits + split) * 32 * d; }
+// of dq of the 32 rows of `tile`, and behind it of the rows' sums of dS.
+__device__ __forceinline__ float* row_part(const WindowArgs& a, int d, int64_t tile, int split) { return a.row_part + (tile * a.row_splits + split) * 32 * (d + 1); }
 
 // f32: one step per tile of 64 keys, bound by the fp32 matrix instructions.
 template <int D>
@@ -114,6 +114,7 @@ __global__ void __launch_bounds__(256, 1) window_dq_f32_kernel(WindowArgs a) {
     for (int c = 0; c < D / 32; ++c)
 #pragma unroll
       for (int i = 0; i < 16; ++i) mine[(c * 16 + i) * 64] = acc[c][i];
+    if (row.h == 0) mine[32 * D] = 0.f;
   } else {
     store_row<T>(row.real, a.dq.at(at.b, row.qh, row.qi), acc, a.scale, row.h);
   }
@@ -122,8 +123,12 @@ __global__ void __launch_bounds__(256, 1) window_dq_f32_kernel(WindowArgs a) {
 // bf16: per piece of 32 keys three runs of products, <do, v>, the next piece's logits and dS k, with the weights worked out beside the first and dS beside the
 // second; operands are asked for AHEAD of their instruction, scheduling fences keep it so.  The logits that a piece starts with are the piece's before.  Keys
 // have three buffers, as the next tile's are read while this one's still are; two work-groups fill the LDS of a CU.
+//
+// dS goes into its product as two bf16 terms, and the rows' sums of dS, which are zero but for what rounding o has cost <do, o>, are added to that: dk
+// is worked out with the corrected one.  In one term and without it dq and dk were 1.6 to 2 times as far from 64 bits as rounding them alone (relative 2-norm
+// 2.5e-3 to 3.3e-3; now 1.8e-3 to 2.4e-3).  Where a row sees few keys the error of <do, o> is most of dq's, so it is worked out from the keys beforehand.
 template <int D>
-__global__ void __launch_bounds__(256, 2) window_dq_kernel(WindowArgs a) {
+__global__ void __launch_bounds__(256, D == 64 ? 3 : 2) window_dq_kernel(WindowArgs a) {
   typedef uint16_t T;
   constexpr int NW = 4, BM = 32 * NW, KN = 64;
   using KTile = Tile<T, D, KN, NW, false>;
@@ -170,7 +175,6 @@ __global__ void __launch_bounds__(256, 2) window_dq_kernel(WindowArgs a) {
     delta = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
   }
   const float lse = a.lse[sums], ref = lse == -INFINITY ? INFINITY : lse * LOG2E;      // a row that sees nothing has weights of zero
-  if (row.real && row.h == 0 && split == 0) a.sums[sums] = make_float2(ref, delta);
   // LDS addresses of a lane's operands: this tile's keys by columns, by rows the keys whose logits come next and this tile's values; chunks by XOR
   const typename KTile::RowReader read(lane);
   const typename KTile::ColumnReader cols(lane);
@@ -182,25 +186,30 @@ __global__ void __launch_bounds__(256, 2) window_dq_kernel(WindowArgs a) {
     const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<LDS_PTR(s16x4)>((x ^ (uint32_t(64 * c) ^ FAR)) + uint32_t((16 * s + 8) * RB)));
     return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
   };
-  f32x16 acc[CS], s;
+  f32x16 acc[CS], s, s1;
   clear(acc);
+  float off = 0.f;                                   // this lane's share of the sum of dS
   const float c2 = a.scale * LOG2E;
-  auto mask = [&](int i) __attribute__((always_inline)) {
+  auto mask = [&](int i, f32x16& s) __attribute__((always_inline)) {
     if (__builtin_expect(span.whole(i), 1)) return;
     asm volatile("");                                // keeps this a branch
     span.mask(a, i, row.p, row.h, s, -INFINITY);
   };
   // A piece, half `half` of this tile.  `between`: in front of the next piece's logits, which are those of half `next` at next_at.
-  auto piece = [&](auto half_, auto between) __attribute__((always_inline)) {
-    constexpr int half = decltype(half_)::value, NF = 2 * STEPS + 2 * CS, AHEAD = 3;
+  auto piece = [&](auto half_, f32x16& s, f32x16& sn, auto between) __attribute__((always_inline)) {
+    constexpr int half = decltype(half_)::value, NF = 2 * STEPS + 4 * CS, AHEAD = 3;
     constexpr bool APART = half == 1;                // nothing is asked for across `between`
     bf16x8 frag[NF];
-    f32x16 g, sn;
-    Weights<T> w;
+    f32x16 g;
+    Weights<T> w, rest;
+    // Slot j of the last run: contraction step, channels, and whether it is the product of dS's second term, which has its operand from the first's.
+    auto step_of = [](int j) { return j / (2 * CS); };
+    auto part_of = [](int j) { return j % CS; };
+    auto second = [](int j) { return j % (2 * CS) >= CS; };
     auto load = [&](int f) {
       if (f < STEPS) frag[f] = by_rows((val_at ^ uint32_t(32 * f)) + uint32_t(half * 32 * RB));
       else if (f < 2 * STEPS) frag[f] = by_rows((next_at ^ uint32_t(32 * (f - STEPS))) + uint32_t((1 - half) * 32 * RB));
-      else frag[f] = by_columns(col_at + uint32_t(half * 32 * RB), (f - 2 * STEPS) / CS, (f - 2 * STEPS) % CS);
+      else if (!second(f - 2 * STEPS)) frag[f] = by_columns(col_at + uint32_t(half * 32 * RB), step_of(f - 2 * STEPS), part_of(f - 2 * STEPS));
     };
 #pragma unroll
     for (int i = 0; i < 16; ++i) g[i] = sn[i] = 0.f;
@@ -218,12 +227,13 @@ __global__ void __launch_bounds__(256, 2) window_dq_kernel(WindowArgs a) {
         __builtin_amdgcn_sched_barrier(0);
       }
       if (f + AHEAD < NF && !(APART && f < STEPS && f + AHEAD >= STEPS)) load(f + AHEAD);
+      const int j = f - 2 * STEPS;
       if (f < STEPS) g = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[f], gf[f], g, 0, 0, 0);
       else if (f < 2 * STEPS) sn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[f], qf[f - STEPS], sn, 0, 0, 0);
-      else {
-        const int j = f - 2 * STEPS;
-        acc[j % CS] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[f], __builtin_bit_cast(bf16x8, w.p[j / CS]), acc[j % CS], 0, 0, 0);
-      }
+      else if (!second(j))
+        acc[part_of(j)] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[f], __builtin_bit_cast(bf16x8, w.p[step_of(j)]), acc[part_of(j)], 0, 0, 0);
+      else
+        acc[part_of(j)] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[f - CS], __builtin_bit_cast(bf16x8, rest.p[step_of(j)]), acc[part_of(j)], 0, 0, 0);
       constexpr int E = 16 / STEPS;
       if (f < STEPS) {
 #pragma unroll
@@ -232,16 +242,45 @@ __global__ void __launch_bounds__(256, 2) window_dq_kernel(WindowArgs a) {
 #pragma unroll
         for (int i = E * (f - STEPS); i < E * (f - STEPS) + E; ++i) {
           g[i] = s[i] * (g[i] - delta);
+          off += g[i];
           if (i % 2) {
             const bf16x2 pair = {(__bf16)g[i - 1], (__bf16)g[i]};
-            w.p[i / 8][i % 8 / 2] = __builtin_bit_cast(uint32_t, pair);
+            const uint32_t p = w.p[i / 8][i % 8 / 2] = __builtin_bit_cast(uint32_t, pair);
+            const bf16x2 left = {(__bf16)(g[i - 1] - __uint_as_float(p << 16)), (__bf16)(g[i] - __uint_as_float(p & 0xFFFF0000u))};
+            rest.p[i / 8][i % 8 / 2] = __builtin_bit_cast(uint32_t, left);
           }
         }
       }
       __builtin_amdgcn_sched_barrier(0);
     }
-    s = sn;
   };
+  if (a.row_splits == 1 && n_tiles <= 4) {
+    float sum = 0.f;
+    for (int t = 0; t < n_tiles; ++t) {
+      wait_loads();
+      __syncthreads();
+#pragma unroll 1
+      for (int half = 0; half < 2; ++half) {
+        const uint32_t k_at = next_at + uint32_t(half * 32 * RB), v_at = val_at + uint32_t(half * 32 * RB);
+        f32x16 g;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = g[i] = 0.f;
+#pragma unroll
+        for (int f = 0; f < STEPS; ++f) {
+          s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(by_rows(k_at ^ uint32_t(32 * f)), qf[f], s, 0, 0, 0);
+          g = __builtin_amdgcn_mfma_f32_32x32x16_bf16(by_rows(v_at ^ uint32_t(32 * f)), gf[f], g, 0, 0, 0);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        mask(2 * t + half, s);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sum = fmaf(__builtin_amdgcn_exp2f(fmaf(s[i], c2, -ref)), g[i], sum);
+      }
+      __syncthreads();                               // every wave has left the tile
+      issue(t + 1 < n_tiles ? t + 1 : 0, 0, 3 * BYTES);
+    }
+    const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum), __float_as_uint(sum), false, false);
+    delta = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+  }
   if (t0 < n_tiles) {
     wait_loads();
     __syncthreads();
@@ -250,26 +289,29 @@ __global__ void __launch_bounds__(256, 2) window_dq_kernel(WindowArgs a) {
     for (int i = 0; i < 16; ++i) s[i] = 0.f;
 #pragma unroll
     for (int f = 0; f < STEPS; ++f) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(by_rows(next_at ^ uint32_t(32 * f)), qf[f], s, 0, 0, 0);
-    mask(2 * t0);
+    mask(2 * t0, s);
   }
   int k_now = 0, v_step = BYTES;                     // buffer of this tile's keys; to the other buffer of values
   for (int t = t0; t < n_tiles; ++t) {
     asm volatile("" : "+v"(next_at), "+v"(val_at), "+v"(col_at));
-    piece(std::integral_constant<int, 0>{}, [] {});
-    mask(2 * t + 1);
+    piece(std::integral_constant<int, 0>{}, s, s1, [] {});
+    mask(2 * t + 1, s1);
     const int k_next = k_now == 2 * BYTES ? 0 : k_now + BYTES, k_far = k_next == 2 * BYTES ? 0 : k_next + BYTES;
     next_at += k_next - k_now;
-    piece(std::integral_constant<int, 1>{}, [&] {
+    piece(std::integral_constant<int, 1>{}, s1, s, [&] {
       wait_loads();                                  // this wave's parts of the next tile are there
       __syncthreads();                               // all parts are, and every wave has left this tile's values and the keys of the tile before
       issue(t + 2, k_far, v_step > 0 ? 3 * BYTES : 4 * BYTES);
     });
-    mask(2 * t + 2);
+    mask(2 * t + 2, s);
     col_at += k_next - k_now;
     val_at += v_step;
     k_now = k_next;
     v_step = -v_step;
   }
+  const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(off), __float_as_uint(off), false, false);
+  off = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+  if (row.real && row.h == 0 && split == 0) a.sums[sums] = make_float2(ref, a.row_splits > 1 ? delta : delta + off);
   wait_loads();                                      // nothing of this work-group's is on its way when its LDS is another's
   if (a.row_splits > 1) {
     float* mine = row_part(a, D, (int64_t(at.bh) * (a.blocks / a.row_splits) + blk) * NW + wave, split) + lane;
@@ -277,6 +319,7 @@ __global__ void __launch_bounds__(256, 2) window_dq_kernel(WindowArgs a) {
     for (int c = 0; c < CS; ++c)
 #pragma unroll
       for (int i = 0; i < 16; ++i) mine[(c * 16 + i) * 64] = acc[c][i];
+    if (row.h == 0) mine[32 * D] = off;
   } else {
     store_row<T>(row.real, a.dq.at(at.b, row.qh, row.qi), acc, a.scale, row.h);
   }
@@ -301,6 +344,10 @@ __global__ void __launch_bounds__(256) window_dq_sum_kernel(WindowArgs a) {
 #pragma unroll 8
   for (int s = 0; s < a.row_splits; ++s) add_four(x, row_part(a, D, blockIdx.x, s) + i * 64 + lane);
   store_four<T>(a.dq.at(b, qh, qi), channel_of(i, lane), x, a.scale);
+  if (at >= 32) return;
+  float off = 0.f;
+  for (int s = 0; s < a.row_splits; ++s) off += row_part(a, D, blockIdx.x, s)[32 * D + lane];
+  a.sums[(int64_t(b) * a.heads + qh) * a.n_q + qi].y += off;
 }
 
 // Two sums of N query rows (32 or 64) to LDS, a row after the other; zeros for those behind `rows`.
