@@ -294,7 +294,8 @@ int dfs_schedule(int32_t total_steps, int32_t t, int32_t delta, double cached_ke
  * A tensor [batch, heads, rows, d] wherever it lies: the address of its first element (device memory) and how many elements it is
  * from one entry, head and row to the next.  The d channels of a row are adjacent; rows start on 16-byte boundaries, so `data` must
  * be 16-byte aligned and the stride of every axis with more than one entry a multiple of 16 bytes, and not negative.  A stride of
- * zero repeats an input.  An output's rows must not overlap one another (DFS_EINVAL) nor, unless an entry point says so, an input's.
+ * zero repeats an input.  An output's rows must not overlap one another (DFS_EINVAL) nor, unless an entry point says so, those of
+ * another tensor of the call (DFS_EINVAL where both begin at one address; else this is the caller's to see to).
  * Structs are HOST memory.  A tensor without elements may have data NULL.
  */
 typedef struct {
@@ -366,7 +367,8 @@ typedef struct {
  *   lse [batch, heads, n_q] fp32 out, dense, or NULL
  *   scale > 0
  * Rows of q at or behind q_len are not read and their o and lse are left as they are.  Keys and values that no row of a sequence sees
- * may hold anything.  A value that is not finite makes the rows that see it, and possibly up to 127 rows beside those, NaN or infinite.
+ * may hold anything.  A value that is not finite makes the rows that see it NaN or infinite, and possibly those of the up to 127 rows beside
+ * them, of the heads that share its key head, that do not.
  * The same call gives the same bits every time; with other sizes a row may differ by rounding.
  * ws: dfs_window_workspace_bytes(w, dtype, 0), which may be 0 (then NULL will do).
  */
@@ -377,8 +379,10 @@ int dfs_window_attn_fwd(const dfs_window* w, int dtype, const dfs_view* q, const
  * Its backward pass: dq, dk and dv from the forward call's inputs, its o and lse, and do, the gradient of o:
  *   P = exp(scale <q, k_j> - lse),  dv_j = sum P do,  dS = P (<do, v_j> - <do, o>),  dq = scale sum dS k_j,  dk_j = scale sum dS q,
  * dk and dv summed over the query heads that share a key head.  No atomics: same call, same bits.  bf16: P and dS are rounded to bf16
- * for the products, sums are fp32; f32: fp32 throughout.  dq rows at or behind q_len, dk and dv rows at or behind k_len are left as they
- * are; rows that nothing sees, or that see nothing, get zeros.  ws: dfs_window_workspace_bytes(w, dtype, 1).
+ * for the products (dS to two terms for that with the keys), sums are fp32, and <do, o> is corrected for the rounding of o; f32: fp32
+ * throughout.  dq rows at or behind q_len, dk and dv rows at or behind k_len are left as they are; rows that nothing sees, or that see
+ * nothing, get zeros.  What is not finite spreads to the gradients of up to 127 rows or keys beside it, as in the forward pass.
+ * ws: dfs_window_workspace_bytes(w, dtype, 1).
  */
 int dfs_window_attn_bwd(const dfs_window* w, int dtype, const dfs_view* q, const dfs_view* k, const dfs_view* v, const dfs_view* o,
                         const float* lse, const dfs_view* d_o, const int32_t* q_len, const int32_t* k_len, float scale, const dfs_view* dq,

@@ -391,6 +391,14 @@ int dfs_qk_norm_rope(const dfs_qk_geom* g, int dtype, const dfs_view* q, const d
   }
   const int64_t n = int64_t(g->batch) * g->tokens;
   if (n == 0) return DFS_OK;
+  for (int i = 0; i < 2 + a.copy_v; ++i)
+    if (moved(a.in[i], a.out[i]) || (i && kv_start && a.in[i].data == a.out[i].data))
+      return fail(DFS_EINVAL, "%s: %s is %s with rows elsewhere", call, out_name[i], in_name[i]);
+  if ((rc = check_apart(call, {{"q_out", &a.out[0]}, {"k_out", &a.out[1]}, {"v_out", &a.out[2]}}, {})) ||
+      (rc = check_apart(call, {{"q_out", &a.out[0]}}, {{"k", &a.in[1]}, {"v", &a.in[2]}})) ||
+      (rc = check_apart(call, {{"k_out", &a.out[1]}}, {{"q", &a.in[0]}, {"v", &a.in[2]}})) ||
+      (rc = check_apart(call, {{"v_out", &a.out[2]}}, {{"q", &a.in[0]}, {"k", &a.in[1]}})))
+    return rc;
   const int L = g->d * elem_size(dtype) / 16, all = g->heads + (1 + a.copy_v) * g->heads_kv;
   // Work-groups of one wave and runs of heads until there are eight waves a SIMD, or a row a lane.
   const int64_t waves = (n * L + 63) / 64, bytes = n * all * L * 16;
@@ -436,6 +444,15 @@ int dfs_qk_norm_rope_bwd(const dfs_qk_geom* g, int dtype, const dfs_view* q, con
     if ((rc = check_view(call, up_name[i], up[i], dtype, g->batch, heads, g->tokens, g->d, false, &a.grad[i]))) return rc;
     if ((rc = check_view(call, out_name[i], out[i], dtype, g->batch, heads, g->tokens, g->d, true, &a.out[i]))) return rc;
   }
+  for (int i = 0; i < 2 + a.copy_v; ++i)
+    if (moved(a.grad[i], a.out[i])) return fail(DFS_EINVAL, "%s: %s is %s with rows elsewhere", call, out_name[i], up_name[i]);
+  if (g->batch && g->tokens &&
+      ((rc = check_apart(call, {{"dq", &a.out[0]}, {"dk", &a.out[1]}, {"dv", &a.out[2]}}, {{"q", &a.in[0]}, {"k", &a.in[1]}})) ||
+       (rc = check_apart(call, {{"dq", &a.out[0]}}, {{"dk_out", &a.grad[1]}, {"dv_out", &a.grad[2]}})) ||
+       (rc = check_apart(call, {{"dk", &a.out[1]}}, {{"dq_out", &a.grad[0]}, {"dv_out", &a.grad[2]}})) ||
+       (rc = check_apart(call, {{"dv", &a.out[2]}}, {{"dq_out", &a.grad[0]}, {"dk_out", &a.grad[1]}}))))
+    return rc;
+  if (dw_q && dw_q == dw_k) return fail(DFS_EINVAL, "%s: dw_q and dw_k are the same memory", call);
   const bool sums = dw_q || dw_k;
   if (sums && (!ws || (uintptr_t(ws) & 255) || ws_bytes < dfs_qk_workspace_bytes(g)))
     return fail(DFS_EWORKSPACE, "%s: workspace of %zu bytes needed (256-byte aligned), got %zu", call, dfs_qk_workspace_bytes(g), ws_bytes);

@@ -45,4 +45,20 @@ inline int check_view(const char* call, const char* name, const dfs_view* v, int
   return DFS_OK;
 }
 
+// Refuses outputs that begin where another tensor of the call does.  (Overlap in general is the caller's to avoid: parts of one buffer interleave.)
+struct Named { const char* name; const View* v; };
+inline int check_apart(const char* call, std::initializer_list<Named> outputs, std::initializer_list<Named> inputs) {
+  for (const Named& o : outputs) {
+    if (!o.v->data) continue;
+    for (const auto* list : {&outputs, &inputs})
+      for (const Named& x : *list)
+        if (x.v != o.v && x.v->data == o.v->data) return fail(DFS_EINVAL, "%s: %s and %s are the same memory", call, o.name, x.name);
+  }
+  return DFS_OK;
+}
+// Whether an output is its own input with other strides.
+inline bool moved(const View& in, const View& out) {
+  return in.data && in.data == out.data && (in.batch != out.batch || in.head != out.head || in.row != out.row);
+}
+
 }  // namespace dfs

@@ -615,6 +615,7 @@ int dfs_window_attn_fwd(const dfs_window* w, int dtype, const dfs_view* q, const
   int rc = fill_window(call, w, dtype, q, k, v, o, true, lse, q_len, k_len, scale, &a);
   if (rc) return rc;
   if (w->batch == 0 || w->n_q == 0) return DFS_OK;
+  if ((rc = check_apart(call, {{"o", &a.o}}, {{"q", &a.q}, {"k", &a.k}, {"v", &a.v}}))) return rc;
   const FwdLayout L = fwd_layout(w, dtype);
   const hipStream_t st = as_stream(stream);
   if (L.total && (!ws || (uintptr_t(ws) & 255) || ws_bytes < L.total))
@@ -669,6 +670,7 @@ int dfs_window_attn_bwd(const dfs_window* w, int dtype, const dfs_view* q, const
   if (need && (!ws || (uintptr_t(ws) & 255) || ws_bytes < need))
     return fail(DFS_EWORKSPACE, "%s: workspace of %zu bytes needed (256-byte aligned), got %zu", call, need, ws_bytes);
   if (w->batch == 0) return DFS_OK;
+  if ((rc = check_apart(call, {{"dq", &a.dq}, {"dk", &a.dk}, {"dv", &a.dv}}, {{"q", &a.q}, {"k", &a.k}, {"v", &a.v}, {"o", &a.o}, {"d_o", &a.d_o}}))) return rc;
   const BwdLayout L = bwd_layout(w);
   a.sums = static_cast<float2*>(ws);
   a.part = reinterpret_cast<float*>(static_cast<char*>(ws) + L.first);

@@ -105,6 +105,25 @@ def test_window_backward_needs_log_sums_and_workspace():
         assert _win(back=True, ws=ws, ws_bytes=n) == -4 and b"workspace" in lib.dfs_last_error()
 
 
+def test_outputs_in_the_place_of_other_tensors_are_refused():
+    v = {n: _view(i + 1) for i, n in enumerate(("q", "k", "v", "q_out", "k_out", "v_out", "dq", "dk", "dv"))}
+    for out, other in (("q_out", "k"), ("k_out", "q"), ("v_out", "k"), ("q_out", "k_out"), ("k_out", "v_out")):
+        assert _rope(**{out: v[other]}) == -1 and b"same memory" in lib.dfs_last_error()
+    assert _rope(q_out=_view(1, row=256)) == -1 and b"elsewhere" in lib.dfs_last_error()
+    assert _rope(start=AT * 9, rows=64, k_out=v["k"]) == -1 and b"elsewhere" in lib.dfs_last_error()
+    for out, other in (("dq", "q"), ("dk", "q"), ("dq", "k_out"), ("dv", "q_out"), ("dk", "dv")):
+        assert _rope(back=True, **{out: v[other]}) == -1 and b"same memory" in lib.dfs_last_error()
+    assert _rope(back=True, dq=_view(4, row=256)) == -1
+    g = P.QkGeom(**QK)
+    views = [_view(i + 1) for i in range(8)]
+    assert lib.dfs_qk_norm_rope_bwd(g, 1, *views[:2], AT * 20, 0, None, None, *views[2:], AT * 21, AT * 21, AT * 22, 1 << 30, None) == -1
+    w = {n: _view(i + 1) for i, n in enumerate(("q", "k", "v", "o", "d_o", "dq", "dk", "dv"))}
+    for other in ("q", "k", "v"):
+        assert _win(o=w[other]) == -1 and b"same memory" in lib.dfs_last_error()
+    for out, other in (("dq", "q"), ("dk", "k"), ("dv", "o"), ("dq", "d_o"), ("dk", "dv"), ("dq", "dk")):
+        assert _win(back=True, **{out: w[other]}) == -1 and b"same memory" in lib.dfs_last_error()
+
+
 def test_null_structs():
     assert lib.dfs_qk_norm_rope(None, 1, *[None] * 3, None, 0, None, None, *[None] * 3, None, 0, None) == -1
     assert lib.dfs_window_attn_fwd(None, 1, *[None] * 3, None, None, 0.1, None, None, None, 0, None) == -1
