@@ -21,6 +21,18 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 constexpr int NO_LIMIT = 1 << 29;                    // of left and right: further than any two positions are apart
 constexpr float LOG2E = 1.4426950408889634f;
 
+// Division of x < 2^31 by a number that the host knows: a work-group makes half a dozen before it can ask for anything, and the compiler's take 40
+// instructions each.  With l the bits of d - 1 and m = floor(2^(31 + l) / d) + 1, (x m) >> (31 + l) is x / d.
+struct Div {
+  uint32_t m = 0, l = 0;
+  Div() = default;
+  explicit Div(uint32_t d) {
+    while ((uint64_t(1) << l) < d) ++l;
+    m = uint32_t((uint64_t(1) << (31 + l)) / d + 1);
+  }
+  __device__ __forceinline__ int operator()(int x) const { return int(__umulhi(uint32_t(x) * 2, m) >> l); }
+};
+
 struct WindowArgs {
   View q, k, v, o, d_o, dq, dk, dv;
   float* lse;                                        // [batch, heads, n_q]
@@ -30,11 +42,16 @@ struct WindowArgs {
   float2* part_sums;                                 // maximum and sum of a row's part
   const int32_t *q_len, *k_len;
   int32_t batch, heads, heads_kv, group, n_q, n_k, left, right, sinks;
-  int32_t blocks;                                    // work-groups of a sequence's key head
+  int32_t blocks, seqs;                              // work-groups of a sequence's key head; key heads of all sequences
+  Div by_blocks, by_kv, by_group, by_splits;         // by_splits: by the work-groups that share a block
   int32_t first_tiles, first_splits;                 // backward: tiles of 32 first keys, and work-groups that share one's queries
   int32_t key_splits, row_splits;                    // backward: work-groups that share a block of keys, a block of rows
   int32_t splits;                                    // forward: work-groups that share the keys of 32 rows
   float scale;
+  void set_blocks(int64_t n) {
+    blocks = int32_t(n);
+    by_blocks = Div(uint32_t(n));
+  }
 };
 
 // A sequence's lengths, and the position of its first query.
@@ -104,23 +121,24 @@ struct Span {
 // of different lengths spread over all.
 struct Place {
   int blk, bh, b, kvh;
-  __device__ __forceinline__ Place(const WindowArgs& a, int id, int n) {
-    const int xcd = id % 8, slot = id / 8, seqs = n / a.blocks;
-    if (seqs % 8 == 0) {
-      blk = slot % a.blocks;
-      bh = slot / a.blocks * 8 + xcd;
+  __device__ __forceinline__ Place(const WindowArgs& a, int id) {
+    const int xcd = id % 8, slot = id / 8;
+    if (a.seqs % 8 == 0) {
+      const int round = a.by_blocks(slot);
+      blk = slot - round * a.blocks;
+      bh = round * 8 + xcd;
     } else {
-      const int per = n / 8, more = n % 8, at = xcd * per + (xcd < more ? xcd : more) + slot;
-      blk = at % a.blocks;
-      bh = at / a.blocks;
+      const int n = a.seqs * a.blocks, per = n / 8, more = n % 8, at = xcd * per + (xcd < more ? xcd : more) + slot;
+      bh = a.by_blocks(at);
+      blk = at - bh * a.blocks;
     }
-    b = bh / a.heads_kv;
-    kvh = bh % a.heads_kv;
+    b = a.by_kv(bh);
+    kvh = bh - b * a.heads_kv;
   }
 };
 
 // Query of row r of a sequence's key head.  Rows are counted in 31 bits.
-__device__ __forceinline__ int query_of(const WindowArgs& a, int r) { return int(uint32_t(r) / uint32_t(a.group)); }
+__device__ __forceinline__ int query_of(const WindowArgs& a, int r) { return a.by_group(r); }
 // Rows of a block of `most` from r0 on that are there.
 __device__ __forceinline__ int rows_of(const WindowArgs& a, const Lengths& len, int r0, int most) { return min_of(len.q * a.group - r0, most); }
 

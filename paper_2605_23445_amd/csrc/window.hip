@@ -14,8 +14,9 @@ namespace dfs {
 constexpr int KN = 64;                               // keys of a tile
 
 // f32: one step per tile of 64 keys, bound by the fp32 matrix instructions.
-template <typename T, int D>
-__global__ void __launch_bounds__(256, sizeof(T) == 2 ? 4 : 1) window_plain_kernel(WindowArgs a) {
+template <int D>
+__global__ void __launch_bounds__(256) window_f32_kernel(WindowArgs a) {
+  using T = float;
   constexpr int NW = 4, BM = 32 * NW;
   using KTile = Tile<T, D, KN, NW, false>;
   using VTile = Tile<T, D, KN, NW, true>;
@@ -24,7 +25,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 4 : 1) window_plain_kern
   const uint32_t lds = uint32_t(reinterpret_cast<uintptr_t>((LDS_PTR(void))(tiles)));
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
-  const Place at(a, blockIdx.x, gridDim.x);
+  const Place at(a, blockIdx.x);
   const Lengths len(a, at.b);
   const int r0 = at.blk * BM, rows = rows_of(a, len, r0, BM);
   if (rows <= 0) return;
@@ -122,7 +123,7 @@ __global__ void __launch_bounds__(256, 2) window_pipe_kernel(WindowArgs a) {
   const uint32_t lds = uint32_t(reinterpret_cast<uintptr_t>((LDS_PTR(void))(tiles)));
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
-  const Place at(a, blockIdx.x, gridDim.x);
+  const Place at(a, blockIdx.x);
   const Lengths len(a, at.b);
   const int r0 = at.blk * BM, rows = rows_of(a, len, r0, BM);
   if (rows <= 0) return;
@@ -329,13 +330,13 @@ __global__ void __launch_bounds__((64 * split_waves<T, D>()), 1) window_split_ke
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 31, h = lane >> 5;
   const uint32_t lds = uint32_t(reinterpret_cast<uintptr_t>((LDS_PTR(void))(tiles))) + uint32_t(wave * 4 * KTile::BYTES);
 
-  const int split = blockIdx.x % a.splits, at = blockIdx.x / a.splits, blk = at % a.blocks, bh = at / a.blocks, b = bh / a.heads_kv, kvh = bh % a.heads_kv;
+  const int at = a.by_splits(blockIdx.x), split = blockIdx.x - at * a.splits, bh = a.by_blocks(at), blk = at - bh * a.blocks, b = a.by_kv(bh), kvh = bh - b * a.heads_kv;
   const Lengths len(a, b);
   const int r0 = blk * 32, rows = rows_of(a, len, r0, 32);
   if (rows <= 0) return;
   const int i0 = query_of(a, r0), i1 = query_of(a, r0 + rows - 1);
   const Span span(a, i0 + len.shift, i1 + len.shift, len.k);
-  const int per = (span.n + a.splits - 1) / a.splits, t_end = min_of(span.n, (split + 1) * per);
+  const int per = a.by_splits(span.n + a.splits - 1), t_end = min_of(span.n, (split + 1) * per);
 
   const bool real = n < rows;
   const int qi = real ? query_of(a, r0 + n) : i0, qh = kvh * a.group + (real ? r0 + n - qi * a.group : 0), p = qi + len.shift;
@@ -462,7 +463,7 @@ template <typename T, int D>
 __global__ void __launch_bounds__(256) window_join_kernel(WindowArgs a) {
   constexpr int TR = D / 4, RB = 256 / TR;           // threads of a row, rows of a work-group
   const int at = blockIdx.x / (32 / RB), n = blockIdx.x % (32 / RB) * RB + threadIdx.x / TR, ch = threadIdx.x % TR * 4;
-  const int blk = at % a.blocks, bh = at / a.blocks, b = bh / a.heads_kv, kvh = bh % a.heads_kv;
+  const int bh = a.by_blocks(at), blk = at - bh * a.blocks, b = a.by_kv(bh), kvh = bh - b * a.heads_kv;
   const Lengths len(a, b);
   const int r = blk * 32 + n;
   if (r >= len.q * a.group) return;
@@ -588,6 +589,9 @@ static int fill_window(const char* call, const dfs_window* w, int dtype, const d
   a->heads = w->heads;
   a->heads_kv = w->heads_kv;
   a->group = w->heads / w->heads_kv;
+  a->seqs = w->batch * w->heads_kv;
+  a->by_kv = Div(uint32_t(w->heads_kv));
+  a->by_group = Div(uint32_t(a->group));
   a->n_q = w->n_q;
   a->n_k = w->n_k;
   a->left = w->left < 0 || w->left > NO_LIMIT ? NO_LIMIT : w->left;
@@ -625,8 +629,9 @@ int dfs_window_attn_fwd(const dfs_window* w, int dtype, const dfs_view* q, const
     dtype == DFS_BF16 ? d(uint16_t{}) : d(float{});
   };
   if (L.splits) {
-    a.blocks = int((int64_t(a.group) * a.n_q + 31) / 32);
+    a.set_blocks((int64_t(a.group) * a.n_q + 31) / 32);
     a.splits = L.splits;
+    a.by_splits = Div(uint32_t(L.splits));
     a.part = static_cast<float*>(ws);
     a.part_sums = reinterpret_cast<float2*>(static_cast<char*>(ws) + L.sums);
     by_type([&](auto t, auto d) {
@@ -644,12 +649,12 @@ int dfs_window_attn_fwd(const dfs_window* w, int dtype, const dfs_view* q, const
     });
     return launch_status(call);
   }
-  a.blocks = int((int64_t(a.group) * a.n_q + 127) / 128);
+  a.set_blocks((int64_t(a.group) * a.n_q + 127) / 128);
   const unsigned grid = unsigned(int64_t(a.blocks) * a.batch * a.heads_kv);
   if (dtype == DFS_BF16)
     w->d == 64 ? window_pipe_kernel<64><<<grid, 256, 0, st>>>(a) : window_pipe_kernel<128><<<grid, 256, 0, st>>>(a);
   else
-    w->d == 64 ? window_plain_kernel<float, 64><<<grid, 256, 0, st>>>(a) : window_plain_kernel<float, 128><<<grid, 256, 0, st>>>(a);
+    w->d == 64 ? window_f32_kernel<64><<<grid, 256, 0, st>>>(a) : window_f32_kernel<128><<<grid, 256, 0, st>>>(a);
   return launch_status(call);
 }
 

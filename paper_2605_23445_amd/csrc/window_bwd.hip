@@ -34,13 +34,13 @@ __global__ void __launch_bounds__(256, 1) window_dq_f32_kernel(WindowArgs a) {
   const uint32_t lds = uint32_t(reinterpret_cast<uintptr_t>((LDS_PTR(void))(tiles)));
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
-  const Place at(a, blockIdx.x, gridDim.x);
+  const Place at(a, blockIdx.x);
   const Lengths len(a, at.b);
-  const int blk = at.blk / a.row_splits, split = at.blk - blk * a.row_splits, r0 = blk * BM, rows = rows_of(a, len, r0, BM);
+  const int blk = a.by_splits(at.blk), split = at.blk - blk * a.row_splits, r0 = blk * BM, rows = rows_of(a, len, r0, BM);
   if (rows <= 0) return;
   const Row row(a, at, len, r0, rows, wave * 32 + (lane & 31), lane);
   const Span span(a, row.i0 + len.shift, row.i1 + len.shift, len.k);
-  const int all_tiles = (span.n + 1) / 2, per = (all_tiles + a.row_splits - 1) / a.row_splits, t0 = split * per, n_tiles = min_of(all_tiles, t0 + per);
+  const int all_tiles = (span.n + 1) / 2, per = a.by_splits(all_tiles + a.row_splits - 1), t0 = split * per, n_tiles = min_of(all_tiles, t0 + per);
   // this wave's positions
   const int first = min_of(wave * 32, rows - 1), last = min_of(wave * 32 + 31, rows - 1);
   const int q0 = query_of(a, r0 + first) + len.shift, q1 = query_of(a, r0 + last) + len.shift;
@@ -137,13 +137,13 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) window_dq_kernel(WindowA
   const uint32_t lds = uint32_t(reinterpret_cast<uintptr_t>((LDS_PTR(void))(tiles)));
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
-  const Place at(a, blockIdx.x, gridDim.x);
+  const Place at(a, blockIdx.x);
   const Lengths len(a, at.b);
-  const int blk = at.blk / a.row_splits, split = at.blk - blk * a.row_splits, r0 = blk * BM, rows = rows_of(a, len, r0, BM);
+  const int blk = a.by_splits(at.blk), split = at.blk - blk * a.row_splits, r0 = blk * BM, rows = rows_of(a, len, r0, BM);
   if (rows <= 0) return;
   const Row row(a, at, len, r0, rows, wave * 32 + (lane & 31), lane);
   const Span span(a, row.i0 + len.shift, row.i1 + len.shift, len.k);
-  const int all_tiles = (span.n + 1) / 2, per = (all_tiles + a.row_splits - 1) / a.row_splits, t0 = split * per, n_tiles = min_of(all_tiles, t0 + per);
+  const int all_tiles = (span.n + 1) / 2, per = a.by_splits(all_tiles + a.row_splits - 1), t0 = split * per, n_tiles = min_of(all_tiles, t0 + per);
   const char *kh = a.k.at(at.b, at.kvh, 0), *vh = a.v.at(at.b, at.kvh, 0);
   const typename KTile::Loader k_load(a.k.row, wave, lane), v_load(a.v.row, wave, lane);
   const uint32_t to = __builtin_amdgcn_readfirstlane(lds + uint32_t(wave) * 1024);
@@ -378,8 +378,8 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) window_dkv_kernel
   const uint32_t lds_sums = uint32_t(reinterpret_cast<uintptr_t>((LDS_PTR(void))(row_sums)));
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 31, h = lane >> 5;
 
-  const Place at(a, blockIdx.x, gridDim.x);
-  const int blk = at.blk / a.key_splits, split = at.blk - blk * a.key_splits, bh = at.bh, b = at.b, kvh = at.kvh;
+  const Place at(a, blockIdx.x);
+  const int blk = a.by_splits(at.blk), split = at.blk - blk * a.key_splits, bh = at.bh, b = at.b, kvh = at.kvh;
   const Lengths len(a, b);
   const int j0 = blk * BN, keys = min_of(len.k - j0, BN);
   if (keys <= 0) return;
@@ -388,8 +388,8 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) window_dkv_kernel
   // queries [lo, hi) see a key of this block in their window
   const int lo = max_of(0, j0 - a.right - len.shift), hi = min_of(len.q, max_of(0, j0 + keys + a.left - len.shift));
   // this work-group's run of their tiles, head by head
-  const int per_head = hi > lo ? (hi - lo + QN - 1) / QN : 0, per = (per_head * a.group + a.key_splits - 1) / a.key_splits;
-  const int tiles_n = max_of(0, min_of(per, per_head * a.group - split * per)), head = per_head ? split * per / per_head : 0;
+  const int per_head = hi > lo ? (hi - lo + QN - 1) / QN : 0, per = a.by_splits(per_head * a.group + a.key_splits - 1);
+  const int tiles_n = max_of(0, min_of(per, per_head * a.group - split * per)), head = split && per_head ? split * per / per_head : 0;
   const int start = lo + (split * per - head * per_head) * QN;
   const typename QTile::Loader q_load(a.q.row, wave, lane), g_load(a.d_o.row, wave, lane);
   const typename QTile::RowReader read(lane);
@@ -446,112 +446,112 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) window_dkv_kernel
     const uint32_t buf = lds + uint32_t((t & 1) * 2 * QTile::BYTES);
     if (t + 1 < tiles_n) issue((t + 1) & 1);
     auto part = [&](auto half_) __attribute__((always_inline)) {
-    constexpr int half = decltype(half_)::value;
-    const int first = row0 + 32 * half, p0 = first + len.shift;          // first query of the 32
-    const bool whole = first + 32 <= hi && keys == BN && j0 + BN - 1 <= p0 + a.right && j0 >= p0 + 31 - a.left;
-    auto mask = [&](f32x16& s) __attribute__((always_inline)) {
-      if (whole) return;
-      asm volatile("");                              // keeps this a branch
-      const int p = p0 + 4 * h;
-      keep(s, key - a.right - p, min_of(key + a.left - p, hi - 1 - first - 4 * h), -INFINITY);
-    };
-    f32x16 s, g;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) s[i] = g[i] = 0.f;
-    if constexpr (sizeof(T) == 2) {
-      // The four products in issue order, operands asked for AHEAD of their instruction, the weights worked out beside the second product and dS beside the
-      // third; scheduling fences keep it so, and keep operands that are asked for early from driving the accumulators to scratch.
-      constexpr uint32_t AT = half * 32 * QTile::RB;
-      constexpr int CS2 = 2 * (D / 32), NF = 2 * STEPS + 2 * CS2, AHEAD = D == 64 ? 3 : 2;
-      bf16x8 frag[NF], vfrag[STEPS];
-      f32x4 sums4[16 / 2];
-      Weights<T> w, ws;
-      auto by_rows = [](uint32_t at) { return __builtin_bit_cast(bf16x8, *reinterpret_cast<LDS_PTR(const u32x4)>(at)); };
-      auto by_columns = [&](uint32_t at, int s, int c) {
-        constexpr uint32_t FAR = uint32_t(QTile::swizzle(8)) * 16;        // rows 8 further on: their chunks are swapped by this
-        const uint32_t lo = (at ^ uint32_t(64 * c)) + uint32_t(16 * s * QTile::RB), hi = (at ^ (uint32_t(64 * c) ^ FAR)) + uint32_t((16 * s + 8) * QTile::RB);
-        const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<LDS_PTR(s16x4)>(lo));
-        const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<LDS_PTR(s16x4)>(hi));
-        return __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+      constexpr int half = decltype(half_)::value;
+      const int first = row0 + 32 * half, p0 = first + len.shift;          // first query of the 32
+      const bool whole = first + 32 <= hi && keys == BN && j0 + BN - 1 <= p0 + a.right && j0 >= p0 + 31 - a.left;
+      auto mask = [&](f32x16& s) __attribute__((always_inline)) {
+        if (whole) return;
+        asm volatile("");                              // keeps this a branch
+        const int p = p0 + 4 * h;
+        keep(s, key - a.right - p, min_of(key + a.left - p, hi - 1 - first - 4 * h), -INFINITY);
       };
-      auto load = [&](int f) {
-        constexpr int C = D / 32;
-        if (f < STEPS) frag[f] = by_rows((row_at ^ uint32_t(32 * f)) + AT);
-        else if (f < 2 * STEPS) {
-          frag[f] = by_rows((row_at ^ uint32_t(32 * (f - STEPS))) + QTile::BYTES + AT);
-          if (V_LDS) vfrag[f - STEPS] = by_rows(val_at ^ uint32_t(32 * (f - STEPS)));
-        } else if (f < 2 * STEPS + CS2) frag[f] = by_columns(col_at + QTile::BYTES + AT, (f - 2 * STEPS) / C, (f - 2 * STEPS) % C);
-        else frag[f] = by_columns(col_at + AT, (f - 2 * STEPS - CS2) / C, (f - 2 * STEPS - CS2) % C);
-      };
-      asm volatile("" : "+v"(row_at), "+v"(col_at), "+v"(val_at));
+      f32x16 s, g;
 #pragma unroll
-      for (int f = 0; f < AHEAD; ++f) load(f);
-      __builtin_amdgcn_sched_barrier(0);
+      for (int i = 0; i < 16; ++i) s[i] = g[i] = 0.f;
+      if constexpr (sizeof(T) == 2) {
+        // The four products in issue order, operands asked for AHEAD of their instruction, the weights worked out beside the second product and dS beside the
+        // third; scheduling fences keep it so, and keep operands that are asked for early from driving the accumulators to scratch.
+        constexpr uint32_t AT = half * 32 * QTile::RB;
+        constexpr int CS2 = 2 * (D / 32), NF = 2 * STEPS + 2 * CS2, AHEAD = D == 64 ? 3 : 2;
+        bf16x8 frag[NF], vfrag[STEPS];
+        f32x4 sums4[16 / 2];
+        Weights<T> w, ws;
+        auto by_rows = [](uint32_t at) { return __builtin_bit_cast(bf16x8, *reinterpret_cast<LDS_PTR(const u32x4)>(at)); };
+        auto by_columns = [&](uint32_t at, int s, int c) {
+          constexpr uint32_t FAR = uint32_t(QTile::swizzle(8)) * 16;        // rows 8 further on: their chunks are swapped by this
+          const uint32_t lo = (at ^ uint32_t(64 * c)) + uint32_t(16 * s * QTile::RB), hi = (at ^ (uint32_t(64 * c) ^ FAR)) + uint32_t((16 * s + 8) * QTile::RB);
+          const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<LDS_PTR(s16x4)>(lo));
+          const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<LDS_PTR(s16x4)>(hi));
+          return __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+        };
+        auto load = [&](int f) {
+          constexpr int C = D / 32;
+          if (f < STEPS) frag[f] = by_rows((row_at ^ uint32_t(32 * f)) + AT);
+          else if (f < 2 * STEPS) {
+            frag[f] = by_rows((row_at ^ uint32_t(32 * (f - STEPS))) + QTile::BYTES + AT);
+            if (V_LDS) vfrag[f - STEPS] = by_rows(val_at ^ uint32_t(32 * (f - STEPS)));
+          } else if (f < 2 * STEPS + CS2) frag[f] = by_columns(col_at + QTile::BYTES + AT, (f - 2 * STEPS) / C, (f - 2 * STEPS) % C);
+          else frag[f] = by_columns(col_at + AT, (f - 2 * STEPS - CS2) / C, (f - 2 * STEPS - CS2) % C);
+        };
+        asm volatile("" : "+v"(row_at), "+v"(col_at), "+v"(val_at));
 #pragma unroll
-      for (int f = 0; f < NF; ++f) {
-        if (f == STEPS) {
-          mask(s);
+        for (int f = 0; f < AHEAD; ++f) load(f);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int f = 0; f < NF; ++f) {
+          if (f == STEPS) {
+            mask(s);
+            __builtin_amdgcn_sched_barrier(0);
+          }
+          if (f + AHEAD < NF) load(f + AHEAD);
+#pragma unroll
+          for (int i = 0; i < 8; ++i)                  // two rows' sums two slots ahead of theirs, for the weights and, without room for them, again for dS
+            if (f == STEPS + i * STEPS / 8 - 2 || (D == 128 && f == 2 * STEPS + i * CS2 / 8 - 2))
+              sums4[i] = *reinterpret_cast<const f32x4*>(&row_sums[t & 1][32 * half + 8 * (i / 2) + 4 * h + i % 2 * 2]);
+          if (f < STEPS) s = Mat<T>::mma(frag[f], kf[f], s);
+          else if (f < 2 * STEPS) g = Mat<T>::mma(frag[f], V_LDS ? vfrag[f - STEPS] : vf[V_LDS ? 0 : f - STEPS], g);
+          else if (f < 2 * STEPS + CS2) {
+            const int j = f - 2 * STEPS;
+            dv[j % (D / 32)] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[f], __builtin_bit_cast(bf16x8, w.p[j / (D / 32)]), dv[j % (D / 32)], 0, 0, 0);
+          } else {
+            const int j = f - 2 * STEPS - CS2;
+            dk[j % (D / 32)] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[f], __builtin_bit_cast(bf16x8, ws.p[j / (D / 32)]), dk[j % (D / 32)], 0, 0, 0);
+          }
+          if (f >= STEPS && f < 2 * STEPS) {           // 16 weights over STEPS slots
+            constexpr int E = 16 / STEPS;
+            const int j = f - STEPS;
+#pragma unroll
+            for (int i = E * j; i < E * j + E; ++i) {
+              s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c2, -sums4[i / 2][i % 2 * 2]));
+              if (i % 2) {
+                const bf16x2 pair = {(__bf16)s[i - 1], (__bf16)s[i]};
+                w.p[i / 8][i % 8 / 2] = __builtin_bit_cast(uint32_t, pair);
+              }
+            }
+          }
+          if (f >= 2 * STEPS && f < 2 * STEPS + CS2) {
+            constexpr int E = 16 / CS2;
+            const int j = f - 2 * STEPS;
+#pragma unroll
+            for (int i = E * j; i < E * j + E; ++i) {
+              g[i] = s[i] * (g[i] - sums4[i / 2][i % 2 * 2 + 1]);
+              if (i % 2) {
+                const bf16x2 pair = {(__bf16)g[i - 1], (__bf16)g[i]};
+                ws.p[i / 8][i % 8 / 2] = __builtin_bit_cast(uint32_t, pair);
+              }
+            }
+          }
           __builtin_amdgcn_sched_barrier(0);
         }
-        if (f + AHEAD < NF) load(f + AHEAD);
+      } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)                  // two rows' sums two slots ahead of theirs, for the weights and, without room for them, again for dS
-          if (f == STEPS + i * STEPS / 8 - 2 || (D == 128 && f == 2 * STEPS + i * CS2 / 8 - 2))
-            sums4[i] = *reinterpret_cast<const f32x4*>(&row_sums[t & 1][32 * half + 8 * (i / 2) + 4 * h + i % 2 * 2]);
-        if (f < STEPS) s = Mat<T>::mma(frag[f], kf[f], s);
-        else if (f < 2 * STEPS) g = Mat<T>::mma(frag[f], V_LDS ? vfrag[f - STEPS] : vf[V_LDS ? 0 : f - STEPS], g);
-        else if (f < 2 * STEPS + CS2) {
-          const int j = f - 2 * STEPS;
-          dv[j % (D / 32)] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[f], __builtin_bit_cast(bf16x8, w.p[j / (D / 32)]), dv[j % (D / 32)], 0, 0, 0);
-        } else {
-          const int j = f - 2 * STEPS - CS2;
-          dk[j % (D / 32)] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[f], __builtin_bit_cast(bf16x8, ws.p[j / (D / 32)]), dk[j % (D / 32)], 0, 0, 0);
+        for (int st = 0; st < STEPS; ++st) {
+          s = Mat<T>::mma(read.get(buf, 0, st), kf[st], s);
+          g = Mat<T>::mma(read.get(buf + QTile::BYTES, 0, st), vf[V_LDS ? 0 : st], g);
         }
-        if (f >= STEPS && f < 2 * STEPS) {           // 16 weights over STEPS slots
-          constexpr int E = 16 / STEPS;
-          const int j = f - STEPS;
+        mask(s);
 #pragma unroll
-          for (int i = E * j; i < E * j + E; ++i) {
-            s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c2, -sums4[i / 2][i % 2 * 2]));
-            if (i % 2) {
-              const bf16x2 pair = {(__bf16)s[i - 1], (__bf16)s[i]};
-              w.p[i / 8][i % 8 / 2] = __builtin_bit_cast(uint32_t, pair);
-            }
-          }
+        for (int i = 0; i < 16; ++i) {
+          const int row = 8 * (i / 4) + 4 * h + i % 4;
+          s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c2, -row_sums[t & 1][row].x));
+          g[i] = s[i] * (g[i] - row_sums[t & 1][row].y);
         }
-        if (f >= 2 * STEPS && f < 2 * STEPS + CS2) {
-          constexpr int E = 16 / CS2;
-          const int j = f - 2 * STEPS;
-#pragma unroll
-          for (int i = E * j; i < E * j + E; ++i) {
-            g[i] = s[i] * (g[i] - sums4[i / 2][i % 2 * 2 + 1]);
-            if (i % 2) {
-              const bf16x2 pair = {(__bf16)g[i - 1], (__bf16)g[i]};
-              ws.p[i / 8][i % 8 / 2] = __builtin_bit_cast(uint32_t, pair);
-            }
-          }
-        }
-        __builtin_amdgcn_sched_barrier(0);
+        Weights<T> w;
+        w.set(s);
+        cols.mma(buf + QTile::BYTES, 0, w, dv);
+        w.set(g);
+        cols.mma(buf, 0, w, dk);
       }
-    } else {
-#pragma unroll
-      for (int st = 0; st < STEPS; ++st) {
-        s = Mat<T>::mma(read.get(buf, 0, st), kf[st], s);
-        g = Mat<T>::mma(read.get(buf + QTile::BYTES, 0, st), vf[V_LDS ? 0 : st], g);
-      }
-      mask(s);
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int row = 8 * (i / 4) + 4 * h + i % 4;
-        s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c2, -row_sums[t & 1][row].x));
-        g[i] = s[i] * (g[i] - row_sums[t & 1][row].y);
-      }
-      Weights<T> w;
-      w.set(s);
-      cols.mma(buf + QTile::BYTES, 0, w, dv);
-      w.set(g);
-      cols.mma(buf, 0, w, dk);
-    }
     };
     part(std::integral_constant<int, 0>{});
     if constexpr (HALVES == 2) part(std::integral_constant<int, 1>{});
@@ -705,7 +705,8 @@ static int launch(const WindowArgs& args, hipStream_t st) {
   const int64_t seqs = int64_t(a.batch) * a.heads_kv;
   const char* call = "dfs_window_attn_bwd";
   if (a.n_q > 0) {
-    a.blocks = (a.group * a.n_q + 127) / 128 * a.row_splits;
+    a.by_splits = Div(uint32_t(a.row_splits));
+    a.set_blocks((int64_t(a.group) * a.n_q + 127) / 128 * a.row_splits);
     if constexpr (sizeof(T) == 2) window_dq_kernel<D><<<unsigned(a.blocks * seqs), 256, 0, st>>>(a);
     else window_dq_f32_kernel<D><<<unsigned(a.blocks * seqs), 256, 0, st>>>(a);
     if (int rc = launch_status(call)) return rc;
@@ -716,7 +717,8 @@ static int launch(const WindowArgs& args, hipStream_t st) {
   }
   if (a.n_k == 0) return DFS_OK;
   const int key_blocks = (a.n_k + 127) / 128, tiles = a.key_splits > 1 ? key_blocks * 4 : a.first_tiles;
-  a.blocks = key_blocks * a.key_splits;
+  a.by_splits = Div(uint32_t(a.key_splits));
+  a.set_blocks(int64_t(key_blocks) * a.key_splits);
   window_dkv_kernel<T, D><<<unsigned(a.blocks * seqs), 256, 0, st>>>(a);
   if (int rc = launch_status(call)) return rc;
   if (a.first_tiles > 0) {
