@@ -305,7 +305,7 @@ typedef struct {
 
 /* Queries and keys of every head in front of attention: their norm and the rotation by position. */
 typedef struct {
-  int32_t batch, tokens;     /* sequences and tokens of each; either may be 0 */
+  int32_t batch, tokens;     /* sequences and tokens of each; either may be 0, together fewer than 2^27 */
   int32_t heads, heads_kv;   /* query heads; key and value heads; at most 65 535 each */
   int32_t d;                 /* head dimension: 64 or 128 */
   int32_t interleaved;       /* 1: channels 2i and 2i + 1 of an axis's share turn together; 0: i and i + half the share */
@@ -354,6 +354,8 @@ typedef struct {
   int32_t n_q, n_k;                    /* rows of the query and of the key tensors, of every sequence; at most 2^28, either may be 0 */
   int32_t left, right;                 /* how far a query sees back and ahead; negative: without limit */
   int32_t sinks;                       /* the first keys that every query sees which may see so far ahead; 0 if none */
+  /* The blocks of 128 rows (query heads of a key head together), of 128 keys and of 32 first keys are each fewer than 2^24 over all batches
+     and key heads: 2^31 rows or keys, 2^29 first ones. */
 } dfs_window;
 
 /*

@@ -488,6 +488,12 @@ __global__ void __launch_bounds__(256) window_join_kernel(WindowArgs a) {
   if (ch == 0 && a.lse) a.lse[(int64_t(b) * a.heads + qh) * a.n_q + qi] = total == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * (1.f / LOG2E);
 }
 
+// First keys that count: none where every window reaches back to them.
+static int first_keys(const dfs_window* w) {
+  if (w->left < 0 || w->left >= w->n_k) return 0;
+  return w->sinks < w->n_k ? w->sinks : w->n_k;
+}
+
 static int check_window(const char* call, const dfs_window* w, int dtype) {
   if (!w) return fail(DFS_EINVAL, "%s: window pointer is NULL", call);
   if (dtype != DFS_F32 && dtype != DFS_BF16) return fail(DFS_EDTYPE, "%s: dtype %d is not DFS_F32 or DFS_BF16", call, dtype);
@@ -497,17 +503,13 @@ static int check_window(const char* call, const dfs_window* w, int dtype) {
     return fail(DFS_ESHAPE, "%s: heads=%d must be in [1, 65535] and a multiple of heads_kv=%d", call, w->heads, w->heads_kv);
   if (w->d != 64 && w->d != 128) return fail(DFS_ESHAPE, "%s: d=%d: head dimension must be 64 or 128", call, w->d);
   if (w->sinks < 0) return fail(DFS_ESHAPE, "%s: sinks=%d is negative", call, w->sinks);
-  // a sequence's rows, which blocks of 128 may pass, and the grids' work-groups are counted in 31 bits
-  const int64_t rows = int64_t(w->heads / w->heads_kv) * w->n_q, most = rows > w->n_k ? rows : w->n_k;
-  if (rows > int64_t(1) << 30 || (most / 32 + 2) * w->batch * int64_t(w->heads_kv) >= int64_t(1) << 31 || int64_t(w->batch) * w->heads >= int64_t(1) << 31)
-    return fail(DFS_ESHAPE, "%s: batch x heads x rows too large", call);
+  // A sequence's rows, which blocks of 128 may pass, are counted in 31 bits; a grid has fewer than 2^32 threads, 256 for a block of 128 rows or keys or
+  // for 32 first keys.
+  const int64_t rows = int64_t(w->heads / w->heads_kv) * w->n_q, most = rows > w->n_k ? rows : w->n_k, tiles = first_keys(w) / 32;
+  const int64_t groups = (most / 128 > tiles ? most / 128 : tiles) + 1, seqs = int64_t(w->batch) * w->heads_kv;
+  if (rows > int64_t(1) << 30 || seqs >= 1 << 24 || groups * seqs >= 1 << 24)
+    return fail(DFS_ESHAPE, "%s: batch=%d x heads_kv=%d x rows of q or k too large", call, w->batch, w->heads_kv);
   return DFS_OK;
-}
-
-// First keys that count: none where every window reaches back to them.
-static int first_keys(const dfs_window* w) {
-  if (w->left < 0 || w->left >= w->n_k) return 0;
-  return w->sinks < w->n_k ? w->sinks : w->n_k;
 }
 
 // Scratch of the backward pass: two sums of every row, then parts of gradients.  The queries of 32 first keys go to as many work-groups as make 256 in all, one a

@@ -141,3 +141,12 @@ def test_binding_refuses_host_tensors():
     with pytest.raises(ValueError):
         P.dfs_window_attn_fwd(P.Window(2, 4, 4, 128, 5, 5, 3, 0, 1), P.DFS_BF16, x, x, x, None, None, 0.1, x.clone())
     assert C.sizeof(P.QkGeom) == 56 and C.sizeof(P.Window) == 36
+
+
+@pytest.mark.parametrize("back", [False, True])
+def test_sizes_that_pass_a_grid_are_refused(back):
+    """A grid has fewer than 2^32 threads: 32 a token, 256 a block of 128 rows or keys or of 32 first keys."""
+    assert _rope(geom=dict(batch=1 << 7, tokens=1 << 20), back=back) == -2 and _rope(geom=dict(batch=2**31 - 1, tokens=2**31 - 1), back=back) == -2
+    for win in (dict(batch=1 << 23, heads=2, heads_kv=2, n_q=1, n_k=1), dict(batch=1 << 8, n_q=1 << 24), dict(batch=1 << 11, n_k=1 << 20, heads=2, heads_kv=1, left=9, sinks=1 << 20),
+                dict(batch=2**31 - 1, heads=65535, heads_kv=65535), dict(batch=1, heads=1 << 15, heads_kv=1, n_q=1 << 16)):
+        assert _win(win=win, back=back) == -2 and b"too large" in lib.dfs_last_error(), win
