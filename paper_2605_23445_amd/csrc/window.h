@@ -198,9 +198,14 @@ struct Tile {
   static constexpr int LOADS = ROWS * CH / (64 * NW);
   static constexpr int FOLD = CH < 16 ? 16 / CH : 1;
   static_assert(ROWS * CH % (64 * NW) == 0, "a load fills 64 chunks");
-  // XOR of the 16-byte chunks of a row, so that the rows which a wave reads at once lie in different banks
+  // XOR of the 16-byte chunks of a row, so that what a wave reads at once lies in different banks: one chunk of 16 rows or, by columns, four chunks of 4
+  // rows.  A bf16 tile's does for both (with row % 16, which is good for rows alone, a fifth of the gradients' cycles at d = 128 were conflicts), and rows 8
+  // further on differ in one bit of those that channels 32 further on count by, so that both take the same addresses.  An fp32 one's is for rows or,
+  // COLUMNS, for columns, where it is known when compiled.
   static constexpr __host__ __device__ __forceinline__ int swizzle(int row) {
-    return COLUMNS ? 4 * ((row / FOLD) % (CH < 16 ? CH / 4 : 4)) : (row / FOLD) % (CH < 16 ? CH : 16);
+    if (sizeof(T) == 4) return COLUMNS ? 4 * (row % 4) : row % 16;
+    const int near = row / FOLD & 1, far = row >> 3 & 1;
+    return (CH == 16 ? (row >> 1 & 1) * 8 : 0) + (near ^ far) * 4 + near * 2 + (row >> 2 & 1);
   }
   // Loads: byte offset of this lane's chunk of load j in a tensor whose rows are `stride` bytes apart.
   struct Loader {
