@@ -9,7 +9,7 @@
  * with their backward passes.
  *
  * Conventions shared by every entry point
- *   - `g` points to HOST memory.  Every other pointer is DEVICE memory owned by the caller;
+ *   - Structs (`g` and its like) are HOST memory.  Every other pointer is DEVICE memory owned by the caller;
  *     the library allocates nothing, frees nothing and keeps no pointer after a call returns.
  *   - `stream` is a hipStream_t passed as void* (NULL = the default stream).  All work is
  *     enqueued on it; no call synchronises or copies to the host.

@@ -23,7 +23,8 @@ __device__ __forceinline__ float* key_part(const WindowArgs& a, int d, int bh, i
 // of dq of the 32 rows of `tile`, and behind it of the rows' sums of dS.
 __device__ __forceinline__ float* row_part(const WindowArgs& a, int d, int64_t tile, int split) { return a.row_part + (tile * a.row_splits + split) * 32 * (d + 1); }
 
-// f32: one step per tile of 64 keys, bound by the fp32 matrix instructions.
+// f32: one step per tile of 64 keys, bound by the fp32 matrix instructions, with one work-group a CU (forward and backward of 4 000 tokens x 16 heads, 1 000 keys
+// each way: d = 64 1.53 ms, d = 128 3.37 ms, 43 and 39 % of a large product's rate).
 template <int D>
 __global__ void __launch_bounds__(256, 1) window_dq_f32_kernel(WindowArgs a) {
   typedef float T;
@@ -127,6 +128,9 @@ __global__ void __launch_bounds__(256, 1) window_dq_f32_kernel(WindowArgs a) {
 // dS goes into its product as two bf16 terms, and the rows' sums of dS, which are zero but for what rounding o has cost <do, o>, are added to that: dk
 // is worked out with the corrected one.  In one term and without it dq and dk were 1.6 to 2 times as far from 64 bits as rounding them alone (relative 2-norm
 // 2.5e-3 to 3.3e-3; now 1.8e-3 to 2.4e-3).  Where a row sees few keys the error of <do, o> is most of dq's, so it is worked out from the keys beforehand.
+//
+// Bound by the matrix cores and the vector port beside them: 17 550 tokens x 30 heads, d = 64, 1 350 keys each way: 790 us, 891 TFLOP/s with the second term's,
+// matrix cores busy 48 % of the cycles; 2 x 4 001 (ragged) x 32 heads of 8 key heads, d = 128, 512 keys back: 119 us, 738 TFLOP/s, 38 %.
 template <int D>
 __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) window_dq_kernel(WindowArgs a) {
   typedef uint16_t T;
@@ -364,7 +368,8 @@ template <int N> __device__ __forceinline__ void load_sums(const float2* from, i
 
 // Keys as columns: register i of a lane holds query row 8 (i / 4) + 4 h + i % 4 of a tile of 32, against the lane's key.  A lone wave a SIMD issues a vector
 // instruction every eight to ten cycles and cannot keep the matrix cores busy, so two work-groups share a CU: in bf16 at d = 128, where the accumulators
-// alone take 128 registers, the keys' rows stay in registers and the values' come from LDS in every tile.
+// alone take 128 registers, the keys' rows stay in registers and the values' come from LDS in every tile.  At the sizes above 800 us, 880 TFLOP/s, 48 %, and
+// 152 us, 578 TFLOP/s, 32 %: two work-groups a CU do not fill what one of them waits for.
 template <typename T, int D>
 __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) window_dkv_kernel(WindowArgs a) {
   constexpr bool BF16 = sizeof(T) == 2, V_LDS = BF16;
@@ -589,7 +594,8 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) window_dkv_kernel
 }
 
 // The first keys against the queries that see them only because they are first.  Every query is one, so the queries are split over work-groups, and
-// the waves of one take tiles of 32 queries in turn against 32 keys; tiles are a wave's own, so that nothing waits for another wave.
+// the waves of one take tiles of 32 queries in turn against 32 keys; tiles are a wave's own, so that nothing waits for another wave.  Bound by the way of q and
+// do: 17 550 x 30, d = 64, 16 first keys: 31 us, 4.3 TB/s; 2 x 4 001 x 32, d = 128, 4 first keys: 24 us.
 template <typename T, int D> constexpr int first_waves() { return sizeof(T) == 4 && D == 128 ? 2 : 4; }
 template <typename T, int D>
 __global__ void __launch_bounds__((64 * first_waves<T, D>()), 1) window_first_kernel(WindowArgs a) {
