@@ -15,8 +15,9 @@ struct View {
 inline int check_view(const char* call, const char* name, const dfs_view* v, int dtype, int64_t batch, int64_t heads, int64_t rows, int d,
                       bool output, View* out) {
   if (!v) return fail(DFS_EINVAL, "%s: %s is NULL", call, name);
-  *out = View{static_cast<char*>(v->data), 0, 0, 0};
-  if (batch == 0 || heads == 0 || rows == 0) return DFS_OK;
+  *out = View{};
+  if (batch == 0 || heads == 0 || rows == 0) return DFS_OK;              // no memory, wherever it points
+  out->data = static_cast<char*>(v->data);
   if (!v->data) return fail(DFS_EINVAL, "%s: %s has no memory", call, name);
   const int e = elem_size(dtype);
   const int64_t n[3] = {batch, heads, rows}, s[3] = {v->batch, v->head, v->row};

@@ -254,6 +254,23 @@ def test_no_rows():
     assert not dq.any()
 
 
+def test_tensors_without_rows_may_point_anywhere():
+    """One of no rows that begins where an output does is not that output."""
+    from paper_2605_23445_amd import binding as B
+    q, o, lse = torch.randn(2, 2, 5, 64, device="cuda"), torch.full((2, 2, 5, 64), 3.0, device="cuda"), torch.full((2, 2, 5), 3.0, device="cuda")
+    w, st = P.Window(2, 2, 2, 64, 5, 0, 3, 0, 1), torch.cuda.current_stream().cuda_stream
+    view = lambda t: B._View(t.data_ptr(), *t.stride()[:3])  # noqa: E731
+    ws = lambda back: (lambda t: (t.data_ptr() if t is not None else None, t.numel() if t is not None else 0, t))(_ws(w, "f32", back))  # noqa: E731
+    at, n, keep = ws(False)
+    assert B._lib.dfs_window_attn_fwd(w, P.DFS_F32, view(q), view(o), view(o), None, None, 0.1, view(o), lse.data_ptr(), at, n, st) == 0
+    dq = torch.full_like(q, 3.0)
+    at, n, keep_too = ws(True)
+    assert B._lib.dfs_window_attn_bwd(w, P.DFS_F32, view(q), view(dq), view(dq), view(o), lse.data_ptr(), view(q), None, None, 0.1, view(dq), view(dq), view(dq),
+                                      at, n, st) == 0
+    assert not o.any() and torch.isneginf(lse).all() and not dq.any()
+    del keep, keep_too
+
+
 def test_refusals_of_the_binding():
     w, q, k, v, d_o, q_len, k_len, _, _ = _make("ragged", "bf16")
     o, lse = torch.zeros_like(q), torch.zeros(w.batch, w.heads, w.n_q, device="cuda")
