@@ -643,6 +643,7 @@ __global__ void __launch_bounds__((64 * first_waves<T, D>()), 1) window_first_ke
     for (int t = t0; t < tiles_n; t += step, parity ^= 1) {
       const int row0 = lo + t % per_head * QN, p0 = row0 + len.shift;
       wait_loads_but<0>();
+      wait_reads();                                  // of the tile before, whose place the next one takes
       if (t + step < tiles_n) issue(t + step, parity ^ 1);
       const uint32_t buf = lds + uint32_t(parity * 2 * QTile::BYTES);
       f32x16 s, g;
