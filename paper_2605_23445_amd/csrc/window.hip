@@ -322,7 +322,7 @@ __global__ void __launch_bounds__(256, 2) window_pipe_kernel(WindowArgs a) {
 // Few queries: the keys of 32 rows are split over the waves of a work-group and over `splits` work-groups, and what they find is joined.  A wave's tiles of 32
 // keys are its own, so that none waits for another before the end, and but for the keys or values
 // that are worked on the LDS is full of loads on their way.  Bound by memory: 48 sequences of 8 key heads, 4 100 keys, bf16, d = 128: 139 us, 5.8 TB/s read; one
-// sequence: 14 us with the join, of which the keys' way is 2.4: a launch each, a chain of loads, three joins.
+// sequence: 13.5 us with the join (11.9 in a graph), of which the keys' way is 2.4: a launch each, a chain of loads, the waves' join and the splits'.
 template <typename T, int D> constexpr int split_waves() { return sizeof(T) == 4 && D == 128 ? 2 : 4; }
 template <typename T, int D, bool ONCE>
 __global__ void __launch_bounds__((64 * split_waves<T, D>()), 1) window_split_kernel(WindowArgs a) {

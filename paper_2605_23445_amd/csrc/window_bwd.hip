@@ -1,8 +1,8 @@
 // Backward pass of attention over a window and a few first keys: the queries' gradient, then those of keys and values.
 //
-// The first kernel goes over keys for a block of queries, as the forward pass does, and leaves <do, o> of every row beside its log-sum-exp; the second goes over queries
-// for a block of keys, head by head of those that share it, so that every sum is one work-group's and no atomics are needed.  Both work the weights
-// out anew from the log-sum-exp.  The second takes the pairs of the windows alone: the first keys, which every query sees, would keep a work-group
+// The first kernel goes over keys for a block of queries, as the forward pass does, and leaves <do, o> of every row beside its log-sum-exp; the second goes
+// over queries for a block of keys, head by head of those that share it, so that every sum is one work-group's and no atomics are needed.  Both work the
+// weights out anew from the log-sum-exp.  The second takes the pairs of the windows alone: the first keys, which every query sees, would keep a work-group
 // for as long as all others take together.  Their other pairs are dealt to work-groups of a third kernel, and a fourth adds the parts up.
 #include <float.h>
 #include <math.h>
