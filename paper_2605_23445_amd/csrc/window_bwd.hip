@@ -127,7 +127,8 @@ __global__ void __launch_bounds__(256, 1) window_dq_f32_kernel(WindowArgs a) {
 //
 // dS goes into its product as two bf16 terms, and the rows' sums of dS, which are zero but for what rounding o has cost <do, o>, are added to that: dk
 // is worked out with the corrected one.  In one term and without it dq and dk were 1.6 to 2 times as far from 64 bits as rounding them alone (relative 2-norm
-// 2.5e-3 to 3.3e-3; now 1.8e-3 to 2.4e-3).  Where a row sees few keys the error of <do, o> is most of dq's, so it is worked out from the keys beforehand.
+// 2.5e-3 to 3.3e-3; now 1.8e-3 to 2.4e-3).  Where a block of rows sees four tiles of keys at most, the error of <do, o> is most of dq's, so it is worked
+// out from the keys beforehand.
 //
 // Bound by the matrix cores and the vector port beside them: 17 550 tokens x 30 heads, d = 64, 1 350 keys each way: 790 us, 891 TFLOP/s with the second term's,
 // matrix cores busy 48 % of the cycles; 2 x 4 001 (ragged) x 32 heads of 8 key heads, d = 128, 512 keys back: 119 us, 738 TFLOP/s, 38 %.
@@ -160,7 +161,8 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) window_dq_kernel(WindowA
 #pragma unroll
     for (int j = 0; j < LOADS; ++j) v_load.issue_one(vs, to + v_buf, j);
   };
-  if (t0 < n_tiles) issue(t0, 0, 3 * BYTES);
+  const bool few = all_tiles <= 4;                   // keys of which <do, o> is worked out beforehand, by every work-group that shares them
+  if (t0 < n_tiles) issue(few ? 0 : t0, 0, 3 * BYTES);
 
   bf16x8 qf[STEPS], gf[STEPS];
   const int64_t sums = (int64_t(at.b) * a.heads + row.qh) * a.n_q + row.qi;
@@ -258,9 +260,9 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) window_dq_kernel(WindowA
       __builtin_amdgcn_sched_barrier(0);
     }
   };
-  if (a.row_splits == 1 && n_tiles <= 4) {
+  if (few && t0 < n_tiles) {
     float sum = 0.f;
-    for (int t = 0; t < n_tiles; ++t) {
+    for (int t = 0; t < all_tiles; ++t) {
       wait_loads();
       __syncthreads();
 #pragma unroll 1
@@ -280,7 +282,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) window_dq_kernel(WindowA
         for (int i = 0; i < 16; ++i) sum = fmaf(__builtin_amdgcn_exp2f(fmaf(s[i], c2, -ref)), g[i], sum);
       }
       __syncthreads();                               // every wave has left the tile
-      issue(t + 1 < n_tiles ? t + 1 : 0, 0, 3 * BYTES);
+      issue(t + 1 < all_tiles ? t + 1 : t0, 0, 3 * BYTES);
     }
     const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum), __float_as_uint(sum), false, false);
     delta = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);

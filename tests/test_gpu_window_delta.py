@@ -1,0 +1,91 @@
+"""<do, o> in the backward pass of windowed attention, bf16: what the rounding of o does to it.
+
+Bounds.  u = 2^-8 is what one rounding to bf16 is off by at most, e = 2^-24.  Where a block of 128 rows sees 256 keys at most, <do, o> comes from the keys and dS
+has two bf16 terms, so that nothing but the result is rounded to bf16: a logit is off by x = (d + 4) e scale sum|q k|, a weight by 2 max x + (n + 16) e of itself,
+<do, v> by (d + 4) e sum|do v|, <do, o> by what these make of it, dS by u^2 of itself besides.  Elsewhere dk has two roundings to bf16, of dS and of the
+result; one is off by 2^-7 / sqrt(12) of its value in the mean at most, both by 3.2e-3 of the 2-norm, with 2^-8 as the bound."""
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+P = pytest.importorskip("paper_2605_23445_amd")
+from oracle import layer_oracle as L  # noqa: E402
+from tests.test_gpu_window import _np, _run, _within, _ws  # noqa: E402
+
+E, U = 2.0 ** -24, 2.0 ** -8
+
+
+def _rand(gen, *s):
+    return torch.randn(*s, generator=gen, device="cuda")
+
+
+def _far(got, want):
+    return np.linalg.norm(got - want) / np.linalg.norm(want)
+
+
+# heads, heads_kv, d, n_q, n_k, left, right, sinks, q_len, k_len
+FEW = {
+    "short_window": (2, 1, 128, 300, 300, 60, 0, 0, None, None),
+    "short_window_d64": (3, 3, 64, 300, 300, 30, 20, 5, None, None),
+    "few_keys": (4, 2, 128, 150, 150, -1, 0, 0, None, None),
+    # work-groups share rows here
+    "early_rows": (1, 1, 128, 1500, 1500, -1, 0, 0, None, None),
+    "early_rows_d64": (1, 1, 64, 2100, 2100, 1200, 0, 4, None, None),
+    "short_sequences": (2, 2, 64, 1100, 1100, -1, 0, 0, [200, 9], [200, 9]),
+    "short_sequence_both_sides": (2, 2, 128, 1100, 1100, -1, -1, 0, [256], [256]),
+}
+
+
+@pytest.mark.parametrize("name", list(FEW))
+def test_queries_that_see_few_keys(name):
+    heads, kv, d, n_q, n_k, left, right, sinks, q_len, k_len = FEW[name]
+    batch, group, scale = len(k_len) if k_len else 2, heads // kv, 0.15
+    gen = torch.Generator(device="cuda").manual_seed(11)
+    q, k, v, d_o = (_rand(gen, batch, h, n, d).bfloat16() for h, n in ((heads, n_q), (kv, n_k), (kv, n_k), (heads, n_q)))
+    w = P.Window(batch, heads, kv, d, n_q, n_k, left, right, sinks)
+    i32 = lambda x: None if x is None else torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    got = _run(w, "bf16", q, k, v, d_o, i32(q_len), i32(k_len), scale)[2]
+    q, k, v, d_o, got = (_np(x) for x in (q, k, v, d_o, got))
+    checked = 0
+    for b in range(batch):
+        n, m = (q_len[b], k_len[b]) if k_len else (n_q, n_k)
+        see = L.window_mask(n, m, left, right, sinks)
+        for h in range(heads):
+            for r0 in range(0, n * group, 128):                            # blocks of rows: query by query, all heads of a key head
+                i0, i1 = r0 // group, min(n - 1, (r0 + 127) // group)
+                rows = np.arange(i0, i1 + 1)
+                keys = np.flatnonzero(see[rows].any(0))
+                if len(keys) > (225 if sinks else 256):                    # eight pieces of 32, of first keys and of the window
+                    continue
+                rows = rows[[r0 <= i * group + h % group < r0 + 128 for i in rows]]
+                kk, vv, g, x = k[b, h // group][keys], v[b, h // group][keys], d_o[b, h][rows], q[b, h][rows]
+                p = L.window_attn(x, kk, vv, see[np.ix_(rows, keys)], scale)[2]
+                off = (d + 4) * E * np.where(p > 0, np.abs(x) @ np.abs(kk).T * scale, 0).max(-1, keepdims=True)
+                rel = 2 * off + (len(keys) + 16) * E
+                dp, e_dp = g @ vv.T, (d + 4) * E * (np.abs(g) @ np.abs(vv).T)
+                delta = (p * dp).sum(-1, keepdims=True)
+                e_delta = (p * (rel * np.abs(dp) + e_dp)).sum(-1, keepdims=True) + (len(keys) + 16) * E * (p * np.abs(dp)).sum(-1, keepdims=True)
+                ds = p * (dp - delta)
+                e_ds = p * (rel * np.abs(dp - delta) + e_dp + e_delta) + (U * U + 4 * E) * np.abs(ds)
+                want = scale * ds @ kk
+                err = scale * (e_ds @ np.abs(kk) + (len(keys) + 16) * E * (np.abs(ds) @ np.abs(kk))) * 1.01 + U * np.abs(want) + 1e-30
+                _within(got[b, h][rows], want, err, name, b, h, r0)
+                checked += len(rows)
+    assert checked >= 100
+
+
+@pytest.mark.parametrize("name,heads,d,n,left", [("shared_rows", 1, 128, 1500, 900), ("shared_rows_d64", 2, 64, 1300, -1), ("rows_of_one", 48, 64, 800, 600),
+                                                 ("rows_of_one_d128", 36, 128, 900, 500)])
+def test_keys_gradients_do_not_see_the_rounding_of_o(name, heads, d, n, left):
+    """Values that have most in common: o is large and what it is rounded by, in <do, o>, is more than a rounding of dS, which holds the differences alone."""
+    gen = torch.Generator(device="cuda").manual_seed(12)
+    q, k, d_o = (_rand(gen, 1, heads, n, d).bfloat16() for _ in range(3))
+    v = (8 * _rand(gen, 1, heads, 1, d) + _rand(gen, 1, heads, n, d)).bfloat16()
+    w = P.Window(1, heads, heads, d, n, n, left, 0, 0)
+    got = _run(w, "bf16", q, k, v, d_o, None, None, 0.1)[3]
+    see = L.window_mask(n, n, left, 0, 0)
+    for h in range(0, heads, 11):
+        want = L.window_attn_bwd(*(_np(x[0, h]) for x in (q, k, v)), see, 0.1, _np(d_o[0, h]))[1]
+        assert _far(_np(got[0, h]), want) <= U, (name, h)
