@@ -555,7 +555,7 @@ static BwdLayout bwd_layout(const dfs_window* w) {
   L.first = align256(size_t(w->batch) * w->heads * w->n_q * sizeof(float2));
   L.keys = L.first + size_t(seqs) * L.tiles * L.splits * part;
   L.rows = L.keys + (L.key_splits > 1 ? size_t(key_blocks) * 4 * L.key_splits : size_t(seqs) * L.tiles) * part;
-  L.total = L.rows + (L.row_splits > 1 ? size_t(row_blocks) * 4 * L.row_splits * (part / 2 + 32 * sizeof(float)) : 0);
+  L.total = L.rows + (L.row_splits > 1 ? size_t(row_blocks) * 4 * L.row_splits * (part / 2 + 64 * sizeof(float)) : 0);
   return L;
 }
 

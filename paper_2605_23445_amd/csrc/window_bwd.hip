@@ -20,8 +20,18 @@ __device__ __forceinline__ float* key_part(const WindowArgs& a, int d, int bh, i
   const int tiles = a.key_splits > 1 ? (a.n_k + 127) / 128 * 4 : a.first_tiles;
   return a.key_part + ((int64_t(bh) * tiles + tile) * a.key_splits + split) * 64 * d;
 }
-// of dq of the 32 rows of `tile`, and behind it of the rows' sums of dS.
-__device__ __forceinline__ float* row_part(const WindowArgs& a, int d, int64_t tile, int split) { return a.row_part + (tile * a.row_splits + split) * 32 * (d + 1); }
+// of dq of the 32 rows of `tile`, and behind it (bf16) of the rows' sums of dS and of weights.
+__device__ __forceinline__ float* row_part(const WindowArgs& a, int d, int64_t tile, int split) { return a.row_part + (tile * a.row_splits + split) * 32 * (d + 2); }
+
+// Whether a row's weights, with this sum, are all that its log-sum-exp counts: not where that was joined with other keys' (fp32 rounds a weight's exponent, of
+// some |log-sum-exp| 2^-23).  Then the sum of dS is zero but for rounding; what a joined row's may be wrong by within this bound is less than a rounding to bf16.
+__device__ __forceinline__ bool own_sum(float x) { return fabsf(x - 1.f) <= 0x1p-9f; }
+
+// Sum of what the two lanes that share a row hold.
+__device__ __forceinline__ float both_halves(float x) {
+  const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+}
 
 // f32: one step per tile of 64 keys, bound by the fp32 matrix instructions, with one work-group a CU (forward and backward of 4 000 tokens x 16 heads, 1 000 keys
 // each way: d = 64 1.53 ms, d = 128 3.37 ms, 43 and 39 % of a large product's rate).
@@ -59,8 +69,7 @@ __global__ void __launch_bounds__(256, 1) window_dq_f32_kernel(WindowArgs a) {
 #pragma unroll
       for (int i = 0; i < int(16 / sizeof(T)); ++i) delta = fmaf(float(gf[s][i]), float(of[i]), delta);
     }
-    const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(delta), __float_as_uint(delta), false, false);
-    delta = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+    delta = both_halves(delta);
   }
   const float lse = a.lse[sums], ref = lse == -INFINITY ? INFINITY : lse * LOG2E;      // a row that sees nothing has weights of zero
   if (row.real && row.h == 0 && split == 0) a.sums[sums] = make_float2(ref, delta);
@@ -115,7 +124,6 @@ __global__ void __launch_bounds__(256, 1) window_dq_f32_kernel(WindowArgs a) {
     for (int c = 0; c < D / 32; ++c)
 #pragma unroll
       for (int i = 0; i < 16; ++i) mine[(c * 16 + i) * 64] = acc[c][i];
-    if (row.h == 0) mine[32 * D] = 0.f;
   } else {
     store_row<T>(row.real, a.dq.at(at.b, row.qh, row.qi), acc, a.scale, row.h);
   }
@@ -126,7 +134,7 @@ __global__ void __launch_bounds__(256, 1) window_dq_f32_kernel(WindowArgs a) {
 // have three buffers, as the next tile's are read while this one's still are; two work-groups fill the LDS of a CU.
 //
 // dS goes into its product as two bf16 terms, and the rows' sums of dS, which are zero but for what rounding o has cost <do, o>, are added to that: dk
-// is worked out with the corrected one.  In one term and without it dq and dk were 1.6 to 2 times as far from 64 bits as rounding them alone (relative 2-norm
+// is worked out with the corrected one.  (Where o and log-sum-exp were joined with other keys' they are not zero, and nothing is corrected.)  In one term and without it dq and dk were 1.6 to 2 times as far from 64 bits as rounding them alone (relative 2-norm
 // 2.5e-3 to 3.3e-3; now 1.8e-3 to 2.4e-3).  Where a block of rows sees four tiles of keys at most, the error of <do, o> is most of dq's, so it is worked
 // out from the keys beforehand.
 //
@@ -177,8 +185,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) window_dq_kernel(WindowA
 #pragma unroll
       for (int i = 0; i < 8; ++i) delta = fmaf(float(gf[s][i]), float(of[i]), delta);
     }
-    const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(delta), __float_as_uint(delta), false, false);
-    delta = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+    delta = both_halves(delta);
   }
   const float lse = a.lse[sums], ref = lse == -INFINITY ? INFINITY : lse * LOG2E;      // a row that sees nothing has weights of zero
   // LDS addresses of a lane's operands: this tile's keys by columns, by rows the keys whose logits come next and this tile's values; chunks by XOR
@@ -194,7 +201,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) window_dq_kernel(WindowA
   };
   f32x16 acc[CS], s, s1;
   clear(acc);
-  float off = 0.f;                                   // this lane's share of the sum of dS
+  float off = 0.f, total = 0.f;                      // this lane's share of the sums of dS and of weights
   const float c2 = a.scale * LOG2E;
   auto mask = [&](int i, f32x16& s) __attribute__((always_inline)) {
     if (__builtin_expect(span.whole(i), 1)) return;
@@ -247,8 +254,10 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) window_dq_kernel(WindowA
       } else if (f < 2 * STEPS) {
 #pragma unroll
         for (int i = E * (f - STEPS); i < E * (f - STEPS) + E; ++i) {
+          total += s[i];
           g[i] = s[i] * (g[i] - delta);
           off += g[i];
+          asm volatile("" : "+v"(total), "+v"(off));   // here: put off, the sums kept 35 registers in scratch (1 990 -> 2 520 us, not 2 010)
           if (i % 2) {
             const bf16x2 pair = {(__bf16)g[i - 1], (__bf16)g[i]};
             const uint32_t p = w.p[i / 8][i % 8 / 2] = __builtin_bit_cast(uint32_t, pair);
@@ -261,7 +270,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) window_dq_kernel(WindowA
     }
   };
   if (few && t0 < n_tiles) {
-    float sum = 0.f;
+    float sum = 0.f, weights = 0.f;
     for (int t = 0; t < all_tiles; ++t) {
       wait_loads();
       __syncthreads();
@@ -279,13 +288,16 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) window_dq_kernel(WindowA
         }
         mask(2 * t + half, s);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) sum = fmaf(__builtin_amdgcn_exp2f(fmaf(s[i], c2, -ref)), g[i], sum);
+        for (int i = 0; i < 16; ++i) {
+          const float x = __builtin_amdgcn_exp2f(fmaf(s[i], c2, -ref));
+          weights += x;
+          sum = fmaf(x, g[i], sum);
+        }
       }
       __syncthreads();                               // every wave has left the tile
       issue(t + 1 < all_tiles ? t + 1 : t0, 0, 3 * BYTES);
     }
-    const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum), __float_as_uint(sum), false, false);
-    delta = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+    if (own_sum(both_halves(weights))) delta = both_halves(sum);
   }
   if (t0 < n_tiles) {
     wait_loads();
@@ -315,9 +327,9 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) window_dq_kernel(WindowA
     k_now = k_next;
     v_step = -v_step;
   }
-  const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(off), __float_as_uint(off), false, false);
-  off = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
-  if (row.real && row.h == 0 && split == 0) a.sums[sums] = make_float2(ref, a.row_splits > 1 ? delta : delta + off);
+  off = both_halves(off);
+  total = both_halves(total);
+  if (row.real && row.h == 0 && split == 0) a.sums[sums] = make_float2(ref, a.row_splits == 1 && own_sum(total) ? delta + off : delta);
   wait_loads();                                      // nothing of this work-group's is on its way when its LDS is another's
   if (a.row_splits > 1) {
     float* mine = row_part(a, D, (int64_t(at.bh) * (a.blocks / a.row_splits) + blk) * NW + wave, split) + lane;
@@ -325,7 +337,10 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) window_dq_kernel(WindowA
     for (int c = 0; c < CS; ++c)
 #pragma unroll
       for (int i = 0; i < 16; ++i) mine[(c * 16 + i) * 64] = acc[c][i];
-    if (row.h == 0) mine[32 * D] = off;
+    if (row.h == 0) {
+      mine[32 * D] = off;
+      mine[32 * D + 32] = total;
+    }
   } else {
     store_row<T>(row.real, a.dq.at(at.b, row.qh, row.qi), acc, a.scale, row.h);
   }
@@ -350,10 +365,14 @@ __global__ void __launch_bounds__(256) window_dq_sum_kernel(WindowArgs a) {
 #pragma unroll 8
   for (int s = 0; s < a.row_splits; ++s) add_four(x, row_part(a, D, blockIdx.x, s) + i * 64 + lane);
   store_four<T>(a.dq.at(b, qh, qi), channel_of(i, lane), x, a.scale);
-  if (at >= 32) return;
-  float off = 0.f;
-  for (int s = 0; s < a.row_splits; ++s) off += row_part(a, D, blockIdx.x, s)[32 * D + lane];
-  a.sums[(int64_t(b) * a.heads + qh) * a.n_q + qi].y += off;
+  if (sizeof(T) == 4 || at >= 32) return;
+  float off = 0.f, total = 0.f;
+  for (int s = 0; s < a.row_splits; ++s) {
+    const float* p = row_part(a, D, blockIdx.x, s) + 32 * D + lane;
+    off += p[0];
+    total += p[32];
+  }
+  if (own_sum(total)) a.sums[(int64_t(b) * a.heads + qh) * a.n_q + qi].y += off;
 }
 
 // Two sums of N query rows (32 or 64) to LDS, a row after the other; zeros for those behind `rows`.

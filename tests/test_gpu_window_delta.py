@@ -1,4 +1,4 @@
-"""<do, o> in the backward pass of windowed attention, bf16: what the rounding of o does to it.
+"""<do, o> in the backward pass of windowed attention, bf16: what the rounding of o does to it, and o and log-sum-exp that were joined with other keys'.
 
 Bounds.  u = 2^-8 is what one rounding to bf16 is off by at most, e = 2^-24.  Where a block of 128 rows sees 256 keys at most, <do, o> comes from the keys and dS
 has two bf16 terms, so that nothing but the result is rounded to bf16: a logit is off by x = (d + 4) e scale sum|q k|, a weight by 2 max x + (n + 16) e of itself,
@@ -89,3 +89,41 @@ def test_keys_gradients_do_not_see_the_rounding_of_o(name, heads, d, n, left):
     for h in range(0, heads, 11):
         want = L.window_attn_bwd(*(_np(x[0, h]) for x in (q, k, v)), see, 0.1, _np(d_o[0, h]))[1]
         assert _far(_np(got[0, h]), want) <= U, (name, h)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("heads,kv,d,n_q,parts", [(2, 2, 64, 200, (300, 40)), (2, 1, 128, 200, (1100, 100)), (40, 40, 64, 300, (700, 300)), (40, 20, 128, 130, (280, 60, 3))])
+def test_joined_with_other_keys(heads, kv, d, n_q, parts, dtype):
+    """o and log-sum-exp over several sets of keys, one call each, joined: the backward pass of each set takes the joined ones.
+
+    Bound: rounding of the result and of dS, and the rounding of the joined o (of parts that were rounded) in <do, o>, each below 2^-8 in 2-norm and of independent
+    signs: 2^-7 for all; fp32 below 1e-5 by the same count."""
+    gen = torch.Generator(device="cuda").manual_seed(13)
+    code, dt, tol = {"f32": (P.DFS_F32, torch.float32, 1e-5), "bf16": (P.DFS_BF16, torch.bfloat16, 2.0 ** -7)}[dtype]
+    q, d_o = (_rand(gen, 1, heads, n_q, d).to(dt) for _ in range(2))
+    k, v = (_rand(gen, 1, kv, sum(parts), d).to(dt) for _ in range(2))
+    scale, cuts = 1.5 * d ** -0.5, np.cumsum((0,) + parts)
+    sets = [(P.Window(1, heads, kv, d, n_q, m, -1, -1, 0), k[:, :, a:a + m], v[:, :, a:a + m]) for a, m in zip(cuts, parts)]
+    os, lses = [], []
+    for w, kk, vv in sets:
+        os.append(torch.empty_like(q))
+        lses.append(torch.empty(1, heads, n_q, device="cuda"))
+        P.dfs_window_attn_fwd(w, code, q, kk, vv, None, None, scale, os[-1], lses[-1], _ws(w, dtype, False))
+    lse = torch.logsumexp(torch.stack(lses).double(), 0)
+    o = sum(x.double() * (y - lse).exp()[..., None] for x, y in zip(os, lses)).to(dt)
+    lse = lse.float()
+    group = heads // kv
+    got = []
+    for w, kk, vv in sets:
+        got.append([torch.empty(x.shape, dtype=dt, device="cuda") for x in (q, kk, vv)])
+        P.dfs_window_attn_bwd(w, code, q, kk, vv, o, lse, d_o, None, None, scale, *got[-1], _ws(w, dtype, True))
+    see = np.ones((n_q, sum(parts)), bool)
+    for h in range(0, heads, 7):
+        x, kk, vv, g = (_np(y) for y in (q[0, h], k[0, h // group], v[0, h // group], d_o[0, h]))
+        want, _, p = L.window_attn(x, kk, vv, see, scale)
+        ds = p * (g @ vv.T - (g * want).sum(-1, keepdims=True))
+        for (dq, dk, dv), a, z in zip(got, cuts, cuts[1:]):
+            assert _far(_np(dq[0, h]), scale * ds[:, a:z] @ kk[a:z]) <= tol, ("dq", h, a)
+            if group == 1:
+                assert _far(_np(dk[0, h]), scale * ds[:, a:z].T @ x) <= tol, ("dk", h, a)
+                assert _far(_np(dv[0, h]), p[:, a:z].T @ g) <= tol, ("dv", h, a)
