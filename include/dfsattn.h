@@ -318,8 +318,8 @@ typedef struct {
 
 /*
  * For every row x of q and k: y = x / sqrt(mean(x^2) + eps) * w, then each pair (a, b) of y turned by its angle t,
- * (a cos t - b sin t, a sin t + b cos t).  Norm and rotation are fp32 and rounded once; angles are reduced in fp64, so any int32
- * position is as good as a small one.  A position of zeros turns nothing (text tokens).  Rows of v are copied.
+ * (a cos t - b sin t, a sin t + b cos t).  Norm and rotation are fp32 and rounded once; angles are counted in 2^-64 revolutions,
+ * so with theta >= 1 any int32 position is as good as a small one.  A position of zeros turns nothing (text tokens).  Rows of v are copied.
  *   q [batch, heads, tokens, d], k, v [batch, heads_kv, tokens, d] in, of `dtype` (DFS_F32, DFS_BF16); v may be NULL
  *   positions  int32, tokens x axes numbers, row by row, `pos_batch` numbers from one sequence to the next (0: all share them)
  *   w_q, w_k   [d] fp32 in, or NULL (ones)

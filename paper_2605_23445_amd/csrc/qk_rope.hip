@@ -6,8 +6,9 @@
 // what they have to do is to keep enough rows in flight and the arithmetic out of the way.
 //
 // A lane owns 16 bytes of a row at one token and walks over heads: the angles depend on the token alone, so that their sines and cosines stay in
-// registers and are worked out once for all heads.  The lanes of a row sit side by side and sum by lane exchanges.  Angles are taken in
-// revolutions and reduced in fp64 (an int32 position times a frequency that is good to 2^-53).
+// registers and are worked out once for all heads.  The lanes of a row sit side by side and sum by lane exchanges.  Angles are
+// counted in 2^-64 revolutions: whole ones fall out of an integer product of position and frequency, which is off by 2^-34 of one at the farthest.
+// (An fp64 product of a frequency that is good to 2^-53 left sines and cosines of far positions off by up to 4.5 x 2^-24.)
 #include <math.h>
 
 #include "view.h"
@@ -31,7 +32,7 @@ struct RopeArgs {
   int32_t rot[3];
   float eps;
   float* part;                                       // backward: sums of g x r of each work-group [groups][2][d]
-  double freq[64];                                   // revolutions per unit of position, pair by pair
+  uint64_t freq[64];                                 // 2^-64 revolutions per unit of position, pair by pair
 };
 
 template <typename T> struct Chunk {};
@@ -99,7 +100,7 @@ template <typename T, int D, bool PAIRS> struct Token {
 #pragma unroll
       for (int i = 0; i < C; ++i) {
         const int ch = c * N + 2 * i;
-        turn(ch < end0 ? p0 : ch < end1 ? p1 : p2, ch < end2 ? a.freq[ch / 2] : 0.0, cs[i], sn[i]);
+        turn(ch < end0 ? p0 : ch < end1 ? p1 : p2, ch < end2 ? a.freq[ch / 2] : 0, cs[i], sn[i]);
       }
     } else {
       const int ch = c * N, axis = ch < end0 ? 0 : ch < end1 ? 1 : 2, begin = axis == 0 ? 0 : axis == 1 ? end0 : end1;
@@ -108,14 +109,14 @@ template <typename T, int D, bool PAIRS> struct Token {
       if (turned) partner = first ? lane + half / N : lane - half / N;
 #pragma unroll
       for (int i = 0; i < C; ++i) {
-        turn(axis == 0 ? p0 : axis == 1 ? p1 : p2, turned ? a.freq[begin / 2 + (ch - begin) + i - (first ? 0 : half)] : 0.0, cs[i], sn[i]);
+        turn(axis == 0 ? p0 : axis == 1 ? p1 : p2, turned ? a.freq[begin / 2 + (ch - begin) + i - (first ? 0 : half)] : 0, cs[i], sn[i]);
         if (first) sn[i] = -sn[i];
       }
     }
   }
-  static __device__ __forceinline__ void turn(int32_t p, double f, float& cos_, float& sin_) {
-    const double rev = double(p) * f;
-    sincospif(float(2.0 * (rev - rint(rev))), &sin_, &cos_);
+  static __device__ __forceinline__ void turn(int32_t p, uint64_t f, float& cos_, float& sin_) {
+    const uint64_t t = uint64_t(int64_t(p)) * f;
+    sincospif(fmaf(float(uint32_t(t)), 0x1p-63f, float(int32_t(t >> 32)) * 0x1p-31f), &sin_, &cos_);
   }
   // Turns a row; BACK: by the opposite angle.
   template <bool BACK> __device__ __forceinline__ void rotate(float (&y)[N]) const {
@@ -313,6 +314,13 @@ static int check_qk(const char* call, const dfs_qk_geom* g) {
   return DFS_OK;
 }
 
+// A frequency in 2^-64 revolutions, whole ones left out.  By way of two doubles: a conversion of a long double costs 50 ns, and a call makes up to 64.
+static uint64_t revolutions(long double f) {
+  const long double x = f < 0.25L ? f : f - floorl(f);
+  const double half = double(x * 0.5L), rest = double(x * 0.5L - (long double)half);         // half a revolution, by rounding, is a whole one twice
+  return (half < 0.5 ? uint64_t(int64_t(half * 0x1p64)) * 2 : 0) + uint64_t(int64_t(rest * 0x1p65));
+}
+
 // What both directions take of the geometry.
 static int fill_qk(const char* call, const dfs_qk_geom* g, int dtype, const int32_t* positions, int64_t pos_batch, const float* w_q, const float* w_k,
                    RopeArgs* a) {
@@ -334,10 +342,10 @@ static int fill_qk(const char* call, const dfs_qk_geom* g, int dtype, const int3
   for (int i = 0; i < 3; ++i) {
     a->rot[i] = i < g->axes ? g->rot[i] : 0;
     if (!a->rot[i]) continue;
-    // in extended precision a frequency is good to 2^-53 after up to 64 products
+    // in extended precision a frequency is good to 2^-57 after up to 64 products; positions are whole, so whole revolutions of it do not matter
     const long double step = powl((long double)g->theta, -2.0L / a->rot[i]);
     long double f = 1.0L / 6.283185307179586476925286766559L;
-    for (int j = 0; j < a->rot[i] / 2; ++j, f *= step) a->freq[pair++] = double(f);
+    for (int j = 0; j < a->rot[i] / 2; ++j, f *= step) a->freq[pair++] = revolutions(f);
   }
   return DFS_OK;
 }
