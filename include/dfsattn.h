@@ -305,7 +305,7 @@ typedef struct {
 
 /* Queries and keys of every head in front of attention: their norm and the rotation by position. */
 typedef struct {
-  int32_t batch, tokens;     /* sequences and tokens of each; either may be 0, together fewer than 2^27 */
+  int32_t batch, tokens;     /* sequences and tokens of each; either may be 0, together 2^27 - 8 at most */
   int32_t heads, heads_kv;   /* query heads; key and value heads; at most 65 535 each */
   int32_t d;                 /* head dimension: 64 or 128 */
   int32_t interleaved;       /* 1: channels 2i and 2i + 1 of an axis's share turn together; 0: i and i + half the share */

@@ -295,9 +295,9 @@ constexpr int BWD_GROUPS = 1024;                     // at most, of rope_bwd_ker
 
 static int check_qk(const char* call, const dfs_qk_geom* g) {
   if (!g) return fail(DFS_EINVAL, "%s: geometry pointer is NULL", call);
-  // a token has 32 lanes at most, and a grid fewer than 2^32
-  if (g->batch < 0 || g->tokens < 0 || int64_t(g->batch) * g->tokens >= (int64_t(1) << 27))
-    return fail(DFS_ESHAPE, "%s: batch=%d x tokens=%d must be in [0, 2^27)", call, g->batch, g->tokens);
+  // a token has 32 lanes at most, and a grid fewer than 2^32 in whole work-groups of 256
+  if (g->batch < 0 || g->tokens < 0 || int64_t(g->batch) * g->tokens > (int64_t(1) << 27) - 8)
+    return fail(DFS_ESHAPE, "%s: batch=%d x tokens=%d must be in [0, 2^27 - 8]", call, g->batch, g->tokens);
   if (g->heads < 1 || g->heads_kv < 1 || g->heads > 65535 || g->heads_kv > 65535)
     return fail(DFS_ESHAPE, "%s: heads=%d, heads_kv=%d must be in [1, 65535]", call, g->heads, g->heads_kv);
   if (g->d != 64 && g->d != 128) return fail(DFS_ESHAPE, "%s: d=%d: head dimension must be 64 or 128", call, g->d);
