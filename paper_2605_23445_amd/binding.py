@@ -444,8 +444,10 @@ def _flat(t: torch.Tensor | None, dtype, numel: int, name: str):
     return _ptr(t, dtype, numel, name)
 
 
-def _positions(g: QkGeom, positions: torch.Tensor):
-    """Address of the positions and how many numbers they are from one sequence to the next."""
+def _positions(g: QkGeom, positions: torch.Tensor | None):
+    """Address of the positions (None -> NULL) and how many numbers they are from one sequence to the next."""
+    if positions is None:
+        return None, 0
     shape = (g.tokens, g.axes)
     if tuple(positions.shape) not in (shape, (1, *shape), (g.batch, *shape)):
         raise ValueError(f"positions must be {list(shape)} or one of these for each sequence, got {list(positions.shape)}")
@@ -472,7 +474,9 @@ def dfs_qk_norm_rope(g: QkGeom, dtype: int, q, k, v, positions, w_q, w_k, q_out,
     if rc is not None:
         _check(rc)
     shape = (g.batch, g.heads_kv, g.tokens, g.d)
-    rows = g.tokens if kv_start is None else k_out.shape[2]
+    if kv_start is not None and k_out is not None and k_out.dim() != 4:
+        raise ValueError(f"k_out must be [batch, heads_kv, rows, d], got {list(k_out.shape)}")
+    rows = g.tokens if kv_start is None or k_out is None else k_out.shape[2]
     pos, pos_batch = _positions(g, positions)
     _check(_lib.dfs_qk_norm_rope(g, dtype, _view(q, dtype, g.batch, g.heads, g.tokens, g.d, "q"), _view(k, dtype, *shape, "k"),
                                  _view(v, dtype, *shape, "v"), pos, pos_batch, _flat(w_q, torch.float32, g.d, "w_q"),
