@@ -149,7 +149,7 @@ template <int N> __device__ __forceinline__ void weights(const float* w, int c, 
 }
 
 // Forward.  Bound by memory: 75 600 tokens x 40 heads of q, k and v, bf16, d = 128: 833 us, 5.6 TB/s (a plain copy: 4.9); 2 642 tokens x 12, fp32, d = 64:
-// 9.9 us, 4.9 TB/s; one token of 4 sequences, 32 + 8 heads, into a cache: 3.8 us, a launch.
+// 9.9 us, 4.9 TB/s; one token of 4 sequences, 32 + 8 heads, into a cache: 4.1 to 4.9 us, a launch.
 template <typename T, int D, bool PAIRS, bool ONCE>
 __global__ void __launch_bounds__(256) rope_kernel(RopeArgs a) {
   using Tok = Token<T, D, PAIRS>;
@@ -197,7 +197,8 @@ __global__ void __launch_bounds__(256) rope_kernel(RopeArgs a) {
 
 // Backward.  A work-group takes several groups of tokens, so that the sums for the weights leave it once; `part` holds a row of both for each
 // work-group, which rope_sum_kernel adds up in a fixed order.  Bound by memory: 17 550 tokens x 40 heads, bf16, d = 128: 290 us with the sums' 6, 5.0 TB/s.
-// Small calls are two launches and the sums' row of loads: 666 tokens x (12 + 2 x 4), fp32, d = 64: 12.3 us.
+// Small calls do not fill this: 666 tokens x (12 + 2 x 4), fp32, d = 64, 16 us (12.3 in a graph), of which 11 are this kernel's, in runs of one row where the loop
+// takes two, behind the angles, and 4.4 the sums'.
 template <typename T, int D, bool PAIRS>
 __global__ void __launch_bounds__(256) rope_bwd_kernel(RopeArgs a) {
   using Tok = Token<T, D, PAIRS>;

@@ -174,7 +174,7 @@ template <> struct Mat<float> {
   }
 };
 
-// A result of 32 x 32 as B operand of a product contracted over its rows.
+// A result of 32 x 32 as B operand of a product contracted over its rows; in bf16 rounded to one term, which the kernels' comments weigh.
 template <typename T> struct Weights;
 template <> struct Weights<uint16_t> {
   u32x4 p[2];

@@ -13,8 +13,9 @@ namespace dfs {
 
 constexpr int KN = 64;                               // keys of a tile
 
-// f32: one step per tile of 64 keys, bound by the fp32 matrix instructions and, with one work-group a CU, by what their waves wait for in between: 4 000 tokens
-// x 16 heads, 1 000 keys each way, d = 64: 323 us, 89 TFLOP/s; d = 128: 757 us, 76 TFLOP/s (a large fp32 product of a library: 154).
+// f32: one step per tile of 64 keys, bound by the fp32 matrix instructions and by what their waves wait for in between, one thing after the other in two
+// work-groups a CU at d = 64 and in one, which fills the LDS, at d = 128: 4 000 tokens x 16 heads, 1 000 keys each way, d = 64: 323 to 340 us, 85 to 89 TFLOP/s,
+// matrix cores busy 60 % of the cycles; d = 128: 755 us, 76 TFLOP/s, 52 % (a large fp32 product of a library: 154).
 template <int D>
 __global__ void __launch_bounds__(256) window_f32_kernel(WindowArgs a) {
   using T = float;
@@ -112,6 +113,9 @@ __global__ void __launch_bounds__(256) window_f32_kernel(WindowArgs a) {
 //
 // A row's weights are taken against a reference that is its largest logit's so far to start with and moves where weights have become large: the sums of a
 // lane's weights, which are needed anyway, tell at the cost of a comparison.
+//
+// Weights are rounded to one bf16 term for the product with the values, which leaves o 2.2e-3 from 64 bits in 2-norm where rounding the result alone costs
+// 1.65e-3; their sum is of the unrounded ones.  A second term would be half as many matrix instructions again in a kernel that these bound.
 //
 // Bound by the matrix cores and the vector port beside them.  d = 128: 75 600 tokens x 40 heads, 3 600 keys each way: 9.6 ms, 1 133 TFLOP/s, matrix cores
 // busy 65 % of the cycles at 1.67 GHz; 2 x 8 192 x 32 heads of 8 key heads, 1 024 keys back: 298 us, 868 TFLOP/s, 45 %: a block meets 17 tiles, and its start,
@@ -322,7 +326,9 @@ __global__ void __launch_bounds__(256, 2) window_pipe_kernel(WindowArgs a) {
 // Few queries: the keys of 32 rows are split over the waves of a work-group and over `splits` work-groups, and what they find is joined.  A wave's tiles of 32
 // keys are its own, so that none waits for another before the end, and but for the keys or values
 // that are worked on the LDS is full of loads on their way.  Bound by memory: 48 sequences of 8 key heads, 4 100 keys, bf16, d = 128: 139 us, 5.8 TB/s read; one
-// sequence: 13.5 us with the join (11.9 in a graph), of which the keys' way is 2.4: a launch each, a chain of loads, the waves' join and the splits'.
+// sequence: 13.5 us with the join (11.9 in a graph), of which the keys' way is 2.4: a launch each, a chain of loads, the waves' join and the splits'.  Weights are one
+// bf16 term here as well, and o 2.0e-3 to 2.2e-3 from 64 bits: two make that 1.65e-3 and cost 0.5 % of the time of these 48 sequences, 3 % of the one's and 12 % of a
+// prompt's of 2 048 tokens x 8 heads, d = 64.
 template <typename T, int D> constexpr int split_waves() { return sizeof(T) == 4 && D == 128 ? 2 : 4; }
 template <typename T, int D, bool ONCE>
 __global__ void __launch_bounds__((64 * split_waves<T, D>()), 1) window_split_kernel(WindowArgs a) {

@@ -1,9 +1,10 @@
 // Backward pass of attention over a window and a few first keys: the queries' gradient, then those of keys and values.
 //
 // The first kernel goes over keys for a block of queries, as the forward pass does, and leaves <do, o> of every row beside its log-sum-exp; the second goes
-// over queries for a block of keys, head by head of those that share it, so that every sum is one work-group's and no atomics are needed.  Both work the
-// weights out anew from the log-sum-exp.  The second takes the pairs of the windows alone: the first keys, which every query sees, would keep a work-group
-// for as long as all others take together.  Their other pairs are dealt to work-groups of a third kernel, and a fourth adds the parts up.
+// over queries for a block of keys, head by head of those that share it.  Both work the weights out anew from the log-sum-exp.  A block is one work-group's
+// or, where blocks are few, shared by several, whose parts another kernel adds up in a fixed order: there are no atomics.  The second takes the pairs of the
+// windows alone: the first keys, which every query sees, would keep a work-group for as long as all others take together.  Their other pairs are dealt to
+// work-groups of a third kernel, and a fourth adds the parts up.
 #include <float.h>
 #include <math.h>
 
@@ -33,8 +34,9 @@ __device__ __forceinline__ float both_halves(float x) {
   return __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
 }
 
-// f32: one step per tile of 64 keys, bound by the fp32 matrix instructions, with one work-group a CU (forward and backward of 4 000 tokens x 16 heads, 1 000 keys
-// each way: d = 64 1.53 ms, d = 128 3.37 ms, 43 and 39 % of a large product's rate).
+// f32: one step per tile of 64 keys, bound by the fp32 matrix instructions and by what their waves wait for in between, as in the forward pass: two work-groups a CU
+// at d = 64, one at d = 128 (4 000 tokens x 16 heads, 1 000 keys each way: 473 and 1 030 us, matrix cores busy 62 and 54 % of the cycles; forward and backward 1.53
+// and 3.37 ms, 43 and 39 % of a large product's rate).
 template <int D>
 __global__ void __launch_bounds__(256, 1) window_dq_f32_kernel(WindowArgs a) {
   typedef float T;
@@ -134,12 +136,13 @@ __global__ void __launch_bounds__(256, 1) window_dq_f32_kernel(WindowArgs a) {
 // have three buffers, as the next tile's are read while this one's still are; two work-groups fill the LDS of a CU.
 //
 // dS goes into its product as two bf16 terms, and the rows' sums of dS, which are zero but for what rounding o has cost <do, o>, are added to that: dk
-// is worked out with the corrected one.  (Where o and log-sum-exp were joined with other keys' they are not zero, and nothing is corrected.)  In one term and without it dq and dk were 1.6 to 2 times as far from 64 bits as rounding them alone (relative 2-norm
-// 2.5e-3 to 3.3e-3; now 1.8e-3 to 2.4e-3).  Where a block of rows sees four tiles of keys at most, the error of <do, o> is most of dq's, so it is worked
-// out from the keys beforehand.
+// is worked out with the corrected one.  (Where o and log-sum-exp were joined with other keys' they are not zero, and nothing is corrected.)  In one term and
+// without it dq and dk were 1.6 to 2 times as far from 64 bits as rounding them alone (relative 2-norm 2.5e-3 to 3.3e-3; now 1.8e-3 to 2.4e-3).  Where a block
+// of rows sees four tiles of keys at most, the error of <do, o> is most of dq's, so it is worked out from the keys beforehand.
 //
-// Bound by the matrix cores and the vector port beside them: 17 550 tokens x 30 heads, d = 64, 1 350 keys each way: 790 us, 891 TFLOP/s with the second term's,
-// matrix cores busy 48 % of the cycles; 2 x 4 001 (ragged) x 32 heads of 8 key heads, d = 128, 512 keys back: 119 us, 738 TFLOP/s, 38 %.
+// Bound by the matrix cores and the vector port beside them: 17 550 tokens x 30 heads, d = 64, 1 350 keys each way: 830 us, 848 TFLOP/s with the second term's,
+// matrix cores busy 45 % of the cycles (790 and 48 % without the sum of weights); 2 x 4 001 (ragged) x 32 heads of 8 key heads, d = 128, 512 keys back: 118 us,
+// 744 TFLOP/s, 38 %.
 template <int D>
 __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) window_dq_kernel(WindowArgs a) {
   typedef uint16_t T;
@@ -388,9 +391,11 @@ template <int N> __device__ __forceinline__ void load_sums(const float2* from, i
 }
 
 // Keys as columns: register i of a lane holds query row 8 (i / 4) + 4 h + i % 4 of a tile of 32, against the lane's key.  A lone wave a SIMD issues a vector
-// instruction every eight to ten cycles and cannot keep the matrix cores busy, so two work-groups share a CU: in bf16 at d = 128, where the accumulators
-// alone take 128 registers, the keys' rows stay in registers and the values' come from LDS in every tile.  At the sizes above 800 us, 880 TFLOP/s, 48 %, and
-// 152 us, 578 TFLOP/s, 32 %: two work-groups a CU do not fill what one of them waits for.
+// instruction every eight to ten cycles and cannot keep the matrix cores busy, so in bf16 two work-groups share a CU: the keys' rows stay in registers and the
+// values' come from LDS in every tile (at d = 128 the accumulators alone take 128 registers).  At the sizes above 770 to 800 us, 880 to 915 TFLOP/s, 47 %, and 148 us,
+// 594 TFLOP/s, 31 %: of 512 places on the CUs the ragged lengths fill 368, and two work-groups a CU do not fill what one of them waits for.  P and dS are one bf16
+// term each: dk and dv are 2.35e-3 from 64 bits in 2-norm where rounding the results alone costs 1.65e-3, and a second term would be half of this kernel's products
+// again.  In fp32 one work-group a CU, whose 263 registers at d = 64 are seven more than two allow (4 000 tokens x 16 heads: 741 us, 54 %; d = 128: 1 490, 52 %).
 template <typename T, int D>
 __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) window_dkv_kernel(WindowArgs a) {
   constexpr bool BF16 = sizeof(T) == 2, V_LDS = BF16;
