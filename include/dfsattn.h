@@ -383,7 +383,7 @@ int dfs_window_attn_fwd(const dfs_window* w, int dtype, const dfs_view* q, const
  *   P = exp(scale <q, k_j> - lse),  dv_j = sum P do,  dS = P (<do, v_j> - <do, o>),  dq = scale sum dS k_j,  dk_j = scale sum dS q,
  * dk and dv summed over the query heads that share a key head.  No atomics: same call, same bits.  bf16: P and dS are rounded to bf16
  * for the products (dS to two terms for that with the keys), sums are fp32, and <do, o> is put right for the rounding of o in rows of which
- * P adds up to 1 within 2^-9 (it does not where o was joined): for dq and dk where 128 rows side by side see 256 keys at most, for dk
+ * P adds up to 1 within 2^-12 (it does not where o was joined): for dq and dk where 128 rows side by side see 256 keys at most, for dk
  * alone where they see more; f32: fp32 throughout.  dq rows at or behind q_len, dk and dv rows at or behind k_len are left as they are;
  * rows that nothing sees, or that see nothing, get zeros.  What is not finite spreads to the gradients of up to 127 rows or keys beside
  * it, as in the forward pass.

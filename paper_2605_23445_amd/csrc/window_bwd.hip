@@ -24,9 +24,10 @@ __device__ __forceinline__ float* key_part(const WindowArgs& a, int d, int bh, i
 // of dq of the 32 rows of `tile`, and behind it (bf16) of the rows' sums of dS and of weights.
 __device__ __forceinline__ float* row_part(const WindowArgs& a, int d, int64_t tile, int split) { return a.row_part + (tile * a.row_splits + split) * 32 * (d + 2); }
 
-// Whether a row's weights, with this sum, are all that its log-sum-exp counts: not where that was joined with other keys' (fp32 rounds a weight's exponent, of
-// some |log-sum-exp| 2^-23).  Then the sum of dS is zero but for rounding; what a joined row's may be wrong by within this bound is less than a rounding to bf16.
-__device__ __forceinline__ bool own_sum(float x) { return fabsf(x - 1.f) <= 0x1p-9f; }
+// Whether a row's weights, with this sum, are all that its log-sum-exp (here `ref`, in base 2) counts: not where that was joined with other keys'.  Then the sum
+// of dS is zero but for rounding.  The sum is off from 1 by what fp32 rounds the weights' exponents by, below 2^-21 |ref|, and by the sums' own rounding; other
+// keys of less weight than that are left out of a joined row's <do, o>.
+__device__ __forceinline__ bool own_sum(float x, float ref) { return fabsf(x - 1.f) <= 0x1p-12f + 0x1p-20f * fabsf(ref); }
 
 // Sum of what the two lanes that share a row hold.
 __device__ __forceinline__ float both_halves(float x) {
@@ -300,7 +301,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) window_dq_kernel(WindowA
       __syncthreads();                               // every wave has left the tile
       issue(t + 1 < all_tiles ? t + 1 : t0, 0, 3 * BYTES);
     }
-    if (own_sum(both_halves(weights))) delta = both_halves(sum);
+    if (own_sum(both_halves(weights), ref)) delta = both_halves(sum);
   }
   if (t0 < n_tiles) {
     wait_loads();
@@ -332,7 +333,7 @@ __global__ void __launch_bounds__(256, D == 64 ? 3 : 2) window_dq_kernel(WindowA
   }
   off = both_halves(off);
   total = both_halves(total);
-  if (row.real && row.h == 0 && split == 0) a.sums[sums] = make_float2(ref, a.row_splits == 1 && own_sum(total) ? delta + off : delta);
+  if (row.real && row.h == 0 && split == 0) a.sums[sums] = make_float2(ref, a.row_splits == 1 && own_sum(total, ref) ? delta + off : delta);
   wait_loads();                                      // nothing of this work-group's is on its way when its LDS is another's
   if (a.row_splits > 1) {
     float* mine = row_part(a, D, (int64_t(at.bh) * (a.blocks / a.row_splits) + blk) * NW + wave, split) + lane;
@@ -375,7 +376,8 @@ __global__ void __launch_bounds__(256) window_dq_sum_kernel(WindowArgs a) {
     off += p[0];
     total += p[32];
   }
-  if (own_sum(total)) a.sums[(int64_t(b) * a.heads + qh) * a.n_q + qi].y += off;
+  float2& sums = a.sums[(int64_t(b) * a.heads + qh) * a.n_q + qi];
+  if (own_sum(total, sums.x)) sums.y += off;
 }
 
 // Two sums of N query rows (32 or 64) to LDS, a row after the other; zeros for those behind `rows`.

@@ -127,3 +127,37 @@ def test_joined_with_other_keys(heads, kv, d, n_q, parts, dtype):
             if group == 1:
                 assert _far(_np(dk[0, h]), scale * ds[:, a:z].T @ x) <= tol, ("dk", h, a)
                 assert _far(_np(dv[0, h]), p[:, a:z].T @ g) <= tol, ("dv", h, a)
+
+
+@pytest.mark.parametrize("d,parts", [(64, (100, 40)), (128, (200, 40)), (64, (900, 40))])
+def test_joined_with_keys_of_little_weight_and_large_values(d, parts):
+    """The other keys have a thousandth of a row's weight and values a hundred times as large, so that they make up half of o.  Bound as above."""
+    gen = torch.Generator(device="cuda").manual_seed(14)
+    n_q, m = 200, parts[0]
+    u = torch.nn.functional.normalize(_rand(gen, d), dim=0)
+    q, d_o = ((x * _rand(gen, 1, 2, n_q, d) + y * u).bfloat16() for x, y in ((0.5, 4.0), (1.0, 0.0)))
+    k, v = (_rand(gen, 1, 2, sum(parts), d) for _ in range(2))
+    k = 2 * d ** -0.5 * (k - u * (k @ u)[..., None])                       # logits that the common part of the queries has no share in
+    k[:, :, m:] += u * (np.log(1e-3 * m / parts[1]) / 4.0)
+    v[:, :, m:] *= 100
+    k, v, scale = k.bfloat16(), v.bfloat16(), 1.0
+    sets = [(P.Window(1, 2, 2, d, n_q, z - a, -1, -1, 0), k[:, :, a:z], v[:, :, a:z]) for a, z in ((0, m), (m, sum(parts)))]
+    os, lses = [], []
+    for w, kk, vv in sets:
+        os.append(torch.empty_like(q))
+        lses.append(torch.empty(1, 2, n_q, device="cuda"))
+        P.dfs_window_attn_fwd(w, P.DFS_BF16, q, kk, vv, None, None, scale, os[-1], lses[-1], _ws(w, "bf16", False))
+    lse = torch.logsumexp(torch.stack(lses).double(), 0)
+    o = sum(x.double() * (y - lse).exp()[..., None] for x, y in zip(os, lses)).bfloat16()
+    w, kk, vv = sets[0]
+    dq, dk, dv = (torch.empty(x.shape, dtype=torch.bfloat16, device="cuda") for x in (q, kk, vv))
+    P.dfs_window_attn_bwd(w, P.DFS_BF16, q, kk, vv, o, lse.float(), d_o, None, None, scale, dq, dk, dv, _ws(w, "bf16", True))
+    for h in range(2):
+        x, kk, vv, g = (_np(y) for y in (q[0, h], k[0, h], v[0, h], d_o[0, h]))
+        want, _, p = L.window_attn(x, kk, vv, np.ones((n_q, sum(parts)), bool), scale)
+        rest = p[:, m:].sum(-1)
+        assert 2.0 ** -11 < np.median(rest) < 2.0 ** -9
+        ds = p * (g @ vv.T - (g * want).sum(-1, keepdims=True))
+        assert _far(_np(dq[0, h]), scale * ds[:, :m] @ kk[:m]) <= 2.0 ** -7, ("dq", h)
+        assert _far(_np(dk[0, h]), scale * ds[:, :m].T @ x) <= 2.0 ** -7, ("dk", h)
+        assert _far(_np(dv[0, h]), p[:, :m].T @ g) <= 2.0 ** -7, ("dv", h)
