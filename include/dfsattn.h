@@ -355,7 +355,8 @@ typedef struct {
   int32_t left, right;                 /* how far a query sees back and ahead; negative: without limit */
   int32_t sinks;                       /* the first keys that every query sees which may see so far ahead; 0 if none */
   /* The blocks of 128 rows (query heads of a key head together), of 128 keys and of 32 first keys are each fewer than 2^24 over all batches
-     and key heads: 2^31 rows or keys, 2^29 first ones. */
+     and key heads: 2^31 rows or keys, 2^29 first ones.  Query rows of a key head (n_q heads / heads_kv) are 2^30 at most in a sequence, and rows
+     of k and v (backward: of q and do as well) lie 2^24 bytes apart at most. */
 } dfs_window;
 
 /*
