@@ -397,6 +397,44 @@ int dfs_window_attn_bwd(const dfs_window* w, int dtype, const dfs_view* q, const
 /* Bytes of scratch of dfs_window_attn_fwd (backward = 0) or dfs_window_attn_bwd (1); 0 also if `w` is invalid.  Host only. */
 size_t dfs_window_workspace_bytes(const dfs_window* w, int dtype, int backward);
 
+/* Sequences of different lengths, one behind the other without padding. */
+typedef struct {
+  int32_t seqs, heads, heads_kv, d;    /* heads a multiple of heads_kv: query heads g*j .. g*j + g - 1 share key head j; d 64 or 128 */
+  int32_t n_q, n_k;                    /* rows of the query and of the key tensors, of all sequences together; at most 2^28, either may be 0 */
+  int32_t left, right;                 /* how far a query sees back and ahead; negative: without limit (causal: left -1, right 0) */
+  /* Blocks of 128 rows (query heads of a key head together) or of 128 keys, and one more for each sequence, are fewer than 2^24 over all key heads.  Query rows
+     of a key head (n_q heads / heads_kv) are 2^30 at most, and rows of k and v (backward: of q and do as well) lie 2^24 bytes apart at most. */
+} dfs_packed;
+
+/*
+ * Attention within each of several sequences.  Sequence s has the rows q_start[s] .. q_start[s+1] - 1 of q and o and the rows k_start[s] .. k_start[s+1] - 1 of k and v,
+ * either of which may be none.  Row i of its q_len queries stands at position p = k_len - q_len + i and sees its key j if p - left <= j <= p + right:
+ *   o = sum_j softmax_j(scale <q, k_j>) v_j,   lse = ln sum_j exp(scale <q, k_j>).
+ * A row that sees nothing has o = 0 and lse = -inf.  Arithmetic and rounding are those of dfs_window_attn_fwd.
+ *   q [heads, n_q, d], k, v [heads_kv, n_k, d] in, o like q out; the `batch` of these views is not read
+ *   q_start [seqs + 1] int32, not falling; k_start alike, or NULL: that of the queries (n_k is n_q then).  Starts outside [0, n_q], [0, n_k] are cut to
+ *   that range; where one falls, which rows are worked out is undefined, but nothing outside the tensors is touched.
+ *   lse [heads, n_q] fp32 out, dense, or NULL;   scale > 0
+ * Rows in front of q_start[0] and from q_start[seqs] on are not read and their o and lse are left as they are.  Keys and values that no row sees may hold anything.  A value
+ * that is not finite makes the rows that see it NaN or infinite, and possibly up to 127 rows beside them of the same sequence.
+ * The same call gives the same bits every time; the same sequence among others may differ by rounding.
+ * ws: dfs_packed_workspace_bytes(w, dtype, 0), which may be 0 (then NULL will do).
+ */
+int dfs_packed_attn_fwd(const dfs_packed* w, int dtype, const dfs_view* q, const dfs_view* k, const dfs_view* v, const int32_t* q_start,
+                        const int32_t* k_start, float scale, const dfs_view* o, float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Its backward pass, as dfs_window_attn_bwd is that of dfs_window_attn_fwd: dq, dk and dv from the forward call's inputs, its o and lse, and do, the gradient of o.
+ * Rows outside the sequences are left as they are; rows that nothing sees, or that see nothing, get zeros.  No atomics: same call, same bits.
+ * ws: dfs_packed_workspace_bytes(w, dtype, 1).
+ */
+int dfs_packed_attn_bwd(const dfs_packed* w, int dtype, const dfs_view* q, const dfs_view* k, const dfs_view* v, const dfs_view* o, const float* lse,
+                        const dfs_view* d_o, const int32_t* q_start, const int32_t* k_start, float scale, const dfs_view* dq, const dfs_view* dk,
+                        const dfs_view* dv, void* ws, size_t ws_bytes, void* stream);
+
+/* Bytes of scratch of dfs_packed_attn_fwd (backward = 0) or dfs_packed_attn_bwd (1); 0 also if `w` is invalid.  Host only. */
+size_t dfs_packed_workspace_bytes(const dfs_packed* w, int dtype, int backward);
+
 /*
  * Diagnostic for measurements, not part of the method: while `counters` (device memory, 3 x uint64, zeroed by
  * the caller) is set, every work-group of the bf16 attention kernel adds to counters[0] the shader-clock

@@ -50,6 +50,11 @@ class Window(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("batch", "heads", "heads_kv", "d", "n_q", "n_k", "left", "right", "sinks")]
 
 
+class Packed(C.Structure):
+    """Mirror of dfs_packed."""
+    _fields_ = [(n, C.c_int32) for n in ("seqs", "heads", "heads_kv", "d", "n_q", "n_k", "left", "right")]
+
+
 class _View(C.Structure):
     """Mirror of dfs_view."""
     _fields_ = [("data", C.c_void_p), ("batch", C.c_int64), ("head", C.c_int64), ("row", C.c_int64)]
@@ -75,7 +80,7 @@ def _load():
                           "(or python paper_2605_23445_amd/build.py) first - there is no fallback path")
     lib = C.CDLL(_LIB_PATH)
     vp, i32, i64, dbl, f32, sz = C.c_void_p, C.c_int32, C.c_int64, C.c_double, C.c_float, C.c_size_t
-    gp, qp, wp, tp = C.POINTER(Geom), C.POINTER(QkGeom), C.POINTER(Window), C.POINTER(_View)
+    gp, qp, wp, kp, tp = C.POINTER(Geom), C.POINTER(QkGeom), C.POINTER(Window), C.POINTER(Packed), C.POINTER(_View)
     sig = {
         "dfs_geom_sizes": (C.c_int, [gp, C.POINTER(Sizes)]),
         "dfs_workspace_bytes": (sz, [gp, C.c_int]),
@@ -106,6 +111,9 @@ def _load():
         "dfs_window_attn_fwd": (C.c_int, [wp, C.c_int, tp, tp, tp, vp, vp, f32, tp, vp, vp, sz, vp]),
         "dfs_window_attn_bwd": (C.c_int, [wp, C.c_int, tp, tp, tp, tp, vp, tp, vp, vp, f32, tp, tp, tp, vp, sz, vp]),
         "dfs_window_workspace_bytes": (sz, [wp, C.c_int, C.c_int]),
+        "dfs_packed_attn_fwd": (C.c_int, [kp, C.c_int, tp, tp, tp, vp, vp, f32, tp, vp, vp, sz, vp]),
+        "dfs_packed_attn_bwd": (C.c_int, [kp, C.c_int, tp, tp, tp, tp, vp, tp, vp, vp, f32, tp, tp, tp, vp, sz, vp]),
+        "dfs_packed_workspace_bytes": (sz, [kp, C.c_int, C.c_int]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -114,7 +122,7 @@ def _load():
 
 
 def _load_calls(names=("forward", "token_order", "permute", "unperm", "block_score", "select_mask", "sparse_attn", "recall",
-                       "qk_norm_rope", "qk_norm_rope_bwd", "window_attn_fwd", "window_attn_bwd")):
+                       "qk_norm_rope", "qk_norm_rope_bwd", "window_attn_fwd", "window_attn_bwd", "packed_attn_fwd", "packed_attn_bwd")):
     """The calls of the _calls module.  They do in native code what those of the same names do below, for plain
     arguments, and return None for what they leave to these: as the stand-ins do for every call where the module is not there or
     was built against another torch, whose classes it reads (another Python does not find it: its name holds the version)."""
@@ -126,7 +134,7 @@ def _load_calls(names=("forward", "token_order", "permute", "unperm", "block_sco
             why = "older than this file"
         else:
             _calls.set_geom_type(Geom)
-            _calls.set_layer_types(QkGeom, Window)
+            _calls.set_layer_types(QkGeom, Window, Packed)
             return [getattr(_calls, name) for name in names]
     except ImportError as e:
         why = str(e)
@@ -137,12 +145,13 @@ def _load_calls(names=("forward", "token_order", "permute", "unperm", "block_sco
 
 _lib = _load()
 (_plain_forward, _plain_token_order, _plain_permute, _plain_unperm, _plain_block_score, _plain_select_mask, _plain_sparse_attn,
- _plain_recall, _plain_qk_norm_rope, _plain_qk_norm_rope_bwd, _plain_window_attn_fwd, _plain_window_attn_bwd) = _load_calls()
+ _plain_recall, _plain_qk_norm_rope, _plain_qk_norm_rope_bwd, _plain_window_attn_fwd, _plain_window_attn_bwd, _plain_packed_attn_fwd,
+ _plain_packed_attn_bwd) = _load_calls()
 EXPORTS = ("dfs_geom_sizes", "dfs_workspace_bytes", "dfs_last_error", "dfs_keep_count", "dfs_hilbert_perm", "dfs_permute",
            "dfs_block_score", "dfs_select_mask", "dfs_sparse_attn_fwd", "dfs_unperm", "dfs_forward", "dfs_token_order", "dfs_recall",
            "dfs_schedule", "dfs_block_score_src", "dfs_sparse_attn_fwd_src", "dfs_attn_clock_probe", "dfs_block_score_fused", "dfs_probe_mfma", "dfs_probe_copy", "dfs_probe_read",
            "dfs_select_mask_static", "dfs_qk_norm_rope", "dfs_qk_norm_rope_bwd", "dfs_qk_workspace_bytes", "dfs_window_attn_fwd",
-           "dfs_window_attn_bwd", "dfs_window_workspace_bytes")
+           "dfs_window_attn_bwd", "dfs_window_workspace_bytes", "dfs_packed_attn_fwd", "dfs_packed_attn_bwd", "dfs_packed_workspace_bytes")
 DFS_ORDER_HILBERT3D, DFS_ORDER_RASTER, DFS_ORDER_HILBERT2D, DFS_ORDER_BLOCK3D = 0, 1, 2, 3
 
 
@@ -534,3 +543,49 @@ def dfs_window_attn_bwd(w: Window, dtype: int, q, k, v, o, lse, d_o, q_len, k_le
                                     _view(o, dtype, *qs, "o"), _flat(lse, torch.float32, w.batch * w.heads * w.n_q, "lse"), _view(d_o, dtype, *qs, "d_o"),
                                     _flat(q_len, torch.int32, w.batch, "q_len"), _flat(k_len, torch.int32, w.batch, "k_len"), float(scale),
                                     _view(dq, dtype, *qs, "dq"), _view(dk, dtype, *ks, "dk"), _view(dv, dtype, *ks, "dv"), wsp, wb, _stream()))
+
+
+# Attention within packed sequences: tensors are [heads, rows of all sequences, d], with any strides whose rows are dense.
+
+
+def _flat_view(t: torch.Tensor | None, dtype: int, heads: int, rows: int, d: int, name: str):
+    """dfs_view of a tensor of one batch without that axis (None -> NULL)."""
+    if t is None:
+        return None
+    if t.dim() != 3:
+        raise ValueError(f"{name} must be {[heads, rows, d]}, got {list(t.shape)}")
+    return _view(t[None], dtype, 1, heads, rows, d, name)
+
+
+def dfs_packed_workspace_bytes(w: Packed, dtype: int, backward: bool) -> int:
+    return int(_lib.dfs_packed_workspace_bytes(w, dtype, int(bool(backward))))
+
+
+def dfs_packed_attn_fwd(w: Packed, dtype: int, q, k, v, q_start, k_start, scale: float, o, lse=None, ws=None):
+    """Attention within sequences that lie behind one another; q_start and k_start are [seqs + 1] int32, k_start None where it is q_start, ws where it
+    takes none."""
+    rc = _plain_packed_attn_fwd(w, dtype, q, k, v, q_start, k_start, scale, o, lse, ws)
+    if rc == 0:
+        return
+    if rc is not None:
+        _check(rc)
+    qs, ks = (w.heads, w.n_q, w.d), (w.heads_kv, w.n_k, w.d)
+    wsp, wb = _scratch(ws)
+    _check(_lib.dfs_packed_attn_fwd(w, dtype, _flat_view(q, dtype, *qs, "q"), _flat_view(k, dtype, *ks, "k"), _flat_view(v, dtype, *ks, "v"),
+                                    _flat(q_start, torch.int32, w.seqs + 1, "q_start"), _flat(k_start, torch.int32, w.seqs + 1, "k_start"), float(scale),
+                                    _flat_view(o, dtype, *qs, "o"), _flat(lse, torch.float32, w.heads * w.n_q, "lse"), wsp, wb, _stream()))
+
+
+def dfs_packed_attn_bwd(w: Packed, dtype: int, q, k, v, o, lse, d_o, q_start, k_start, scale: float, dq, dk, dv, ws):
+    """Gradients of dfs_packed_attn_fwd from its inputs, its o and lse, and d_o, the gradient of o."""
+    rc = _plain_packed_attn_bwd(w, dtype, q, k, v, o, lse, d_o, q_start, k_start, scale, dq, dk, dv, ws)
+    if rc == 0:
+        return
+    if rc is not None:
+        _check(rc)
+    qs, ks = (w.heads, w.n_q, w.d), (w.heads_kv, w.n_k, w.d)
+    wsp, wb = _scratch(ws)
+    _check(_lib.dfs_packed_attn_bwd(w, dtype, _flat_view(q, dtype, *qs, "q"), _flat_view(k, dtype, *ks, "k"), _flat_view(v, dtype, *ks, "v"),
+                                    _flat_view(o, dtype, *qs, "o"), _flat(lse, torch.float32, w.heads * w.n_q, "lse"), _flat_view(d_o, dtype, *qs, "d_o"),
+                                    _flat(q_start, torch.int32, w.seqs + 1, "q_start"), _flat(k_start, torch.int32, w.seqs + 1, "k_start"), float(scale),
+                                    _flat_view(dq, dtype, *qs, "dq"), _flat_view(dk, dtype, *ks, "dk"), _flat_view(dv, dtype, *ks, "dv"), wsp, wb, _stream()))

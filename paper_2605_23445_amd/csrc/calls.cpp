@@ -19,8 +19,8 @@
 
 namespace {
 
-// binding.Geom, QkGeom and Window, ctypes structures with the layouts of dfs_geom, dfs_qk_geom and dfs_window
-PyObject *g_geom_type = nullptr, *g_qk_type = nullptr, *g_window_type = nullptr;
+// binding.Geom, QkGeom, Window and Packed, ctypes structures with the layouts of dfs_geom, dfs_qk_geom, dfs_window and dfs_packed
+PyObject *g_geom_type = nullptr, *g_qk_type = nullptr, *g_window_type = nullptr, *g_packed_type = nullptr;
 PyObject *s_kv_idx, *s_kv_cnt, *s_mask, *s_k_head, *s_K_max;
 
 struct NotPlain {};                                 // thrown where binding.py has to look at an argument
@@ -264,6 +264,18 @@ struct Here {
     r.there = true;
     return r;
   }
+  // Of one batch, without that axis.
+  MaybeView flat_view(PyObject* x, int dtype, int64_t heads, int64_t rows, int64_t d) const {
+    MaybeView r = {};
+    if (x == Py_None) return r;
+    const at::Tensor& t = tensor(x, tensor_type(dtype));
+    need(t.dim() == 3);
+    const auto n = t.sizes(), s = t.strides();
+    need(n[0] == heads && n[1] == rows && n[2] == d && (s[2] == 1 || t.numel() == 0));
+    r.v = dfs_view{t.data_ptr(), 0, s[0], s[1]};
+    r.there = true;
+    return r;
+  }
   template <class T> T* flat(PyObject* x, at::ScalarType type, int64_t numel, int64_t* bytes = nullptr) const {
     if (x == Py_None) return nullptr;
     const at::Tensor& t = tensor(x, type);
@@ -357,12 +369,38 @@ PyObject* window_attn(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+template <bool BACK>
+PyObject* packed_attn(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> int {
+    need(n == (BACK ? 15 : 11));
+    const auto w = to_struct<dfs_packed>(a[0], g_packed_type);
+    const int dtype = to_int(a[1]);
+    const Here here;
+    int64_t ws_bytes = 0;
+    const auto of_q = [&](PyObject* x) { return here.flat_view(x, dtype, w.heads, w.n_q, w.d); };
+    const auto of_k = [&](PyObject* x) { return here.flat_view(x, dtype, w.heads_kv, w.n_k, w.d); };
+    const auto q = of_q(a[2]), k = of_k(a[3]), v = of_k(a[4]), o = of_q(a[BACK ? 5 : 8]);
+    auto* lse = here.flat<float>(a[BACK ? 6 : 9], at::kFloat, int64_t(w.heads) * w.n_q);
+    PyObject* const* start = a + (BACK ? 8 : 5);
+    const auto *q_start = here.flat<const int32_t>(start[0], at::kInt, int64_t(w.seqs) + 1), *k_start = here.flat<const int32_t>(start[1], at::kInt, int64_t(w.seqs) + 1);
+    const float scale = float(to_double(start[2]));
+    void *ws = here.flat<void>(a[n - 1], at::ScalarType::Undefined, 0, &ws_bytes), *st = stream();
+    if (!BACK)
+      return without_gil([&] { return dfs_packed_attn_fwd(&w, dtype, q.get(), k.get(), v.get(), q_start, k_start, scale, o.get(), lse, ws, size_t(ws_bytes), st); });
+    const auto d_o = of_q(a[7]), dq = of_q(a[BACK ? 11 : 0]), dk = of_k(a[BACK ? 12 : 0]), dv = of_k(a[BACK ? 13 : 0]);
+    return without_gil([&] {
+      return dfs_packed_attn_bwd(&w, dtype, q.get(), k.get(), v.get(), o.get(), lse, d_o.get(), q_start, k_start, scale, dq.get(), dk.get(), dv.get(), ws,
+                                 size_t(ws_bytes), st);
+    });
+  });
+}
+
 PyObject* set_layer_types(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  if (n == 2) {
-    Py_INCREF(a[0]);
-    Py_INCREF(a[1]);
+  if (n == 3) {
+    for (int i = 0; i < 3; ++i) Py_INCREF(a[i]);
     g_qk_type = a[0];
     g_window_type = a[1];
+    g_packed_type = a[2];
   }
   Py_RETURN_NONE;
 }
@@ -386,6 +424,8 @@ PyMethodDef methods[] = {
     {"qk_norm_rope_bwd", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(qk_norm_rope_bwd)), METH_FASTCALL, nullptr},
     {"window_attn_fwd", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(window_attn<false>)), METH_FASTCALL, nullptr},
     {"window_attn_bwd", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(window_attn<true>)), METH_FASTCALL, nullptr},
+    {"packed_attn_fwd", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(packed_attn<false>)), METH_FASTCALL, nullptr},
+    {"packed_attn_bwd", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(packed_attn<true>)), METH_FASTCALL, nullptr},
     {"set_geom_type", set_geom_type, METH_O, nullptr},
     {"set_layer_types", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(set_layer_types)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};

@@ -6,6 +6,8 @@
 // With 32x32 products a lane holds, of the result, column lane % 32 and rows 8 (i / 4) + 4 (lane / 32) + i % 4 in register i: as B operand of a product
 // contracted over those rows the registers serve as they are.
 #pragma once
+#include <type_traits>
+
 #include "view.h"
 
 namespace dfs {
@@ -41,11 +43,14 @@ struct WindowArgs {
   float *key_part, *row_part;                        // backward: sums of a split's part of 32 keys' gradients, of 32 rows'
   float2* part_sums;                                 // maximum and sum of a row's part
   const int32_t *q_len, *k_len;
+  const int32_t *q_start, *k_start;                  // packed sequences: their first rows, and the end of the last one's
+  int32_t packed;                                    // packed sequences; batch is 1 then, n_q and n_k are the rows of all
   int32_t batch, heads, heads_kv, group, n_q, n_k, left, right, sinks;
   int32_t blocks, seqs;                              // work-groups of a sequence's key head; key heads of all sequences
   Div by_blocks, by_kv, by_group, by_splits;         // by_splits: by the work-groups that share a block
   int32_t first_tiles, first_splits;                 // backward: tiles of 32 first keys, and work-groups that share one's queries
   int32_t key_splits, row_splits;                    // backward: work-groups that share a block of keys, a block of rows
+  int32_t key_tiles;                                 // backward: tiles of 32 keys of a key head of which parts are kept
   int32_t splits;                                    // forward: work-groups that share the keys of 32 rows
   float scale;
   void set_blocks(int64_t n) {
@@ -54,9 +59,14 @@ struct WindowArgs {
   }
 };
 
+__device__ __forceinline__ int min_of(int a, int b) { return a < b ? a : b; }
+__device__ __forceinline__ int max_of(int a, int b) { return a > b ? a : b; }
+
 // A sequence's lengths, and the position of its first query.
 struct Lengths {
   int q, k, shift;
+  Lengths() = default;
+  __device__ __forceinline__ Lengths(int q_, int k_) : q(q_), k(k_), shift(k_ - q_) {}
   __device__ __forceinline__ Lengths(const WindowArgs& a, int b) {
     q = a.q_len ? a.q_len[b] : a.n_q;
     k = a.k_len ? a.k_len[b] : a.n_k;
@@ -65,9 +75,6 @@ struct Lengths {
     shift = k - q;
   }
 };
-
-__device__ __forceinline__ int min_of(int a, int b) { return a < b ? a : b; }
-__device__ __forceinline__ int max_of(int a, int b) { return a > b ? a : b; }
 
 // Puts `none` where register i of a lane's 32 x 32 result stands for a row outside [lo, hi] (and at or behind `more`) of those from 4 (lane / 32) on.  By
 // selects and whole conditions: written with && and an assignment under `if`, the compiler (ROCm 7.2) made branches of it and lost the assignment to
@@ -137,16 +144,113 @@ struct Place {
   }
 };
 
+// The same for packed sequences, whose blocks come in the order of their work, the longest first: eight key heads at a time go to an XCD each, and what is left
+// over is dealt out block by block, as an XCD of its own for a run of blocks would get the long ones or the short ones.
+struct PackedPlace {
+  int blk, bh, kvh;
+  static constexpr int b = 0;
+  __device__ __forceinline__ PackedPlace(const WindowArgs& a, int id) {
+    const int xcd = id % 8, slot = id / 8, whole = a.heads_kv / 8, rest = a.heads_kv % 8, round = a.by_blocks(slot);
+    if (round < whole) {
+      blk = slot - round * a.blocks;
+      kvh = round * 8 + xcd;
+    } else {                                         // rest > 0
+      const int left = id - whole * 8 * a.blocks;
+      blk = int(uint32_t(left) / uint32_t(rest));
+      kvh = whole * 8 + left - blk * rest;
+    }
+    bh = kvh;
+  }
+};
+
 // Query of row r of a sequence's key head.  Rows are counted in 31 bits.
 __device__ __forceinline__ int query_of(const WindowArgs& a, int r) { return a.by_group(r); }
 // Rows of a block of `most` from r0 on that are there.
 __device__ __forceinline__ int rows_of(const WindowArgs& a, const Lengths& len, int r0, int most) { return min_of(len.q * a.group - r0, most); }
 
+// The sequence that block i of a key head lies in: its lengths, its first rows in the tensors, which of its blocks this is (blk), and a number for it that no other
+// block of the key head has (slot).  U: rows of a block, of queries (of all heads that share the key head) or of keys.
+template <bool PACKED> struct Seq;
+template <> struct Seq<false> {
+  static constexpr int q0 = 0, k0 = 0;
+  static constexpr bool real = true;
+  int blk, slot;
+  Lengths len;
+  template <int U, bool KEYS> static __device__ __forceinline__ Seq of(const WindowArgs& a, int b, int i, bool) { return Seq{i, i, Lengths(a, b)}; }
+};
+
+// Sum over a wave, the same in all lanes.
+__device__ __forceinline__ int wave_sum(int x) {
+  x += __builtin_amdgcn_mov_dpp(x, 0xB1, 0xF, 0xF, true);              // within a quad: 1 0 3 2
+  x += __builtin_amdgcn_mov_dpp(x, 0x4E, 0xF, 0xF, true);              // 2 3 0 1
+  x += __builtin_amdgcn_mov_dpp(x, 0x141, 0xF, 0xF, true);             // mirrored within 8
+  x += __builtin_amdgcn_mov_dpp(x, 0x140, 0xF, 0xF, true);             // within 16
+  const auto half = __builtin_amdgcn_permlane16_swap(uint32_t(x), uint32_t(x), false, false);
+  x = int(half[0] + half[1]);
+  const auto all = __builtin_amdgcn_permlane32_swap(uint32_t(x), uint32_t(x), false, false);
+  return __builtin_amdgcn_readfirstlane(int(all[0] + all[1]));
+}
+
+// Packed: how many blocks a sequence has is known on the device alone.  Sequence s has room for those from start[s] * group / U + s on, counted down to whole ones, so that
+// no sum over the sequences in front of it is needed; a block between its last and the next one's room is not real.  Up to 64 sequences are looked at by a wave's
+// lanes at once, and their blocks can be had in another order (`long_first`): all sequences' blocks number x before those number x - 1, or of keys, counted from
+// the last, so that under a causal mask those come first that see most.
+template <> struct Seq<true> {
+  int blk, slot, q0, k0;
+  bool real;
+  Lengths len;
+  static __device__ __forceinline__ int start_of(const int32_t* p, int s, int n) { return max_of(0, min_of(p[s], n)); }
+  template <int U, bool KEYS> static __device__ __forceinline__ Seq of(const WindowArgs& a, int, int i, bool long_first) {
+    const int lane = threadIdx.x & 63, per = KEYS ? 1 : a.group, most = KEYS ? a.n_k : a.n_q;
+    const int32_t* start = KEYS ? a.k_start : a.q_start;
+    Seq r;
+    int s = 0;
+    if (a.packed <= 64 && long_first) {
+      const int mine = min_of(lane, a.packed - 1), from = start_of(start, mine, most), to = start_of(start, mine + 1, most);
+      const int n = lane < a.packed && to > from ? int(uint32_t((to - from) * per + U - 1) / U) : 0;
+      int lo = 0, hi = 1;                            // the blocks number lo and more are more than i, those number hi and more are not
+      r.real = wave_sum(n) > i;
+      if (!r.real) return r;
+      while (__builtin_amdgcn_ballot_w64(n > hi)) hi *= 2;
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2, more = wave_sum(max_of(0, n - mid));
+        if (more > i) lo = mid;
+        else hi = mid;
+      }
+      const int place = i - wave_sum(max_of(0, n - lo - 1));               // among the sequences that have a block number lo
+      const uint64_t have = __builtin_amdgcn_ballot_w64(n > lo);
+      const int before = __builtin_amdgcn_mbcnt_hi(uint32_t(have >> 32), __builtin_amdgcn_mbcnt_lo(uint32_t(have), 0));
+      s = __builtin_ctzll(__builtin_amdgcn_ballot_w64(n > lo && before == place));
+      r.blk = KEYS ? __builtin_amdgcn_readlane(n, s) - 1 - lo : lo;
+    } else {
+      for (int n = a.packed; n > 0;) {
+        const int step = (n + 63) / 64, at = lane * step;
+        const bool begun = at < n && int(uint32_t(start_of(start, s + min_of(at, n - 1), most) * per) / U) + s + at <= i;
+        const int c = __builtin_popcountll(__builtin_amdgcn_ballot_w64(begun));
+        r.real = c > 0;
+        if (!r.real) return r;
+        s += (c - 1) * step;
+        n = min_of(step, n - (c - 1) * step);
+        if (step == 1) break;
+      }
+      r.blk = i - int(uint32_t(start_of(start, s, most) * per) / U) - s;
+      r.real = r.blk >= 0;                           // not where the starts go down
+    }
+    s = __builtin_amdgcn_readfirstlane(s);
+    r.q0 = start_of(a.q_start, s, a.n_q);
+    r.k0 = start_of(a.k_start, s, a.n_k);
+    r.len = Lengths(max_of(0, start_of(a.q_start, s + 1, a.n_q) - r.q0), max_of(0, start_of(a.k_start, s + 1, a.n_k) - r.k0));
+    r.slot = int(uint32_t((KEYS ? r.k0 : r.q0) * per) / U) + s + r.blk;
+    return r;
+  }
+};
+template <bool PACKED> using PlaceOf = typename std::conditional<PACKED, PackedPlace, Place>::type;
+
 // What a lane of a block of rows knows of its row.
 struct Row {
   int n, h, i0, i1, qi, qh, p;                       // column and half of the wave; first and last query of the block; query, head, position
   bool real;
-  __device__ __forceinline__ Row(const WindowArgs& a, const Place& at, const Lengths& len, int r0, int rows, int mine, int lane) {
+  template <class P> __device__ __forceinline__ Row(const WindowArgs& a, const P& at, const Lengths& len, int r0, int rows, int mine, int lane) {
     n = lane & 31;
     h = lane >> 5;
     i0 = query_of(a, r0);
@@ -374,6 +478,21 @@ template <typename T, int N> __device__ __forceinline__ void store_row(bool real
     }
 }
 
+// Into how many work-groups a block of the backward pass is split that has `tiles` tiles to go over: as many as make 256 of `blocks`, four tiles each at least.
+inline int share(int64_t blocks, int64_t tiles) {
+  int64_t n = blocks ? 256 / blocks : 1;
+  if (n > tiles / 4) n = tiles / 4;
+  return n < 1 ? 1 : int(n);
+}
+
+// Rows of tiles are addressed by 32 bits within a tile.
+inline int check_tiles(const char* call, const char* name, const View& v) {
+  if (v.row > (int64_t(1) << 24)) return fail(DFS_ESHAPE, "%s: rows of %s are more than 2^24 bytes apart", call, name);
+  return DFS_OK;
+}
+
+// The launches of both passes behind their checks, in files of their own for sequences of one length and packed ones.
 int run_window_bwd(const WindowArgs& a, int d, int dtype, hipStream_t st);
+int run_packed_bwd(const WindowArgs& a, int d, int dtype, hipStream_t st);
 
 }  // namespace dfs
