@@ -43,7 +43,7 @@ typedef enum {
   DFS_EHIP = -5        /* a HIP call failed; dfs_last_error() holds its message */
 } dfs_status;
 
-typedef enum { DFS_F32 = 0, DFS_BF16 = 1 } dfs_dtype;
+typedef enum { DFS_F32 = 0, DFS_BF16 = 1, DFS_E4M3 = 2 /* of a cache in pages alone: 8 bits, with a scale */ } dfs_dtype;
 
 typedef enum {
   DFS_SELECT_TOPK = 0,     /* Eq. 9: every query block keeps ceil((1-sparsity)*M_v) key blocks */
@@ -434,6 +434,36 @@ int dfs_packed_attn_bwd(const dfs_packed* w, int dtype, const dfs_view* q, const
 
 /* Bytes of scratch of dfs_packed_attn_fwd (backward = 0) or dfs_packed_attn_bwd (1); 0 also if `w` is invalid.  Host only. */
 size_t dfs_packed_workspace_bytes(const dfs_packed* w, int dtype, int backward);
+
+/*
+ * A cache of keys and values in pages (device memory; the struct is HOST memory).  Token p of sequence s is row p % page of page table[s][p / page].  In DFS_E4M3 (with
+ * bf16 queries) an element stands for its value times the scale of its page and key head, a power of two (dfs_paged_append keeps it one; of another number the
+ * exponent alone counts); in DFS_F32 and DFS_BF16, which are the queries' type then, for itself.
+ */
+typedef struct {
+  dfs_view k, v;                  /* [pages, heads_kv, page, d]: `batch` is from one page to the next; rows lie 2^24 bytes apart at most */
+  float *k_scale, *v_scale;       /* DFS_E4M3: [pages, heads_kv], dense; else NULL */
+  const int32_t* table;           /* [seqs, table_row], dense.  An entry that no token of its sequence is on is not read; one outside [0, pages) is no page */
+  int32_t pages, page, table_row; /* page 16, 32, 64 or 128 rows; table_row x page at most 2^28, pages x heads_kv below 2^31 */
+  int32_t dtype;
+} dfs_pages;
+
+/*
+ * New tokens of several sequences on their way into a cache: queries and keys normed and turned by their position as by dfs_qk_norm_rope, queries to q_out, keys and values to
+ * their rows of the pages.  Rows of q, k and v are packed: sequence s has rows q_start[s] .. q_start[s+1] - 1, the last of them at position k_len[s] - 1.
+ *   g: batch is the number of sequences (below 2^24), tokens the rows of all of them
+ *   q [heads, tokens, d], k, v [heads_kv, tokens, d] in, q_out like q out (it may be q itself, with the same strides); the `batch` of these views is not read
+ *   q_start [batch + 1] int32, not falling (cut to [0, tokens]);  k_len [batch] int32: tokens of each sequence, the new ones among them (cut to [0, table_row x page])
+ *   positions  NULL (axes 1): a token's place in its sequence turns it; or [tokens x axes] int32
+ *   norm  0: no norm (w_q and w_k are NULL then);  w_q, w_k [d] fp32 or NULL (ones)
+ * Tokens at places below 0, or on no page, go into no page; rows outside the sequences are left as they are, in q_out and in the pages.  A page that new tokens go to
+ * belongs to one sequence alone.
+ * DFS_E4M3: the scale of a page and key head is the smallest power of two c, 2^-120 at least, by which the largest of the page's values is 448 c at most, or, with rows from
+ * before the call, their scale if that is larger.  Values are normed and turned in fp32 and rounded once; where a scale grows the rows from before are rounded anew, which
+ * moves only what falls below the type's smallest value.  An infinite value is stored as NaN; NaN and infinities do not count for the scale.
+ */
+int dfs_paged_append(const dfs_qk_geom* g, int dtype, const dfs_view* q, const dfs_view* k, const dfs_view* v, const int32_t* q_start, const int32_t* k_len,
+                     const int32_t* positions, const float* w_q, const float* w_k, const dfs_view* q_out, const dfs_pages* pages, int norm, void* stream);
 
 /*
  * Diagnostic for measurements, not part of the method: while `counters` (device memory, 3 x uint64, zeroed by

@@ -12,7 +12,7 @@ import torch
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libdfsattn.so")
 
-DFS_F32, DFS_BF16 = 0, 1
+DFS_F32, DFS_BF16, DFS_E4M3 = 0, 1, 2
 DFS_SELECT_TOPK, DFS_SELECT_MASS_HEAD, DFS_SELECT_MASS_ROW = 0, 1, 2
 DFS_WS_HILBERT_PERM, DFS_WS_BLOCK_SCORE, DFS_WS_SELECT_MASK, DFS_WS_FORWARD, DFS_WS_FORWARD_BF16 = 0, 1, 2, 3, 4
 
@@ -60,6 +60,23 @@ class _View(C.Structure):
     _fields_ = [("data", C.c_void_p), ("batch", C.c_int64), ("head", C.c_int64), ("row", C.c_int64)]
 
 
+class _PagesC(C.Structure):
+    """Mirror of dfs_pages."""
+    _fields_ = [("k", _View), ("v", _View), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p), ("table", C.c_void_p)] + \
+        [(n, C.c_int32) for n in ("pages", "page", "table_row", "dtype")]
+
+
+@dataclass
+class Pages:
+    """Caller-owned cache in pages: k and v [pages, heads_kv, page, d] (float32, bfloat16, or float8_e4m3fn with scales), table [seqs, entries] int32, k_scale and
+    v_scale [pages, heads_kv] float32."""
+    k: torch.Tensor
+    v: torch.Tensor
+    table: torch.Tensor
+    k_scale: torch.Tensor | None = None
+    v_scale: torch.Tensor | None = None
+
+
 @dataclass
 class MaskState:
     """Caller-owned mask buffers of one attention layer (kept across diffusion steps)."""
@@ -81,6 +98,7 @@ def _load():
     lib = C.CDLL(_LIB_PATH)
     vp, i32, i64, dbl, f32, sz = C.c_void_p, C.c_int32, C.c_int64, C.c_double, C.c_float, C.c_size_t
     gp, qp, wp, kp, tp = C.POINTER(Geom), C.POINTER(QkGeom), C.POINTER(Window), C.POINTER(Packed), C.POINTER(_View)
+    cp = C.POINTER(_PagesC)
     sig = {
         "dfs_geom_sizes": (C.c_int, [gp, C.POINTER(Sizes)]),
         "dfs_workspace_bytes": (sz, [gp, C.c_int]),
@@ -114,6 +132,7 @@ def _load():
         "dfs_packed_attn_fwd": (C.c_int, [kp, C.c_int, tp, tp, tp, vp, vp, f32, tp, vp, vp, sz, vp]),
         "dfs_packed_attn_bwd": (C.c_int, [kp, C.c_int, tp, tp, tp, tp, vp, tp, vp, vp, f32, tp, tp, tp, vp, sz, vp]),
         "dfs_packed_workspace_bytes": (sz, [kp, C.c_int, C.c_int]),
+        "dfs_paged_append": (C.c_int, [qp, C.c_int, tp, tp, tp, vp, vp, vp, vp, vp, tp, cp, C.c_int, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -122,7 +141,8 @@ def _load():
 
 
 def _load_calls(names=("forward", "token_order", "permute", "unperm", "block_score", "select_mask", "sparse_attn", "recall",
-                       "qk_norm_rope", "qk_norm_rope_bwd", "window_attn_fwd", "window_attn_bwd", "packed_attn_fwd", "packed_attn_bwd")):
+                       "qk_norm_rope", "qk_norm_rope_bwd", "window_attn_fwd", "window_attn_bwd", "packed_attn_fwd", "packed_attn_bwd",
+                       "paged_append")):
     """The calls of the _calls module.  They do in native code what those of the same names do below, for plain
     arguments, and return None for what they leave to these: as the stand-ins do for every call where the module is not there or
     was built against another torch, whose classes it reads (another Python does not find it: its name holds the version)."""
@@ -146,12 +166,13 @@ def _load_calls(names=("forward", "token_order", "permute", "unperm", "block_sco
 _lib = _load()
 (_plain_forward, _plain_token_order, _plain_permute, _plain_unperm, _plain_block_score, _plain_select_mask, _plain_sparse_attn,
  _plain_recall, _plain_qk_norm_rope, _plain_qk_norm_rope_bwd, _plain_window_attn_fwd, _plain_window_attn_bwd, _plain_packed_attn_fwd,
- _plain_packed_attn_bwd) = _load_calls()
+ _plain_packed_attn_bwd, _plain_paged_append) = _load_calls()
 EXPORTS = ("dfs_geom_sizes", "dfs_workspace_bytes", "dfs_last_error", "dfs_keep_count", "dfs_hilbert_perm", "dfs_permute",
            "dfs_block_score", "dfs_select_mask", "dfs_sparse_attn_fwd", "dfs_unperm", "dfs_forward", "dfs_token_order", "dfs_recall",
            "dfs_schedule", "dfs_block_score_src", "dfs_sparse_attn_fwd_src", "dfs_attn_clock_probe", "dfs_block_score_fused", "dfs_probe_mfma", "dfs_probe_copy", "dfs_probe_read",
            "dfs_select_mask_static", "dfs_qk_norm_rope", "dfs_qk_norm_rope_bwd", "dfs_qk_workspace_bytes", "dfs_window_attn_fwd",
-           "dfs_window_attn_bwd", "dfs_window_workspace_bytes", "dfs_packed_attn_fwd", "dfs_packed_attn_bwd", "dfs_packed_workspace_bytes")
+           "dfs_window_attn_bwd", "dfs_window_workspace_bytes", "dfs_packed_attn_fwd", "dfs_packed_attn_bwd", "dfs_packed_workspace_bytes",
+           "dfs_paged_append")
 DFS_ORDER_HILBERT3D, DFS_ORDER_RASTER, DFS_ORDER_HILBERT2D, DFS_ORDER_BLOCK3D = 0, 1, 2, 3
 
 
@@ -435,7 +456,7 @@ def _view(t: torch.Tensor | None, dtype: int, batch: int, heads: int, rows: int,
     if t is None:
         return None
     _here(t, name)
-    td = _torch_dtype(dtype)
+    td = torch.float8_e4m3fn if dtype == DFS_E4M3 else _torch_dtype(dtype)
     if t.dtype is not td:
         raise ValueError(f"{name} must be {td}, got {t.dtype}")
     if tuple(t.shape) != (batch, heads, rows, d):
@@ -589,3 +610,41 @@ def dfs_packed_attn_bwd(w: Packed, dtype: int, q, k, v, o, lse, d_o, q_start, k_
                                     _flat_view(o, dtype, *qs, "o"), _flat(lse, torch.float32, w.heads * w.n_q, "lse"), _flat_view(d_o, dtype, *qs, "d_o"),
                                     _flat(q_start, torch.int32, w.seqs + 1, "q_start"), _flat(k_start, torch.int32, w.seqs + 1, "k_start"), float(scale),
                                     _flat_view(dq, dtype, *qs, "dq"), _flat_view(dk, dtype, *ks, "dk"), _flat_view(dv, dtype, *ks, "dv"), wsp, wb, _stream()))
+
+
+# A cache in pages.
+
+_CACHE_TYPES = {torch.float32: DFS_F32, torch.bfloat16: DFS_BF16, torch.float8_e4m3fn: DFS_E4M3}
+
+
+def _pages(p: Pages | None, seqs: int, heads_kv: int, d: int):
+    """dfs_pages of a cache (None -> NULL)."""
+    if p is None:
+        return None
+    if p.k.dtype not in _CACHE_TYPES:
+        raise ValueError(f"pages.k must be float32, bfloat16 or float8_e4m3fn, got {p.k.dtype}")
+    if p.k.dim() != 4:
+        raise ValueError(f"pages.k must be [pages, heads_kv, page, d], got {list(p.k.shape)}")
+    if p.table.dim() != 2 or p.table.shape[0] != seqs:
+        raise ValueError(f"pages.table must be [{seqs}, entries], got {list(p.table.shape)}")
+    code, n, page = _CACHE_TYPES[p.k.dtype], p.k.shape[0], p.k.shape[2]
+    return _PagesC(_view(p.k, code, n, heads_kv, page, d, "pages.k"), _view(p.v, code, n, heads_kv, page, d, "pages.v"),
+                   _flat(p.k_scale, torch.float32, n * heads_kv, "pages.k_scale"), _flat(p.v_scale, torch.float32, n * heads_kv, "pages.v_scale"),
+                   _flat(p.table, torch.int32, 0, "pages.table"), n, page, p.table.shape[1], code)
+
+
+def dfs_paged_append(g: QkGeom, dtype: int, q, k, v, q_start, k_len, positions, w_q, w_k, q_out, pages: Pages, norm: bool = True):
+    """Norm and rotation of the queries and keys of new tokens; queries to q_out, keys and values into the pages.  Tensors are [heads, rows of all sequences, d]; q_start is
+    [batch + 1] int32, k_len [batch] int32 with the new tokens counted; positions [tokens, axes] int32 or None: places in the sequences."""
+    rc = _plain_paged_append(g, dtype, q, k, v, q_start, k_len, positions, w_q, w_k, q_out, pages, norm)
+    if rc == 0:
+        return
+    if rc is not None:
+        _check(rc)
+    if positions is not None and tuple(positions.shape) != (g.tokens, g.axes):
+        raise ValueError(f"positions must be {[g.tokens, g.axes]}, got {list(positions.shape)}")
+    ks = (g.heads_kv, g.tokens, g.d)
+    _check(_lib.dfs_paged_append(g, dtype, _flat_view(q, dtype, g.heads, g.tokens, g.d, "q"), _flat_view(k, dtype, *ks, "k"), _flat_view(v, dtype, *ks, "v"),
+                                 _flat(q_start, torch.int32, g.batch + 1, "q_start"), _flat(k_len, torch.int32, g.batch, "k_len"),
+                                 _flat(positions, torch.int32, 0, "positions"), _flat(w_q, torch.float32, g.d, "w_q"), _flat(w_k, torch.float32, g.d, "w_k"),
+                                 _flat_view(q_out, dtype, g.heads, g.tokens, g.d, "q_out"), _pages(pages, g.batch, g.heads_kv, g.d), int(bool(norm)), _stream()))

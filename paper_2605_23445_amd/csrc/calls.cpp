@@ -22,6 +22,7 @@ namespace {
 // binding.Geom, QkGeom, Window and Packed, ctypes structures with the layouts of dfs_geom, dfs_qk_geom, dfs_window and dfs_packed
 PyObject *g_geom_type = nullptr, *g_qk_type = nullptr, *g_window_type = nullptr, *g_packed_type = nullptr;
 PyObject *s_kv_idx, *s_kv_cnt, *s_mask, *s_k_head, *s_K_max;
+PyObject *s_k, *s_v, *s_table, *s_k_scale, *s_v_scale;
 
 struct NotPlain {};                                 // thrown where binding.py has to look at an argument
 
@@ -146,7 +147,7 @@ PyObject* token_order(PyObject*, PyObject* const* a, Py_ssize_t n) {
 void* to_ptr_or_null(PyObject* x, at::ScalarType type, int64_t numel, int64_t* bytes = nullptr) {
   return x == Py_None ? nullptr : to_ptr(x, type, numel, bytes);
 }
-at::ScalarType tensor_type(int dtype) { return dtype == DFS_BF16 ? at::kBFloat16 : at::kFloat; }
+at::ScalarType tensor_type(int dtype) { return dtype == DFS_E4M3 ? at::kFloat8_e4m3fn : dtype == DFS_BF16 ? at::kBFloat16 : at::kFloat; }
 struct Problem {
   dfs_geom g;
   dfs_sizes s;
@@ -395,6 +396,55 @@ PyObject* packed_attn(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// binding.Pages; its tensors are held while the call runs.
+struct PagesOf {
+  const Attr k, v, table, k_scale, v_scale;
+  dfs_pages p = {};
+  PagesOf(const Here& here, PyObject* x, int64_t seqs, int64_t heads_kv, int64_t d)
+      : k(x, s_k), v(x, s_v), table(x, s_table), k_scale(x, s_k_scale), v_scale(x, s_v_scale) {
+    const at::Tensor &t = here.tensor(k.o, at::ScalarType::Undefined), &rows = here.tensor(table.o, at::kInt);
+    p.dtype = t.scalar_type() == at::kFloat ? DFS_F32 : t.scalar_type() == at::kBFloat16 ? DFS_BF16 : DFS_E4M3;
+    need(t.scalar_type() == tensor_type(p.dtype) && t.dim() == 4 && rows.dim() == 2 && rows.size(0) == seqs && rows.is_contiguous());
+    const int64_t n = t.size(0), page = t.size(2), row = rows.size(1);
+    need(n == int64_t(int32_t(n)) && page == int64_t(int32_t(page)) && row == int64_t(int32_t(row)));
+    p.pages = int32_t(n);
+    p.page = int32_t(page);
+    p.table_row = int32_t(row);
+    p.k = here.view(k.o, p.dtype, n, heads_kv, page, d).v;
+    const auto values = here.view(v.o, p.dtype, n, heads_kv, page, d);
+    need(values.there);
+    p.v = values.v;
+    p.table = static_cast<const int32_t*>(rows.data_ptr());
+    p.k_scale = here.flat<float>(k_scale.o, at::kFloat, n * heads_kv);
+    p.v_scale = here.flat<float>(v_scale.o, at::kFloat, n * heads_kv);
+  }
+};
+
+PyObject* paged_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> int {
+    need(n == 13);
+    const auto g = to_struct<dfs_qk_geom>(a[0], g_qk_type);
+    const int dtype = to_int(a[1]), norm = PyObject_IsTrue(a[12]);
+    need(norm >= 0);
+    const Here here;
+    const auto rows = [&](PyObject* x, int64_t heads) { return here.flat_view(x, dtype, heads, g.tokens, g.d); };
+    const auto q = rows(a[2], g.heads), k = rows(a[3], g.heads_kv), v = rows(a[4], g.heads_kv), q_out = rows(a[10], g.heads);
+    const auto *q_start = here.flat<const int32_t>(a[5], at::kInt, int64_t(g.batch) + 1), *k_len = here.flat<const int32_t>(a[6], at::kInt, g.batch);
+    const int32_t* pos = nullptr;
+    if (a[7] != Py_None) {
+      const at::Tensor& t = here.tensor(a[7], at::kInt);
+      need(t.is_contiguous() && t.dim() == 2 && t.size(0) == g.tokens && t.size(1) == g.axes);
+      pos = static_cast<const int32_t*>(t.data_ptr());
+    }
+    const auto *w_q = here.flat<const float>(a[8], at::kFloat, g.d), *w_k = here.flat<const float>(a[9], at::kFloat, g.d);
+    const PagesOf pages(here, a[11], g.batch, g.heads_kv, g.d);
+    void* st = stream();
+    return without_gil([&] {
+      return dfs_paged_append(&g, dtype, q.get(), k.get(), v.get(), q_start, k_len, pos, w_q, w_k, q_out.get(), &pages.p, norm, st);
+    });
+  });
+}
+
 PyObject* set_layer_types(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (n == 3) {
     for (int i = 0; i < 3; ++i) Py_INCREF(a[i]);
@@ -426,6 +476,7 @@ PyMethodDef methods[] = {
     {"window_attn_bwd", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(window_attn<true>)), METH_FASTCALL, nullptr},
     {"packed_attn_fwd", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(packed_attn<false>)), METH_FASTCALL, nullptr},
     {"packed_attn_bwd", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(packed_attn<true>)), METH_FASTCALL, nullptr},
+    {"paged_append", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(paged_append)), METH_FASTCALL, nullptr},
     {"set_geom_type", set_geom_type, METH_O, nullptr},
     {"set_layer_types", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(set_layer_types)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
@@ -440,6 +491,11 @@ PyMODINIT_FUNC PyInit__calls() {
   s_mask = PyUnicode_InternFromString("mask");
   s_k_head = PyUnicode_InternFromString("k_head");
   s_K_max = PyUnicode_InternFromString("K_max");
+  s_k = PyUnicode_InternFromString("k");
+  s_v = PyUnicode_InternFromString("v");
+  s_table = PyUnicode_InternFromString("table");
+  s_k_scale = PyUnicode_InternFromString("k_scale");
+  s_v_scale = PyUnicode_InternFromString("v_scale");
   PyObject* m = PyModule_Create(&module);
   if (m && PyModule_AddStringConstant(m, "torch_version", DFS_TORCH_VERSION) != 0) Py_CLEAR(m);
   return m;

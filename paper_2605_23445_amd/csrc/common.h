@@ -26,7 +26,7 @@ inline bool misaligned(size_t a, std::initializer_list<const void*> ps) {
     if (reinterpret_cast<uintptr_t>(p) & (a - 1)) return true;
   return false;
 }
-inline int elem_size(int dtype) { return dtype == DFS_BF16 ? 2 : 4; }
+inline int elem_size(int dtype) { return dtype == DFS_E4M3 ? 1 : dtype == DFS_BF16 ? 2 : 4; }
 
 // Stage entry points without argument checks, used by dfs_forward after it has validated once.
 // x2, x2_perm (may be NULL): a second tensor, reordered in the same launch.  n_zero words at `zero` are cleared.

@@ -1,0 +1,345 @@
+// New tokens on their way into a cache in pages: queries and keys normed and turned by their position, keys and values put into the pages of their sequence.
+//
+// The arithmetic of a row is that of qk_rope.hip.  Queries are worked on as there: a lane owns 16 bytes of a row at one token and walks over heads.  Keys and values
+// are worked on page by page: a work-group takes the new rows of one page and key head.  In 8 bits (e4m3, largest value 448) a page's rows share one power of two c,
+// the smallest with which the largest of them is at most 448 c: it is known when all of a page's new rows are, which therefore stay in registers, and
+// where there are rows from before it is not less than it was; if it grows they are divided by the quotient, which is exact but for what falls below e4m3's smallest.
+// Memory bound, the smallest calls by their chain of loads (starts, lengths and rows, table, scale).
+#include <float.h>
+
+#include "pages.h"
+#include "rope.h"
+#include "seqs.h"
+
+namespace dfs {
+
+struct AppendArgs : Turns {
+  View in[3], q_out;
+  PageArgs pages;
+  const int32_t *q_start, *k_len, *positions;
+  const float* w[2];
+  int32_t seqs, tokens, heads, heads_kv, norm;
+  int32_t q_groups, q_blocks, per;                   // work-groups of all tokens, of all queries; heads that one walks over
+};
+
+// A sequence's new tokens: its first row, how many there are, and the position of the first.
+struct Piece {
+  int q0, n, begin;
+  __device__ __forceinline__ Piece(const AppendArgs& a, int s) {
+    q0 = start_of(a.q_start, s, a.tokens);
+    n = max_of(0, start_of(a.q_start, s + 1, a.tokens) - q0);
+    begin = max_of(0, min_of(a.k_len[s], a.pages.row << a.pages.bits)) - n;
+  }
+};
+
+template <class Tok> __device__ __forceinline__ void set_turn(const AppendArgs& a, Tok& t, int lane, int row, int p) {
+  if (a.positions) {
+    const int32_t* pos = a.positions + int64_t(row) * a.axes;
+    t.set(a, lane, pos[0], a.axes > 1 ? pos[1] : 0, a.axes > 2 ? pos[2] : 0);
+  } else {
+    t.set(a, lane, p, 0, 0);
+  }
+}
+
+// Norm and turn of a chunk of a row.
+template <typename T, int D, bool PAIRS>
+__device__ __forceinline__ void norm_and_turn(const AppendArgs& a, const Turn<T, D, PAIRS>& t, const float (&w)[Chunk<T>::N], float (&x)[Chunk<T>::N]) {
+  constexpr int N = Chunk<T>::N;
+  if (a.norm) {
+    float sq = 0.f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) sq = fmaf(x[i], x[i], sq);
+    const float r = rsqrtf(row_sum<D / N>(sq) * (1.f / D) + a.eps);
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = x[i] * r * w[i];
+  }
+  t.template rotate<false>(x);
+}
+
+template <typename T, int D, bool PAIRS>
+__device__ __forceinline__ void append_queries(const AppendArgs& a, int id) {
+  using Tok = Turn<T, D, PAIRS>;
+  constexpr int N = Tok::N, L = Tok::L, U = 2;
+  const int lane = threadIdx.x & 63, y = id / a.q_groups, x = id - y * a.q_groups, t = x * (256 / L) + threadIdx.x / L;
+  const int row = min_of(t, a.tokens - 1);
+  // the last sequence that begins at or in front of this token
+  int s = -1;
+  if (a.seqs <= 64) {
+    const int mine = lane < a.seqs ? start_of(a.q_start, lane, a.tokens) : a.tokens;
+    const int first = __builtin_amdgcn_readfirstlane(row);
+#pragma unroll
+    for (int j = 0; j < 64 / L; ++j) {
+      const int c = __builtin_popcountll(__builtin_amdgcn_ballot_w64(lane < a.seqs && mine <= min_of(first + j, a.tokens - 1)));
+      if (lane / L == j) s = c - 1;
+    }
+  } else {
+    for (int lo = 0, hi = a.seqs; lo < hi;) {
+      const int mid = (lo + hi) / 2;
+      if (start_of(a.q_start, mid, a.tokens) <= row) {
+        s = mid;
+        lo = mid + 1;
+      } else {
+        hi = mid;
+      }
+    }
+  }
+  const Piece piece(a, max_of(s, 0));
+  const bool real = t < a.tokens && s >= 0 && row - piece.q0 < piece.n && row >= piece.q0;
+  Tok tok;
+  set_turn(a, tok, lane, row, piece.begin + row - piece.q0);
+  float w[N];
+  weights<N>(a.w[0], tok.c, w);
+  const int h0 = y * a.per, h1 = min_of(h0 + a.per, a.heads);
+  const char* src = a.in[0].at(0, 0, row) + tok.c * 16;
+  char* dst = a.q_out.at(0, 0, row) + tok.c * 16;
+  for (int h = h0; h < h1; h += U) {
+    u32x4 raw[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) raw[u] = load_chunk<false>(src + (h + u < h1 ? h + u : h) * a.in[0].head);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      float v[N];
+      Chunk<T>::open(raw[u], v);
+      norm_and_turn<T, D, PAIRS>(a, tok, w, v);
+      if (real && h + u < h1) *reinterpret_cast<u32x4*>(dst + (h + u) * a.q_out.head) = Chunk<T>::close(v);
+    }
+  }
+}
+
+// The new rows of a page: which sequence, page and key head, and the rows [r0, r1) of the page, row r at tensor row `row0` + r.
+struct Fresh {
+  bool real = false;
+  int page, kvh, r0, r1, row0, p0;                   // p0: position of the page's row 0
+  __device__ __forceinline__ Fresh(const AppendArgs& a, int id) {
+    // A sequence has room for as many pages as whole ones lie between its start and the next one's, and two more.
+    const int slot = id / a.heads_kv, bits = a.pages.bits;
+    kvh = id - slot * a.heads_kv;
+    const int s = run_of(a.seqs, slot, [&](int x) { return (start_of(a.q_start, x, a.tokens) >> bits) + 2 * x; });
+    if (s < 0) return;
+    const Piece piece(a, s);
+    const int begin = max_of(piece.begin, 0), i = (begin >> bits) + slot - (piece.q0 >> bits) - 2 * s, end = piece.begin + piece.n;
+    p0 = i << bits;
+    if (i < begin >> bits || p0 >= end || end <= begin) return;          // (in front: where starts fall)
+    page = page_of(a.pages, s, i);
+    if (page < 0) return;
+    r0 = max_of(begin - p0, 0);
+    r1 = min_of(end - p0, 1 << bits);
+    row0 = piece.q0 + p0 - piece.begin;
+    real = r0 < r1;
+  }
+};
+
+// Rows as they are.
+template <typename T, int D, bool PAIRS>
+__device__ __forceinline__ void append_rows(const AppendArgs& a, int id) {
+  using Tok = Turn<T, D, PAIRS>;
+  constexpr int N = Tok::N, L = Tok::L, R = 256 / L;
+  const Fresh f(a, id);
+  if (!f.real) return;
+  const int lane = threadIdx.x & 63;
+  float w[N];
+  weights<N>(a.w[1], lane % L, w);
+  for (int r = f.r0 + threadIdx.x / L; r - int(threadIdx.x / L) < f.r1; r += R) {
+    const int at = min_of(r, f.r1 - 1), row = f.row0 + at;
+    const u32x4 k = load_chunk<false>(a.in[1].at(0, f.kvh, row) + lane % L * 16), v = load_chunk<false>(a.in[2].at(0, f.kvh, row) + lane % L * 16);
+    Tok tok;
+    set_turn(a, tok, lane, row, f.p0 + at);
+    float x[N];
+    Chunk<T>::open(k, x);
+    norm_and_turn<T, D, PAIRS>(a, tok, w, x);
+    if (r < f.r1) {
+      *reinterpret_cast<u32x4*>(a.pages.k.at(f.page, f.kvh, r) + tok.c * 16) = Chunk<T>::close(x);
+      *reinterpret_cast<u32x4*>(a.pages.v.at(f.page, f.kvh, r) + tok.c * 16) = v;
+    }
+  }
+}
+
+// Exponent, as fp32 has it, of the smallest power of two c >= 2^-120 with m <= 448 c.
+__device__ __forceinline__ int scale_exponent(float m) {
+  const uint32_t b = __float_as_uint(m);
+  return max_of(int(b >> 23) - 8 + ((b & 0x7FFFFFu) > 0x600000u), 7);
+}
+// Infinities and NaN do not count for a scale.
+__device__ __forceinline__ float size_of(float x) { return fabsf(x) <= FLT_MAX ? fabsf(x) : 0.f; }
+__device__ __forceinline__ uint32_t four_bytes(float a, float b, float c, float d) {
+  return uint32_t(__builtin_amdgcn_cvt_pk_fp8_f32(c, d, __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false), true));
+}
+
+// Rows [0, n) of a page in 8 bits, times f.
+template <int D> __device__ __forceinline__ void shrink(const View& v, int page, int kvh, int n, float f) {
+  for (int i = threadIdx.x; i < n * (D / 16); i += 256) {
+    u32x4* p = reinterpret_cast<u32x4*>(v.at(page, kvh, i / (D / 16)) + i % (D / 16) * 16);
+    u32x4 x = *p;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(int(x[j]), false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(int(x[j]), true);
+      x[j] = four_bytes(lo[0] * f, lo[1] * f, hi[0] * f, hi[1] * f);
+    }
+    *p = x;
+  }
+}
+
+// Rows in 8 bits; PASSES of 256 / L rows are a page.
+template <int D, bool PAIRS, int PASSES>
+__device__ __forceinline__ void append_bytes(const AppendArgs& a, int id) {
+  using Tok = Turn<uint16_t, D, PAIRS>;
+  constexpr int N = Tok::N, L = Tok::L, R = 256 / L;
+  __shared__ float most[2][4];
+  const Fresh f(a, id);
+  if (!f.real) return;
+  const int lane = threadIdx.x & 63, c = lane % L, mine = f.r0 + threadIdx.x / L, scale_at = f.page * a.heads_kv + f.kvh;
+  const float was[2] = {a.pages.k_scale[scale_at], a.pages.v_scale[scale_at]};
+  float w[N], y[PASSES][N], top[2] = {};
+  u32x4 raw[PASSES], v[PASSES];
+#pragma unroll
+  for (int u = 0; u < PASSES; ++u) {
+    if (f.r0 + u * R >= f.r1) continue;
+    const int row = f.row0 + min_of(mine + u * R, f.r1 - 1);
+    raw[u] = load_chunk<false>(a.in[1].at(0, f.kvh, row) + c * 16);
+    v[u] = load_chunk<false>(a.in[2].at(0, f.kvh, row) + c * 16);
+  }
+  weights<N>(a.w[1], c, w);
+#pragma unroll
+  for (int u = 0; u < PASSES; ++u) {
+    if (f.r0 + u * R >= f.r1) continue;
+    const int at = min_of(mine + u * R, f.r1 - 1);   // past the last row that once more, which changes no maximum
+    Tok tok;
+    set_turn(a, tok, lane, f.row0 + at, f.p0 + at);
+    Chunk<uint16_t>::open(raw[u], y[u]);
+    norm_and_turn<uint16_t, D, PAIRS>(a, tok, w, y[u]);
+    float z[N];
+    Chunk<uint16_t>::open(v[u], z);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      top[0] = fmaxf(top[0], size_of(y[u][i]));
+      top[1] = fmaxf(top[1], size_of(z[i]));
+    }
+  }
+#pragma unroll
+  for (int x = 0; x < 2; ++x) {
+#pragma unroll
+    for (int m = 1; m < 64; m *= 2) top[x] = fmaxf(top[x], __shfl_xor(top[x], m));
+    if (lane == 0) most[x][threadIdx.x >> 6] = top[x];
+  }
+  __syncthreads();
+  float back[2];                                     // 1 / c
+#pragma unroll
+  for (int x = 0; x < 2; ++x) {
+    const int e = scale_exponent(fmaxf(fmaxf(most[x][0], most[x][1]), fmaxf(most[x][2], most[x][3])));
+    float scale = __uint_as_float(uint32_t(e) << 23);
+    if (f.r0 > 0) {
+      if (was[x] >= scale) scale = was[x];
+      else shrink<D>(x ? a.pages.v : a.pages.k, f.page, f.kvh, f.r0, was[x] / scale);
+    }
+    back[x] = 1.f / scale;
+    if (threadIdx.x == 0) (x ? a.pages.v_scale : a.pages.k_scale)[scale_at] = scale;
+  }
+#pragma unroll
+  for (int u = 0; u < PASSES; ++u) {
+    const int r = mine + u * R;
+    if (r >= f.r1) continue;
+    float z[N];
+    Chunk<uint16_t>::open(v[u], z);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      y[u][i] *= back[0];
+      z[i] *= back[1];
+    }
+    *reinterpret_cast<uint2*>(a.pages.k.at(f.page, f.kvh, r) + c * 8) =
+        make_uint2(four_bytes(y[u][0], y[u][1], y[u][2], y[u][3]), four_bytes(y[u][4], y[u][5], y[u][6], y[u][7]));
+    *reinterpret_cast<uint2*>(a.pages.v.at(f.page, f.kvh, r) + c * 8) = make_uint2(four_bytes(z[0], z[1], z[2], z[3]), four_bytes(z[4], z[5], z[6], z[7]));
+  }
+}
+
+// PASSES 0: pages of T.
+template <typename T, int D, bool PAIRS, int PASSES>
+__global__ void __launch_bounds__(256) paged_append_kernel(AppendArgs a) {
+  const int id = blockIdx.x;
+  if (id < a.q_blocks) append_queries<T, D, PAIRS>(a, id);
+  else if constexpr (PASSES == 0) append_rows<T, D, PAIRS>(a, id - a.q_blocks);
+  else append_bytes<D, PAIRS, PASSES>(a, id - a.q_blocks);
+}
+
+constexpr int RUN = 10;                              // heads of queries that a work-group walks over, at most
+
+}  // namespace dfs
+
+using namespace dfs;
+
+extern "C" {
+
+int dfs_paged_append(const dfs_qk_geom* g, int dtype, const dfs_view* q, const dfs_view* k, const dfs_view* v, const int32_t* q_start, const int32_t* k_len,
+                     const int32_t* positions, const float* w_q, const float* w_k, const dfs_view* q_out, const dfs_pages* pages, int norm, void* stream) {
+  const char* call = "dfs_paged_append";
+  if (!g) return fail(DFS_EINVAL, "%s: geometry pointer is NULL", call);
+  if (g->batch < 0 || g->batch >= 1 << 24) return fail(DFS_ESHAPE, "%s: batch=%d sequences must be in [0, 2^24)", call, g->batch);
+  dfs_qk_geom one = *g;
+  one.batch = 1;
+  int rc = check_qk(call, &one);
+  if (rc) return rc;
+  if (dtype != DFS_F32 && dtype != DFS_BF16) return fail(DFS_EDTYPE, "%s: dtype %d is not DFS_F32 or DFS_BF16", call, dtype);
+  AppendArgs a = {};
+  if (misaligned(4, {positions, w_q, w_k, q_start, k_len})) return fail(DFS_EINVAL, "%s: starts, lengths, positions and weights must be 4-byte aligned", call);
+  if (g->batch && g->tokens && (!q_start || !k_len)) return fail(DFS_EINVAL, "%s: q_start or k_len is NULL", call);
+  if (!positions && g->axes > 1) return fail(DFS_EINVAL, "%s: positions is NULL, which takes axes=1", call);
+  if (!norm && (w_q || w_k)) return fail(DFS_EINVAL, "%s: weights without a norm", call);
+  const dfs_view* in[3] = {q, k, v};
+  const char* in_name[3] = {"q", "k", "v"};
+  for (int i = 0; i < 3; ++i)
+    if ((rc = check_view(call, in_name[i], in[i], dtype, 1, i ? g->heads_kv : g->heads, g->tokens, g->d, false, &a.in[i]))) return rc;
+  if ((rc = check_view(call, "q_out", q_out, dtype, 1, g->heads, g->tokens, g->d, true, &a.q_out))) return rc;
+  if ((rc = check_pages(call, pages, dtype, g->batch, g->heads_kv, g->d, true, &a.pages))) return rc;
+  if (int64_t(a.pages.pages) * g->heads_kv >= int64_t(1) << 31) return fail(DFS_ESHAPE, "%s: pages=%d x heads_kv=%d too many", call, a.pages.pages, g->heads_kv);
+  const int L = g->d * elem_size(dtype) / 16;
+  const int64_t n = g->tokens, waves = (n * L + 63) / 64, slots = (n >> a.pages.bits) + 2 * int64_t(g->batch);
+  if (slots * g->heads_kv >= 1 << 23) return fail(DFS_ESHAPE, "%s: tokens=%d, batch=%d x heads_kv=%d too large", call, g->tokens, g->batch, g->heads_kv);
+  if (n == 0 || g->batch == 0) return DFS_OK;
+  if (moved(a.in[0], a.q_out)) return fail(DFS_EINVAL, "%s: q_out is q with rows elsewhere", call);
+  if ((rc = check_apart(call, {{"pages.k", &a.pages.k}, {"pages.v", &a.pages.v}}, {{"q", &a.in[0]}, {"k", &a.in[1]}, {"v", &a.in[2]}, {"q_out", &a.q_out}})) ||
+      (rc = check_apart(call, {{"q_out", &a.q_out}}, {{"k", &a.in[1]}, {"v", &a.in[2]}})))
+    return rc;
+  fill_turns(g, &a);
+  a.q_start = q_start;
+  a.k_len = k_len;
+  a.positions = positions;
+  a.w[0] = w_q;
+  a.w[1] = w_k;
+  a.seqs = g->batch;
+  a.tokens = g->tokens;
+  a.heads = g->heads;
+  a.heads_kv = g->heads_kv;
+  a.norm = norm != 0;
+  // runs of heads until there are eight waves a SIMD, or a row a lane
+  int64_t y = (8192 + waves - 1) / waves, runs = (g->heads + RUN - 1) / RUN;
+  if (y < runs) y = runs;
+  if (y > g->heads) y = g->heads;
+  a.per = int((g->heads + y - 1) / y);
+  a.q_groups = int((n * L + 255) / 256);
+  const int64_t q_blocks = int64_t(a.q_groups) * ((g->heads + a.per - 1) / a.per), blocks = q_blocks + (a.pages.row ? slots * g->heads_kv : 0);
+  if (blocks >= 1 << 24) return fail(DFS_ESHAPE, "%s: tokens=%d x heads=%d too large", call, g->tokens, g->heads);
+  a.q_blocks = int(q_blocks);
+  const bool bytes = pages->dtype == DFS_E4M3;
+  const int passes = !bytes ? 0 : pages->page * L / 256 > 1 ? pages->page * L / 256 : 1;
+  const hipStream_t st = as_stream(stream);
+  auto run = [&](auto t, auto d, auto p, auto s) {
+    paged_append_kernel<decltype(t), decltype(d)::value, decltype(p)::value, decltype(s)::value><<<unsigned(blocks), 256, 0, st>>>(a);
+  };
+  auto by_passes = [&](auto t, auto d, auto p) {
+    if (!passes) run(t, d, p, std::integral_constant<int, 0>{});
+    if constexpr (sizeof(t) == 2) {
+      if (passes == 1) run(t, d, p, std::integral_constant<int, 1>{});
+      if (passes == 2) run(t, d, p, std::integral_constant<int, 2>{});
+      if (passes == 4) run(t, d, p, std::integral_constant<int, 4>{});
+      if constexpr (decltype(d)::value == 128)
+        if (passes == 8) run(t, d, p, std::integral_constant<int, 8>{});
+    }
+  };
+  auto by_dim = [&](auto t) {
+    auto p = [&](auto d) { g->interleaved ? by_passes(t, d, std::true_type{}) : by_passes(t, d, std::false_type{}); };
+    g->d == 64 ? p(std::integral_constant<int, 64>{}) : p(std::integral_constant<int, 128>{});
+  };
+  dtype == DFS_BF16 ? by_dim(uint16_t{}) : by_dim(float{});
+  return launch_status(call);
+}
+
+}  // extern "C"

@@ -8,6 +8,7 @@
 #pragma once
 #include <type_traits>
 
+#include "seqs.h"
 #include "view.h"
 
 namespace dfs {
@@ -58,9 +59,6 @@ struct WindowArgs {
     by_blocks = Div(uint32_t(n));
   }
 };
-
-__device__ __forceinline__ int min_of(int a, int b) { return a < b ? a : b; }
-__device__ __forceinline__ int max_of(int a, int b) { return a > b ? a : b; }
 
 // A sequence's lengths, and the position of its first query.
 struct Lengths {
@@ -179,18 +177,6 @@ template <> struct Seq<false> {
   template <int U, bool KEYS> static __device__ __forceinline__ Seq of(const WindowArgs& a, int b, int i, bool) { return Seq{i, i, Lengths(a, b)}; }
 };
 
-// Sum over a wave, the same in all lanes.
-__device__ __forceinline__ int wave_sum(int x) {
-  x += __builtin_amdgcn_mov_dpp(x, 0xB1, 0xF, 0xF, true);              // within a quad: 1 0 3 2
-  x += __builtin_amdgcn_mov_dpp(x, 0x4E, 0xF, 0xF, true);              // 2 3 0 1
-  x += __builtin_amdgcn_mov_dpp(x, 0x141, 0xF, 0xF, true);             // mirrored within 8
-  x += __builtin_amdgcn_mov_dpp(x, 0x140, 0xF, 0xF, true);             // within 16
-  const auto half = __builtin_amdgcn_permlane16_swap(uint32_t(x), uint32_t(x), false, false);
-  x = int(half[0] + half[1]);
-  const auto all = __builtin_amdgcn_permlane32_swap(uint32_t(x), uint32_t(x), false, false);
-  return __builtin_amdgcn_readfirstlane(int(all[0] + all[1]));
-}
-
 // Packed: how many blocks a sequence has is known on the device alone.  Sequence s has room for those from start[s] * group / U + s on, counted down to whole ones, so that
 // no sum over the sequences in front of it is needed; a block between its last and the next one's room is not real.  Up to 64 sequences are looked at by a wave's
 // lanes at once, and their blocks can be had in another order (`long_first`): all sequences' blocks number x before those number x - 1, or of keys, counted from
@@ -199,7 +185,6 @@ template <> struct Seq<true> {
   int blk, slot, q0, k0;
   bool real;
   Lengths len;
-  static __device__ __forceinline__ int start_of(const int32_t* p, int s, int n) { return max_of(0, min_of(p[s], n)); }
   template <int U, bool KEYS> static __device__ __forceinline__ Seq of(const WindowArgs& a, int, int i, bool long_first) {
     const int lane = threadIdx.x & 63, per = KEYS ? 1 : a.group, most = KEYS ? a.n_k : a.n_q;
     const int32_t* start = KEYS ? a.k_start : a.q_start;
@@ -223,16 +208,9 @@ template <> struct Seq<true> {
       s = __builtin_ctzll(__builtin_amdgcn_ballot_w64(n > lo && before == place));
       r.blk = KEYS ? __builtin_amdgcn_readlane(n, s) - 1 - lo : lo;
     } else {
-      for (int n = a.packed; n > 0;) {
-        const int step = (n + 63) / 64, at = lane * step;
-        const bool begun = at < n && int(uint32_t(start_of(start, s + min_of(at, n - 1), most) * per) / U) + s + at <= i;
-        const int c = __builtin_popcountll(__builtin_amdgcn_ballot_w64(begun));
-        r.real = c > 0;
-        if (!r.real) return r;
-        s += (c - 1) * step;
-        n = min_of(step, n - (c - 1) * step);
-        if (step == 1) break;
-      }
+      s = run_of(a.packed, i, [&](int x) { return int(uint32_t(start_of(start, x, most) * per) / U) + x; });
+      r.real = s >= 0;
+      if (!r.real) return r;
       r.blk = i - int(uint32_t(start_of(start, s, most) * per) / U) - s;
       r.real = r.blk >= 0;                           // not where the starts go down
     }
