@@ -465,6 +465,36 @@ typedef struct {
 int dfs_paged_append(const dfs_qk_geom* g, int dtype, const dfs_view* q, const dfs_view* k, const dfs_view* v, const int32_t* q_start, const int32_t* k_len,
                      const int32_t* positions, const float* w_q, const float* w_k, const dfs_view* q_out, const dfs_pages* pages, int norm, void* stream);
 
+/* Queries of several sequences over a cache in pages. */
+typedef struct {
+  int32_t seqs, heads, heads_kv, d;    /* seqs below 2^20; heads a multiple of heads_kv: query heads g*j .. g*j + g - 1 share key head j; d 64 or 128 */
+  int32_t n_q;                         /* rows of q, of all sequences together */
+  int32_t left;                        /* how far a query sees back; negative: without limit */
+  int32_t sinks;                       /* the first keys, which every query behind them sees in any case; 0 if none */
+  /* Blocks of 32 rows (query heads of a key head together), and one more for each sequence, are fewer than 2^22 over all key heads. */
+} dfs_paged;
+
+/*
+ * Causal attention over a cache in pages, from one new token of each sequence to whole prompts.  Sequence s has the rows q_start[s] .. q_start[s+1] - 1 of q and o and
+ * k_len[s] keys, those of its rows among them (dfs_paged_append puts them there): row i of q_len stands at position p = k_len - q_len + i and sees key j if j <= p, and j >= p - left or
+ * j < sinks.
+ *   o = sum_j softmax_j(scale <q, k_j>) v_j,   lse = ln sum_j exp(scale <q, k_j>)
+ * with keys and values as the cache's elements and scales stand for them; a row that sees nothing has o = 0 and lse = -inf.  Arithmetic and rounding are those of
+ * dfs_window_attn_fwd; what 8 bits and a scale stand for is exact in bf16.
+ *   q [heads, n_q, d] in, o like q out; the `batch` of these views is not read
+ *   q_start [seqs + 1] int32, not falling (cut to [0, n_q]);  k_len [seqs] int32 (cut to [0, table_row x page])
+ *   lse [heads, n_q] fp32 out, dense, or NULL;   scale > 0
+ * An entry of the table outside [0, pages) is read as page 0.  Rows outside the sequences are not read and their o and lse are left as they are.  Keys and values that no row of a
+ * sequence sees may hold anything; a value that is not finite makes the rows that see it NaN or infinite, and possibly up to 127 rows beside them of the same sequence.
+ * The same call gives the same bits every time; the same sequence among others may differ by rounding.
+ * ws: dfs_paged_workspace_bytes(w, dtype, pages).
+ */
+int dfs_paged_attn_fwd(const dfs_paged* w, int dtype, const dfs_view* q, const dfs_pages* pages, const int32_t* q_start, const int32_t* k_len, float scale,
+                       const dfs_view* o, float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/* Bytes of scratch of dfs_paged_attn_fwd (0 also if `w` or `pages` is invalid); it follows from `w` and the types alone, not from the lengths.  Host only. */
+size_t dfs_paged_workspace_bytes(const dfs_paged* w, int dtype, const dfs_pages* pages);
+
 /*
  * Diagnostic for measurements, not part of the method: while `counters` (device memory, 3 x uint64, zeroed by
  * the caller) is set, every work-group of the bf16 attention kernel adds to counters[0] the shader-clock

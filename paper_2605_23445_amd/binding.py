@@ -55,6 +55,11 @@ class Packed(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("seqs", "heads", "heads_kv", "d", "n_q", "n_k", "left", "right")]
 
 
+class Paged(C.Structure):
+    """Mirror of dfs_paged."""
+    _fields_ = [(n, C.c_int32) for n in ("seqs", "heads", "heads_kv", "d", "n_q", "left", "sinks")]
+
+
 class _View(C.Structure):
     """Mirror of dfs_view."""
     _fields_ = [("data", C.c_void_p), ("batch", C.c_int64), ("head", C.c_int64), ("row", C.c_int64)]
@@ -98,7 +103,7 @@ def _load():
     lib = C.CDLL(_LIB_PATH)
     vp, i32, i64, dbl, f32, sz = C.c_void_p, C.c_int32, C.c_int64, C.c_double, C.c_float, C.c_size_t
     gp, qp, wp, kp, tp = C.POINTER(Geom), C.POINTER(QkGeom), C.POINTER(Window), C.POINTER(Packed), C.POINTER(_View)
-    cp = C.POINTER(_PagesC)
+    cp, dp = C.POINTER(_PagesC), C.POINTER(Paged)
     sig = {
         "dfs_geom_sizes": (C.c_int, [gp, C.POINTER(Sizes)]),
         "dfs_workspace_bytes": (sz, [gp, C.c_int]),
@@ -133,6 +138,8 @@ def _load():
         "dfs_packed_attn_bwd": (C.c_int, [kp, C.c_int, tp, tp, tp, tp, vp, tp, vp, vp, f32, tp, tp, tp, vp, sz, vp]),
         "dfs_packed_workspace_bytes": (sz, [kp, C.c_int, C.c_int]),
         "dfs_paged_append": (C.c_int, [qp, C.c_int, tp, tp, tp, vp, vp, vp, vp, vp, tp, cp, C.c_int, vp]),
+        "dfs_paged_attn_fwd": (C.c_int, [dp, C.c_int, tp, cp, vp, vp, f32, tp, vp, vp, sz, vp]),
+        "dfs_paged_workspace_bytes": (sz, [dp, C.c_int, cp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -142,7 +149,7 @@ def _load():
 
 def _load_calls(names=("forward", "token_order", "permute", "unperm", "block_score", "select_mask", "sparse_attn", "recall",
                        "qk_norm_rope", "qk_norm_rope_bwd", "window_attn_fwd", "window_attn_bwd", "packed_attn_fwd", "packed_attn_bwd",
-                       "paged_append")):
+                       "paged_append", "paged_attn_fwd")):
     """The calls of the _calls module.  They do in native code what those of the same names do below, for plain
     arguments, and return None for what they leave to these: as the stand-ins do for every call where the module is not there or
     was built against another torch, whose classes it reads (another Python does not find it: its name holds the version)."""
@@ -154,7 +161,7 @@ def _load_calls(names=("forward", "token_order", "permute", "unperm", "block_sco
             why = "older than this file"
         else:
             _calls.set_geom_type(Geom)
-            _calls.set_layer_types(QkGeom, Window, Packed)
+            _calls.set_layer_types(QkGeom, Window, Packed, Paged)
             return [getattr(_calls, name) for name in names]
     except ImportError as e:
         why = str(e)
@@ -166,13 +173,13 @@ def _load_calls(names=("forward", "token_order", "permute", "unperm", "block_sco
 _lib = _load()
 (_plain_forward, _plain_token_order, _plain_permute, _plain_unperm, _plain_block_score, _plain_select_mask, _plain_sparse_attn,
  _plain_recall, _plain_qk_norm_rope, _plain_qk_norm_rope_bwd, _plain_window_attn_fwd, _plain_window_attn_bwd, _plain_packed_attn_fwd,
- _plain_packed_attn_bwd, _plain_paged_append) = _load_calls()
+ _plain_packed_attn_bwd, _plain_paged_append, _plain_paged_attn_fwd) = _load_calls()
 EXPORTS = ("dfs_geom_sizes", "dfs_workspace_bytes", "dfs_last_error", "dfs_keep_count", "dfs_hilbert_perm", "dfs_permute",
            "dfs_block_score", "dfs_select_mask", "dfs_sparse_attn_fwd", "dfs_unperm", "dfs_forward", "dfs_token_order", "dfs_recall",
            "dfs_schedule", "dfs_block_score_src", "dfs_sparse_attn_fwd_src", "dfs_attn_clock_probe", "dfs_block_score_fused", "dfs_probe_mfma", "dfs_probe_copy", "dfs_probe_read",
            "dfs_select_mask_static", "dfs_qk_norm_rope", "dfs_qk_norm_rope_bwd", "dfs_qk_workspace_bytes", "dfs_window_attn_fwd",
            "dfs_window_attn_bwd", "dfs_window_workspace_bytes", "dfs_packed_attn_fwd", "dfs_packed_attn_bwd", "dfs_packed_workspace_bytes",
-           "dfs_paged_append")
+           "dfs_paged_append", "dfs_paged_attn_fwd", "dfs_paged_workspace_bytes")
 DFS_ORDER_HILBERT3D, DFS_ORDER_RASTER, DFS_ORDER_HILBERT2D, DFS_ORDER_BLOCK3D = 0, 1, 2, 3
 
 
@@ -648,3 +655,21 @@ def dfs_paged_append(g: QkGeom, dtype: int, q, k, v, q_start, k_len, positions, 
                                  _flat(q_start, torch.int32, g.batch + 1, "q_start"), _flat(k_len, torch.int32, g.batch, "k_len"),
                                  _flat(positions, torch.int32, 0, "positions"), _flat(w_q, torch.float32, g.d, "w_q"), _flat(w_k, torch.float32, g.d, "w_k"),
                                  _flat_view(q_out, dtype, g.heads, g.tokens, g.d, "q_out"), _pages(pages, g.batch, g.heads_kv, g.d), int(bool(norm)), _stream()))
+
+
+def dfs_paged_workspace_bytes(w: Paged, dtype: int, pages: Pages) -> int:
+    return int(_lib.dfs_paged_workspace_bytes(w, dtype, _pages(pages, w.seqs, w.heads_kv, w.d)))
+
+
+def dfs_paged_attn_fwd(w: Paged, dtype: int, q, pages: Pages, q_start, k_len, scale: float, o, lse=None, ws=None):
+    """Causal attention of the packed rows of several sequences over their keys in a cache; q_start is [seqs + 1] int32, k_len [seqs] int32."""
+    rc = _plain_paged_attn_fwd(w, dtype, q, pages, q_start, k_len, scale, o, lse, ws)
+    if rc == 0:
+        return
+    if rc is not None:
+        _check(rc)
+    qs = (w.heads, w.n_q, w.d)
+    wsp, wb = _scratch(ws)
+    _check(_lib.dfs_paged_attn_fwd(w, dtype, _flat_view(q, dtype, *qs, "q"), _pages(pages, w.seqs, w.heads_kv, w.d), _flat(q_start, torch.int32, w.seqs + 1, "q_start"),
+                                   _flat(k_len, torch.int32, w.seqs, "k_len"), float(scale), _flat_view(o, dtype, *qs, "o"),
+                                   _flat(lse, torch.float32, w.heads * w.n_q, "lse"), wsp, wb, _stream()))

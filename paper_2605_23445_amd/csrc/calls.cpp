@@ -19,8 +19,9 @@
 
 namespace {
 
-// binding.Geom, QkGeom, Window and Packed, ctypes structures with the layouts of dfs_geom, dfs_qk_geom, dfs_window and dfs_packed
-PyObject *g_geom_type = nullptr, *g_qk_type = nullptr, *g_window_type = nullptr, *g_packed_type = nullptr;
+// binding.Geom, QkGeom, Window, Packed and Paged, ctypes structures with the layouts of dfs_geom, dfs_qk_geom, dfs_window, dfs_packed and
+// dfs_paged
+PyObject *g_geom_type = nullptr, *g_qk_type = nullptr, *g_window_type = nullptr, *g_packed_type = nullptr, *g_paged_type = nullptr;
 PyObject *s_kv_idx, *s_kv_cnt, *s_mask, *s_k_head, *s_K_max;
 PyObject *s_k, *s_v, *s_table, *s_k_scale, *s_v_scale;
 
@@ -445,12 +446,30 @@ PyObject* paged_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+PyObject* paged_attn(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> int {
+    need(n == 10);
+    const auto w = to_struct<dfs_paged>(a[0], g_paged_type);
+    const int dtype = to_int(a[1]);
+    const Here here;
+    int64_t ws_bytes = 0;
+    const auto q = here.flat_view(a[2], dtype, w.heads, w.n_q, w.d), o = here.flat_view(a[7], dtype, w.heads, w.n_q, w.d);
+    const PagesOf pages(here, a[3], w.seqs, w.heads_kv, w.d);
+    const auto *q_start = here.flat<const int32_t>(a[4], at::kInt, int64_t(w.seqs) + 1), *k_len = here.flat<const int32_t>(a[5], at::kInt, w.seqs);
+    const float scale = float(to_double(a[6]));
+    auto* lse = here.flat<float>(a[8], at::kFloat, int64_t(w.heads) * w.n_q);
+    void *ws = here.flat<void>(a[9], at::ScalarType::Undefined, 0, &ws_bytes), *st = stream();
+    return without_gil([&] { return dfs_paged_attn_fwd(&w, dtype, q.get(), &pages.p, q_start, k_len, scale, o.get(), lse, ws, size_t(ws_bytes), st); });
+  });
+}
+
 PyObject* set_layer_types(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  if (n == 3) {
-    for (int i = 0; i < 3; ++i) Py_INCREF(a[i]);
+  if (n == 4) {
+    for (int i = 0; i < 4; ++i) Py_INCREF(a[i]);
     g_qk_type = a[0];
     g_window_type = a[1];
     g_packed_type = a[2];
+    g_paged_type = a[3];
   }
   Py_RETURN_NONE;
 }
@@ -477,6 +496,7 @@ PyMethodDef methods[] = {
     {"packed_attn_fwd", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(packed_attn<false>)), METH_FASTCALL, nullptr},
     {"packed_attn_bwd", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(packed_attn<true>)), METH_FASTCALL, nullptr},
     {"paged_append", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(paged_append)), METH_FASTCALL, nullptr},
+    {"paged_attn_fwd", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(paged_attn)), METH_FASTCALL, nullptr},
     {"set_geom_type", set_geom_type, METH_O, nullptr},
     {"set_layer_types", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(set_layer_types)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};

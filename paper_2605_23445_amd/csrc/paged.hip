@@ -1,0 +1,500 @@
+// Attention over a cache in pages: few rows of each sequence over long lists of keys.
+//
+// The rows of 32 queries (of all heads that share a key head) and the keys that they see, in pieces of 32, are an item.  How many pieces there are is known on the device
+// alone, so the pieces of all items, put behind one another, are dealt out to the work-groups in equal runs: one may end an item, take whole ones and begin
+// another.  An item that one work-group has whole is stored at once, parts of items go to the workspace, and a second kernel joins them.
+//
+// Within a work-group the waves take pieces in turn, each with tiles of its own, so that none waits for another before the end of a run of pieces; but for what is being
+// worked on the LDS is full of loads on their way.  Pieces begin at multiples of 32, so that each lies on one page, or with pages of 16 rows on two.  In 8 bits a tile holds the
+// bytes as they lie in memory; they become bf16, times their scale, on the way from LDS to the matrix cores, which is exact.
+#include <float.h>
+#include <math.h>
+
+#include "pages.h"
+#include "window.h"
+
+namespace dfs {
+
+struct PagedArgs : WindowArgs {                      // n_k: what the table has room for
+  PageArgs pages;
+  int32_t unit;                                      // pieces that are dealt out together
+  int32_t least;                                     // units that a work-group takes at least
+};
+
+constexpr int GROUPS = 512;                          // work-groups: two a CU
+
+// A sequence's rows and keys, its blocks of 32 rows, and the units of each of these with each key head (the pieces of all its rows together, one at least).
+struct PagedSeq {
+  int q0, n, k, blocks, units;
+  __device__ __forceinline__ PagedSeq(const PagedArgs& a, int s) {
+    q0 = start_of(a.q_start, s, a.n_q);
+    n = max_of(0, start_of(a.q_start, s + 1, a.n_q) - q0);
+    k = max_of(0, min_of(a.k_len[s], a.n_k));
+    blocks = (n * a.group + 31) / 32;
+    const Span all(a, k - n, k - 1, k, 32);
+    units = max_of(1, (all.n + a.unit - 1) / a.unit);
+  }
+  __device__ __forceinline__ int work(const PagedArgs& a) const { return blocks * units * a.heads_kv; }
+};
+
+// Units of all sequences in front of each, as a work-group's threads work them out: thread t adds up `each` sequences from t * each on.
+template <int NT> struct Deal {
+  int each, mine, before, total, per;                // a thread's sum, the sum in front of it, all, and a work-group's share
+  __device__ __forceinline__ Deal(const PagedArgs& a, int (&sums)[NT / 64]) {
+    each = (a.packed + NT - 1) / NT;
+    mine = 0;
+    for (int i = 0, s = threadIdx.x * each; i < each && s < a.packed; ++i, ++s) mine += PagedSeq(a, s).work(a);
+    const int upto = wave_sums(mine), wave = threadIdx.x >> 6;
+    if ((threadIdx.x & 63) == 63) sums[wave] = upto;
+    __syncthreads();
+    before = upto - mine;
+    total = 0;
+#pragma unroll
+    for (int w = 0; w < NT / 64; ++w) {
+      if (w < wave) before += sums[w];
+      total += sums[w];
+    }
+    per = max_of((total + GROUPS - 1) / GROUPS, a.least);
+  }
+};
+
+// Tiles of 32 rows of a page's elements in LDS, chunks of 16 bytes swapped within a row so that what is read at once lies in different banks.
+template <typename T, int D, bool E4M3> struct PageTile {
+  static constexpr int RB = E4M3 ? D : D * int(sizeof(T)), CH = RB / 16, BYTES = 32 * RB, LOADS = BYTES / 1024;
+  using Rows = Tile<T, D, 32, 1, false>;
+  using Columns = Tile<T, D, 32, 1, true>;
+  template <bool COLUMNS> static __device__ __forceinline__ int swizzle(int row) {
+    if constexpr (E4M3) return row * RB / 256 % CH;
+    else return COLUMNS ? Columns::swizzle(row) : Rows::swizzle(row);
+  }
+  // Byte offset of this lane's chunk of load j of 16 rows.
+  template <bool COLUMNS> static __device__ __forceinline__ uint32_t offset(int j, int lane, int64_t stride) {
+    const int p = j * 64 + lane, row = p / CH;
+    return uint32_t(row) * uint32_t(stride) + uint32_t((p % CH ^ swizzle<COLUMNS>(row)) * 16);
+  }
+};
+
+__device__ __forceinline__ bf16x8 eight(uint32_t a, uint32_t b, float scale) {
+  const bf16x2 p = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, false), q = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, true);
+  const bf16x2 r = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, false), s = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, true);
+  return bf16x8{p[0], p[1], q[0], q[1], r[0], r[1], s[0], s[1]};
+}
+
+// The pages of a sequence, 64 entries of the table at a time, one a lane: page and scales.
+template <bool E4M3> struct Entries {
+  int first, id;
+  float ks, vs;
+  const int32_t* row;
+  __device__ __forceinline__ Entries(const PagedArgs& a, int s) : first(-(1 << 30)), id(0), ks(0.f), vs(0.f), row(a.pages.table + int64_t(s) * a.pages.row) {}
+  // Lane that holds entry i.
+  __device__ __forceinline__ int lane_of(const PagedArgs& a, int i, int kvh) {
+    if (uint32_t(i - first) >= 64u) {
+      first = i;
+      const int lane = threadIdx.x & 63;
+      id = row[min_of(i + lane, a.pages.row - 1)];
+      if (uint32_t(id) >= uint32_t(a.pages.pages)) id = 0;
+      if constexpr (E4M3) {
+        const int64_t at = int64_t(id) * a.pages.heads_kv + kvh;
+        ks = a.pages.k_scale[at];
+        vs = a.pages.v_scale[at];
+      }
+    }
+    return i - first;
+  }
+};
+
+template <typename T, int D, bool E4M3> constexpr int paged_waves() { return sizeof(T) == 4 && D == 128 ? 2 : 4; }
+
+template <typename T, int D, bool E4M3, bool ONCE>
+__global__ void __launch_bounds__((64 * paged_waves<T, D, E4M3>()), (E4M3 || D * sizeof(T) <= 128 ? 2 : 1)) paged_split_kernel(PagedArgs a) {
+  constexpr int NW = paged_waves<T, D, E4M3>(), NT = 64 * NW, REGS = D / 2;
+  using PT = PageTile<T, D, E4M3>;
+  constexpr int LOADS = PT::LOADS, STEPS = D * int(sizeof(T)) / 32, BYTES = PT::BYTES;
+  static_assert(REGS * 64 * 4 <= 4 * BYTES || !E4M3, "a wave's sums fit where its tiles were");
+  __shared__ __attribute__((aligned(1024))) char tiles[NW * 4 * BYTES];
+  __shared__ float s_m[NW][32], s_l[NW][32];
+  __shared__ int s_sums[NW], s_seq, s_off;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 31, h = lane >> 5;
+  const uint32_t lds = uint32_t(reinterpret_cast<uintptr_t>((LDS_PTR(void))(tiles))) + uint32_t(wave * 4 * BYTES);
+
+  const Deal<NT> deal(a, s_sums);
+  int at = blockIdx.x * deal.per;
+  const int end = min_of(deal.total, at + deal.per), start = at;
+  if (at >= end) return;
+  if (threadIdx.x == 0) s_seq = a.packed;            // nobody's: where starts fall so far that the units of all pass 31 bits
+  __syncthreads();
+  if (deal.before <= at && at < deal.before + deal.mine) {
+    int s = threadIdx.x * deal.each, off = at - deal.before;
+    for (; s < a.packed; ++s) {
+      const int w = PagedSeq(a, s).work(a);
+      if (off < w) break;
+      off -= w;
+    }
+    s_seq = s;
+    s_off = off;
+  }
+  __syncthreads();
+  int s = __builtin_amdgcn_readfirstlane(s_seq), off = __builtin_amdgcn_readfirstlane(s_off);
+
+  uint32_t k_off[LOADS / 2], v_off[LOADS / 2];
+#pragma unroll
+  for (int j = 0; j < LOADS / 2; ++j) {
+    k_off[j] = PT::template offset<false>(j, lane, a.pages.k.row);
+    v_off[j] = PT::template offset<true>(j, lane, a.pages.v.row);
+  }
+  const float c2 = a.scale * LOG2E;
+  while (at < end && s < a.packed) {
+    const PagedSeq seq(a, s);
+    if (off >= seq.work(a)) {                        // sequences without rows
+      ++s;
+      off = 0;
+      continue;
+    }
+    const int item = off / seq.units, u0 = off - item * seq.units, u1 = min_of(seq.units, u0 + end - at), blk = item / a.heads_kv, kvh = item - blk * a.heads_kv;
+    const int r0 = blk * 32, rows = min_of(seq.n * a.group - r0, 32), shift = seq.k - seq.n;
+    const int i0 = query_of(a, r0), i1 = query_of(a, r0 + rows - 1);
+    const Span span(a, i0 + shift, i1 + shift, seq.k, 32);
+    const int t_end = min_of(span.n, u1 * a.unit), lo = max_of(0, i0 + shift - a.left);        // lo: first key of the window
+    const bool real = n < rows;
+    const int qi = real ? query_of(a, r0 + n) : i0, qh = kvh * a.group + (real ? r0 + n - qi * a.group : 0), p = qi + shift;
+
+    Entries<E4M3> entries(a, s);
+    float k_scale[2][2], v_scale[2][2];              // of both halves of the two pieces that are on their way
+    // Asks for a piece's keys or values.  Behind the last one nothing is asked for, by as many loads, so that the waits count the same.
+    auto ask = [&](const View& v, const uint32_t (&offs)[LOADS / 2], int t, int parity, bool values) __attribute__((always_inline)) {
+      const int key = span.begin(t), last = t < t_end ? span.end(t) : 0;
+      const bool front = values && t >= span.n_first && key < lo;         // values that no row sees must not be read: they may be anything
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const int k0 = key + 16 * half, there = min_of(last - k0, 16);
+        const int l = there > 0 ? entries.lane_of(a, k0 >> a.pages.bits, kvh) : 0, id = there > 0 ? __builtin_amdgcn_readlane(entries.id, l) : 0;
+        const uint64_t from = reinterpret_cast<uint64_t>(v.at(id, kvh, k0 & ((1 << a.pages.bits) - 1)));
+        const uint32_t bytes = there > 0 ? uint32_t(there - 1) * uint32_t(v.row) + PT::RB : 0;
+        const u32x4 desc = {uint32_t(__builtin_amdgcn_readfirstlane(uint32_t(from))), uint32_t(__builtin_amdgcn_readfirstlane(uint32_t(from >> 32))) & 0xFFFFu,
+                            uint32_t(__builtin_amdgcn_readfirstlane(bytes)), 0x00020000u};
+        if constexpr (E4M3) (values ? v_scale : k_scale)[parity][half] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(values ? entries.vs : entries.ks), l));
+        const uint32_t to = __builtin_amdgcn_readfirstlane(lds + uint32_t((parity * 2 + values) * BYTES + half * (BYTES / 2)));
+#pragma unroll
+        for (int j = 0; j < LOADS / 2; ++j) {
+          uint32_t o = offs[j];
+          if (front) {
+            const int k = k0 + (j * 64 + lane) / PT::CH;
+            if (k < lo && k >= a.sinks) o = 0x80000000u;
+          }
+          if (ONCE)
+            asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen nt lds" ::"s"(to), "v"(o), "s"(desc), "i"(j * 1024) : "memory", "m0", "scc");
+          else
+            asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(o), "s"(desc), "i"(j * 1024) : "memory", "m0", "scc");
+        }
+      }
+    };
+    int t = u0 * a.unit + wave;
+    typename Mat<T>::Frag qf[STEPS];
+    {
+      const char* qp = a.q.at(0, qh, seq.q0 + qi);
+#pragma unroll
+      for (int st = 0; st < STEPS; ++st) {
+        // in 8 bits a lane reads 16 channels at once, for two products
+        const int chunk = E4M3 ? st / 2 * 4 + 2 * h + st % 2 : 2 * st + h;
+        qf[st] = *reinterpret_cast<const typename Mat<T>::Frag*>(qp + chunk * 16);
+      }
+    }
+    if (t < t_end) {
+      ask(a.pages.k, k_off, t, 0, false);
+      ask(a.pages.v, v_off, t, 0, true);
+      ask(a.pages.k, k_off, t + NW, 1, false);
+      ask(a.pages.v, v_off, t + NW, 1, true);
+    }
+    // The queries are waited for here, with what was asked for behind them, or the compiler does it in every piece and for all loads.
+#pragma unroll
+    for (int st = 0; st < STEPS; ++st) asm volatile("" : "+v"(qf[st]));
+    f32x16 acc[D / 32];
+    clear(acc);
+    float m = -INFINITY, l = 0.f;
+    auto piece = [&](auto parity_) __attribute__((always_inline)) {
+      constexpr int parity = decltype(parity_)::value;
+      const uint32_t buf = lds + uint32_t(parity * 2 * BYTES);
+      wait_loads_but<3 * LOADS>();
+      f32x16 x;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x[i] = 0.f;
+      if constexpr (E4M3) {
+        const float scale = n < 16 ? k_scale[parity][0] : k_scale[parity][1];
+        u32x4 raw[STEPS / 2];
+#pragma unroll
+        for (int st = 0; st < STEPS / 2; ++st)
+          raw[st] = *reinterpret_cast<LDS_PTR(const u32x4)>(buf + uint32_t(n * PT::RB + ((2 * st + h) ^ PT::template swizzle<false>(n)) * 16));
+        __builtin_amdgcn_sched_barrier(0);           // operands that are worked out early drive the accumulators to scratch
+#pragma unroll
+        for (int st = 0; st < STEPS / 2; ++st) {
+          x = Mat<T>::mma(eight(raw[st][0], raw[st][1], scale), qf[2 * st], x);
+          x = Mat<T>::mma(eight(raw[st][2], raw[st][3], scale), qf[2 * st + 1], x);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      } else {
+        const typename PT::Rows::RowReader read(lane);
+#pragma unroll
+        for (int st = 0; st < STEPS; ++st) x = Mat<T>::mma(read.get(buf, 0, st), qf[st], x);
+      }
+      wait_reads();
+      ask(a.pages.k, k_off, t + 2 * NW, parity, false);
+      if (!span.whole(t)) span.mask(a, t, p, h, x, -INFINITY);
+      float mx = x[0];
+#pragma unroll
+      for (int i = 1; i < 16; ++i) mx = fmaxf(mx, x[i]);
+      const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+      const float m_new = fmaxf(m, fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * c2), ref = m_new == -INFINITY ? 0.f : m_new;
+      if (__builtin_amdgcn_ballot_w64(m_new > m)) {
+        const float alpha = __builtin_amdgcn_exp2f(m - ref);
+        m = m_new;
+        l *= alpha;
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) acc[c][i] *= alpha;
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        x[i] = __builtin_amdgcn_exp2f(fmaf(x[i], c2, -ref));
+        l += x[i];
+      }
+      Weights<T> w;
+      w.set(x);
+      wait_loads_but<3 * LOADS>();
+      if constexpr (E4M3) {
+        const int i = (lane & 15) >> 1, row = 4 * h + i + (i < 4 ? 0 : 4);                   // 8 rows of 16 channels from 16 lanes, 8 rows of one channel to each
+        typedef int i32x2 __attribute__((ext_vector_type(2)));
+        i32x2 raw[2][D / 32];
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+          for (int c = 0; c < D / 32; ++c) {
+            const uint32_t chunk = uint32_t((2 * c + ((lane >> 4) & 1)) ^ PT::template swizzle<true>(row));
+            raw[half][c] = __builtin_amdgcn_ds_read_tr8_b64_v2i32(reinterpret_cast<LDS_PTR(i32x2)>(buf + BYTES + uint32_t((16 * half + row) * PT::RB) + chunk * 16 + (lane & 1) * 8));
+          }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+          for (int c = 0; c < D / 32; ++c) {
+            acc[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(eight(uint32_t(raw[half][c][0]), uint32_t(raw[half][c][1]), v_scale[parity][half]),
+                                                             __builtin_bit_cast(bf16x8, w.p[half]), acc[c], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+          }
+      } else {
+        const typename PT::Columns::ColumnReader read(lane);
+        read.mma(buf + BYTES, 0, w, acc);
+      }
+      wait_reads();
+      ask(a.pages.v, v_off, t + 2 * NW, parity, true);
+    };
+    for (; t < t_end; t += NW) {
+      piece(std::integral_constant<int, 0>{});
+      t += NW;
+      if (t >= t_end) break;
+      piece(std::integral_constant<int, 1>{});
+    }
+    wait_loads();                                    // the last ones, of nothing, still write zeros where the sums go
+    const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
+    l = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+    // The waves' sums meet where the tiles were; each wave joins a share of the channels.
+    float* all = reinterpret_cast<float*>(tiles);
+    __syncthreads();
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) all[(wave * REGS + c * 16 + i) * 64 + lane] = acc[c][i];
+    if (h == 0) {
+      s_m[wave][n] = m;
+      s_l[wave][n] = l;
+    }
+    __syncthreads();
+    float top = s_m[0][n], total = 0.f, share_[NW];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) top = fmaxf(top, s_m[w][n]);
+    const float ref = top == -INFINITY ? 0.f : top;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      share_[w] = __builtin_amdgcn_exp2f(s_m[w][n] - ref);
+      total += share_[w] * s_l[w][n];
+    }
+    const bool whole = u0 == 0 && u1 == seq.units;
+    const float f = !whole ? 1.f : total == 0.f ? 0.f : 1.f / total;
+    const int64_t slot = (int64_t(blockIdx.x) * 2 + (at != start)) * 32 + n;                 // a run has two ends: parts of two items at most
+    if (real) {
+      char* out = whole ? a.o.at(0, qh, seq.q0 + qi) : reinterpret_cast<char*>(a.part + slot * D);
+#pragma unroll
+      for (int g = 0; g < REGS / NW; g += 4) {
+        const int reg = wave * (REGS / NW) + g, ch = reg / 16 * 32 + reg % 16 * 2 + 4 * h;
+        float x[4] = {};
+#pragma unroll
+        for (int w = 0; w < NW; ++w)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) x[j] = fmaf(share_[w], all[(w * REGS + reg + j) * 64 + lane], x[j]);
+        if (whole) store_four<T>(out, ch, x, f);
+        else store_four<float>(out, ch, x, f);
+      }
+      if (wave == 0 && h == 0) {
+        if (!whole) a.part_sums[slot] = make_float2(top, total);
+        else if (a.lse) a.lse[int64_t(qh) * a.n_q + seq.q0 + qi] = total == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * (1.f / LOG2E);
+      }
+    }
+    at += u1 - u0;
+    off += u1 - u0;
+    __syncthreads();                                 // the sums have been read: the next item's tiles may come
+  }
+}
+
+// Joins the parts of an item: a thread takes four channels of a row.  Items in the order of blocks of 32 rows, as packed sequences have them, and key heads.
+template <typename T, int D>
+__global__ void __launch_bounds__(256) paged_join_kernel(PagedArgs a) {
+  constexpr int TR = D / 4, RB = 256 / TR, U = 8;    // threads of a row, rows of a work-group, parts asked for at once
+  __shared__ int s_sums[4], s_base;
+  const int id = blockIdx.x / (32 / RB), n = blockIdx.x % (32 / RB) * RB + threadIdx.x / TR, ch = threadIdx.x % TR * 4;
+  const int slot = id / a.heads_kv, kvh = id - slot * a.heads_kv;
+  const int s = run_of(a.packed, slot, [&](int x) { return int(uint32_t(start_of(a.q_start, x, a.n_q) * a.group) / 32) + x; });
+  const Deal<256> deal(a, s_sums);
+  if (s < 0) return;
+  const PagedSeq seq(a, s);
+  const int blk = slot - int(uint32_t(seq.q0 * a.group) / 32) - s;
+  if (blk < 0 || blk >= seq.blocks) return;
+  if (s / deal.each == int(threadIdx.x)) {
+    int base = deal.before;
+    for (int x = threadIdx.x * deal.each; x < s; ++x) base += PagedSeq(a, x).work(a);
+    s_base = base + (blk * a.heads_kv + kvh) * seq.units;
+  }
+  __syncthreads();
+  const int base = s_base, g0 = base / deal.per, g1 = (base + seq.units - 1) / deal.per;
+  if (g0 == g1) return;                              // one work-group had it whole
+  const int r = blk * 32 + n;
+  if (r >= seq.n * a.group) return;
+  const int qi = query_of(a, r), qh = kvh * a.group + r - qi * a.group;
+  float top = -INFINITY, total = 0.f, x[4] = {};
+  for (int g = g0; g <= g1; g += U) {
+    float2 ml[U];
+    float4 y[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {                    // behind the last part that once more, with a weight of zero
+      const int w = min_of(g + u, g1);
+      const int64_t i = (int64_t(w) * 2 + (w == g0 && base != w * deal.per)) * 32 + n;
+      ml[u] = a.part_sums[i];
+      y[u] = *reinterpret_cast<const float4*>(a.part + i * D + ch);
+    }
+    const float before = top;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (g + u > g1) ml[u].x = -INFINITY;
+      top = fmaxf(top, ml[u].x);
+    }
+    const float ref = top == -INFINITY ? 0.f : top, f = __builtin_amdgcn_exp2f(before - ref);
+    total *= f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] *= f;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const float part = __builtin_amdgcn_exp2f(ml[u].x - ref);
+      total = fmaf(part, ml[u].y, total);
+      x[0] = fmaf(part, y[u].x, x[0]);
+      x[1] = fmaf(part, y[u].y, x[1]);
+      x[2] = fmaf(part, y[u].z, x[2]);
+      x[3] = fmaf(part, y[u].w, x[3]);
+    }
+  }
+  store_four<T>(a.o.at(0, qh, seq.q0 + qi), ch, x, total == 0.f ? 0.f : 1.f / total);
+  if (ch == 0 && a.lse) a.lse[int64_t(qh) * a.n_q + seq.q0 + qi] = total == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * (1.f / LOG2E);
+}
+
+static int check_paged(const char* call, const dfs_paged* w, int dtype) {
+  if (!w) return fail(DFS_EINVAL, "%s: geometry pointer is NULL", call);
+  if (dtype != DFS_F32 && dtype != DFS_BF16) return fail(DFS_EDTYPE, "%s: dtype %d is not DFS_F32 or DFS_BF16", call, dtype);
+  if (w->seqs < 0 || w->n_q < 0 || w->n_q > 1 << 28) return fail(DFS_ESHAPE, "%s: seqs=%d must not be negative, n_q=%d be in [0, 2^28]", call, w->seqs, w->n_q);
+  if (w->heads < 1 || w->heads_kv < 1 || w->heads > 65535 || w->heads % w->heads_kv)
+    return fail(DFS_ESHAPE, "%s: heads=%d must be in [1, 65535] and a multiple of heads_kv=%d", call, w->heads, w->heads_kv);
+  if (w->d != 64 && w->d != 128) return fail(DFS_ESHAPE, "%s: d=%d: head dimension must be 64 or 128", call, w->d);
+  if (w->sinks < 0) return fail(DFS_ESHAPE, "%s: sinks=%d is negative", call, w->sinks);
+  const int64_t rows = int64_t(w->heads / w->heads_kv) * w->n_q;
+  if (rows > int64_t(1) << 30 || w->seqs >= 1 << 20 || (rows / 32 + w->seqs) * w->heads_kv >= 1 << 22)
+    return fail(DFS_ESHAPE, "%s: heads_kv=%d x rows of q, or seqs=%d, too large", call, w->heads_kv, w->seqs);
+  return DFS_OK;
+}
+
+// The parts of GROUPS runs, two each, and their sums.
+static size_t part_bytes(const dfs_paged* w) { return size_t(GROUPS) * 2 * 32 * w->d * sizeof(float); }
+
+}  // namespace dfs
+
+using namespace dfs;
+
+extern "C" {
+
+size_t dfs_paged_workspace_bytes(const dfs_paged* w, int dtype, const dfs_pages* pages) {
+  const char* call = "dfs_paged_workspace_bytes";
+  PageArgs p;
+  if (check_paged(call, w, dtype) != DFS_OK || check_pages(call, pages, dtype, w->seqs, w->heads_kv, w->d, false, &p) != DFS_OK) return 0;
+  if (w->seqs == 0 || w->n_q == 0) return 0;
+  return part_bytes(w) + size_t(GROUPS) * 2 * 32 * sizeof(float2);
+}
+
+int dfs_paged_attn_fwd(const dfs_paged* w, int dtype, const dfs_view* q, const dfs_pages* pages, const int32_t* q_start, const int32_t* k_len, float scale,
+                       const dfs_view* o, float* lse, void* ws, size_t ws_bytes, void* stream) {
+  const char* call = "dfs_paged_attn_fwd";
+  PagedArgs a = {};
+  int rc = check_paged(call, w, dtype);
+  if (rc) return rc;
+  if (!(scale > 0.f) || !isfinite(scale)) return fail(DFS_EINVAL, "%s: scale must be positive and finite", call);
+  if (misaligned(4, {lse, q_start, k_len})) return fail(DFS_EINVAL, "%s: lse, starts and lengths must be 4-byte aligned", call);
+  if (w->seqs && (!q_start || !k_len)) return fail(DFS_EINVAL, "%s: q_start or k_len is NULL", call);
+  if ((rc = check_view(call, "q", q, dtype, 1, w->heads, w->n_q, w->d, false, &a.q))) return rc;
+  if ((rc = check_view(call, "o", o, dtype, 1, w->heads, w->n_q, w->d, true, &a.o))) return rc;
+  if ((rc = check_pages(call, pages, dtype, w->seqs, w->heads_kv, w->d, false, &a.pages))) return rc;
+  if (w->seqs == 0 || w->n_q == 0) return DFS_OK;
+  const size_t need = part_bytes(w) + size_t(GROUPS) * 2 * 32 * sizeof(float2);
+  if (!ws || (uintptr_t(ws) & 255) || ws_bytes < need)
+    return fail(DFS_EWORKSPACE, "%s: workspace of %zu bytes needed (256-byte aligned), got %zu", call, need, ws_bytes);
+  if ((rc = check_apart(call, {{"o", &a.o}}, {{"q", &a.q}, {"pages.k", &a.pages.k}, {"pages.v", &a.pages.v}}))) return rc;
+  a.lse = lse;
+  a.q_start = q_start;
+  a.k_len = k_len;
+  a.packed = w->seqs;
+  a.batch = 1;
+  a.heads = w->heads;
+  a.heads_kv = w->heads_kv;
+  a.group = w->heads / w->heads_kv;
+  a.seqs = w->heads_kv;
+  a.by_kv = Div(uint32_t(w->heads_kv));
+  a.by_group = Div(uint32_t(a.group));
+  a.n_q = w->n_q;
+  a.n_k = a.pages.row << a.pages.bits;
+  a.left = w->left < 0 || w->left > NO_LIMIT ? NO_LIMIT : w->left;
+  a.right = 0;
+  a.sinks = a.left == NO_LIMIT ? 0 : w->sinks < a.n_k ? w->sinks : a.n_k;
+  a.scale = scale;
+  a.part = static_cast<float*>(ws);
+  a.part_sums = reinterpret_cast<float2*>(static_cast<char*>(ws) + part_bytes(w));
+  // work is counted in 31 bits
+  const int64_t items = (int64_t(a.group) * a.n_q / 32 + w->seqs) * w->heads_kv, pieces = a.n_k / 32 + 2;
+  a.unit = 4;
+  while (items * ((pieces + a.unit - 1) / a.unit) >= int64_t(1) << 31) a.unit *= 2;
+  a.least = 1;
+  const bool bytes = pages->dtype == DFS_E4M3;
+  const hipStream_t st = as_stream(stream);
+  const unsigned joins = unsigned(items * (w->d / 32));
+  auto run = [&](auto t, auto d, auto b) {
+    using T = decltype(t);
+    constexpr int D = decltype(d)::value;
+    constexpr bool E4M3 = decltype(b)::value;
+    paged_split_kernel<T, D, E4M3, false><<<GROUPS, 64 * paged_waves<T, D, E4M3>(), 0, st>>>(a);
+  };
+  auto join = [&](auto t, auto d) { paged_join_kernel<decltype(t), decltype(d)::value><<<joins, 256, 0, st>>>(a); };
+  auto by_dim = [&](auto f) { w->d == 64 ? f(std::integral_constant<int, 64>{}) : f(std::integral_constant<int, 128>{}); };
+  by_dim([&](auto d) {
+    if (dtype == DFS_F32) run(float{}, d, std::false_type{});
+    else if (bytes) run(uint16_t{}, d, std::true_type{});
+    else run(uint16_t{}, d, std::false_type{});
+  });
+  if ((rc = launch_status(call))) return rc;
+  by_dim([&](auto d) { dtype == DFS_F32 ? join(float{}, d) : join(uint16_t{}, d); });
+  return launch_status(call);
+}
+
+}  // extern "C"

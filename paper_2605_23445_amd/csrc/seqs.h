@@ -19,6 +19,17 @@ __device__ __forceinline__ int wave_sum(int x) {
   return __builtin_amdgcn_readfirstlane(int(all[0] + all[1]));
 }
 
+// Sums over the lanes up to each one.
+__device__ __forceinline__ int wave_sums(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);      // from 1, 2, 4 and 8 lanes in front, of the same 16
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);      // the last of 16 to the next 16: rows 1 and 3
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);      // of 32 to the next 32
+  return x;
+}
+
 // Where sequence s begins; past the last one, where that ends.  Cut to the n rows that there are.
 __device__ __forceinline__ int start_of(const int32_t* starts, int s, int n) { return max_of(0, min_of(starts[s], n)); }
 

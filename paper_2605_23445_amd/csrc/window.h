@@ -91,8 +91,9 @@ __device__ __forceinline__ void keep(f32x16& x, int lo, int hi, int more, float 
 struct Span {
   int p0, p1, lo, hi, first, n_first, n;             // positions; window [lo, hi); first keys [0, first) in front of it; pieces of these, and of all
   int first_whole, w0, w1;                           // pieces that every query sees whole: of first keys those in front of first_whole, [w0, w1)
-  __device__ __forceinline__ Span(const WindowArgs& a, int p0_, int p1_, int k_len) : p0(p0_), p1(p1_) {
-    lo = max_of(0, p0 - a.left);
+  // step: what the window's pieces begin at multiples of, a power of two; the keys in front of its first one count as the window's.
+  __device__ __forceinline__ Span(const WindowArgs& a, int p0_, int p1_, int k_len, int step = 1) : p0(p0_), p1(p1_) {
+    lo = max_of(0, p0 - a.left) & -step;
     hi = min_of(k_len, p1 + a.right + 1);
     if (hi < 0) hi = 0;
     first = min_of(min_of(a.sinks, lo), hi);

@@ -1,0 +1,309 @@
+"""Attention over a cache in pages against the fp64 oracle, sequence by sequence with the bounds of windowed attention: a cache's elements times their scales are exact in bf16,
+and the arithmetic from there on is the same."""
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+P = pytest.importorskip("paper_2605_23445_amd")
+from oracle import layer_oracle as L  # noqa: E402
+from tests import test_gpu_window as W  # noqa: E402
+
+E = W.E
+KINDS = {"f32": ("f32", torch.float32), "bf16": ("bf16", torch.bfloat16), "e4m3": ("bf16", torch.float8_e4m3fn)}
+
+# heads, heads_kv, d, page, query rows of each sequence, their keys, left, sinks, rows in front of the first and behind the last sequence
+CASES = {
+    "one_token": (1, 1, 128, 16, [1], [1], -1, 0, 0, 0),
+    "one_token_each": (8, 2, 128, 64, [1, 1, 1, 1, 1, 1], [300, 1, 64, 65, 31, 1000], -1, 0, 0, 0),
+    "one_token_each_d64": (16, 4, 64, 16, [1, 1, 1, 0, 1], [300, 17, 16, 70, 1000], -1, 0, 0, 0),
+    "long_stream": (8, 2, 128, 128, [1], [5000], -1, 0, 0, 0),
+    "long_and_short": (4, 1, 128, 32, [1, 1, 1], [4000, 3, 900], -1, 0, 0, 0),
+    "window": (8, 2, 128, 64, [1, 1, 1, 1], [700, 40, 129, 64], 100, 0, 0, 0),
+    "window_and_first_keys": (8, 2, 64, 16, [1, 1, 1, 1], [700, 40, 129, 64], 100, 4, 0, 0),
+    "many_first_keys": (4, 4, 128, 32, [1, 3, 2], [600, 200, 90], 33, 75, 0, 0),
+    "first_keys_reach_the_window": (4, 2, 64, 64, [1, 5, 20], [150, 140, 100], 60, 70, 0, 0),
+    "itself_only": (2, 2, 64, 16, [1, 4], [50, 90], 0, 0, 0, 0),
+    "few_tokens_each": (12, 4, 128, 32, [4, 3, 0, 7], [333, 4, 60, 130], -1, 0, 2, 1),
+    "no_keys": (4, 2, 64, 16, [1, 2, 1], [0, 0, 9], -1, 0, 0, 0),
+    "more_queries_than_keys": (4, 2, 128, 16, [40, 5], [20, 3], -1, 0, 0, 3),
+    "pieces": (6, 2, 128, 64, [70, 1, 33, 200], [700, 390, 33, 200], -1, 0, 5, 0),
+    "pieces_d64": (4, 4, 64, 16, [130, 64, 3], [130, 500, 777], -1, 0, 0, 4),
+    "pieces_with_window": (8, 2, 64, 32, [150, 90, 31], [150, 400, 300], 70, 10, 0, 0),
+    "many_streams": (4, 2, 64, 16, [i % 2 for i in range(300)], [(7 * i) % 90 + 1 for i in range(300)], -1, 0, 1, 0),
+    "wide_group": (24, 1, 128, 64, [3, 9], [100, 300], -1, 0, 0, 0),
+    # enough blocks of 128 rows: the kernel of long calls
+    "blocks": (16, 16, 128, 64, [500, 129, 1], [500, 700, 300], -1, 0, 0, 0),
+    "blocks_group": (32, 8, 128, 128, [300, 130, 257], [300, 1000, 511], -1, 0, 3, 2),
+    "blocks_d64": (32, 16, 64, 32, [400, 1, 333], [600, 64, 333], -1, 0, 0, 0),
+    "blocks_small_pages": (32, 16, 64, 16, [250, 130, 128], [250, 463, 777], -1, 0, 0, 0),
+    "blocks_small_pages_d128": (20, 20, 128, 16, [300, 150], [399, 150], -1, 0, 0, 1),
+    "blocks_window": (32, 8, 128, 64, [300, 260, 90], [300, 1200, 600], 130, 0, 0, 0),
+    "blocks_window_and_first_keys": (24, 12, 64, 32, [300, 260, 90], [300, 900, 600], 77, 40, 0, 0),
+    "blocks_many": (16, 8, 128, 32, [(29 * i) % 70 for i in range(70)], [(29 * i) % 70 + 3 * i for i in range(70)], -1, 0, 0, 0),
+    "blocks_more_queries_than_keys": (64, 64, 64, 16, [140, 130], [70, 3], -1, 0, 0, 0),
+}
+
+
+def _make(name, kind, seed=0, token_major=False):
+    heads, kv, d, page, q_lens, k_lens, left, sinks, front, back = CASES[name]
+    dtype, ct = KINDS[kind]
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    rand = lambda *s: torch.randn(*s, generator=gen, device="cuda")  # noqa: E731
+    n = sum(q_lens) + front + back
+    q = rand(n, heads, d).to(W.DT[dtype][1]).transpose(0, 1) if token_major else rand(heads, n, d).to(W.DT[dtype][1])
+    need = [(x + page - 1) // page for x in k_lens]
+    pages, row = sum(need) + 2, max(need) + 1
+    order = np.random.default_rng(seed).permutation(pages)[:sum(need)]
+    table, at = np.full((len(k_lens), row), 1 << 30, dtype=np.int32), 0
+    for i, m in enumerate(need):
+        table[i, :m] = order[at:at + m]
+        at += m
+    shape = (pages, page, kv, d) if token_major else (pages, kv, page, d)
+    cache = [rand(*shape) for _ in range(2)]
+    if token_major:
+        cache = [x.transpose(1, 2) for x in cache]
+    scale = [None, None]
+    if kind == "e4m3":
+        scale = [torch.exp2(torch.randint(-9, -5, (pages, kv), generator=gen, device="cuda").float()) for _ in range(2)]
+        cache = [(x / s[:, :, None, None]).clamp_(-448, 448) for x, s in zip(cache, scale)]
+    p = P.Pages(*(x.to(ct) for x in cache), torch.from_numpy(table).cuda(), *scale)
+    w = P.Paged(len(q_lens), heads, kv, d, n, left, sinks)
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    return w, dtype, q, p, i32(front + np.concatenate([[0], np.cumsum(q_lens)])), i32(k_lens), q_lens, k_lens, front, table
+
+
+def _ws(w, dtype, p):
+    return torch.full((P.dfs_paged_workspace_bytes(w, W.DT[dtype][0], p),), 255, dtype=torch.uint8, device="cuda")
+
+
+def _run(w, dtype, q, p, q_start, k_len, scale, mark=7.0, lse=True):
+    o, sums = torch.full(q.shape, mark, dtype=q.dtype, device="cuda"), torch.full((w.heads, w.n_q), mark, device="cuda") if lse else None
+    P.dfs_paged_attn_fwd(w, W.DT[dtype][0], q, p, q_start, k_len, scale, o, sums, _ws(w, dtype, p))
+    return o, sums
+
+
+def _rows(p, table, s, m):
+    """Keys and values [heads_kv, m, d] of a sequence in fp64."""
+    page, got = p.k.shape[2], []
+    ids = torch.from_numpy(table[s, :(m + page - 1) // page].astype(np.int64)).cuda()
+    for x, scale in ((p.k, p.k_scale), (p.v, p.v_scale)):
+        y = torch.stack([x[int(i)].float() for i in ids]).double() if len(ids) else torch.zeros(0, *x.shape[1:], dtype=torch.float64, device="cuda")
+        if scale is not None:
+            y = y * scale[ids].double()[:, :, None, None]
+        got.append(y.permute(1, 0, 2, 3).reshape(x.shape[1], -1, x.shape[3])[:, :m].cpu().numpy())
+    return got
+
+
+def _check(w, dtype, q, p, q_lens, k_lens, front, table, scale, o, lse, mark=7.0):
+    u, group, at = W.DT[dtype][2], w.heads // w.heads_kv, front
+    n_all = sum(q_lens)
+    for x in (o, lse):
+        assert (x[:, :front] == mark).all() and (x[:, front + n_all:] == mark).all(), "rows outside the sequences were written"
+    q, o, lse = (W._np(x) for x in (q, o, lse))
+    for s, (n, m) in enumerate(zip(q_lens, k_lens)):
+        k, v = _rows(p, table, s, m)
+        see = L.window_mask(n, m, w.left, 0, w.sinks)
+        for h in range(w.heads if n else 0):
+            kk, vv, x = k[h // group], v[h // group], q[h, at:at + n]
+            want, want_lse, pr = L.window_attn(x, kk, vv, see, scale)
+            size = np.where(see, np.abs(x) @ np.abs(kk).T * scale, 0.0)
+            off = (w.d + 4) * E * (size.max(-1, keepdims=True) if m else np.zeros((n, 1)))
+            err = (u + 2 * off + (m + 16) * E) * (pr @ np.abs(vv)) + u * np.abs(want) + 1e-30
+            W._within(o[h, at:at + n], want, err, "o", s, h)
+            got, full = lse[h, at:at + n], ~np.isneginf(want_lse)
+            assert (np.isneginf(got) == ~full).all(), ("lse", s, h)
+            with np.errstate(invalid="ignore"):
+                assert (np.abs(got - want_lse) <= off[:, 0] + (m + 16) * E + 4 * E * np.abs(want_lse))[full].all(), ("lse", s, h)
+        at += n
+
+
+@pytest.mark.parametrize("kind", list(KINDS))
+@pytest.mark.parametrize("name", list(CASES))
+def test_against_the_oracle(name, kind):
+    w, dtype, q, p, q_start, k_len, q_lens, k_lens, front, table = _make(name, kind)
+    scale = 1 / np.sqrt(w.d)
+    o, lse = _run(w, dtype, q, p, q_start, k_len, scale)
+    _check(w, dtype, q, p, q_lens, k_lens, front, table, scale, o, lse)
+    again, _ = _run(w, dtype, q, p, q_start, k_len, scale, lse=False)
+    assert torch.equal(o, again)
+
+
+@pytest.mark.parametrize("kind", list(KINDS))
+@pytest.mark.parametrize("name", ["one_token_each", "window_and_first_keys", "pieces", "blocks_d64", "blocks_small_pages_d128"])
+def test_token_major_pages(name, kind):
+    w, dtype, q, p, q_start, k_len, q_lens, k_lens, front, table = _make(name, kind, 1, True)
+    o, lse = _run(w, dtype, q, p, q_start, k_len, 0.2)
+    dense = P.Pages(p.k.float().contiguous().to(p.k.dtype), p.v.float().contiguous().to(p.v.dtype), p.table, p.k_scale, p.v_scale)
+    want = _run(w, dtype, q.contiguous(), dense, q_start, k_len, 0.2)
+    assert torch.equal(o, want[0]) and torch.equal(lse, want[1])
+    _check(w, dtype, q, p, q_lens, k_lens, front, table, 0.2, o, lse)
+
+
+@pytest.mark.parametrize("kind", list(KINDS))
+@pytest.mark.parametrize("name", ["one_token_each", "window_and_first_keys", "many_first_keys", "first_keys_reach_the_window", "pieces_with_window", "blocks_window",
+                                  "blocks_window_and_first_keys", "blocks_small_pages"])
+def test_what_nothing_sees_may_hold_anything(name, kind):
+    """NaN in keys and values behind the last one and in front of every window, in pages that are nobody's, and in rows outside the sequences."""
+    w, dtype, q, p, q_start, k_len, q_lens, k_lens, front, table = _make(name, kind, 2)
+    want = _run(w, dtype, q, p, q_start, k_len, 0.1)
+    page = p.k.shape[2]
+    seen = np.zeros((p.k.shape[0], page), bool)
+    for s, (n, m) in enumerate(zip(q_lens, k_lens)):
+        for j in np.flatnonzero(L.window_mask(n, m, w.left, 0, w.sinks).any(0)):
+            seen[table[s, j // page], j % page] = True
+    blind = torch.from_numpy(~seen).cuda()
+    bad = []
+    for x in (p.k, p.v):
+        y = x.float()
+        y.transpose(1, 2)[blind] = float("nan")
+        bad.append(y.to(x.dtype))
+    got = _run(w, dtype, q, P.Pages(*bad, p.table, p.k_scale, p.v_scale), q_start, k_len, 0.1)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("kind", list(KINDS))
+@pytest.mark.parametrize("name", ["one_token_each", "pieces", "blocks", "many_streams"])
+def test_starts_lengths_and_tables_that_break_the_format(name, kind):
+    """Lengths are cut to the table's room and entries that name no page are page 0; starts that fall touch nothing outside."""
+    w, dtype, q, p, q_start, k_len, q_lens, k_lens, front, table = _make(name, kind, 3)
+    room = table.shape[1] * p.k.shape[2]
+    far = k_len.clone()
+    far[0], bad = 1 << 30, np.where((table < 0) | (table >= p.k.shape[0]), 0, table)
+    bad[0, 0] = 0
+    broken = p.table.clone()
+    broken[0, 0] = -5
+    got = _run(w, dtype, q, P.Pages(p.k, p.v, broken, p.k_scale, p.v_scale), q_start, far, 0.1)
+    far[0] = room
+    want = _run(w, dtype, q, P.Pages(p.k, p.v, torch.from_numpy(bad).cuda(), p.k_scale, p.v_scale), q_start, far, 0.1)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    assert far.shape == k_len.shape
+    negative = torch.full_like(k_len, -3)
+    o, lse = _run(w, dtype, q, p, q_start, negative, 0.1)
+    n = sum(q_lens)
+    assert not o[:, front:front + n].any() and torch.isneginf(lse[:, front:front + n]).all()
+    for falling in (q_start.flip(0), torch.where(torch.arange(w.seqs + 1, device="cuda") % 2 == 0, q_start, -q_start)):
+        around = torch.full((2, w.heads + 2, w.n_q, w.d), 7.0, dtype=q.dtype, device="cuda")
+        P.dfs_paged_attn_fwd(w, W.DT[dtype][0], q, p, falling.int(), k_len, 0.1, around[0, 1:-1], None, _ws(w, dtype, p))
+        torch.cuda.synchronize()
+        assert (around[1] == 7).all() and (around[0, 0] == 7).all() and (around[0, -1] == 7).all()
+
+
+def test_pages_past_32_bits():
+    """Pages more than 2^32 bytes behind the first."""
+    w = P.Paged(1, 4, 1, 128, 1, -1, 0)
+    pages = (1 << 19) + 900                          # of 8 KB
+    gen = torch.Generator(device="cuda").manual_seed(6)
+    last = [torch.randn(5, 1, 64, 128, generator=gen, device="cuda").to(torch.float8_e4m3fn) for _ in range(2)]
+    k, v = (torch.zeros(pages, 1, 64, 128, dtype=torch.float8_e4m3fn, device="cuda") for _ in range(2))
+    for x, y in zip((k, v), last):
+        x.view(torch.uint8)[-5:] = y.view(torch.uint8)
+    ones, q = torch.ones(pages, 1, device="cuda"), torch.randn(4, 1, 128, generator=gen, device="cuda").bfloat16()
+    start, length = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in ([0, 1], [300]))
+    table = torch.arange(5, dtype=torch.int32, device="cuda")[None]
+    a = _run(w, "bf16", q, P.Pages(k, v, table + (pages - 5), ones, ones), start, length, 0.1)
+    b = _run(w, "bf16", q, P.Pages(*last, table, ones[:5], ones[:5]), start, length, 0.1)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1]) and a[0].any()
+
+
+@pytest.mark.parametrize("kind", list(KINDS))
+def test_a_prompt_and_its_tokens(kind):
+    """Appending and attending: a prompt whole, in two pieces, and token by token, against attention over its keys as they were; pages in 8 bits hold what was
+    rounded, so there the reference reads them."""
+    heads, kv, d, n = 8, 2, 64, 150
+    dtype, ct = KINDS[kind]
+    code, dt, u = W.DT[dtype]
+    gen = torch.Generator(device="cuda").manual_seed(7)
+    x = torch.randn(n, heads + 2 * kv, d, generator=gen, device="cuda").to(dt).transpose(0, 1)
+    wq, wk = (1 + 0.2 * torch.randn(d, generator=gen, device="cuda") for _ in range(2))
+    i32 = lambda y: torch.tensor(y, dtype=torch.int32, device="cuda")  # noqa: E731
+    scales = [torch.ones(8, kv, device="cuda") if kind == "e4m3" else None for _ in range(2)]
+    outs = []
+    for cuts in ([n], [90, 60], [140] + [1] * 10):
+        p = P.Pages(*(torch.zeros(8, kv, 32, d, device="cuda").to(ct) for _ in range(2)), i32([[6, 1, 7, 0, 3, 2]]), *(None if s is None else s.clone() for s in scales))
+        at, o = 0, torch.empty(heads, n, d, dtype=dt, device="cuda")
+        for m in cuts:
+            g = P.QkGeom(1, m, heads, kv, d, 0, 1, d, 0, 0, 1e4, 1e-5)
+            part, rows = x[:, at:at + m], torch.empty(heads, m, d, dtype=dt, device="cuda")
+            start, length = i32([0, m]), i32([at + m])
+            P.dfs_paged_append(g, code, part[:heads], part[heads:heads + kv], part[heads + kv:], start, length, None, wq, wk, rows, p)
+            w = P.Paged(1, heads, kv, d, m, -1, 0)
+            out = torch.empty_like(rows)
+            P.dfs_paged_attn_fwd(w, code, rows, p, start, length, 0.125, out, None, _ws(w, dtype, p))
+            o[:, at:at + m] = out
+            at += m
+        outs.append(o.double())
+    rope = [torch.empty(1, h, n, d, dtype=dt, device="cuda") for h in (heads, kv, kv)]
+    g = P.QkGeom(1, n, heads, kv, d, 0, 1, d, 0, 0, 1e4, 1e-5)
+    P.dfs_qk_norm_rope(g, code, x[None, :heads], x[None, heads:heads + kv], x[None, heads + kv:], torch.arange(n, device="cuda", dtype=torch.int32)[:, None], wq, wk, *rope)
+    w, o = P.Packed(1, heads, kv, d, n, n, -1, 0), torch.empty(heads, n, d, dtype=dt, device="cuda")
+    ws = torch.empty(max(256, P.dfs_packed_workspace_bytes(w, code, False)), dtype=torch.uint8, device="cuda")
+    P.dfs_packed_attn_fwd(w, code, rope[0][0], rope[1][0], rope[2][0], i32([0, n]), None, 0.125, o, None, ws)
+    # o is a mean of values: off by the weights' and its own rounding, and in 8 bits by what keys (through the logits) and values are rounded by, 2^-4 each
+    most = float(rope[2].abs().max())
+    logit = float((rope[0][0].float().norm(dim=-1).max() * rope[1][0].float().norm(dim=-1).max()) * 0.125)
+    near = {"f32": 1e-5 * most, "bf16": 4 * u * most, "e4m3": (4 * u + 2.0 ** -4 + 2 * 2.0 ** -4 * logit) * most}[kind]
+    for y in outs:
+        assert (y - o.double()).abs().max() <= near
+    if kind != "e4m3":                               # pieces see the same rows: only sums' order differs
+        assert all((y - outs[0]).abs().max() <= 4 * max(u, 1e-6) * most for y in outs)
+
+
+def test_captured_and_replayed():
+    """Decoding steps in a graph whose lengths grow, and a graph with another workspace beside it."""
+    w, dtype, q, p, q_start, k_len, q_lens, k_lens, front, table = _make("one_token_each", "e4m3", 8)
+    other = _make("blocks_group", "bf16", 8)
+    want_other = _run(*other[:2], *other[2:6], 0.1)
+    k_len[:] = torch.tensor([200, 1, 30, 64, 20, 900], dtype=torch.int32)
+    lengths = k_len.clone()
+    o, lse, ws = torch.empty_like(q), torch.empty(w.heads, w.n_q, device="cuda"), _ws(w, dtype, p)
+    o2, lse2, ws2 = torch.empty_like(other[2]), torch.empty(other[0].heads, other[0].n_q, device="cuda"), _ws(other[0], other[1], other[3])
+    graphs = [torch.cuda.CUDAGraph() for _ in range(2)]
+    with torch.cuda.graph(graphs[0]):
+        P.dfs_paged_attn_fwd(w, P.DFS_BF16, q, p, q_start, k_len, 0.1, o, lse, ws)
+        k_len.add_(1)
+    with torch.cuda.graph(graphs[1]):
+        P.dfs_paged_attn_fwd(other[0], P.DFS_BF16, *other[2:6], 0.1, o2, lse2, ws2)
+    n = sum(other[6])
+    for _ in range(4):
+        graphs[0].replay()
+        graphs[1].replay()
+        want = _run(w, dtype, q, p, q_start, lengths, 0.1)
+        lengths += 1
+        torch.cuda.synchronize()
+        assert torch.equal(o, want[0]) and torch.equal(lse, want[1])
+        a = slice(other[8], other[8] + n)
+        assert torch.equal(o2[:, a], want_other[0][:, a]) and torch.equal(lse2[:, a], want_other[1][:, a])
+
+
+def test_no_rows():
+    e = torch.empty(2, 0, 64, device="cuda")
+    p = P.Pages(torch.empty(0, 2, 16, 64, device="cuda"), torch.empty(0, 2, 16, 64, device="cuda"), torch.zeros(1, 0, dtype=torch.int32, device="cuda"))
+    start, length = torch.zeros(2, dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    P.dfs_paged_attn_fwd(P.Paged(1, 2, 2, 64, 0, -1, 0), P.DFS_F32, e, p, start, length, 0.1, torch.empty_like(e), None, None)
+    start[1] = 3                                     # a cache without pages: nothing is seen
+    length[0] = 5
+    q, o, lse = torch.randn(2, 3, 64, device="cuda"), torch.full((2, 3, 64), 3.0, device="cuda"), torch.zeros(2, 3, device="cuda")
+    w = P.Paged(1, 2, 2, 64, 3, -1, 0)
+    P.dfs_paged_attn_fwd(w, P.DFS_F32, q, p, start, length, 0.1, o, lse, _ws(w, "f32", p))
+    assert not o.any() and torch.isneginf(lse).all()
+
+
+def test_refusals_of_the_binding():
+    w, dtype, q, p, q_start, k_len, _, _, _, _ = _make("pieces", "e4m3")
+    o, lse = torch.zeros_like(q), torch.zeros(w.heads, w.n_q, device="cuda")
+    good = [w, P.DFS_BF16, q, p, q_start, k_len, 0.1, o, lse, _ws(w, dtype, p)]
+    pg = lambda **kw: P.Pages(**dict(dict(k=p.k, v=p.v, table=p.table, k_scale=p.k_scale, v_scale=p.v_scale), **kw))  # noqa: E731
+    for i, bad in ((2, q.float()), (2, q.cpu()), (2, q[1:]), (3, pg(k=p.k[:, 1:])), (3, pg(v=p.v[1:])), (3, pg(table=p.table[1:])), (3, pg(table=p.table.t())), (3, pg(k_scale=p.k_scale[1:])),
+                   (4, q_start[:-1]), (4, q_start.long()), (5, k_len[:-1]), (5, k_len.cpu()), (7, o.float()), (8, lse.double()), (8, lse[:1])):
+        args = list(good)
+        args[i] = bad
+        with pytest.raises(ValueError):
+            P.dfs_paged_attn_fwd(*args)
+    for i, bad in ((3, None), (3, pg(v_scale=None)), (3, pg(k=p.k[:, :, :48], v=p.v[:, :, :48])), (4, None), (5, None), (6, 0.0), (7, q), (9, None), (9, good[9][:-256])):
+        args = list(good)
+        args[i] = bad
+        with pytest.raises(P.DfsError):
+            P.dfs_paged_attn_fwd(*args)
+    assert not o.any() and not lse.any()
