@@ -1,0 +1,48 @@
+// What the kernels of attention over a cache in pages share: their arguments, and how a wave finds pages.
+#pragma once
+#include "pages.h"
+#include "window.h"
+
+namespace dfs {
+
+struct PagedArgs : WindowArgs {                      // n_k: what the table has room for
+  PageArgs pages;
+  int32_t unit;                                      // pieces that are dealt out together
+  int32_t least;                                     // units that a work-group takes at least
+};
+
+// Eight bytes of e4m3 times a power of two, exactly.
+__device__ __forceinline__ bf16x8 eight(uint32_t a, uint32_t b, float scale) {
+  const bf16x2 p = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, false), q = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, true);
+  const bf16x2 r = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, false), s = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, true);
+  return bf16x8{p[0], p[1], q[0], q[1], r[0], r[1], s[0], s[1]};
+}
+
+// The pages of a sequence, 64 entries of the table at a time, one a lane: page and scales.
+template <bool E4M3> struct Entries {
+  int first, id;
+  float ks, vs;
+  const int32_t* row;
+  __device__ __forceinline__ Entries(const PagedArgs& a, int s) : first(-(1 << 30)), id(0), ks(0.f), vs(0.f), row(a.pages.table + int64_t(s) * a.pages.row) {}
+  // Lane that holds entry i.
+  __device__ __forceinline__ int lane_of(const PagedArgs& a, int i, int kvh) {
+    if (uint32_t(i - first) >= 64u) {
+      first = i;
+      const int lane = threadIdx.x & 63;
+      id = row[min_of(i + lane, a.pages.row - 1)];
+      if (uint32_t(id) >= uint32_t(a.pages.pages)) id = 0;
+      if constexpr (E4M3) {
+        const int64_t at = int64_t(id) * a.pages.heads_kv + kvh;
+        ks = a.pages.k_scale[at];
+        vs = a.pages.v_scale[at];
+      }
+    }
+    return i - first;
+  }
+};
+
+// Whether the rows are so many that blocks of 128 of them, each over all its keys, fill the chip, and the launch of these.
+bool paged_is_long(const dfs_paged* w);
+int run_paged_long(const PagedArgs& a, int d, int dtype, bool bytes, hipStream_t st);
+
+}  // namespace dfs

@@ -10,16 +10,9 @@
 #include <float.h>
 #include <math.h>
 
-#include "pages.h"
-#include "window.h"
+#include "paged.h"
 
 namespace dfs {
-
-struct PagedArgs : WindowArgs {                      // n_k: what the table has room for
-  PageArgs pages;
-  int32_t unit;                                      // pieces that are dealt out together
-  int32_t least;                                     // units that a work-group takes at least
-};
 
 constexpr int GROUPS = 512;                          // work-groups: two a CU
 
@@ -71,35 +64,6 @@ template <typename T, int D, bool E4M3> struct PageTile {
   template <bool COLUMNS> static __device__ __forceinline__ uint32_t offset(int j, int lane, int64_t stride) {
     const int p = j * 64 + lane, row = p / CH;
     return uint32_t(row) * uint32_t(stride) + uint32_t((p % CH ^ swizzle<COLUMNS>(row)) * 16);
-  }
-};
-
-__device__ __forceinline__ bf16x8 eight(uint32_t a, uint32_t b, float scale) {
-  const bf16x2 p = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, false), q = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, true);
-  const bf16x2 r = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, false), s = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, true);
-  return bf16x8{p[0], p[1], q[0], q[1], r[0], r[1], s[0], s[1]};
-}
-
-// The pages of a sequence, 64 entries of the table at a time, one a lane: page and scales.
-template <bool E4M3> struct Entries {
-  int first, id;
-  float ks, vs;
-  const int32_t* row;
-  __device__ __forceinline__ Entries(const PagedArgs& a, int s) : first(-(1 << 30)), id(0), ks(0.f), vs(0.f), row(a.pages.table + int64_t(s) * a.pages.row) {}
-  // Lane that holds entry i.
-  __device__ __forceinline__ int lane_of(const PagedArgs& a, int i, int kvh) {
-    if (uint32_t(i - first) >= 64u) {
-      first = i;
-      const int lane = threadIdx.x & 63;
-      id = row[min_of(i + lane, a.pages.row - 1)];
-      if (uint32_t(id) >= uint32_t(a.pages.pages)) id = 0;
-      if constexpr (E4M3) {
-        const int64_t at = int64_t(id) * a.pages.heads_kv + kvh;
-        ks = a.pages.k_scale[at];
-        vs = a.pages.v_scale[at];
-      }
-    }
-    return i - first;
   }
 };
 
@@ -166,13 +130,14 @@ __global__ void __launch_bounds__((64 * paged_waves<T, D, E4M3>()), (E4M3 || D *
       const bool front = values && t >= span.n_first && key < lo;         // values that no row sees must not be read: they may be anything
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
-        const int k0 = key + 16 * half, there = min_of(last - k0, 16);
+        const int k0 = key + 16 * half, there = front && k0 + 15 < lo && k0 >= a.sinks ? 0 : min_of(last - k0, 16);
         const int l = there > 0 ? entries.lane_of(a, k0 >> a.pages.bits, kvh) : 0, id = there > 0 ? __builtin_amdgcn_readlane(entries.id, l) : 0;
         const uint64_t from = reinterpret_cast<uint64_t>(v.at(id, kvh, k0 & ((1 << a.pages.bits) - 1)));
         const uint32_t bytes = there > 0 ? uint32_t(there - 1) * uint32_t(v.row) + PT::RB : 0;
         const u32x4 desc = {uint32_t(__builtin_amdgcn_readfirstlane(uint32_t(from))), uint32_t(__builtin_amdgcn_readfirstlane(uint32_t(from >> 32))) & 0xFFFFu,
                             uint32_t(__builtin_amdgcn_readfirstlane(bytes)), 0x00020000u};
-        if constexpr (E4M3) (values ? v_scale : k_scale)[parity][half] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(values ? entries.vs : entries.ks), l));
+        if constexpr (E4M3)
+          (values ? v_scale : k_scale)[parity][half] = there > 0 ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(values ? entries.vs : entries.ks), l)) : 1.f;
         const uint32_t to = __builtin_amdgcn_readfirstlane(lds + uint32_t((parity * 2 + values) * BYTES + half * (BYTES / 2)));
 #pragma unroll
         for (int j = 0; j < LOADS / 2; ++j) {
@@ -431,7 +396,7 @@ size_t dfs_paged_workspace_bytes(const dfs_paged* w, int dtype, const dfs_pages*
   const char* call = "dfs_paged_workspace_bytes";
   PageArgs p;
   if (check_paged(call, w, dtype) != DFS_OK || check_pages(call, pages, dtype, w->seqs, w->heads_kv, w->d, false, &p) != DFS_OK) return 0;
-  if (w->seqs == 0 || w->n_q == 0) return 0;
+  if (w->seqs == 0 || w->n_q == 0 || paged_is_long(w)) return 0;
   return part_bytes(w) + size_t(GROUPS) * 2 * 32 * sizeof(float2);
 }
 
@@ -448,8 +413,8 @@ int dfs_paged_attn_fwd(const dfs_paged* w, int dtype, const dfs_view* q, const d
   if ((rc = check_view(call, "o", o, dtype, 1, w->heads, w->n_q, w->d, true, &a.o))) return rc;
   if ((rc = check_pages(call, pages, dtype, w->seqs, w->heads_kv, w->d, false, &a.pages))) return rc;
   if (w->seqs == 0 || w->n_q == 0) return DFS_OK;
-  const size_t need = part_bytes(w) + size_t(GROUPS) * 2 * 32 * sizeof(float2);
-  if (!ws || (uintptr_t(ws) & 255) || ws_bytes < need)
+  const size_t need = paged_is_long(w) ? 0 : part_bytes(w) + size_t(GROUPS) * 2 * 32 * sizeof(float2);
+  if (need && (!ws || (uintptr_t(ws) & 255) || ws_bytes < need))
     return fail(DFS_EWORKSPACE, "%s: workspace of %zu bytes needed (256-byte aligned), got %zu", call, need, ws_bytes);
   if ((rc = check_apart(call, {{"o", &a.o}}, {{"q", &a.q}, {"pages.k", &a.pages.k}, {"pages.v", &a.pages.v}}))) return rc;
   a.lse = lse;
@@ -487,6 +452,7 @@ int dfs_paged_attn_fwd(const dfs_paged* w, int dtype, const dfs_view* q, const d
   };
   auto join = [&](auto t, auto d) { paged_join_kernel<decltype(t), decltype(d)::value><<<joins, 256, 0, st>>>(a); };
   auto by_dim = [&](auto f) { w->d == 64 ? f(std::integral_constant<int, 64>{}) : f(std::integral_constant<int, 128>{}); };
+  if (paged_is_long(w)) return run_paged_long(a, w->d, dtype, bytes, st);
   by_dim([&](auto d) {
     if (dtype == DFS_F32) run(float{}, d, std::false_type{});
     else if (bytes) run(uint16_t{}, d, std::true_type{});

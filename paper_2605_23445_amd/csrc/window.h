@@ -169,8 +169,10 @@ __device__ __forceinline__ int rows_of(const WindowArgs& a, const Lengths& len, 
 
 // The sequence that block i of a key head lies in: its lengths, its first rows in the tensors, which of its blocks this is (blk), and a number for it that no other
 // block of the key head has (slot).  U: rows of a block, of queries (of all heads that share the key head) or of keys.
-template <bool PACKED> struct Seq;
-template <> struct Seq<false> {
+// KIND: sequences of one length, packed ones, or packed rows over a cache in pages, whose lengths are in k_len.
+enum { PADDED = 0, PACKED_ROWS = 1, IN_PAGES = 2 };
+template <int KIND> struct Seq;
+template <> struct Seq<PADDED> {
   static constexpr int q0 = 0, k0 = 0;
   static constexpr bool real = true;
   int blk, slot;
@@ -180,12 +182,16 @@ template <> struct Seq<false> {
 
 // Packed: how many blocks a sequence has is known on the device alone.  Sequence s has room for those from start[s] * group / U + s on, counted down to whole ones, so that
 // no sum over the sequences in front of it is needed; a block between its last and the next one's room is not real.  Up to 64 sequences are looked at by a wave's
-// lanes at once, and their blocks can be had in another order (`long_first`): all sequences' blocks number x before those number x - 1, or of keys, counted from
-// the last, so that under a causal mask those come first that see most.
-template <> struct Seq<true> {
-  int blk, slot, q0, k0;
+// lanes at once, and their blocks can be had in another order (`long_first`): those come first that see most under a causal mask, blocks of rows by their last position,
+// blocks of keys by how many are behind them.
+template <int KIND> struct Seq {
+  int seq, blk, slot, q0, k0;                        // which sequence; the first rows of its queries and keys
   bool real;
   Lengths len;
+  static __device__ __forceinline__ int keys_of(const WindowArgs& a, int s) {
+    if (KIND == IN_PAGES) return max_of(0, min_of(a.k_len[s], a.n_k));
+    return max_of(0, start_of(a.k_start, s + 1, a.n_k) - start_of(a.k_start, s, a.n_k));
+  }
   template <int U, bool KEYS> static __device__ __forceinline__ Seq of(const WindowArgs& a, int, int i, bool long_first) {
     const int lane = threadIdx.x & 63, per = KEYS ? 1 : a.group, most = KEYS ? a.n_k : a.n_q;
     const int32_t* start = KEYS ? a.k_start : a.q_start;
@@ -194,20 +200,24 @@ template <> struct Seq<true> {
     if (a.packed <= 64 && long_first) {
       const int mine = min_of(lane, a.packed - 1), from = start_of(start, mine, most), to = start_of(start, mine + 1, most);
       const int n = lane < a.packed && to > from ? int(uint32_t((to - from) * per + U - 1) / U) : 0;
+      // a sequence's blocks have the numbers base .. base + n - 1; those of the largest number come first
+      const int base = KEYS ? 0 : int(int64_t(max_of(0, keys_of(a, mine) - (to - from))) * per / U);
       int lo = 0, hi = 1;                            // the blocks number lo and more are more than i, those number hi and more are not
       r.real = wave_sum(n) > i;
       if (!r.real) return r;
-      while (__builtin_amdgcn_ballot_w64(n > hi)) hi *= 2;
+      while (__builtin_amdgcn_ballot_w64(n > 0 && base + n > hi)) hi *= 2;
+      auto from_number = [&](int x) { return wave_sum(n == 0 ? 0 : min_of(n, max_of(0, base + n - x))); };
       while (hi - lo > 1) {
-        const int mid = (lo + hi) / 2, more = wave_sum(max_of(0, n - mid));
-        if (more > i) lo = mid;
+        const int mid = lo + (hi - lo) / 2;
+        if (from_number(mid) > i) lo = mid;
         else hi = mid;
       }
-      const int place = i - wave_sum(max_of(0, n - lo - 1));               // among the sequences that have a block number lo
-      const uint64_t have = __builtin_amdgcn_ballot_w64(n > lo);
+      const int place = i - from_number(lo + 1);     // among the sequences that have a block number lo
+      const bool has = n > 0 && base <= lo && lo < base + n;
+      const uint64_t have = __builtin_amdgcn_ballot_w64(has);
       const int before = __builtin_amdgcn_mbcnt_hi(uint32_t(have >> 32), __builtin_amdgcn_mbcnt_lo(uint32_t(have), 0));
-      s = __builtin_ctzll(__builtin_amdgcn_ballot_w64(n > lo && before == place));
-      r.blk = KEYS ? __builtin_amdgcn_readlane(n, s) - 1 - lo : lo;
+      s = __builtin_ctzll(__builtin_amdgcn_ballot_w64(has && before == place));
+      r.blk = KEYS ? __builtin_amdgcn_readlane(n, s) - 1 - lo : lo - __builtin_amdgcn_readlane(base, s);
     } else {
       s = run_of(a.packed, i, [&](int x) { return int(uint32_t(start_of(start, x, most) * per) / U) + x; });
       r.real = s >= 0;
@@ -216,14 +226,15 @@ template <> struct Seq<true> {
       r.real = r.blk >= 0;                           // not where the starts go down
     }
     s = __builtin_amdgcn_readfirstlane(s);
+    r.seq = s;
     r.q0 = start_of(a.q_start, s, a.n_q);
-    r.k0 = start_of(a.k_start, s, a.n_k);
-    r.len = Lengths(max_of(0, start_of(a.q_start, s + 1, a.n_q) - r.q0), max_of(0, start_of(a.k_start, s + 1, a.n_k) - r.k0));
+    r.k0 = KIND == IN_PAGES ? 0 : start_of(a.k_start, s, a.n_k);
+    r.len = Lengths(max_of(0, start_of(a.q_start, s + 1, a.n_q) - r.q0), keys_of(a, s));
     r.slot = int(uint32_t((KEYS ? r.k0 : r.q0) * per) / U) + s + r.blk;
     return r;
   }
 };
-template <bool PACKED> using PlaceOf = typename std::conditional<PACKED, PackedPlace, Place>::type;
+template <int KIND> using PlaceOf = typename std::conditional<KIND != PADDED, PackedPlace, Place>::type;
 
 // What a lane of a block of rows knows of its row.
 struct Row {

@@ -14,11 +14,29 @@ namespace dfs {
 
 constexpr int KN = 64;                               // keys of a tile
 
+// How tiles of 64 keys and values come to LDS: rows of tensors, straight.
+template <typename T, int D> struct RowFeed {
+  static constexpr int STEP = 1;                     // what a window's first piece begins at a multiple of
+  static constexpr bool STRAIGHT = true;
+  using KLoader = typename Tile<T, D, KN, 4, false>::Loader;
+  using VLoader = typename Tile<T, D, KN, 4, true>::Loader;
+  const char *kh, *vh;
+  int64_t k_row, v_row;
+  KLoader k_load;
+  VLoader v_load;
+  template <class P, class S> __device__ __forceinline__ RowFeed(const WindowArgs& a, const P& at, const S& seq, int wave, int lane)
+      : kh(a.k.at(at.b, at.kvh, seq.k0)), vh(a.v.at(at.b, at.kvh, seq.k0)), k_row(a.k.row), v_row(a.v.row), k_load(a.k.row, wave, lane), v_load(a.v.row, wave, lane) {}
+  __device__ __forceinline__ typename KLoader::Pair keys(const Span& span, int t) { return k_load.of(span, kh, k_row, t); }
+  __device__ __forceinline__ typename VLoader::Pair values(const Span& span, int t) { return v_load.of(span, vh, v_row, t); }
+  __device__ __forceinline__ void ask_keys(const typename KLoader::Pair& p, uint32_t to, int j) const { k_load.issue_one(p, to, j); }
+  __device__ __forceinline__ void ask_values(const typename VLoader::Pair& p, uint32_t to, int j) const { v_load.issue_one(p, to, j); }
+};
+
 // f32: one step per tile of 64 keys, bound by the fp32 matrix instructions and by what their waves wait for in between, one thing after the other in two
 // work-groups a CU at d = 64 and in one, which fills the LDS, at d = 128: 4 000 tokens x 16 heads, 1 000 keys each way, d = 64: 323 to 340 us, 85 to 89 TFLOP/s,
 // matrix cores busy 60 % of the cycles; d = 128: 755 us, 76 TFLOP/s, 52 % (a large fp32 product of a library: 154).
-template <int D, bool PACKED>
-__global__ void __launch_bounds__(256) window_f32_kernel(WindowArgs a) {
+template <int D, int KIND, class Feed = RowFeed<float, D>, class Args = WindowArgs>
+__global__ void __launch_bounds__(256) window_f32_kernel(Args a) {
   using T = float;
   constexpr int NW = 4, BM = 32 * NW;
   using KTile = Tile<T, D, KN, NW, false>;
@@ -28,14 +46,14 @@ __global__ void __launch_bounds__(256) window_f32_kernel(WindowArgs a) {
   const uint32_t lds = uint32_t(reinterpret_cast<uintptr_t>((LDS_PTR(void))(tiles)));
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
-  const PlaceOf<PACKED> at(a, blockIdx.x);
-  const auto seq = Seq<PACKED>::template of<BM, false>(a, at.b, at.blk, true);
+  const PlaceOf<KIND> at(a, blockIdx.x);
+  const auto seq = Seq<KIND>::template of<BM, false>(a, at.b, at.blk, true);
   if (!seq.real) return;
   const Lengths& len = seq.len;
   const int r0 = seq.blk * BM, rows = rows_of(a, len, r0, BM);
   if (rows <= 0) return;
   const Row row(a, at, len, r0, rows, wave * 32 + (lane & 31), lane);
-  const Span span(a, row.i0 + len.shift, row.i1 + len.shift, len.k);
+  const Span span(a, row.i0 + len.shift, row.i1 + len.shift, len.k, Feed::STEP);
   const int n_tiles = (span.n + 1) / 2;
   typename Mat<T>::Frag qf[STEPS];
   {
@@ -43,20 +61,18 @@ __global__ void __launch_bounds__(256) window_f32_kernel(WindowArgs a) {
 #pragma unroll
     for (int s = 0; s < STEPS; ++s) qf[s] = *reinterpret_cast<const typename Mat<T>::Frag*>(qp + (2 * s + row.h) * 16);
   }
-  const char *kh = a.k.at(at.b, at.kvh, seq.k0), *vh = a.v.at(at.b, at.kvh, seq.k0);
-  const typename KTile::Loader k_load(a.k.row, wave, lane);
-  const typename VTile::Loader v_load(a.v.row, wave, lane);
+  Feed feed(a, at, seq, wave, lane);
   const typename KTile::RowReader k_read(lane);
   const typename VTile::ColumnReader v_read(lane);
   const uint32_t to = __builtin_amdgcn_readfirstlane(lds + uint32_t(wave) * 1024);
   auto issue = [&](int t) {
     const uint32_t buf = to + uint32_t((t & 1) * 2 * KTile::BYTES);
-    const auto ks = k_load.of(span, kh, a.k.row, t);
-    const auto vs = v_load.of(span, vh, a.v.row, t);
+    const auto ks = feed.keys(span, t);
+    const auto vs = feed.values(span, t);
 #pragma unroll
-    for (int j = 0; j < KTile::LOADS; ++j) k_load.issue_one(ks, buf, j);
+    for (int j = 0; j < KTile::LOADS; ++j) feed.ask_keys(ks, buf, j);
 #pragma unroll
-    for (int j = 0; j < KTile::LOADS; ++j) v_load.issue_one(vs, buf + KTile::BYTES, j);
+    for (int j = 0; j < KTile::LOADS; ++j) feed.ask_values(vs, buf + KTile::BYTES, j);
   };
 
   f32x16 acc[D / 32];
@@ -123,8 +139,8 @@ __global__ void __launch_bounds__(256) window_f32_kernel(WindowArgs a) {
 // Bound by the matrix cores and the vector port beside them.  d = 128: 75 600 tokens x 40 heads, 3 600 keys each way: 9.6 ms, 1 133 TFLOP/s, matrix cores
 // busy 65 % of the cycles at 1.67 GHz; 2 x 8 192 x 32 heads of 8 key heads, 1 024 keys back: 298 us, 868 TFLOP/s, 45 %: a block meets 17 tiles, and its start,
 // the first tiles' way and the end are a part of its time.  d = 64: 17 550 x 30, 1 350 each way: 433 us, 813 TFLOP/s, 43 %.
-template <int D, bool PACKED>
-__global__ void __launch_bounds__(256, 2) window_pipe_kernel(WindowArgs a) {
+template <int D, int KIND, class Feed = RowFeed<uint16_t, D>, class Args = WindowArgs>
+__global__ void __launch_bounds__(256, 2) window_pipe_kernel(Args a) {
   constexpr int NW = 4, BM = 32 * NW;
   using KTile = Tile<uint16_t, D, KN, NW, false>;
   using VTile = Tile<uint16_t, D, KN, NW, true>;
@@ -135,29 +151,38 @@ __global__ void __launch_bounds__(256, 2) window_pipe_kernel(WindowArgs a) {
   const uint32_t lds = uint32_t(reinterpret_cast<uintptr_t>((LDS_PTR(void))(tiles)));
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
 
-  const PlaceOf<PACKED> at(a, blockIdx.x);
-  const auto seq = Seq<PACKED>::template of<BM, false>(a, at.b, at.blk, true);
+  const PlaceOf<KIND> at(a, blockIdx.x);
+  const auto seq = Seq<KIND>::template of<BM, false>(a, at.b, at.blk, true);
   if (!seq.real) return;
   const Lengths& len = seq.len;
   const int r0 = seq.blk * BM, rows = rows_of(a, len, r0, BM);
   if (rows <= 0) return;
   const Row row(a, at, len, r0, rows, wave * 32 + (lane & 31), lane);
-  const Span span(a, row.i0 + len.shift, row.i1 + len.shift, len.k);
+  const Span span(a, row.i0 + len.shift, row.i1 + len.shift, len.k, Feed::STEP);
   const int n_tiles = (span.n + 1) / 2;
 
-  const char *kh = a.k.at(at.b, at.kvh, seq.k0), *vh = a.v.at(at.b, at.kvh, seq.k0);
-  const typename KTile::Loader k_load(a.k.row, wave, lane);
-  const typename VTile::Loader v_load(a.v.row, wave, lane);
+  Feed feed(a, at, seq, wave, lane);
   const uint32_t to = __builtin_amdgcn_readfirstlane(lds + uint32_t(wave) * 1024);
-  if (n_tiles > 0) {
-    const auto k0 = k_load.of(span, kh, a.k.row, 0), k1 = k_load.of(span, kh, a.k.row, 1);
-    const auto v0 = v_load.of(span, vh, a.v.row, 0);
+  if constexpr (Feed::STRAIGHT) {
+    if (n_tiles > 0) {
+      const auto k0 = feed.keys(span, 0), k1 = feed.keys(span, 1);
+      const auto v0 = feed.values(span, 0);
 #pragma unroll
-    for (int j = 0; j < LOADS; ++j) k_load.issue_one(k0, to, j);
+      for (int j = 0; j < LOADS; ++j) feed.ask_keys(k0, to, j);
 #pragma unroll
-    for (int j = 0; j < LOADS; ++j) v_load.issue_one(v0, to + 2 * BYTES, j);
+      for (int j = 0; j < LOADS; ++j) feed.ask_values(v0, to + 2 * BYTES, j);
 #pragma unroll
-    for (int j = 0; j < LOADS; ++j) k_load.issue_one(k1, to + BYTES, j);
+      for (int j = 0; j < LOADS; ++j) feed.ask_keys(k1, to + BYTES, j);
+    }
+  } else if (n_tiles > 0) {                          // through registers: two tiles of keys and one of values put, the next ones on their way
+    feed.ask_keys(span, 0);
+    feed.ask_values(span, 0);
+    feed.put_keys(lds);
+    feed.put_values(lds + 2 * BYTES);
+    feed.ask_keys(span, 1);
+    feed.ask_values(span, 1);
+    feed.put_keys(lds + BYTES);
+    feed.ask_keys(span, 2);
   }
   bf16x8 qf[STEPS];
   {
@@ -267,7 +292,7 @@ __global__ void __launch_bounds__(256, 2) window_pipe_kernel(WindowArgs a) {
   int k_step = BYTES, v_step = BYTES;                // to the other buffer of keys, of values
   if (n_tiles > 0) {
     // the logits of tile 0 and the weights of its first half
-    wait_loads();
+    if constexpr (Feed::STRAIGHT) wait_loads();
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < 16; ++i) s0[i] = s1[i] = 0.f;
@@ -284,27 +309,42 @@ __global__ void __launch_bounds__(256, 2) window_pipe_kernel(WindowArgs a) {
   }
   // Tile t's values and tile t + 1's keys: s1 holds the logits of tile t's second half, w0 the weights of its first.
   for (int t = 0; t + 1 < n_tiles; ++t) {
-    wait_loads();                                    // this wave's parts of K(t + 1) and V(t) are there
+    if constexpr (Feed::STRAIGHT) wait_loads();      // this wave's parts of K(t + 1) and V(t) are there
     __syncthreads();                                 // all parts are, and every wave has left K(t) and V(t - 1)
     const int t2 = t + 2 < n_tiles ? t + 2 : t + 1;  // behind the last tile that once more, into a buffer that nothing reads
-    const auto ks = k_load.of(span, kh, a.k.row, t2);
-    const auto vs = v_load.of(span, vh, a.v.row, t + 1);
-    const uint32_t k_to = to + (t & 1 ? BYTES : 0), v_to = to + (t & 1 ? 2 : 3) * BYTES;
+    const uint32_t k_to = t & 1 ? BYTES : 0, v_to = (t & 1 ? 2 : 3) * BYTES;
+    const auto ks = [&] { if constexpr (Feed::STRAIGHT) return feed.keys(span, t2); else return 0; }();
+    const auto vs = [&] { if constexpr (Feed::STRAIGHT) return feed.values(span, t + 1); else return 0; }();
 #pragma unroll
     for (int s = 0; s < STEPS; ++s) k_at[s] += k_step;
     k_step = -k_step;
     float sum;
     stage(std::integral_constant<int, 0>{}, w0, s0, s1, w1, sum, [&](int f) {
-      constexpr int NF = 2 * STEPS;
+      if constexpr (Feed::STRAIGHT) {
+        constexpr int NF = 2 * STEPS;
 #pragma unroll
-      for (int j = f * 2 * LOADS / NF; j < (f + 1) * 2 * LOADS / NF; ++j) {
-        if (j < LOADS) v_load.issue_one(vs, v_to, j);
-        else k_load.issue_one(ks, k_to, j - LOADS);
+        for (int j = f * 2 * LOADS / NF; j < (f + 1) * 2 * LOADS / NF; ++j) {
+          if (j < LOADS) feed.ask_values(vs, to + v_to, j);
+          else feed.ask_keys(ks, to + k_to, j - LOADS);
+        }
       }
     });
     settle(s1, w1, sum);
     mask(2 * t + 2, s0);
-    stage(std::integral_constant<int, 1>{}, w1, s1, s0, w0, sum, [](int) {});
+    stage(std::integral_constant<int, 1>{}, w1, s1, s0, w0, sum, [&](int f) {
+      if constexpr (!Feed::STRAIGHT) {               // V(t + 1) and K(t + 2) to LDS, a load's share at a time
+        constexpr int NF = 2 * STEPS, SHARES = 2 * Feed::SHARES;
+        if (f % (NF / SHARES) == 0) {
+          const int j = f / (NF / SHARES);
+          if (j < Feed::SHARES) feed.put_values(lds + v_to, j);
+          else feed.put_keys(lds + k_to, j - Feed::SHARES);
+        }
+      }
+    });
+    if constexpr (!Feed::STRAIGHT) {
+      feed.ask_values(span, t + 2);
+      feed.ask_keys(span, t + 3);
+    }
     settle(s0, w0, sum);
     mask(2 * t + 3, s1);
 #pragma unroll
@@ -314,7 +354,7 @@ __global__ void __launch_bounds__(256, 2) window_pipe_kernel(WindowArgs a) {
     v_step = -v_step;
   }
   if (n_tiles > 0) {
-    wait_loads();
+    if constexpr (Feed::STRAIGHT) wait_loads();
     __syncthreads();
     v_read.mma(0, 0, w0, acc);
     float sum;
