@@ -14,15 +14,17 @@
 
 namespace dfs {
 
-constexpr int GROUPS = 512;                          // work-groups: two a CU
+constexpr int GROUPS = 256;                          // work-groups: one a CU
 
 // A sequence's rows and keys, its blocks of 32 rows, and the units of each of these with each key head (the pieces of all its rows together, one at least).
 struct PagedSeq {
   int q0, n, k, blocks, units;
-  __device__ __forceinline__ PagedSeq(const PagedArgs& a, int s) {
-    q0 = start_of(a.q_start, s, a.n_q);
-    n = max_of(0, start_of(a.q_start, s + 1, a.n_q) - q0);
-    k = max_of(0, min_of(a.k_len[s], a.n_k));
+  PagedSeq() = default;
+  __device__ __forceinline__ PagedSeq(const PagedArgs& a, int s) : PagedSeq(a, start_of(a.q_start, s, a.n_q), start_of(a.q_start, s + 1, a.n_q), a.k_len[s]) {}
+  __device__ __forceinline__ PagedSeq(const PagedArgs& a, int from, int to, int k_) {
+    q0 = from;
+    n = max_of(0, to - from);
+    k = max_of(0, min_of(k_, a.n_k));
     blocks = (n * a.group + 31) / 32;
     const Span all(a, k - n, k - 1, k, 32);
     units = max_of(1, (all.n + a.unit - 1) / a.unit);
@@ -33,10 +35,14 @@ struct PagedSeq {
 // Units of all sequences in front of each, as a work-group's threads work them out: thread t adds up `each` sequences from t * each on.
 template <int NT> struct Deal {
   int each, mine, before, total, per;                // a thread's sum, the sum in front of it, all, and a work-group's share
+  PagedSeq last;                                     // a thread's last sequence, which is its only one where there are up to NT
   __device__ __forceinline__ Deal(const PagedArgs& a, int (&sums)[NT / 64]) {
     each = (a.packed + NT - 1) / NT;
     mine = 0;
-    for (int i = 0, s = threadIdx.x * each; i < each && s < a.packed; ++i, ++s) mine += PagedSeq(a, s).work(a);
+    for (int i = 0, s = threadIdx.x * each; i < each && s < a.packed; ++i, ++s) {
+      last = PagedSeq(a, s);
+      mine += last.work(a);
+    }
     const int upto = wave_sums(mine), wave = threadIdx.x >> 6;
     if ((threadIdx.x & 63) == 63) sums[wave] = upto;
     __syncthreads();
@@ -67,17 +73,18 @@ template <typename T, int D, bool E4M3> struct PageTile {
   }
 };
 
-template <typename T, int D, bool E4M3> constexpr int paged_waves() { return sizeof(T) == 4 && D == 128 ? 2 : 4; }
+// Waves of a work-group: as many as have room in LDS for two tiles of keys and two of values each.
+template <typename T, int D, bool E4M3> constexpr int paged_waves() { return 1024 / (D * (E4M3 ? 1 : int(sizeof(T)))) < 8 ? 1024 / (D * (E4M3 ? 1 : int(sizeof(T)))) : 8; }
 
-template <typename T, int D, bool E4M3, bool ONCE>
-__global__ void __launch_bounds__((64 * paged_waves<T, D, E4M3>()), (E4M3 || D * sizeof(T) <= 128 ? 2 : 1)) paged_split_kernel(PagedArgs a) {
+template <typename T, int D, bool E4M3, bool SMALL>
+__global__ void __launch_bounds__((64 * paged_waves<T, D, E4M3>()), 1) paged_split_kernel(PagedArgs a) {
   constexpr int NW = paged_waves<T, D, E4M3>(), NT = 64 * NW, REGS = D / 2;
   using PT = PageTile<T, D, E4M3>;
   constexpr int LOADS = PT::LOADS, STEPS = D * int(sizeof(T)) / 32, BYTES = PT::BYTES;
   static_assert(REGS * 64 * 4 <= 4 * BYTES || !E4M3, "a wave's sums fit where its tiles were");
   __shared__ __attribute__((aligned(1024))) char tiles[NW * 4 * BYTES];
   __shared__ float s_m[NW][32], s_l[NW][32];
-  __shared__ int s_sums[NW], s_seq, s_off;
+  __shared__ int s_sums[NW], s_first[5];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 31, h = lane >> 5;
   const uint32_t lds = uint32_t(reinterpret_cast<uintptr_t>((LDS_PTR(void))(tiles))) + uint32_t(wave * 4 * BYTES);
 
@@ -85,33 +92,42 @@ __global__ void __launch_bounds__((64 * paged_waves<T, D, E4M3>()), (E4M3 || D *
   int at = blockIdx.x * deal.per;
   const int end = min_of(deal.total, at + deal.per), start = at;
   if (at >= end) return;
-  if (threadIdx.x == 0) s_seq = a.packed;            // nobody's: where starts fall so far that the units of all pass 31 bits
+  if (threadIdx.x == 0) s_first[0] = a.packed;       // nobody's: where starts fall so far that the units of all pass 31 bits
   __syncthreads();
   if (deal.before <= at && at < deal.before + deal.mine) {
     int s = threadIdx.x * deal.each, off = at - deal.before;
-    for (; s < a.packed; ++s) {
-      const int w = PagedSeq(a, s).work(a);
-      if (off < w) break;
-      off -= w;
-    }
-    s_seq = s;
-    s_off = off;
+    PagedSeq x = deal.last;
+    if (deal.each > 1)
+      for (; s < a.packed; ++s) {
+        x = PagedSeq(a, s);
+        const int w = x.work(a);
+        if (off < w) break;
+        off -= w;
+      }
+    s_first[0] = s;
+    s_first[1] = off;
+    s_first[2] = x.q0;
+    s_first[3] = x.n;
+    s_first[4] = x.k;
   }
   __syncthreads();
-  int s = __builtin_amdgcn_readfirstlane(s_seq), off = __builtin_amdgcn_readfirstlane(s_off);
+  auto first = [&](int i) { return __builtin_amdgcn_readfirstlane(s_first[i]); };
+  int s = first(0), off = first(1);
+  if (s >= a.packed) return;
+  PagedSeq seq(a, first(2), first(2) + first(3), first(4));
 
-  uint32_t k_off[LOADS / 2], v_off[LOADS / 2];
+  uint32_t k_off[LOADS], v_off[LOADS];
 #pragma unroll
-  for (int j = 0; j < LOADS / 2; ++j) {
+  for (int j = 0; j < LOADS; ++j) {
     k_off[j] = PT::template offset<false>(j, lane, a.pages.k.row);
     v_off[j] = PT::template offset<true>(j, lane, a.pages.v.row);
   }
   const float c2 = a.scale * LOG2E;
-  while (at < end && s < a.packed) {
-    const PagedSeq seq(a, s);
-    if (off >= seq.work(a)) {                        // sequences without rows
-      ++s;
+  while (at < end) {
+    if (off >= seq.work(a)) {
+      if (++s >= a.packed) return;
       off = 0;
+      seq = PagedSeq(a, s);
       continue;
     }
     const int item = off / seq.units, u0 = off - item * seq.units, u1 = min_of(seq.units, u0 + end - at), blk = item / a.heads_kv, kvh = item - blk * a.heads_kv;
@@ -123,36 +139,53 @@ __global__ void __launch_bounds__((64 * paged_waves<T, D, E4M3>()), (E4M3 || D *
     const int qi = real ? query_of(a, r0 + n) : i0, qh = kvh * a.group + (real ? r0 + n - qi * a.group : 0), p = qi + shift;
 
     Entries<E4M3> entries(a, s);
-    float k_scale[2][2], v_scale[2][2];              // of both halves of the two pieces that are on their way
-    // Asks for a piece's keys or values.  Behind the last one nothing is asked for, by as many loads, so that the waits count the same.
-    auto ask = [&](const View& v, const uint32_t (&offs)[LOADS / 2], int t, int parity, bool values) __attribute__((always_inline)) {
-      const int key = span.begin(t), last = t < t_end ? span.end(t) : 0;
-      const bool front = values && t >= span.n_first && key < lo;         // values that no row sees must not be read: they may be anything
+    // Where a piece lies: on one page, or with pages of 16 rows on two.
+    constexpr int H = SMALL ? 2 : 1, RPH = 32 / H;
+    uint64_t k_at[H], v_at[H];
+    int there[H], key = 0;
+    float k_scale[2][H], v_scale[2][H];              // of the two pieces that are on their way
+    auto locate = [&](int t, int parity) __attribute__((always_inline)) {
+      key = span.begin(t);
+      const int last = t < t_end ? span.end(t) : 0;
 #pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        const int k0 = key + 16 * half, there = front && k0 + 15 < lo && k0 >= a.sinks ? 0 : min_of(last - k0, 16);
-        const int l = there > 0 ? entries.lane_of(a, k0 >> a.pages.bits, kvh) : 0, id = there > 0 ? __builtin_amdgcn_readlane(entries.id, l) : 0;
-        const uint64_t from = reinterpret_cast<uint64_t>(v.at(id, kvh, k0 & ((1 << a.pages.bits) - 1)));
-        const uint32_t bytes = there > 0 ? uint32_t(there - 1) * uint32_t(v.row) + PT::RB : 0;
-        const u32x4 desc = {uint32_t(__builtin_amdgcn_readfirstlane(uint32_t(from))), uint32_t(__builtin_amdgcn_readfirstlane(uint32_t(from >> 32))) & 0xFFFFu,
-                            uint32_t(__builtin_amdgcn_readfirstlane(bytes)), 0x00020000u};
-        if constexpr (E4M3)
-          (values ? v_scale : k_scale)[parity][half] = there > 0 ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(values ? entries.vs : entries.ks), l)) : 1.f;
-        const uint32_t to = __builtin_amdgcn_readfirstlane(lds + uint32_t((parity * 2 + values) * BYTES + half * (BYTES / 2)));
-#pragma unroll
-        for (int j = 0; j < LOADS / 2; ++j) {
-          uint32_t o = offs[j];
-          if (front) {
-            const int k = k0 + (j * 64 + lane) / PT::CH;
-            if (k < lo && k >= a.sinks) o = 0x80000000u;
-          }
-          if (ONCE)
-            asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen nt lds" ::"s"(to), "v"(o), "s"(desc), "i"(j * 1024) : "memory", "m0", "scc");
-          else
-            asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(o), "s"(desc), "i"(j * 1024) : "memory", "m0", "scc");
+      for (int half = 0; half < H; ++half) {
+        const int k0 = key + RPH * half, in = k0 & ((1 << a.pages.bits) - 1);
+        there[half] = min_of(last - k0, RPH);
+        const int l = there[half] > 0 ? entries.lane_of(a, k0 >> a.pages.bits, kvh) : 0;
+        k_at[half] = entries.of(entries.k, l) + uint32_t(in) * uint32_t(a.pages.k.row);
+        v_at[half] = entries.of(entries.v, l) + uint32_t(in) * uint32_t(a.pages.v.row);
+        if constexpr (E4M3) {
+          k_scale[parity][half] = entries.of(entries.ks, l);
+          v_scale[parity][half] = entries.of(entries.vs, l);
         }
       }
     };
+    // Asks for the keys or values of the piece that was located.  Behind the last piece nothing is asked for, by as many loads, so that the waits count the same.
+    auto ask = [&](const uint64_t (&from)[H], int64_t stride, const uint32_t (&offs)[LOADS], int parity, bool values) __attribute__((always_inline)) {
+      const bool front = values && key >= span.first && key < lo;         // values that no row sees must not be read: they may be anything, and their scale
+#pragma unroll
+      for (int half = 0; half < H; ++half) {
+        const uint32_t bytes = there[half] > 0 ? uint32_t(there[half] - 1) * uint32_t(stride) + PT::RB : 0;
+        const u32x4 desc = {uint32_t(from[half]), uint32_t(from[half] >> 32) & 0xFFFFu, bytes, 0x00020000u};
+        const uint32_t to = __builtin_amdgcn_readfirstlane(lds + uint32_t((parity * 2 + values) * BYTES + half * (BYTES / 2)));
+#pragma unroll
+        for (int j = 0; j < LOADS / H; ++j) {
+          uint32_t o = offs[j];
+          if (front) {
+            const int k = key + RPH * half + (j * 64 + lane) / PT::CH;
+            if (k < lo && k >= a.sinks) o = 0x80000000u;
+          }
+          asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(o), "s"(desc), "i"(j * 1024) : "memory", "m0", "scc");
+        }
+        if constexpr (E4M3)
+          if (values && (there[half] <= 0 || (front && key + RPH * half + RPH - 1 < lo && key + RPH * half >= a.sinks))) v_scale[parity][half] = 1.f;
+      }
+    };
+    auto ask_keys = [&](int t, int parity) __attribute__((always_inline)) {
+      locate(t, parity);
+      ask(k_at, a.pages.k.row, k_off, parity, false);
+    };
+    auto ask_values = [&](int parity) __attribute__((always_inline)) { ask(v_at, a.pages.v.row, v_off, parity, true); };
     int t = u0 * a.unit + wave;
     typename Mat<T>::Frag qf[STEPS];
     {
@@ -165,10 +198,10 @@ __global__ void __launch_bounds__((64 * paged_waves<T, D, E4M3>()), (E4M3 || D *
       }
     }
     if (t < t_end) {
-      ask(a.pages.k, k_off, t, 0, false);
-      ask(a.pages.v, v_off, t, 0, true);
-      ask(a.pages.k, k_off, t + NW, 1, false);
-      ask(a.pages.v, v_off, t + NW, 1, true);
+      ask_keys(t, 0);
+      ask_values(0);
+      ask_keys(t + NW, 1);
+      ask_values(1);
     }
     // The queries are waited for here, with what was asked for behind them, or the compiler does it in every piece and for all loads.
 #pragma unroll
@@ -179,12 +212,15 @@ __global__ void __launch_bounds__((64 * paged_waves<T, D, E4M3>()), (E4M3 || D *
     auto piece = [&](auto parity_) __attribute__((always_inline)) {
       constexpr int parity = decltype(parity_)::value;
       const uint32_t buf = lds + uint32_t(parity * 2 * BYTES);
+      float v_now[H];                                // the next piece's comes where it was
+#pragma unroll
+      for (int i = 0; i < H; ++i) v_now[i] = v_scale[parity][i];
       wait_loads_but<3 * LOADS>();
       f32x16 x;
 #pragma unroll
       for (int i = 0; i < 16; ++i) x[i] = 0.f;
       if constexpr (E4M3) {
-        const float scale = n < 16 ? k_scale[parity][0] : k_scale[parity][1];
+        const float scale = n < 16 ? k_scale[parity][0] : k_scale[parity][H - 1];
         u32x4 raw[STEPS / 2];
 #pragma unroll
         for (int st = 0; st < STEPS / 2; ++st)
@@ -202,7 +238,7 @@ __global__ void __launch_bounds__((64 * paged_waves<T, D, E4M3>()), (E4M3 || D *
         for (int st = 0; st < STEPS; ++st) x = Mat<T>::mma(read.get(buf, 0, st), qf[st], x);
       }
       wait_reads();
-      ask(a.pages.k, k_off, t + 2 * NW, parity, false);
+      ask_keys(t + 2 * NW, parity);
       if (!span.whole(t)) span.mask(a, t, p, h, x, -INFINITY);
       float mx = x[0];
 #pragma unroll
@@ -242,7 +278,7 @@ __global__ void __launch_bounds__((64 * paged_waves<T, D, E4M3>()), (E4M3 || D *
         for (int half = 0; half < 2; ++half)
 #pragma unroll
           for (int c = 0; c < D / 32; ++c) {
-            acc[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(eight(uint32_t(raw[half][c][0]), uint32_t(raw[half][c][1]), v_scale[parity][half]),
+            acc[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(eight(uint32_t(raw[half][c][0]), uint32_t(raw[half][c][1]), v_now[half < H ? half : 0]),
                                                              __builtin_bit_cast(bf16x8, w.p[half]), acc[c], 0, 0, 0);
             __builtin_amdgcn_sched_barrier(0);
           }
@@ -251,7 +287,7 @@ __global__ void __launch_bounds__((64 * paged_waves<T, D, E4M3>()), (E4M3 || D *
         read.mma(buf + BYTES, 0, w, acc);
       }
       wait_reads();
-      ask(a.pages.v, v_off, t + 2 * NW, parity, true);
+      ask_values(parity);
     };
     for (; t < t_end; t += NW) {
       piece(std::integral_constant<int, 0>{});
@@ -310,63 +346,103 @@ __global__ void __launch_bounds__((64 * paged_waves<T, D, E4M3>()), (E4M3 || D *
   }
 }
 
-// Joins the parts of an item: a thread takes four channels of a row.  Items in the order of blocks of 32 rows, as packed sequences have them, and key heads.
+// Joins the parts of an item: four rows a work-group, a thread takes four channels of a row and every so-manieth part; items in the order of blocks of 32 rows, as packed
+// sequences have them, and key heads.  Bound by a chain of trips to memory: lengths, the parts, the row.
 template <typename T, int D>
-__global__ void __launch_bounds__(256) paged_join_kernel(PagedArgs a) {
-  constexpr int TR = D / 4, RB = 256 / TR, U = 8;    // threads of a row, rows of a work-group, parts asked for at once
-  __shared__ int s_sums[4], s_base;
-  const int id = blockIdx.x / (32 / RB), n = blockIdx.x % (32 / RB) * RB + threadIdx.x / TR, ch = threadIdx.x % TR * 4;
+__global__ void __launch_bounds__(256) paged_join_kernel(PagedArgs a, int row_groups) {
+  constexpr int TR = D / 4, RB = 4, SETS = 256 / TR / RB, U = 8;         // threads of a row, rows, sets of parts, parts that a thread asks for at once
+  __shared__ int s_sums[4], s_owner, s_item[5];
+  __shared__ float2 s_ml[SETS][RB];
+  __shared__ float4 s_x[SETS][RB][TR];
+  const int id = blockIdx.x / row_groups, in = threadIdx.x / TR % RB, set = threadIdx.x / TR / RB, ch = threadIdx.x % TR;
   const int slot = id / a.heads_kv, kvh = id - slot * a.heads_kv;
-  const int s = run_of(a.packed, slot, [&](int x) { return int(uint32_t(start_of(a.q_start, x, a.n_q) * a.group) / 32) + x; });
   const Deal<256> deal(a, s_sums);
-  if (s < 0) return;
-  const PagedSeq seq(a, s);
-  const int blk = slot - int(uint32_t(seq.q0 * a.group) / 32) - s;
-  if (blk < 0 || blk >= seq.blocks) return;
-  if (s / deal.each == int(threadIdx.x)) {
-    int base = deal.before;
-    for (int x = threadIdx.x * deal.each; x < s; ++x) base += PagedSeq(a, x).work(a);
-    s_base = base + (blk * a.heads_kv + kvh) * seq.units;
+  if (threadIdx.x == 0) s_owner = -1;
+  __syncthreads();
+  // The sequence that this block is of, and the units in front of its item: some thread has it.
+  int s = threadIdx.x * deal.each, base = deal.before, blk = 0;
+  PagedSeq seq = deal.last;
+  bool mine = false;
+  for (int i = 0; i < deal.each && s < a.packed; ++i, ++s) {
+    if (deal.each > 1) seq = PagedSeq(a, s);
+    blk = slot - int(uint32_t(seq.q0 * a.group) / 32) - s;
+    mine = blk >= 0 && blk < seq.blocks;
+    if (mine) break;
+    base += seq.work(a);
+  }
+  if (mine) s_owner = threadIdx.x;
+  __syncthreads();
+  if (s_owner < 0) return;
+  if (s_owner == int(threadIdx.x)) {                 // one thread's numbers, also where starts fall and several have some
+    s_item[0] = seq.q0;
+    s_item[1] = seq.n;
+    s_item[2] = seq.k;
+    s_item[3] = base + (blk * a.heads_kv + kvh) * seq.units;
+    s_item[4] = blk;
   }
   __syncthreads();
-  const int base = s_base, g0 = base / deal.per, g1 = (base + seq.units - 1) / deal.per;
-  if (g0 == g1) return;                              // one work-group had it whole
-  const int r = blk * 32 + n;
-  if (r >= seq.n * a.group) return;
-  const int qi = query_of(a, r), qh = kvh * a.group + r - qi * a.group;
-  float top = -INFINITY, total = 0.f, x[4] = {};
-  for (int g = g0; g <= g1; g += U) {
-    float2 ml[U];
-    float4 y[U];
+  seq = PagedSeq(a, s_item[0], s_item[0] + s_item[1], s_item[2]);
+  base = s_item[3];
+  blk = s_item[4];
+  const int g0 = base / deal.per, g1 = (base + seq.units - 1) / deal.per;
+  if (g0 == g1 || g0 < 0 || g1 >= GROUPS) return;    // one work-group had it whole; (past the runs: where starts fall so far that 31 bits do not count all)
+  for (int n = (blockIdx.x - id * row_groups) * RB + in; blk * 32 + n - in < min_of(blk * 32 + 32, seq.n * a.group); n += row_groups * RB) {
+    const int r = min_of(blk * 32 + n, seq.n * a.group - 1), row = r - blk * 32;
+    float top = -INFINITY, total = 0.f, x[4] = {};
+    for (int g = g0 + set; g <= g1; g += U * SETS) {
+      float2 ml[U];
+      float4 y[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {                    // behind the last part that once more, with a weight of zero
-      const int w = min_of(g + u, g1);
-      const int64_t i = (int64_t(w) * 2 + (w == g0 && base != w * deal.per)) * 32 + n;
-      ml[u] = a.part_sums[i];
-      y[u] = *reinterpret_cast<const float4*>(a.part + i * D + ch);
+      for (int u = 0; u < U; ++u) {                    // behind the last part that once more, with a weight of zero
+        const int w = min_of(g + u * SETS, g1);
+        const int64_t i = (int64_t(w) * 2 + (w == g0 && base != w * deal.per)) * 32 + row;
+        ml[u] = a.part_sums[i];
+        y[u] = reinterpret_cast<const float4*>(a.part + i * D)[ch];
+      }
+      const float before = top;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (g + u * SETS > g1) ml[u].x = -INFINITY;
+        top = fmaxf(top, ml[u].x);
+      }
+      const float ref = top == -INFINITY ? 0.f : top, f = __builtin_amdgcn_exp2f(before - ref);
+      total *= f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[j] *= f;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const float part = __builtin_amdgcn_exp2f(ml[u].x - ref);
+        total = fmaf(part, ml[u].y, total);
+        x[0] = fmaf(part, y[u].x, x[0]);
+        x[1] = fmaf(part, y[u].y, x[1]);
+        x[2] = fmaf(part, y[u].z, x[2]);
+        x[3] = fmaf(part, y[u].w, x[3]);
+      }
     }
-    const float before = top;
+    s_x[set][in][ch] = make_float4(x[0], x[1], x[2], x[3]);
+    if (ch == 0) s_ml[set][in] = make_float2(top, total);
+    __syncthreads();
+    if (set == 0 && blk * 32 + n < seq.n * a.group) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (g + u > g1) ml[u].x = -INFINITY;
-      top = fmaxf(top, ml[u].x);
+      for (int i = 1; i < SETS; ++i) top = fmaxf(top, s_ml[i][in].x);
+      const float ref = top == -INFINITY ? 0.f : top;
+      total = x[0] = x[1] = x[2] = x[3] = 0.f;
+#pragma unroll
+      for (int i = 0; i < SETS; ++i) {
+        const float part = __builtin_amdgcn_exp2f(s_ml[i][in].x - ref);
+        const float4 y = s_x[i][in][ch];
+        total = fmaf(part, s_ml[i][in].y, total);
+        x[0] = fmaf(part, y.x, x[0]);
+        x[1] = fmaf(part, y.y, x[1]);
+        x[2] = fmaf(part, y.z, x[2]);
+        x[3] = fmaf(part, y.w, x[3]);
+      }
+      const int qi = query_of(a, r), qh = kvh * a.group + r - qi * a.group;
+      store_four<T>(a.o.at(0, qh, seq.q0 + qi), ch * 4, x, total == 0.f ? 0.f : 1.f / total);
+      if (ch == 0 && a.lse) a.lse[int64_t(qh) * a.n_q + seq.q0 + qi] = total == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * (1.f / LOG2E);
     }
-    const float ref = top == -INFINITY ? 0.f : top, f = __builtin_amdgcn_exp2f(before - ref);
-    total *= f;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) x[j] *= f;
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const float part = __builtin_amdgcn_exp2f(ml[u].x - ref);
-      total = fmaf(part, ml[u].y, total);
-      x[0] = fmaf(part, y[u].x, x[0]);
-      x[1] = fmaf(part, y[u].y, x[1]);
-      x[2] = fmaf(part, y[u].z, x[2]);
-      x[3] = fmaf(part, y[u].w, x[3]);
-    }
+    __syncthreads();                                   // the sets' sums have been read
   }
-  store_four<T>(a.o.at(0, qh, seq.q0 + qi), ch, x, total == 0.f ? 0.f : 1.f / total);
-  if (ch == 0 && a.lse) a.lse[int64_t(qh) * a.n_q + seq.q0 + qi] = total == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * (1.f / LOG2E);
 }
 
 static int check_paged(const char* call, const dfs_paged* w, int dtype) {
@@ -438,19 +514,29 @@ int dfs_paged_attn_fwd(const dfs_paged* w, int dtype, const dfs_view* q, const d
   a.part_sums = reinterpret_cast<float2*>(static_cast<char*>(ws) + part_bytes(w));
   // work is counted in 31 bits
   const int64_t items = (int64_t(a.group) * a.n_q / 32 + w->seqs) * w->heads_kv, pieces = a.n_k / 32 + 2;
-  a.unit = 4;
+  const bool bytes = pages->dtype == DFS_E4M3;
+  const int row_bytes = w->d * (bytes ? 1 : elem_size(dtype));
+  a.unit = 1024 / row_bytes < 8 ? 1024 / row_bytes : 8;                  // a piece for each wave
   while (items * ((pieces + a.unit - 1) / a.unit) >= int64_t(1) << 31) a.unit *= 2;
   a.least = 1;
-  const bool bytes = pages->dtype == DFS_E4M3;
+  // Where no row sees more than 64 pieces an item is one unit: no parts, no second launch.
+  const int64_t reach = a.left == NO_LIMIT ? pieces : (int64_t(a.left) + a.n_q) / 32 + 2 + (a.sinks + 31) / 32, longest = reach < pieces ? reach : pieces;
+  const bool whole = longest <= 64;
+  if (whole) a.unit = 64;
   const hipStream_t st = as_stream(stream);
-  const unsigned joins = unsigned(items * (w->d / 32));
+  // work-groups of an item's join, four rows a turn, by the rows that a sequence has on average
+  const int64_t mean = (int64_t(a.group) * a.n_q + w->seqs - 1) / w->seqs;
+  const int row_groups = mean < 32 ? int(mean + 3) / 4 : 8;
+  const unsigned joins = unsigned(items * row_groups);
   auto run = [&](auto t, auto d, auto b) {
     using T = decltype(t);
     constexpr int D = decltype(d)::value;
     constexpr bool E4M3 = decltype(b)::value;
-    paged_split_kernel<T, D, E4M3, false><<<GROUPS, 64 * paged_waves<T, D, E4M3>(), 0, st>>>(a);
+    constexpr int NT = 64 * paged_waves<T, D, E4M3>();
+    if (a.pages.bits == 4) paged_split_kernel<T, D, E4M3, true><<<GROUPS, NT, 0, st>>>(a);
+    else paged_split_kernel<T, D, E4M3, false><<<GROUPS, NT, 0, st>>>(a);
   };
-  auto join = [&](auto t, auto d) { paged_join_kernel<decltype(t), decltype(d)::value><<<joins, 256, 0, st>>>(a); };
+  auto join = [&](auto t, auto d) { paged_join_kernel<decltype(t), decltype(d)::value><<<joins, 256, 0, st>>>(a, row_groups); };
   auto by_dim = [&](auto f) { w->d == 64 ? f(std::integral_constant<int, 64>{}) : f(std::integral_constant<int, 128>{}); };
   if (paged_is_long(w)) return run_paged_long(a, w->d, dtype, bytes, st);
   by_dim([&](auto d) {
@@ -458,7 +544,7 @@ int dfs_paged_attn_fwd(const dfs_paged* w, int dtype, const dfs_view* q, const d
     else if (bytes) run(uint16_t{}, d, std::true_type{});
     else run(uint16_t{}, d, std::false_type{});
   });
-  if ((rc = launch_status(call))) return rc;
+  if ((rc = launch_status(call)) || whole) return rc;
   by_dim([&](auto d) { dtype == DFS_F32 ? join(float{}, d) : join(uint16_t{}, d); });
   return launch_status(call);
 }

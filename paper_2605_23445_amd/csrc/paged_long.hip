@@ -15,8 +15,7 @@ struct Sixteen {
     rows = piece < span.n ? max_of(0, min_of(span.end(piece) - key, 16)) : 0;
     if (values && piece >= span.n_first && key + 15 < lo && key >= a.sinks) rows = 0;        // in front of every window
     lane = rows > 0 ? entries.lane_of(a, key >> a.pages.bits, kvh) : 0;
-    const int id = rows > 0 ? __builtin_amdgcn_readlane(entries.id, lane) : 0;
-    at = reinterpret_cast<uint64_t>(v.at(id, kvh, key & ((1 << a.pages.bits) - 1)));
+    at = Entries<E4M3>::of(values ? entries.v : entries.k, lane) + uint32_t(key & ((1 << a.pages.bits) - 1)) * uint32_t(v.row);
   }
 };
 
@@ -103,7 +102,7 @@ template <int D> struct ByteFeed {
     for (int j = 0; j < SHARES; ++j) {
       const Sixteen x(a, entries, a.pages.k, span, kvh, t, (j * NW + wave) * 4 / CH, false);
       k[j] = load(a.pages.k, x, row[j]);
-      k_scale[j] = x.rows > 0 ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(entries.ks), x.lane)) : 1.f;
+      k_scale[j] = x.rows > 0 ? entries.of(entries.ks, x.lane) : 1.f;
     }
   }
   __device__ __forceinline__ void ask_values(const Span& span, int t) {
@@ -112,7 +111,7 @@ template <int D> struct ByteFeed {
     for (int j = 0; j < SHARES; ++j) {
       const Sixteen x(a, entries, a.pages.v, span, kvh, t, (j * NW + wave) * 4 / CH, true);
       v[j] = load(a.pages.v, x, row[j] >= u.from && row[j] < u.to ? -1 : row[j]);
-      v_scale[j] = x.rows > 0 ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(entries.vs), x.lane)) : 1.f;
+      v_scale[j] = x.rows > 0 ? entries.of(entries.vs, x.lane) : 1.f;
     }
   }
   template <class TileT> __device__ __forceinline__ void put(const u32x4& x, float scale, uint32_t lds, int r) const {
