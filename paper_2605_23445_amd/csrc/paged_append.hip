@@ -19,16 +19,28 @@ struct AppendArgs : Turns {
   const int32_t *q_start, *k_len, *positions;
   const float* w[2];
   int32_t seqs, tokens, heads, heads_kv, norm;
-  int32_t q_groups, q_blocks, per;                   // work-groups of all tokens, of all queries; heads that one walks over
+  int32_t page_blocks, q_groups, per;                // work-groups of pages in 8 bits, of all tokens; heads that one of the latter walks over
 };
 
 // A sequence's new tokens: its first row, how many there are, and the position of the first.
 struct Piece {
   int q0, n, begin;
-  __device__ __forceinline__ Piece(const AppendArgs& a, int s) {
-    q0 = start_of(a.q_start, s, a.tokens);
-    n = max_of(0, start_of(a.q_start, s + 1, a.tokens) - q0);
-    begin = max_of(0, min_of(a.k_len[s], a.pages.row << a.pages.bits)) - n;
+  __device__ __forceinline__ Piece(const AppendArgs& a, int from, int to, int k_len) {
+    q0 = from;
+    n = max_of(0, to - from);
+    begin = max_of(0, min_of(k_len, a.pages.row << a.pages.bits)) - n;
+  }
+  __device__ __forceinline__ Piece(const AppendArgs& a, int s) : Piece(a, start_of(a.q_start, s, a.tokens), start_of(a.q_start, s + 1, a.tokens), a.k_len[s]) {}
+};
+
+// Up to 64 sequences, one a lane.
+struct Lanes {
+  int from, to, k_len;
+  __device__ __forceinline__ Lanes(const AppendArgs& a) {
+    const int lane = threadIdx.x & 63, s = min_of(lane, a.seqs - 1);
+    from = lane < a.seqs ? start_of(a.q_start, s, a.tokens) : a.tokens;
+    to = start_of(a.q_start, s + 1, a.tokens);
+    k_len = a.k_len[s];
   }
 };
 
@@ -56,21 +68,40 @@ __device__ __forceinline__ void norm_and_turn(const AppendArgs& a, const Turn<T,
   t.template rotate<false>(x);
 }
 
-template <typename T, int D, bool PAIRS>
-__device__ __forceinline__ void append_queries(const AppendArgs& a, int id) {
+// Rows of tokens, those of all heads in turn: queries and, where they are stored as they are (KV), keys and values.
+template <typename T, int D, bool PAIRS, bool KV>
+__device__ __forceinline__ void append_tokens(const AppendArgs& a, int id) {
   using Tok = Turn<T, D, PAIRS>;
   constexpr int N = Tok::N, L = Tok::L, U = 2;
   const int lane = threadIdx.x & 63, y = id / a.q_groups, x = id - y * a.q_groups, t = x * (256 / L) + threadIdx.x / L;
-  const int row = min_of(t, a.tokens - 1);
+  const int row = min_of(t, a.tokens - 1), c16 = lane % L * 16, h0 = y * a.per, h1 = min_of(h0 + a.per, a.heads + (KV ? 2 * a.heads_kv : 0));
+  const char* src[3];
+#pragma unroll
+  for (int i = 0; i < 3; ++i) src[i] = a.in[i].at(0, 0, row) + c16;
+  auto which = [&](int h) { return !KV || h < a.heads ? 0 : h < a.heads + a.heads_kv ? 1 : 2; };
+  int64_t step[3] = {a.in[0].head, a.in[1].head, a.in[2].head}, to_step[3] = {a.q_out.head, a.pages.k.head, a.pages.v.head};
+#pragma unroll
+  for (int i = 0; i < 3; ++i) asm volatile("" : "+s"(step[i]), "+s"(to_step[i]));         // or the compiler selects addresses of arguments, which it then copies to scratch
+  auto load = [&](int h_) {
+    const int h = min_of(h_, h1 - 1);
+    const int i = which(h);
+    return load_chunk<false>(i == 0 ? src[0] + h * step[0] : i == 1 ? src[1] + (h - a.heads) * step[1] : src[2] + (h - a.heads - a.heads_kv) * step[2]);
+  };
+  u32x4 next[U];                                     // asked for in front of everything that takes a trip to memory
+#pragma unroll
+  for (int u = 0; u < U; ++u) next[u] = load(h0 + u);
+  float w[2][N];
+  weights<N>(a.w[0], lane % L, w[0]);
+  if (KV) weights<N>(a.w[1], lane % L, w[1]);
   // the last sequence that begins at or in front of this token
   int s = -1;
   if (a.seqs <= 64) {
-    const int mine = lane < a.seqs ? start_of(a.q_start, lane, a.tokens) : a.tokens;
+    const Lanes all(a);
     const int first = __builtin_amdgcn_readfirstlane(row);
 #pragma unroll
     for (int j = 0; j < 64 / L; ++j) {
-      const int c = __builtin_popcountll(__builtin_amdgcn_ballot_w64(lane < a.seqs && mine <= min_of(first + j, a.tokens - 1)));
-      if (lane / L == j) s = c - 1;
+      const int n = __builtin_popcountll(__builtin_amdgcn_ballot_w64(lane < a.seqs && all.from <= min_of(first + j, a.tokens - 1)));
+      if (lane / L == j) s = n - 1;
     }
   } else {
     for (int lo = 0, hi = a.seqs; lo < hi;) {
@@ -85,74 +116,73 @@ __device__ __forceinline__ void append_queries(const AppendArgs& a, int id) {
   }
   const Piece piece(a, max_of(s, 0));
   const bool real = t < a.tokens && s >= 0 && row - piece.q0 < piece.n && row >= piece.q0;
+  const int p = piece.begin + row - piece.q0;
   Tok tok;
-  set_turn(a, tok, lane, row, piece.begin + row - piece.q0);
-  float w[N];
-  weights<N>(a.w[0], tok.c, w);
-  const int h0 = y * a.per, h1 = min_of(h0 + a.per, a.heads);
-  const char* src = a.in[0].at(0, 0, row) + tok.c * 16;
-  char* dst = a.q_out.at(0, 0, row) + tok.c * 16;
+  set_turn(a, tok, lane, row, p);
+  char* dst[3] = {a.q_out.at(0, 0, row) + c16, nullptr, nullptr};
+  bool stored = false;                               // whether keys and values have a place
+  if (KV) {
+    const int page = real ? page_of(a.pages, max_of(s, 0), p >> a.pages.bits) : -1, in = p & ((1 << a.pages.bits) - 1);
+    stored = page >= 0;
+    dst[1] = a.pages.k.at(max_of(page, 0), 0, in) + c16;
+    dst[2] = a.pages.v.at(max_of(page, 0), 0, in) + c16;
+  }
   for (int h = h0; h < h1; h += U) {
     u32x4 raw[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) raw[u] = load_chunk<false>(src + (h + u < h1 ? h + u : h) * a.in[0].head);
+    for (int u = 0; u < U; ++u) raw[u] = next[u];
+    if (h + U < h1) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) next[u] = load(h + U + u);
+    }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      float v[N];
-      Chunk<T>::open(raw[u], v);
-      norm_and_turn<T, D, PAIRS>(a, tok, w, v);
-      if (real && h + u < h1) *reinterpret_cast<u32x4*>(dst + (h + u) * a.q_out.head) = Chunk<T>::close(v);
+      if (h + u >= h1) break;
+      const int i = which(h + u);
+      if (i < 2) {
+        float v[N];
+        Chunk<T>::open(raw[u], v);
+        if (i == 0) norm_and_turn<T, D, PAIRS>(a, tok, w[0], v);
+        else norm_and_turn<T, D, PAIRS>(a, tok, w[1], v);
+        raw[u] = Chunk<T>::close(v);
+      }
+      char* to = i == 0 ? dst[0] + (h + u) * to_step[0] : i == 1 ? dst[1] + (h + u - a.heads) * to_step[1] : dst[2] + (h + u - a.heads - a.heads_kv) * to_step[2];
+      if (i == 0 ? real : stored) __builtin_nontemporal_store(raw[u], reinterpret_cast<u32x4*>(to));
     }
   }
 }
 
 // The new rows of a page: which sequence, page and key head, and the rows [r0, r1) of the page, row r at tensor row `row0` + r.
 struct Fresh {
-  bool real = false;
+  bool real = false;                                 // (whether there is such a page is not known yet)
   int page, kvh, r0, r1, row0, p0;                   // p0: position of the page's row 0
   __device__ __forceinline__ Fresh(const AppendArgs& a, int id) {
     // A sequence has room for as many pages as whole ones lie between its start and the next one's, and two more.
     const int slot = id / a.heads_kv, bits = a.pages.bits;
     kvh = id - slot * a.heads_kv;
-    const int s = run_of(a.seqs, slot, [&](int x) { return (start_of(a.q_start, x, a.tokens) >> bits) + 2 * x; });
-    if (s < 0) return;
-    const Piece piece(a, s);
+    int s;
+    Piece piece(a, 0, 0, 0);
+    if (a.seqs <= 64) {
+      const Lanes all(a);
+      const int lane = threadIdx.x & 63;
+      s = __builtin_popcountll(__builtin_amdgcn_ballot_w64(lane < a.seqs && (all.from >> bits) + 2 * lane <= slot)) - 1;
+      if (s < 0) return;
+      piece = Piece(a, __builtin_amdgcn_readlane(all.from, s), __builtin_amdgcn_readlane(all.to, s), __builtin_amdgcn_readlane(all.k_len, s));
+    } else {
+      s = run_of(a.seqs, slot, [&](int x) { return (start_of(a.q_start, x, a.tokens) >> bits) + 2 * x; });
+      if (s < 0) return;
+      piece = Piece(a, s);
+    }
     const int begin = max_of(piece.begin, 0), i = (begin >> bits) + slot - (piece.q0 >> bits) - 2 * s, end = piece.begin + piece.n;
     p0 = i << bits;
     if (i < begin >> bits || p0 >= end || end <= begin) return;          // (in front: where starts fall)
     page = page_of(a.pages, s, i);
-    if (page < 0) return;
     r0 = max_of(begin - p0, 0);
     r1 = min_of(end - p0, 1 << bits);
     row0 = piece.q0 + p0 - piece.begin;
     real = r0 < r1;
   }
 };
-
-// Rows as they are.
-template <typename T, int D, bool PAIRS>
-__device__ __forceinline__ void append_rows(const AppendArgs& a, int id) {
-  using Tok = Turn<T, D, PAIRS>;
-  constexpr int N = Tok::N, L = Tok::L, R = 256 / L;
-  const Fresh f(a, id);
-  if (!f.real) return;
-  const int lane = threadIdx.x & 63;
-  float w[N];
-  weights<N>(a.w[1], lane % L, w);
-  for (int r = f.r0 + threadIdx.x / L; r - int(threadIdx.x / L) < f.r1; r += R) {
-    const int at = min_of(r, f.r1 - 1), row = f.row0 + at;
-    const u32x4 k = load_chunk<false>(a.in[1].at(0, f.kvh, row) + lane % L * 16), v = load_chunk<false>(a.in[2].at(0, f.kvh, row) + lane % L * 16);
-    Tok tok;
-    set_turn(a, tok, lane, row, f.p0 + at);
-    float x[N];
-    Chunk<T>::open(k, x);
-    norm_and_turn<T, D, PAIRS>(a, tok, w, x);
-    if (r < f.r1) {
-      *reinterpret_cast<u32x4*>(a.pages.k.at(f.page, f.kvh, r) + tok.c * 16) = Chunk<T>::close(x);
-      *reinterpret_cast<u32x4*>(a.pages.v.at(f.page, f.kvh, r) + tok.c * 16) = v;
-    }
-  }
-}
 
 // Exponent, as fp32 has it, of the smallest power of two c >= 2^-120 with m <= 448 c.
 __device__ __forceinline__ int scale_exponent(float m) {
@@ -187,8 +217,7 @@ __device__ __forceinline__ void append_bytes(const AppendArgs& a, int id) {
   __shared__ float most[2][4];
   const Fresh f(a, id);
   if (!f.real) return;
-  const int lane = threadIdx.x & 63, c = lane % L, mine = f.r0 + threadIdx.x / L, scale_at = f.page * a.heads_kv + f.kvh;
-  const float was[2] = {a.pages.k_scale[scale_at], a.pages.v_scale[scale_at]};
+  const int lane = threadIdx.x & 63, c = lane % L, mine = f.r0 + threadIdx.x / L;
   float w[N], y[PASSES][N], top[2] = {};
   u32x4 raw[PASSES], v[PASSES];
 #pragma unroll
@@ -199,6 +228,9 @@ __device__ __forceinline__ void append_bytes(const AppendArgs& a, int id) {
     v[u] = load_chunk<false>(a.in[2].at(0, f.kvh, row) + c * 16);
   }
   weights<N>(a.w[1], c, w);
+  if (f.page < 0) return;
+  const int scale_at = f.page * a.heads_kv + f.kvh;
+  const float was[2] = {a.pages.k_scale[scale_at], a.pages.v_scale[scale_at]};
 #pragma unroll
   for (int u = 0; u < PASSES; ++u) {
     if (f.r0 + u * R >= f.r1) continue;
@@ -251,16 +283,19 @@ __device__ __forceinline__ void append_bytes(const AppendArgs& a, int id) {
   }
 }
 
-// PASSES 0: pages of T.
+// PASSES 0: pages of T.  The work-groups of pages come first, which take longer.
 template <typename T, int D, bool PAIRS, int PASSES>
 __global__ void __launch_bounds__(256) paged_append_kernel(AppendArgs a) {
   const int id = blockIdx.x;
-  if (id < a.q_blocks) append_queries<T, D, PAIRS>(a, id);
-  else if constexpr (PASSES == 0) append_rows<T, D, PAIRS>(a, id - a.q_blocks);
-  else append_bytes<D, PAIRS, PASSES>(a, id - a.q_blocks);
+  if constexpr (PASSES > 0) {
+    if (id < a.page_blocks) append_bytes<D, PAIRS, PASSES>(a, id);
+    else append_tokens<T, D, PAIRS, false>(a, id - a.page_blocks);
+  } else {
+    append_tokens<T, D, PAIRS, true>(a, id);
+  }
 }
 
-constexpr int RUN = 10;                              // heads of queries that a work-group walks over, at most
+constexpr int RUN = 10;                              // rows that a work-group's lanes walk over, at most
 
 }  // namespace dfs
 
@@ -310,15 +345,16 @@ int dfs_paged_append(const dfs_qk_geom* g, int dtype, const dfs_view* q, const d
   a.heads_kv = g->heads_kv;
   a.norm = norm != 0;
   // runs of heads until there are eight waves a SIMD, or a row a lane
-  int64_t y = (8192 + waves - 1) / waves, runs = (g->heads + RUN - 1) / RUN;
-  if (y < runs) y = runs;
-  if (y > g->heads) y = g->heads;
-  a.per = int((g->heads + y - 1) / y);
-  a.q_groups = int((n * L + 255) / 256);
-  const int64_t q_blocks = int64_t(a.q_groups) * ((g->heads + a.per - 1) / a.per), blocks = q_blocks + (a.pages.row ? slots * g->heads_kv : 0);
-  if (blocks >= 1 << 24) return fail(DFS_ESHAPE, "%s: tokens=%d x heads=%d too large", call, g->tokens, g->heads);
-  a.q_blocks = int(q_blocks);
   const bool bytes = pages->dtype == DFS_E4M3;
+  const int all = g->heads + (bytes ? 0 : 2 * g->heads_kv);
+  int64_t y = (8192 + waves - 1) / waves, runs = (all + RUN - 1) / RUN;
+  if (y < runs) y = runs;
+  if (y > all) y = all;
+  a.per = int((all + y - 1) / y);
+  a.q_groups = int((n * L + 255) / 256);
+  a.page_blocks = bytes && a.pages.row ? int(slots * g->heads_kv) : 0;
+  const int64_t blocks = int64_t(a.q_groups) * ((all + a.per - 1) / a.per) + a.page_blocks;
+  if (blocks >= 1 << 24) return fail(DFS_ESHAPE, "%s: tokens=%d x heads=%d too large", call, g->tokens, g->heads);
   const int passes = !bytes ? 0 : pages->page * L / 256 > 1 ? pages->page * L / 256 : 1;
   const hipStream_t st = as_stream(stream);
   auto run = [&](auto t, auto d, auto p, auto s) {

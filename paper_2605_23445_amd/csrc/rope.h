@@ -82,10 +82,17 @@ template <typename T, int D, bool PAIRS> struct Turn {
       const int half = (axis == 0 ? a.rot[0] : axis == 1 ? a.rot[1] : a.rot[2]) / 2, first = (ch - begin) < half;
       const bool turned = ch < end2;
       if (turned) partner = first ? lane + half / N : lane - half / N;
+      // the two lanes of a pair's channels work out half of their angles each and exchange them
+      const int mine = first ? 0 : C / 2, base = begin / 2 + (ch - begin) - (first ? 0 : half) + mine;
 #pragma unroll
-      for (int i = 0; i < C; ++i) {
-        turn(axis == 0 ? p0 : axis == 1 ? p1 : p2, turned ? a.freq[begin / 2 + (ch - begin) + i - (first ? 0 : half)] : 0, cs[i], sn[i]);
-        if (first) sn[i] = -sn[i];
+      for (int i = 0; i < C / 2; ++i) {
+        float c0, s0;
+        turn(axis == 0 ? p0 : axis == 1 ? p1 : p2, turned ? a.freq[base + i] : 0, c0, s0);
+        const float c1 = __shfl(c0, partner), s1 = __shfl(s0, partner);
+        cs[i] = first ? c0 : c1;
+        cs[i + C / 2] = first ? c1 : c0;
+        sn[i] = first ? -s0 : s1;
+        sn[i + C / 2] = first ? -s1 : s0;
       }
     }
   }
