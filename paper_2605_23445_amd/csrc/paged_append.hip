@@ -19,7 +19,8 @@ struct AppendArgs : Turns {
   const int32_t *q_start, *k_len, *positions;
   const float* w[2];
   int32_t seqs, tokens, heads, heads_kv, norm;
-  int32_t page_blocks, q_groups, per;                // work-groups of pages in 8 bits, of all tokens; heads that one of the latter walks over
+  int32_t q_groups, per;                             // work-groups of all tokens; heads that one walks over
+  uint32_t page_share;                               // work-groups of pages in 8 bits out of all, in 2^-32, rounded up
 };
 
 // A sequence's new tokens: its first row, how many there are, and the position of the first.
@@ -283,13 +284,14 @@ __device__ __forceinline__ void append_bytes(const AppendArgs& a, int id) {
   }
 }
 
-// PASSES 0: pages of T.  The work-groups of pages come first, which take longer.
+// PASSES 0: pages of T.  The work-groups of pages, which compute more, are spread evenly among those of tokens, which move more.
 template <typename T, int D, bool PAIRS, int PASSES>
 __global__ void __launch_bounds__(256) paged_append_kernel(AppendArgs a) {
   const int id = blockIdx.x;
   if constexpr (PASSES > 0) {
-    if (id < a.page_blocks) append_bytes<D, PAIRS, PASSES>(a, id);
-    else append_tokens<T, D, PAIRS, false>(a, id - a.page_blocks);
+    const int pages = int(__umulhi(uint32_t(id), a.page_share));         // of the work-groups in front of this one
+    if (int(__umulhi(uint32_t(id) + 1, a.page_share)) > pages) append_bytes<D, PAIRS, PASSES>(a, pages);
+    else append_tokens<T, D, PAIRS, false>(a, id - pages);
   } else {
     append_tokens<T, D, PAIRS, true>(a, id);
   }
@@ -352,9 +354,9 @@ int dfs_paged_append(const dfs_qk_geom* g, int dtype, const dfs_view* q, const d
   if (y > all) y = all;
   a.per = int((all + y - 1) / y);
   a.q_groups = int((n * L + 255) / 256);
-  a.page_blocks = bytes && a.pages.row ? int(slots * g->heads_kv) : 0;
-  const int64_t blocks = int64_t(a.q_groups) * ((all + a.per - 1) / a.per) + a.page_blocks;
+  const int64_t page_blocks = bytes && a.pages.row ? slots * g->heads_kv : 0, blocks = int64_t(a.q_groups) * ((all + a.per - 1) / a.per) + page_blocks;
   if (blocks >= 1 << 24) return fail(DFS_ESHAPE, "%s: tokens=%d x heads=%d too large", call, g->tokens, g->heads);
+  a.page_share = uint32_t(((uint64_t(page_blocks) << 32) + blocks - 1) / blocks);
   const int passes = !bytes ? 0 : pages->page * L / 256 > 1 ? pages->page * L / 256 : 1;
   const hipStream_t st = as_stream(stream);
   auto run = [&](auto t, auto d, auto p, auto s) {
