@@ -5,68 +5,81 @@
 
 namespace dfs {
 
-// Where a tile's 16 rows number g lie (16 rows are on one page): their address, how many of them there are, and on which lane of the entries their scales.
+// Where 16 rows of a tile lie, which are on one page: their keys and values, how many there are, and on which lane of the entries the page is.  (The entries may be other
+// ones when the values are asked for.)
 struct Sixteen {
-  uint64_t at;
-  int rows, lane;
-  template <bool E4M3>
-  __device__ __forceinline__ Sixteen(const PagedArgs& a, Entries<E4M3>& entries, const View& v, const Span& span, int kvh, int t, int g, bool values) {
-    const int piece = 2 * t + g / 2, key = span.begin(piece) + 16 * (g % 2), lo = max_of(0, span.p0 - a.left);
-    rows = piece < span.n ? max_of(0, min_of(span.end(piece) - key, 16)) : 0;
-    if (values && piece >= span.n_first && key + 15 < lo && key >= a.sinks) rows = 0;        // in front of every window
+  uint64_t k, v;
+  int lane, rows;
+  // Number g of tile t.
+  template <bool E4M3> __device__ __forceinline__ void find(const PagedArgs& a, Entries<E4M3>& entries, const Span& span, int kvh, int t, int g) {
+    const int piece = 2 * t + g / 2, key = span.begin(piece) + 16 * (g % 2);
+    const uint32_t in = uint32_t(key) & ((1u << a.pages.bits) - 1);
+    rows = max_of(0, min_of(span.end(piece) - key, 16));                 // (behind the last piece `key` is past the end)
     lane = rows > 0 ? entries.lane_of(a, key >> a.pages.bits, kvh) : 0;
-    at = Entries<E4M3>::of(values ? entries.v : entries.k, lane) + uint32_t(key & ((1 << a.pages.bits) - 1)) * uint32_t(v.row);
+    k = entries.of(entries.k, lane) + in * uint32_t(a.pages.k.row);
+    v = entries.of(entries.v, lane) + in * uint32_t(a.pages.v.row);
   }
 };
 
-// Rows [from, to) of tile t that no query of the block sees although some behind them are seen: their values, which may be anything, are left out.
+// The first tile with rows of the window, and its rows [from, to) that no query of the block sees although some behind them are seen: their values, and what scales them, may be
+// anything, and are left out.
 struct Unseen {
-  int from, to;
-  __device__ __forceinline__ Unseen(const PagedArgs& a, const Span& span, int t) : from(0), to(0) {
-    const int piece = span.n_first, lo = max_of(0, span.p0 - a.left);
-    if (piece / 2 != t) return;
-    const int key = span.begin(piece), row = piece % 2 * 32;
+  int tile, from, to;
+  __device__ __forceinline__ Unseen(const PagedArgs& a, const Span& span) {
+    const int piece = span.n_first, key = span.begin(piece), row = piece % 2 * 32;
+    tile = piece / 2;
     from = row + max_of(0, a.sinks - key);
-    to = row + min_of(lo - key, 32);
+    to = row + min_of(max_of(0, span.p0 - a.left) - key, 32);
   }
 };
 
-// Rows of pages as they are, straight to LDS.
+// Rows of pages as they are, straight to LDS.  Values are asked for behind the same tile's keys.
 template <typename T, int D> struct PageFeed {
   static constexpr int STEP = 32, NW = 4;
   static constexpr bool STRAIGHT = true;
   using KTile = Tile<T, D, KN, NW, false>;
   using VTile = Tile<T, D, KN, NW, true>;
-  static constexpr int LOADS = KTile::LOADS, CH = KTile::CH, RB = KTile::RB;
+  static constexpr int LOADS = KTile::LOADS, CH = KTile::CH;
   const PagedArgs& a;
   int kvh, wave, lane;
   Entries<false> entries;
   typename KTile::Loader k_load;
   typename VTile::Loader v_load;
+  Sixteen place[LOADS];                              // of the keys asked for last
+  Unseen unseen;
   struct Want {
     u32x4 desc[LOADS];
     int from, to;
   };
-  template <class P, class S> __device__ __forceinline__ PageFeed(const PagedArgs& a_, const P& at, const S& seq, int wave_, int lane_)
-      : a(a_), kvh(at.kvh), wave(wave_), lane(lane_), entries(a_, seq.seq), k_load(a_.pages.k.row, wave_, lane_), v_load(a_.pages.v.row, wave_, lane_) {}
-  __device__ __forceinline__ Want tile(const View& v, const Span& span, int t, bool values) {
+  template <class P, class S> __device__ __forceinline__ PageFeed(const PagedArgs& a_, const P& at, const S& seq, const Span& span, int wave_, int lane_)
+      : a(a_), kvh(at.kvh), wave(wave_), lane(lane_), entries(a_, seq.seq), k_load(a_.pages.k.row, wave_, lane_), v_load(a_.pages.v.row, wave_, lane_), unseen(a_, span) {}
+  __device__ __forceinline__ int group(int j) const { return (j * NW + wave) * 4 / CH; }
+  __device__ __forceinline__ u32x4 desc(int j, uint64_t from, const View& v) const {
+    const uint32_t front = uint32_t(16 * group(j)) * uint32_t(v.row);     // offsets count from the tile's first row
+    const uint64_t at = from - front;
+    const uint32_t bytes = place[j].rows > 0 ? front + uint32_t(place[j].rows) * uint32_t(v.row) : 0;
+    return u32x4{uint32_t(__builtin_amdgcn_readfirstlane(uint32_t(at))), uint32_t(__builtin_amdgcn_readfirstlane(uint32_t(at >> 32))) & 0xFFFFu,
+                 uint32_t(__builtin_amdgcn_readfirstlane(bytes)), 0x00020000u};
+  }
+  __device__ __forceinline__ Want keys(const Span& span, int t) {
     Want w;
 #pragma unroll
     for (int j = 0; j < LOADS; ++j) {
-      const int g = (j * NW + wave) * 4 / CH;
-      const Sixteen x(a, entries, v, span, kvh, t, g, values);
-      const uint64_t at = x.at - uint64_t(16 * g) * uint64_t(v.row);
-      const uint32_t bytes = x.rows > 0 ? uint32_t(16 * g + x.rows - 1) * uint32_t(v.row) + RB : 0;
-      w.desc[j] = u32x4{uint32_t(__builtin_amdgcn_readfirstlane(uint32_t(at))), uint32_t(__builtin_amdgcn_readfirstlane(uint32_t(at >> 32))) & 0xFFFFu,
-                        uint32_t(__builtin_amdgcn_readfirstlane(bytes)), 0x00020000u};
+      if (j > 0 && CH >= 16 && group(j) == group(j - 1)) place[j] = place[j - 1];
+      else place[j].find(a, entries, span, kvh, t, group(j));
+      w.desc[j] = desc(j, place[j].k, a.pages.k);
     }
-    const Unseen u(a, span, t);
-    w.from = values ? u.from : 0;
-    w.to = values ? u.to : 0;
+    w.from = w.to = 0;
     return w;
   }
-  __device__ __forceinline__ Want keys(const Span& span, int t) { return tile(a.pages.k, span, t, false); }
-  __device__ __forceinline__ Want values(const Span& span, int t) { return tile(a.pages.v, span, t, true); }
+  __device__ __forceinline__ Want values(const Span& span, int t) {
+    Want w;
+#pragma unroll
+    for (int j = 0; j < LOADS; ++j) w.desc[j] = desc(j, place[j].v, a.pages.v);
+    w.from = t == unseen.tile ? unseen.from : 0;
+    w.to = t == unseen.tile ? unseen.to : 0;
+    return w;
+  }
   __device__ __forceinline__ void ask_keys(const Want& w, uint32_t to, int j) const { k_load.issue_one(w.desc[j], to, j); }
   __device__ __forceinline__ void ask_values(const Want& w, uint32_t to, int j) const {
     const int row = ((j * NW + wave) * 64 + lane) / CH;
@@ -84,51 +97,70 @@ template <int D> struct ByteFeed {
   using VTile = Tile<uint16_t, D, KN, NW, true>;
   static constexpr int SHARES = D / 64, CH = D / 16;                     // loads of a thread for a tile; chunks of a row
   const PagedArgs& a;
-  int kvh, wave, row[SHARES], c;
+  int kvh, wave, c, row[SHARES];
+  uint32_t k_off[SHARES], v_off[SHARES], put_at[SHARES];                 // in a page's 16 rows; in a tile in LDS
   Entries<true> entries;
+  Sixteen place[SHARES];                             // of the keys asked for last
+  Unseen unseen;
   u32x4 k[SHARES], v[SHARES];
-  float k_scale[SHARES], v_scale[SHARES];
-  template <class P, class S> __device__ __forceinline__ ByteFeed(const PagedArgs& a_, const P& at, const S& seq, int wave_, int lane)
-      : a(a_), kvh(at.kvh), wave(wave_), c(lane % CH), entries(a_, seq.seq) {
+  float k_scale[SHARES], v_scale[SHARES], next_scale[SHARES];            // next: of the values that lie beside the keys asked for last
+  template <class P, class S> __device__ __forceinline__ ByteFeed(const PagedArgs& a_, const P& at, const S& seq, const Span& span, int wave_, int lane)
+      : a(a_), kvh(at.kvh), wave(wave_), c(lane % CH), entries(a_, seq.seq), unseen(a_, span) {
+    static_assert(KTile::swizzle(5) == VTile::swizzle(5) && KTile::swizzle(13) == VTile::swizzle(13), "keys and values lie alike");
 #pragma unroll
-    for (int j = 0; j < SHARES; ++j) row[j] = ((j * NW + wave) * 64 + lane) / CH;
+    for (int j = 0; j < SHARES; ++j) {
+      row[j] = ((j * NW + wave) * 64 + lane) / CH;
+      k_off[j] = uint32_t(row[j] % 16) * uint32_t(a.pages.k.row) + c * 16;
+      v_off[j] = uint32_t(row[j] % 16) * uint32_t(a.pages.v.row) + c * 16;
+      put_at[j] = uint32_t(row[j] * KTile::RB) + (uint32_t(2 * c) ^ uint32_t(KTile::swizzle(row[j]))) * 16;
+    }
   }
-  __device__ __forceinline__ u32x4 load(const View& view, const Sixteen& x, int r) const {
-    const auto from = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(x.at), 0, x.rows > 0 ? uint32_t(x.rows - 1) * uint32_t(view.row) + D : 0, 0x00020000);
-    return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(from, r < 0 ? int(0x80000000u) : int(uint32_t(r % 16) * uint32_t(view.row)) + c * 16, 0, 0));
+  static __device__ __forceinline__ u32x4 load(uint64_t at, uint32_t bytes, uint32_t off) {
+    return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(__builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(at), 0, bytes, 0x00020000), off, 0, 0));
   }
   __device__ __forceinline__ void ask_keys(const Span& span, int t) {
 #pragma unroll
     for (int j = 0; j < SHARES; ++j) {
-      const Sixteen x(a, entries, a.pages.k, span, kvh, t, (j * NW + wave) * 4 / CH, false);
-      k[j] = load(a.pages.k, x, row[j]);
-      k_scale[j] = x.rows > 0 ? entries.of(entries.ks, x.lane) : 1.f;
+      place[j].find(a, entries, span, kvh, t, (j * NW + wave) * 4 / CH);
+      k[j] = load(place[j].k, uint32_t(place[j].rows) * uint32_t(a.pages.k.row), k_off[j]);
+      k_scale[j] = entries.of(entries.ks, place[j].lane);
+      next_scale[j] = place[j].rows > 0 ? entries.of(entries.vs, place[j].lane) : 1.f;
     }
   }
+  // Behind the same tile's keys.
   __device__ __forceinline__ void ask_values(const Span& span, int t) {
-    const Unseen u(a, span, t);
 #pragma unroll
     for (int j = 0; j < SHARES; ++j) {
-      const Sixteen x(a, entries, a.pages.v, span, kvh, t, (j * NW + wave) * 4 / CH, true);
-      v[j] = load(a.pages.v, x, row[j] >= u.from && row[j] < u.to ? -1 : row[j]);
-      v_scale[j] = x.rows > 0 ? entries.of(entries.vs, x.lane) : 1.f;
+      uint32_t off = v_off[j];
+      v_scale[j] = next_scale[j];
+      if (t == unseen.tile) {
+        if (row[j] >= unseen.from && row[j] < unseen.to) off = 0x80000000u;                  // zeros
+        const int first = (j * NW + wave) * 4 / CH * 16;
+        if (first >= unseen.from && first + 16 <= unseen.to) v_scale[j] = 1.f;
+      }
+      v[j] = load(place[j].v, uint32_t(place[j].rows) * uint32_t(a.pages.v.row), off);
     }
   }
-  template <class TileT> __device__ __forceinline__ void put(const u32x4& x, float scale, uint32_t lds, int r) const {
-    const uint32_t at = lds + uint32_t(r * TileT::RB) + (uint32_t(2 * c) ^ uint32_t(TileT::swizzle(r))) * 16;
-    const bf16x8 lo = eight(x[0], x[1], scale), hi = eight(x[2], x[3], scale);
-    *reinterpret_cast<LDS_PTR(u32x4)>(at) = __builtin_bit_cast(u32x4, lo);
-    *reinterpret_cast<LDS_PTR(u32x4)>(at ^ 16) = __builtin_bit_cast(u32x4, hi);
+  // Half `h` of a thread's chunk to a tile.
+  __device__ __forceinline__ void put(const u32x4& x, float scale, uint32_t to, int h) const {
+    *reinterpret_cast<LDS_PTR(u32x4)>(to ^ uint32_t(16 * h)) = __builtin_bit_cast(u32x4, h ? eight(x[2], x[3], scale) : eight(x[0], x[1], scale));
   }
-  __device__ __forceinline__ void put_keys(uint32_t lds, int j) const { put<KTile>(k[j], k_scale[j], lds, row[j]); }
-  __device__ __forceinline__ void put_values(uint32_t lds, int j) const { put<VTile>(v[j], v_scale[j], lds, row[j]); }
   __device__ __forceinline__ void put_keys(uint32_t lds) const {
 #pragma unroll
-    for (int j = 0; j < SHARES; ++j) put_keys(lds, j);
+    for (int i = 0; i < 2 * SHARES; ++i) put(k[i / 2], k_scale[i / 2], lds + put_at[i / 2], i % 2);
   }
   __device__ __forceinline__ void put_values(uint32_t lds) const {
 #pragma unroll
-    for (int j = 0; j < SHARES; ++j) put_values(lds, j);
+    for (int i = 0; i < 2 * SHARES; ++i) put(v[i / 2], v_scale[i / 2], lds + put_at[i / 2], i % 2);
+  }
+  // Slot f of a stage of tile t, of which there are 4 SHARES + 2 at least: the values of tile t + 1 and the keys of tile t + 2 go to LDS, and the next ones of both are
+  // asked for, a little in every slot, so that matrix instructions go out between.
+  __device__ __forceinline__ void step(int f, const Span& span, int t, uint32_t v_to, uint32_t k_to) {
+    constexpr int U = 2 * SHARES;
+    if (f < U) put(v[f / 2], v_scale[f / 2], v_to + put_at[f / 2], f % 2);
+    else if (f == U) ask_values(span, t + 2);
+    else if (f <= 2 * U) put(k[(f - U - 1) / 2], k_scale[(f - U - 1) / 2], k_to + put_at[(f - U - 1) / 2], (f - U - 1) % 2);
+    else if (f == 2 * U + 1) ask_keys(span, t + 3);
   }
 };
 

@@ -24,7 +24,7 @@ template <typename T, int D> struct RowFeed {
   int64_t k_row, v_row;
   KLoader k_load;
   VLoader v_load;
-  template <class P, class S> __device__ __forceinline__ RowFeed(const WindowArgs& a, const P& at, const S& seq, int wave, int lane)
+  template <class P, class S> __device__ __forceinline__ RowFeed(const WindowArgs& a, const P& at, const S& seq, const Span&, int wave, int lane)
       : kh(a.k.at(at.b, at.kvh, seq.k0)), vh(a.v.at(at.b, at.kvh, seq.k0)), k_row(a.k.row), v_row(a.v.row), k_load(a.k.row, wave, lane), v_load(a.v.row, wave, lane) {}
   __device__ __forceinline__ typename KLoader::Pair keys(const Span& span, int t) { return k_load.of(span, kh, k_row, t); }
   __device__ __forceinline__ typename VLoader::Pair values(const Span& span, int t) { return v_load.of(span, vh, v_row, t); }
@@ -61,7 +61,7 @@ __global__ void __launch_bounds__(256) window_f32_kernel(Args a) {
 #pragma unroll
     for (int s = 0; s < STEPS; ++s) qf[s] = *reinterpret_cast<const typename Mat<T>::Frag*>(qp + (2 * s + row.h) * 16);
   }
-  Feed feed(a, at, seq, wave, lane);
+  Feed feed(a, at, seq, span, wave, lane);
   const typename KTile::RowReader k_read(lane);
   const typename VTile::ColumnReader v_read(lane);
   const uint32_t to = __builtin_amdgcn_readfirstlane(lds + uint32_t(wave) * 1024);
@@ -161,12 +161,13 @@ __global__ void __launch_bounds__(256, 2) window_pipe_kernel(Args a) {
   const Span span(a, row.i0 + len.shift, row.i1 + len.shift, len.k, Feed::STEP);
   const int n_tiles = (span.n + 1) / 2;
 
-  Feed feed(a, at, seq, wave, lane);
+  Feed feed(a, at, seq, span, wave, lane);
   const uint32_t to = __builtin_amdgcn_readfirstlane(lds + uint32_t(wave) * 1024);
   if constexpr (Feed::STRAIGHT) {
     if (n_tiles > 0) {
-      const auto k0 = feed.keys(span, 0), k1 = feed.keys(span, 1);
+      const auto k0 = feed.keys(span, 0);
       const auto v0 = feed.values(span, 0);
+      const auto k1 = feed.keys(span, 1);
 #pragma unroll
       for (int j = 0; j < LOADS; ++j) feed.ask_keys(k0, to, j);
 #pragma unroll
@@ -182,7 +183,7 @@ __global__ void __launch_bounds__(256, 2) window_pipe_kernel(Args a) {
     feed.ask_keys(span, 1);
     feed.ask_values(span, 1);
     feed.put_keys(lds + BYTES);
-    feed.ask_keys(span, 2);
+    feed.ask_keys(span, 2);                          // (the values of a tile are asked for behind its keys and in front of the next tile's)
   }
   bf16x8 qf[STEPS];
   {
@@ -313,8 +314,8 @@ __global__ void __launch_bounds__(256, 2) window_pipe_kernel(Args a) {
     __syncthreads();                                 // all parts are, and every wave has left K(t) and V(t - 1)
     const int t2 = t + 2 < n_tiles ? t + 2 : t + 1;  // behind the last tile that once more, into a buffer that nothing reads
     const uint32_t k_to = t & 1 ? BYTES : 0, v_to = (t & 1 ? 2 : 3) * BYTES;
-    const auto ks = [&] { if constexpr (Feed::STRAIGHT) return feed.keys(span, t2); else return 0; }();
     const auto vs = [&] { if constexpr (Feed::STRAIGHT) return feed.values(span, t + 1); else return 0; }();
+    const auto ks = [&] { if constexpr (Feed::STRAIGHT) return feed.keys(span, t2); else return 0; }();
 #pragma unroll
     for (int s = 0; s < STEPS; ++s) k_at[s] += k_step;
     k_step = -k_step;
@@ -332,19 +333,8 @@ __global__ void __launch_bounds__(256, 2) window_pipe_kernel(Args a) {
     settle(s1, w1, sum);
     mask(2 * t + 2, s0);
     stage(std::integral_constant<int, 1>{}, w1, s1, s0, w0, sum, [&](int f) {
-      if constexpr (!Feed::STRAIGHT) {               // V(t + 1) and K(t + 2) to LDS, a load's share at a time
-        constexpr int NF = 2 * STEPS, SHARES = 2 * Feed::SHARES;
-        if (f % (NF / SHARES) == 0) {
-          const int j = f / (NF / SHARES);
-          if (j < Feed::SHARES) feed.put_values(lds + v_to, j);
-          else feed.put_keys(lds + k_to, j - Feed::SHARES);
-        }
-      }
+      if constexpr (!Feed::STRAIGHT) feed.step(f, span, t, lds + v_to, lds + k_to);          // V(t + 1) and K(t + 2) to LDS, V(t + 2) and K(t + 3) asked for
     });
-    if constexpr (!Feed::STRAIGHT) {
-      feed.ask_values(span, t + 2);
-      feed.ask_keys(span, t + 3);
-    }
     settle(s0, w0, sum);
     mask(2 * t + 3, s1);
 #pragma unroll

@@ -32,6 +32,7 @@ CASES = {
     "pieces_d64": (4, 4, 64, 16, [130, 64, 3], [130, 500, 777], -1, 0, 0, 4),
     "pieces_with_window": (8, 2, 64, 32, [150, 90, 31], [150, 400, 300], 70, 10, 0, 0),
     "many_streams": (4, 2, 64, 16, [i % 2 for i in range(300)], [(7 * i) % 90 + 1 for i in range(300)], -1, 0, 1, 0),
+    "long_small_pages": (4, 1, 64, 16, [1, 2, 1], [3000, 1500, 40], -1, 0, 0, 0),
     "wide_group": (24, 1, 128, 64, [3, 9], [100, 300], -1, 0, 0, 0),
     # enough blocks of 128 rows: the kernel of long calls
     "blocks": (16, 16, 128, 64, [500, 129, 1], [500, 700, 300], -1, 0, 0, 0),
@@ -42,6 +43,8 @@ CASES = {
     "blocks_window": (32, 8, 128, 64, [300, 260, 90], [300, 1200, 600], 130, 0, 0, 0),
     "blocks_window_and_first_keys": (24, 12, 64, 32, [300, 260, 90], [300, 900, 600], 77, 40, 0, 0),
     "blocks_many": (16, 8, 128, 32, [(29 * i) % 70 for i in range(70)], [(29 * i) % 70 + 3 * i for i in range(70)], -1, 0, 0, 0),
+    "blocks_long_small_pages": (32, 32, 64, 16, [130, 260], [2600, 1800], -1, 0, 0, 0),
+    "blocks_long_small_pages_window": (32, 16, 128, 16, [130, 260], [2600, 1800], 1500, 33, 0, 0),
     "blocks_more_queries_than_keys": (64, 64, 64, 16, [140, 130], [70, 3], -1, 0, 0, 0),
 }
 
