@@ -468,9 +468,9 @@ template <typename T, int N> __device__ __forceinline__ void store_row(bool real
     }
 }
 
-// Into how many work-groups a block of the backward pass is split that has `tiles` tiles to go over: as many as make 256 of `blocks`, four tiles each at least.
-inline int share(int64_t blocks, int64_t tiles) {
-  int64_t n = blocks ? 256 / blocks : 1;
+// Into how many work-groups a block of the backward pass is split that has `tiles` tiles to go over: as many as make `all` of `blocks`, four tiles each at least.
+inline int share(int64_t blocks, int64_t tiles, int64_t all = 256) {
+  int64_t n = blocks ? all / blocks : 1;
   if (n > tiles / 4) n = tiles / 4;
   return n < 1 ? 1 : int(n);
 }

@@ -405,18 +405,25 @@ template <int N> __device__ __forceinline__ void load_sums(const float2* from, i
 // 594 TFLOP/s, 31 %: of 512 places on the CUs the ragged lengths fill 368, and two work-groups a CU do not fill what one of them waits for.  P and dS are one bf16
 // term each: dk and dv are 2.35e-3 from 64 bits in 2-norm where rounding the results alone costs 1.65e-3, and a second term would be half of this kernel's products
 // again.  In fp32 one work-group a CU, whose 263 registers at d = 64 are seven more than two allow (4 000 tokens x 16 heads: 741 us, 54 %; d = 128: 1 490, 52 %).
-template <typename T, int D, bool PACKED>
-__global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) window_dkv_kernel(WindowArgs a) {
+//
+// QG: groups of four waves that take the tiles of queries in turn, each with tiles of its own; what they find is added up in the end.  Two for packed sequences in bf16: the
+// blocks of the first keys of long sequences, which under a causal mask have several times the work of others, are done in half the time, and the CU has as many
+// waves as with two work-groups of one.
+template <typename T, int D, bool PACKED, int QG>
+__global__ void __launch_bounds__(256 * QG, sizeof(T) == 2 ? 2 / QG : 1) window_dkv_kernel(WindowArgs a) {
   constexpr bool BF16 = sizeof(T) == 2, V_LDS = BF16;
   constexpr int NW = 4, BN = 32 * NW, QN = BF16 && D == 64 ? 64 : 32, HALVES = QN / 32;
   using QTile = Tile<T, D, QN, NW, false>;
   using VTile = Tile<T, D, BN, NW, false>;
   constexpr int STEPS = QTile::STEPS;
-  __shared__ __attribute__((aligned(1024))) char tiles[4 * QTile::BYTES + (V_LDS ? VTile::BYTES : 0)];
-  __shared__ __attribute__((aligned(1024))) float2 row_sums[2][QN];
-  const uint32_t lds = uint32_t(reinterpret_cast<uintptr_t>((LDS_PTR(void))(tiles))), lds_v = lds + 4 * QTile::BYTES;
+  __shared__ __attribute__((aligned(1024))) char tiles[QG * 4 * QTile::BYTES + (V_LDS ? VTile::BYTES : 0)];
+  __shared__ __attribute__((aligned(1024))) float2 all_sums[QG][2][QN];
+  const int lane = threadIdx.x & 63, all_waves = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), qg = QG == 1 ? 0 : all_waves / NW, wave = all_waves - qg * NW;
+  const int n = lane & 31, h = lane >> 5;
+  float2 (&row_sums)[2][QN] = all_sums[qg];
+  const uint32_t lds_tiles = uint32_t(reinterpret_cast<uintptr_t>((LDS_PTR(void))(tiles))), lds = lds_tiles + uint32_t(qg * 4 * QTile::BYTES);
+  const uint32_t lds_v = lds_tiles + QG * 4 * QTile::BYTES;
   const uint32_t lds_sums = uint32_t(reinterpret_cast<uintptr_t>((LDS_PTR(void))(row_sums)));
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 31, h = lane >> 5;
 
   const PlaceOf<PACKED> at(a, blockIdx.x);
   const int i = a.by_splits(at.blk), split = at.blk - i * a.key_splits, bh = at.bh, b = at.b, kvh = at.kvh;
@@ -441,11 +448,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) window_dkv_kernel
   const char *q_at = a.q.at(b, kvh * a.group + head, seq.q0 + start), *g_at = a.d_o.at(b, kvh * a.group + head, seq.q0 + start);
   const int64_t q_step = QN * a.q.row, g_step = QN * a.d_o.row, q_back = a.q.head - per_head * q_step, g_back = a.d_o.head - per_head * g_step;
   const float2* sums_at = a.sums + (int64_t(b) * a.heads + kvh * a.group + head) * a.n_q + seq.q0 + start;
-  auto issue = [&](int buf) {
-    const uint32_t to = lds + uint32_t(buf * 2 * QTile::BYTES);
-    q_load.issue(q_at, hi - begin, a.q.row, to, wave);
-    g_load.issue(g_at, hi - begin, a.d_o.row, to + QTile::BYTES, wave);
-    if (wave == 0) load_sums<QN>(sums_at, hi - begin, lds_sums + uint32_t(buf * QN * 8), lane);
+  auto pass = [&] {
     begin += QN;
     q_at += q_step;
     g_at += g_step;
@@ -457,12 +460,21 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) window_dkv_kernel
       sums_at += a.n_q - per_head * QN;
     }
   };
+  auto issue = [&](int buf) {
+    const uint32_t to = lds + uint32_t(buf * 2 * QTile::BYTES);
+    q_load.issue(q_at, hi - begin, a.q.row, to, wave);
+    g_load.issue(g_at, hi - begin, a.d_o.row, to + QTile::BYTES, wave);
+    if (wave == 0) load_sums<QN>(sums_at, hi - begin, lds_sums + uint32_t(buf * QN * 8), lane);
+#pragma unroll
+    for (int i = 0; i < QG; ++i) pass();
+  };
+  if (QG == 2 && qg) pass();
   if (tiles_n > 0) {
-    if (V_LDS) {
+    if (V_LDS && qg == 0) {
       const typename VTile::Loader v_load(a.v.row, wave, lane);
       v_load.issue(a.v.at(b, kvh, seq.k0 + j0), keys, a.v.row, lds_v, wave);
     }
-    issue(0);
+    if (qg < tiles_n) issue(0);
   }
   typename Mat<T>::Frag kf[STEPS], vf[V_LDS ? 1 : STEPS];
   {
@@ -478,15 +490,21 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) window_dkv_kernel
   clear(dv);
   const float c2 = a.scale * LOG2E;
   int row0 = start;                                  // first query of this tile
+  auto next_row0 = [&] {
+    row0 += QN;
+    if (row0 >= hi) row0 = lo;
+  };
+  if (QG == 2 && qg) next_row0();
   // bf16: LDS addresses of a lane's operands by rows and by columns in this tile's queries, by rows in the values; the others follow by XOR of the chunk, so that
   // three registers do for forty.
   uint32_t row_at = lds + read.at + ((uint32_t(h) ^ read.sw) * 16), col_at = lds + cols.at[0][0], val_at = lds_v + uint32_t(wave * 32 * QTile::RB) + read.at + ((uint32_t(h) ^ read.sw) * 16);
   int to_other = 2 * QTile::BYTES;
-  for (int t = 0; t < tiles_n; ++t) {
+  for (int t = 0; t * QG < tiles_n; ++t) {
     wait_loads();
     __syncthreads();
     const uint32_t buf = lds + uint32_t((t & 1) * 2 * QTile::BYTES);
-    if (t + 1 < tiles_n) issue((t + 1) & 1);
+    if ((t + 1) * QG + qg < tiles_n) issue((t + 1) & 1);
+    if (QG == 2 && t * QG + qg >= tiles_n) break;    // an odd number of tiles: the other group has the last one
     auto part = [&](auto half_) __attribute__((always_inline)) {
       constexpr int half = decltype(half_)::value;
       const int first = row0 + 32 * half, p0 = first + len.shift;          // first query of the 32
@@ -597,11 +615,35 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) window_dkv_kernel
     };
     part(std::integral_constant<int, 0>{});
     if constexpr (HALVES == 2) part(std::integral_constant<int, 1>{});
-    row0 += QN;
-    if (row0 >= hi) row0 = lo;
+#pragma unroll
+    for (int i = 0; i < QG; ++i) next_row0();
     row_at += to_other;
     col_at += to_other;
     to_other = -to_other;
+  }
+  if constexpr (QG == 2) {                           // the first group adds up keys' gradients, the second those of values
+    static_assert(D / 2 * 64 * 4 * NW <= QG * 4 * QTile::BYTES, "four waves' sums fit where the tiles were");
+    float* all = reinterpret_cast<float*>(tiles) + (wave * (D / 2) * 64 + lane);
+    auto give = [&](const f32x16 (&x)[D / 32]) {
+#pragma unroll
+      for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) all[(c * 16 + i) * 64] = x[c][i];
+    };
+    auto take = [&](f32x16 (&x)[D / 32]) {
+#pragma unroll
+      for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[c][i] += all[(c * 16 + i) * 64];
+    };
+    __syncthreads();
+    if (qg == 1) give(dk);
+    __syncthreads();
+    if (qg == 0) take(dk);
+    __syncthreads();
+    if (qg == 0) give(dv);
+    __syncthreads();
+    if (qg == 1) take(dv);
   }
   // A key that no window has in it may hold anything: its products may be too.
   if (!(key <= len.k - 1 + a.right && key >= len.shift - a.left)) {
@@ -614,8 +656,8 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) window_dkv_kernel
     for (int c = 0; c < D / 32; ++c)
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        mine[(c * 16 + i) * 64] = dk[c][i];
-        mine[(D / 2 + c * 16 + i) * 64] = dv[c][i];
+        if (qg == 0) mine[(c * 16 + i) * 64] = dk[c][i];
+        if (QG == 1 || qg == 1) mine[(D / 2 + c * 16 + i) * 64] = dv[c][i];
       }
     return;
   }
@@ -625,8 +667,8 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) window_dkv_kernel
 #pragma unroll
     for (int i = 0; i < 16; i += 4) {
       const float x[4] = {dk[c][i], dk[c][i + 1], dk[c][i + 2], dk[c][i + 3]}, y[4] = {dv[c][i], dv[c][i + 1], dv[c][i + 2], dv[c][i + 3]};
-      store_four<T>(a.dk.at(b, kvh, seq.k0 + key), 32 * c + 2 * i + 4 * h, x, a.scale);
-      store_four<T>(a.dv.at(b, kvh, seq.k0 + key), 32 * c + 2 * i + 4 * h, y, 1.f);
+      if (qg == 0) store_four<T>(a.dk.at(b, kvh, seq.k0 + key), 32 * c + 2 * i + 4 * h, x, a.scale);
+      if (QG == 1 || qg == 1) store_four<T>(a.dv.at(b, kvh, seq.k0 + key), 32 * c + 2 * i + 4 * h, y, 1.f);
     }
 }
 
@@ -765,7 +807,8 @@ static int launch(const char* call, const WindowArgs& args, hipStream_t st) {
   if (a.n_k == 0) return DFS_OK;
   a.by_splits = Div(uint32_t(a.key_splits));
   a.set_blocks(blocks_of<PACKED>(a, a.n_k) * a.key_splits);
-  window_dkv_kernel<T, D, PACKED><<<unsigned(a.blocks * seqs), 256, 0, st>>>(a);
+  constexpr int QG = PACKED && sizeof(T) == 2 ? 2 : 1;
+  window_dkv_kernel<T, D, PACKED, QG><<<unsigned(a.blocks * seqs), 256 * QG, 0, st>>>(a);
   if (int rc = launch_status(call)) return rc;
   if constexpr (!PACKED)
     if (a.first_tiles > 0) {
