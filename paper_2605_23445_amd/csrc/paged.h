@@ -5,18 +5,22 @@
 
 namespace dfs {
 
+typedef int i32x2 __attribute__((ext_vector_type(2)));
+
 struct PagedArgs : WindowArgs {                      // n_k: what the table has room for
   PageArgs pages;
   int32_t unit;                                      // pieces that are dealt out together
   int32_t least;                                     // units that a work-group takes at least
+  int32_t row_bits;                                  // a block has 1 << row_bits rows
 };
 
 // Eight bytes of e4m3 times a power of two, exactly.
-__device__ __forceinline__ bf16x8 eight(uint32_t a, uint32_t b, float scale) {
-  const bf16x2 p = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, false), q = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, true);
-  const bf16x2 r = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, false), s = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, true);
+__device__ __forceinline__ bf16x8 eight(uint32_t a, uint32_t b, float scale_a, float scale_b) {
+  const bf16x2 p = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale_a, false), q = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale_a, true);
+  const bf16x2 r = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale_b, false), s = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale_b, true);
   return bf16x8{p[0], p[1], q[0], q[1], r[0], r[1], s[0], s[1]};
 }
+__device__ __forceinline__ bf16x8 eight(uint32_t a, uint32_t b, float scale) { return eight(a, b, scale, scale); }
 
 // The pages of a sequence, 64 entries of the table at a time, one a lane: where a page's keys and values of a key head begin, and their scales.
 template <bool E4M3> struct Entries {

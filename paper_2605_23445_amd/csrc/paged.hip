@@ -16,7 +16,7 @@ namespace dfs {
 
 constexpr int GROUPS = 256;                          // work-groups: one a CU
 
-// A sequence's rows and keys, its blocks of 32 rows, and the units of each of these with each key head (the pieces of all its rows together, one at least).
+// A sequence's rows and keys, its blocks of 32 or 16 rows, and the units of each of these with each key head (the pieces of all its rows together, one at least).
 struct PagedSeq {
   int q0, n, k, blocks, units;
   PagedSeq() = default;
@@ -25,7 +25,7 @@ struct PagedSeq {
     q0 = from;
     n = max_of(0, to - from);
     k = max_of(0, min_of(k_, a.n_k));
-    blocks = (n * a.group + 31) / 32;
+    blocks = (n * a.group + (1 << a.row_bits) - 1) >> a.row_bits;
     const Span all(a, k - n, k - 1, k, 32);
     units = max_of(1, (all.n + a.unit - 1) / a.unit);
   }
@@ -76,16 +76,244 @@ template <typename T, int D, bool E4M3> struct PageTile {
 // Waves of a work-group: as many as have room in LDS for two tiles of keys and two of values each.
 template <typename T, int D, bool E4M3> constexpr int paged_waves() { return 1024 / (D * (E4M3 ? 1 : int(sizeof(T)))) < 8 ? 1024 / (D * (E4M3 ? 1 : int(sizeof(T)))) : 8; }
 
-template <typename T, int D, bool E4M3, bool SMALL>
-__global__ void __launch_bounds__((64 * paged_waves<T, D, E4M3>()), 1) paged_split_kernel(PagedArgs a) {
-  constexpr int NW = paged_waves<T, D, E4M3>(), NT = 64 * NW, REGS = D / 2;
+// The arithmetic of a wave: 32 rows, or 16, against the 32 keys of a tile.  A lane holds, of the logits and of the sums, one row's (n): with 32 rows keys and channels 8 (i / 4) + 4 h +
+// i % 4 of 32, h = lane / 32, with 16 rows 4 g + i of 16, g = lane / 16.  Bytes become operands on the way from LDS: of keys a lane reads 16 channels at once, for
+// two products; of values the transposing read hands it eight keys of a channel.  H: scales of a tile, of 16 rows each or of all.
+template <typename T, int D, bool E4M3, int H> struct Wave32 {
   using PT = PageTile<T, D, E4M3>;
-  constexpr int LOADS = PT::LOADS, STEPS = D * int(sizeof(T)) / 32, BYTES = PT::BYTES;
-  static_assert(REGS * 64 * 4 <= 4 * BYTES || !E4M3, "a wave's sums fit where its tiles were");
+  using Frag = typename Mat<T>::Frag;
+  static constexpr int ROWS = 32, STEPS = D * int(sizeof(T)) / 32, REGS = D / 2;
+  int lane, n, h;
+  Frag qf[STEPS];
+  f32x16 acc[D / 32], x;
+  Weights<T> w;
+  float m, l;
+  __device__ __forceinline__ Wave32(int lane_) : lane(lane_), n(lane_ & 31), h(lane_ >> 5) {}
+  __device__ __forceinline__ void start(const char* q) {
+#pragma unroll
+    for (int st = 0; st < STEPS; ++st) qf[st] = *reinterpret_cast<const Frag*>(q + (E4M3 ? st / 2 * 4 + 2 * h + st % 2 : 2 * st + h) * 16);
+    clear(acc);
+    m = -INFINITY;
+    l = 0.f;
+  }
+  __device__ __forceinline__ void wait_queries() {
+#pragma unroll
+    for (int st = 0; st < STEPS; ++st) asm volatile("" : "+v"(qf[st]));
+  }
+  __device__ __forceinline__ void keys(uint32_t buf, const float (&scale)[H]) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] = 0.f;
+    if constexpr (E4M3) {
+      const float mine = n < 16 ? scale[0] : scale[H - 1];
+      u32x4 raw[STEPS / 2];
+#pragma unroll
+      for (int st = 0; st < STEPS / 2; ++st)
+        raw[st] = *reinterpret_cast<LDS_PTR(const u32x4)>(buf + uint32_t(n * PT::RB + ((2 * st + h) ^ PT::template swizzle<false>(n)) * 16));
+      __builtin_amdgcn_sched_barrier(0);             // operands that are worked out early drive the accumulators to scratch
+#pragma unroll
+      for (int st = 0; st < STEPS / 2; ++st) {
+        x = Mat<T>::mma(eight(raw[st][0], raw[st][1], mine), qf[2 * st], x);
+        x = Mat<T>::mma(eight(raw[st][2], raw[st][3], mine), qf[2 * st + 1], x);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    } else {
+      const typename PT::Rows::RowReader read(lane);
+#pragma unroll
+      for (int st = 0; st < STEPS; ++st) x = Mat<T>::mma(read.get(buf, 0, st), qf[st], x);
+    }
+  }
+  // Logits to weights; p: the row's position.
+  __device__ __forceinline__ void weigh(const PagedArgs& a, const Span& span, int t, int p, float c2) {
+    if (!span.whole(t)) span.mask(a, t, p, h, x, -INFINITY);
+    float mx = x[0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) mx = fmaxf(mx, x[i]);
+    const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+    const float m_new = fmaxf(m, fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * c2), ref = m_new == -INFINITY ? 0.f : m_new;
+    if (__builtin_amdgcn_ballot_w64(m_new > m)) {
+      const float alpha = __builtin_amdgcn_exp2f(m - ref);
+      m = m_new;
+      l *= alpha;
+#pragma unroll
+      for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[c][i] *= alpha;
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      x[i] = __builtin_amdgcn_exp2f(fmaf(x[i], c2, -ref));
+      l += x[i];
+    }
+    w.set(x);
+  }
+  __device__ __forceinline__ void values(uint32_t buf, const float (&scale)[H]) {
+    if constexpr (E4M3) {
+      const int i = (lane & 15) >> 1, row = 4 * h + i + (i < 4 ? 0 : 4);                     // 8 rows of 16 channels from 16 lanes, 8 rows of one channel to each
+      i32x2 raw[2][D / 32];
+#pragma unroll
+      for (int half = 0; half < 2; ++half)
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c) {
+          const uint32_t chunk = uint32_t((2 * c + ((lane >> 4) & 1)) ^ PT::template swizzle<true>(row));
+          raw[half][c] = __builtin_amdgcn_ds_read_tr8_b64_v2i32(reinterpret_cast<LDS_PTR(i32x2)>(buf + uint32_t((16 * half + row) * PT::RB) + chunk * 16 + (lane & 1) * 8));
+        }
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int half = 0; half < 2; ++half)
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c) {
+          acc[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(eight(uint32_t(raw[half][c][0]), uint32_t(raw[half][c][1]), scale[half < H ? half : 0]),
+                                                           __builtin_bit_cast(bf16x8, w.p[half]), acc[c], 0, 0, 0);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+    } else {
+      const typename PT::Columns::ColumnReader read(lane);
+      read.mma(buf, 0, w, acc);
+    }
+  }
+  __device__ __forceinline__ void finish() {
+    const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
+    l = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+  }
+  __device__ __forceinline__ float sum(int reg) const { return acc[reg / 16][reg % 16]; }
+  __device__ __forceinline__ int channel(int reg) const { return reg / 16 * 32 + reg % 16 * 2 + 4 * h; }         // of the first of four
+  __device__ __forceinline__ bool first() const { return h == 0; }
+};
+
+template <int D, bool E4M3, int H> struct Wave16 {
+  using PT = PageTile<uint16_t, D, E4M3>;
+  static constexpr int ROWS = 16, STEPS = D / 32, REGS = D / 4;
+  int lane, n, g;
+  bf16x8 qf[STEPS];
+  f32x4 acc[D / 16], x[2];
+  u32x4 w;
+  float m, l;
+  __device__ __forceinline__ Wave16(int lane_) : lane(lane_), n(lane_ & 15), g(lane_ >> 4) {}
+  __device__ __forceinline__ void start(const char* q) {
+#pragma unroll
+    for (int st = 0; st < STEPS; ++st) qf[st] = *reinterpret_cast<const bf16x8*>(q + (E4M3 ? (st / 2 * 4 + g) * 2 + st % 2 : 4 * st + g) * 16);
+#pragma unroll
+    for (int c = 0; c < D / 16; ++c) acc[c] = f32x4{0.f, 0.f, 0.f, 0.f};
+    m = -INFINITY;
+    l = 0.f;
+  }
+  __device__ __forceinline__ void wait_queries() {
+#pragma unroll
+    for (int st = 0; st < STEPS; ++st) asm volatile("" : "+v"(qf[st]));
+  }
+  __device__ __forceinline__ void keys(uint32_t buf, const float (&scale)[H]) {
+    constexpr int READS = E4M3 ? D / 64 : STEPS;
+    u32x4 raw[2][READS];
+#pragma unroll
+    for (int half = 0; half < 2; ++half)
+#pragma unroll
+      for (int st = 0; st < READS; ++st) {
+        const int row = 16 * half + n;
+        raw[half][st] = *reinterpret_cast<LDS_PTR(const u32x4)>(buf + uint32_t(row * PT::RB + ((4 * st + g) ^ PT::template swizzle<false>(row)) * 16));
+      }
+    x[0] = x[1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int st = 0; st < READS; ++st)
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const u32x4 r = raw[half][st];
+        if constexpr (E4M3) {
+          x[half] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(eight(r[0], r[1], scale[half < H ? half : 0]), qf[2 * st], x[half], 0, 0, 0);
+          x[half] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(eight(r[2], r[3], scale[half < H ? half : 0]), qf[2 * st + 1], x[half], 0, 0, 0);
+        } else {
+          x[half] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, r), qf[st], x[half], 0, 0, 0);
+        }
+      }
+  }
+  static __device__ __forceinline__ float across(float v, bool add) {    // largest or sum over the four lanes of a row
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = add ? __uint_as_float(a[0]) + __uint_as_float(a[1]) : fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return add ? __uint_as_float(b[0]) + __uint_as_float(b[1]) : fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+  }
+  __device__ __forceinline__ void weigh(const PagedArgs& a, const Span& span, int t, int p, float c2) {
+    if (!span.whole(t)) {
+      const int key = span.begin(t) + 4 * g, top = min_of(span.end(t) - 1, p), low = t < span.n_first ? 0 : p - a.left, more = t < span.n_first ? 0 : a.sinks;
+#pragma unroll
+      for (int half = 0; half < 2; ++half)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int j = key + 16 * half + i;
+          x[half][i] = ((j <= top) & ((j >= low) | (j < more))) ? x[half][i] : -INFINITY;
+        }
+    }
+    float mx = fmaxf(x[0][0], x[1][0]);
+#pragma unroll
+    for (int i = 1; i < 4; ++i) mx = fmaxf(mx, fmaxf(x[0][i], x[1][i]));
+    const float m_new = fmaxf(m, across(mx, false) * c2), ref = m_new == -INFINITY ? 0.f : m_new;
+    if (__builtin_amdgcn_ballot_w64(m_new > m)) {
+      const float alpha = __builtin_amdgcn_exp2f(m - ref);
+      m = m_new;
+      l *= alpha;
+#pragma unroll
+      for (int c = 0; c < D / 16; ++c)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[c][i] *= alpha;
+    }
+#pragma unroll
+    for (int half = 0; half < 2; ++half)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        x[half][i] = __builtin_amdgcn_exp2f(fmaf(x[half][i], c2, -ref));
+        l += x[half][i];
+        if (i % 2) {
+          const bf16x2 pair = {(__bf16)x[half][i - 1], (__bf16)x[half][i]};
+          w[2 * half + i / 2] = __builtin_bit_cast(uint32_t, pair);
+        }
+      }
+  }
+  __device__ __forceinline__ void values(uint32_t buf, const float (&scale)[H]) {
+    if constexpr (E4M3) {
+      const int i = (lane & 15) >> 1, row = 4 * g + i + (i < 4 ? 0 : 12);                    // keys 4 g .. 4 g + 3 of both halves
+      i32x2 raw[D / 16];
+#pragma unroll
+      for (int c = 0; c < D / 16; ++c)
+        raw[c] = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+            reinterpret_cast<LDS_PTR(i32x2)>(buf + uint32_t(row * PT::RB) + uint32_t(c ^ PT::template swizzle<true>(row)) * 16 + (lane & 1) * 8));
+#pragma unroll
+      for (int c = 0; c < D / 16; ++c) {
+        const bf16x8 v = eight(uint32_t(raw[c][0]), uint32_t(raw[c][1]), scale[0], scale[H - 1]);
+        acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, __builtin_bit_cast(bf16x8, w), acc[c], 0, 0, 0);
+      }
+    } else {
+      const int row = 4 * g + ((lane & 15) >> 2), byte = (lane & 1) * 8;
+#pragma unroll
+      for (int c = 0; c < D / 16; ++c) {
+        const int chunk = 2 * c + ((lane & 3) >> 1);
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<LDS_PTR(s16x4)>(buf + uint32_t(row * PT::RB + (chunk ^ PT::template swizzle<true>(row)) * 16 + byte)));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            reinterpret_cast<LDS_PTR(s16x4)>(buf + uint32_t((row + 16) * PT::RB + (chunk ^ PT::template swizzle<true>(row + 16)) * 16 + byte)));
+        acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7)), __builtin_bit_cast(bf16x8, w), acc[c], 0, 0, 0);
+      }
+    }
+  }
+  __device__ __forceinline__ void finish() { l = across(l, true); }
+  __device__ __forceinline__ float sum(int reg) const { return acc[reg / 4][reg % 4]; }
+  __device__ __forceinline__ int channel(int reg) const { return reg / 4 * 16 + 4 * g; }
+  __device__ __forceinline__ bool first() const { return g == 0; }
+};
+
+template <int ROWS, typename T, int D, bool E4M3, int H> struct WaveOf { using type = Wave32<T, D, E4M3, H>; };
+template <typename T, int D, bool E4M3, int H> struct WaveOf<16, T, D, E4M3, H> { using type = Wave16<D, E4M3, H>; };
+
+template <int ROWS, typename T, int D, bool E4M3, bool SMALL>
+__global__ void __launch_bounds__((64 * paged_waves<T, D, E4M3>()), 1) paged_split_kernel(PagedArgs a) {
+  constexpr int NW = paged_waves<T, D, E4M3>(), NT = 64 * NW, H = SMALL ? 2 : 1, RPH = 32 / H;        // H: pages of a piece
+  using Wave = typename WaveOf<ROWS, T, D, E4M3, H>::type;
+  using PT = PageTile<T, D, E4M3>;
+  constexpr int LOADS = PT::LOADS, BYTES = PT::BYTES, REGS = Wave::REGS;
+  static_assert(REGS * 64 * 4 <= 4 * BYTES, "a wave's sums fit where its tiles were");
   __shared__ __attribute__((aligned(1024))) char tiles[NW * 4 * BYTES];
-  __shared__ float s_m[NW][32], s_l[NW][32];
+  __shared__ float s_m[NW][ROWS], s_l[NW][ROWS];
   __shared__ int s_sums[NW], s_first[5];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = lane & 31, h = lane >> 5;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  Wave wv(lane);
+  const int n = wv.n;
   const uint32_t lds = uint32_t(reinterpret_cast<uintptr_t>((LDS_PTR(void))(tiles))) + uint32_t(wave * 4 * BYTES);
 
   const Deal<NT> deal(a, s_sums);
@@ -131,7 +359,7 @@ __global__ void __launch_bounds__((64 * paged_waves<T, D, E4M3>()), 1) paged_spl
       continue;
     }
     const int item = off / seq.units, u0 = off - item * seq.units, u1 = min_of(seq.units, u0 + end - at), blk = item / a.heads_kv, kvh = item - blk * a.heads_kv;
-    const int r0 = blk * 32, rows = min_of(seq.n * a.group - r0, 32), shift = seq.k - seq.n;
+    const int r0 = blk * ROWS, rows = min_of(seq.n * a.group - r0, ROWS), shift = seq.k - seq.n;
     const int i0 = query_of(a, r0), i1 = query_of(a, r0 + rows - 1);
     const Span span(a, i0 + shift, i1 + shift, seq.k, 32);
     const int t_end = min_of(span.n, u1 * a.unit), lo = max_of(0, i0 + shift - a.left);        // lo: first key of the window
@@ -140,7 +368,6 @@ __global__ void __launch_bounds__((64 * paged_waves<T, D, E4M3>()), 1) paged_spl
 
     Entries<E4M3> entries(a, s);
     // Where a piece lies: on one page, or with pages of 16 rows on two.
-    constexpr int H = SMALL ? 2 : 1, RPH = 32 / H;
     uint64_t k_at[H], v_at[H];
     int there[H], key = 0;
     float k_scale[2][H], v_scale[2][H];              // of the two pieces that are on their way
@@ -187,16 +414,7 @@ __global__ void __launch_bounds__((64 * paged_waves<T, D, E4M3>()), 1) paged_spl
     };
     auto ask_values = [&](int parity) __attribute__((always_inline)) { ask(v_at, a.pages.v.row, v_off, parity, true); };
     int t = u0 * a.unit + wave;
-    typename Mat<T>::Frag qf[STEPS];
-    {
-      const char* qp = a.q.at(0, qh, seq.q0 + qi);
-#pragma unroll
-      for (int st = 0; st < STEPS; ++st) {
-        // in 8 bits a lane reads 16 channels at once, for two products
-        const int chunk = E4M3 ? st / 2 * 4 + 2 * h + st % 2 : 2 * st + h;
-        qf[st] = *reinterpret_cast<const typename Mat<T>::Frag*>(qp + chunk * 16);
-      }
-    }
+    wv.start(a.q.at(0, qh, seq.q0 + qi));
     if (t < t_end) {
       ask_keys(t, 0);
       ask_values(0);
@@ -204,11 +422,7 @@ __global__ void __launch_bounds__((64 * paged_waves<T, D, E4M3>()), 1) paged_spl
       ask_values(1);
     }
     // The queries are waited for here, with what was asked for behind them, or the compiler does it in every piece and for all loads.
-#pragma unroll
-    for (int st = 0; st < STEPS; ++st) asm volatile("" : "+v"(qf[st]));
-    f32x16 acc[D / 32];
-    clear(acc);
-    float m = -INFINITY, l = 0.f;
+    wv.wait_queries();
     auto piece = [&](auto parity_) __attribute__((always_inline)) {
       constexpr int parity = decltype(parity_)::value;
       const uint32_t buf = lds + uint32_t(parity * 2 * BYTES);
@@ -216,76 +430,12 @@ __global__ void __launch_bounds__((64 * paged_waves<T, D, E4M3>()), 1) paged_spl
 #pragma unroll
       for (int i = 0; i < H; ++i) v_now[i] = v_scale[parity][i];
       wait_loads_but<3 * LOADS>();
-      f32x16 x;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) x[i] = 0.f;
-      if constexpr (E4M3) {
-        const float scale = n < 16 ? k_scale[parity][0] : k_scale[parity][H - 1];
-        u32x4 raw[STEPS / 2];
-#pragma unroll
-        for (int st = 0; st < STEPS / 2; ++st)
-          raw[st] = *reinterpret_cast<LDS_PTR(const u32x4)>(buf + uint32_t(n * PT::RB + ((2 * st + h) ^ PT::template swizzle<false>(n)) * 16));
-        __builtin_amdgcn_sched_barrier(0);           // operands that are worked out early drive the accumulators to scratch
-#pragma unroll
-        for (int st = 0; st < STEPS / 2; ++st) {
-          x = Mat<T>::mma(eight(raw[st][0], raw[st][1], scale), qf[2 * st], x);
-          x = Mat<T>::mma(eight(raw[st][2], raw[st][3], scale), qf[2 * st + 1], x);
-          __builtin_amdgcn_sched_barrier(0);
-        }
-      } else {
-        const typename PT::Rows::RowReader read(lane);
-#pragma unroll
-        for (int st = 0; st < STEPS; ++st) x = Mat<T>::mma(read.get(buf, 0, st), qf[st], x);
-      }
+      wv.keys(buf, k_scale[parity]);
       wait_reads();
       ask_keys(t + 2 * NW, parity);
-      if (!span.whole(t)) span.mask(a, t, p, h, x, -INFINITY);
-      float mx = x[0];
-#pragma unroll
-      for (int i = 1; i < 16; ++i) mx = fmaxf(mx, x[i]);
-      const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
-      const float m_new = fmaxf(m, fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * c2), ref = m_new == -INFINITY ? 0.f : m_new;
-      if (__builtin_amdgcn_ballot_w64(m_new > m)) {
-        const float alpha = __builtin_amdgcn_exp2f(m - ref);
-        m = m_new;
-        l *= alpha;
-#pragma unroll
-        for (int c = 0; c < D / 32; ++c)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) acc[c][i] *= alpha;
-      }
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        x[i] = __builtin_amdgcn_exp2f(fmaf(x[i], c2, -ref));
-        l += x[i];
-      }
-      Weights<T> w;
-      w.set(x);
+      wv.weigh(a, span, t, p, c2);
       wait_loads_but<3 * LOADS>();
-      if constexpr (E4M3) {
-        const int i = (lane & 15) >> 1, row = 4 * h + i + (i < 4 ? 0 : 4);                   // 8 rows of 16 channels from 16 lanes, 8 rows of one channel to each
-        typedef int i32x2 __attribute__((ext_vector_type(2)));
-        i32x2 raw[2][D / 32];
-#pragma unroll
-        for (int half = 0; half < 2; ++half)
-#pragma unroll
-          for (int c = 0; c < D / 32; ++c) {
-            const uint32_t chunk = uint32_t((2 * c + ((lane >> 4) & 1)) ^ PT::template swizzle<true>(row));
-            raw[half][c] = __builtin_amdgcn_ds_read_tr8_b64_v2i32(reinterpret_cast<LDS_PTR(i32x2)>(buf + BYTES + uint32_t((16 * half + row) * PT::RB) + chunk * 16 + (lane & 1) * 8));
-          }
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int half = 0; half < 2; ++half)
-#pragma unroll
-          for (int c = 0; c < D / 32; ++c) {
-            acc[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(eight(uint32_t(raw[half][c][0]), uint32_t(raw[half][c][1]), v_now[half < H ? half : 0]),
-                                                             __builtin_bit_cast(bf16x8, w.p[half]), acc[c], 0, 0, 0);
-            __builtin_amdgcn_sched_barrier(0);
-          }
-      } else {
-        const typename PT::Columns::ColumnReader read(lane);
-        read.mma(buf + BYTES, 0, w, acc);
-      }
+      wv.values(buf + BYTES, v_now);
       wait_reads();
       ask_values(parity);
     };
@@ -296,18 +446,15 @@ __global__ void __launch_bounds__((64 * paged_waves<T, D, E4M3>()), 1) paged_spl
       piece(std::integral_constant<int, 1>{});
     }
     wait_loads();                                    // the last ones, of nothing, still write zeros where the sums go
-    const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
-    l = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+    wv.finish();
     // The waves' sums meet where the tiles were; each wave joins a share of the channels.
     float* all = reinterpret_cast<float*>(tiles);
     __syncthreads();
 #pragma unroll
-    for (int c = 0; c < D / 32; ++c)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) all[(wave * REGS + c * 16 + i) * 64 + lane] = acc[c][i];
-    if (h == 0) {
-      s_m[wave][n] = m;
-      s_l[wave][n] = l;
+    for (int i = 0; i < REGS; ++i) all[(wave * REGS + i) * 64 + lane] = wv.sum(i);
+    if (wv.first()) {
+      s_m[wave][n] = wv.m;
+      s_l[wave][n] = wv.l;
     }
     __syncthreads();
     float top = s_m[0][n], total = 0.f, share_[NW];
@@ -321,12 +468,13 @@ __global__ void __launch_bounds__((64 * paged_waves<T, D, E4M3>()), 1) paged_spl
     }
     const bool whole = u0 == 0 && u1 == seq.units;
     const float f = !whole ? 1.f : total == 0.f ? 0.f : 1.f / total;
-    const int64_t slot = (int64_t(blockIdx.x) * 2 + (at != start)) * 32 + n;                 // a run has two ends: parts of two items at most
+    const int64_t slot = (int64_t(blockIdx.x) * 2 + (at != start)) * ROWS + n;                 // a run has two ends: parts of two items at most
     if (real) {
       char* out = whole ? a.o.at(0, qh, seq.q0 + qi) : reinterpret_cast<char*>(a.part + slot * D);
 #pragma unroll
-      for (int g = 0; g < REGS / NW; g += 4) {
-        const int reg = wave * (REGS / NW) + g, ch = reg / 16 * 32 + reg % 16 * 2 + 4 * h;
+      for (int i = 0; i < (REGS / 4 + NW - 1) / NW; ++i) {
+        const int reg = 4 * (i * NW + wave), ch = wv.channel(reg);
+        if (reg >= REGS) break;
         float x[4] = {};
 #pragma unroll
         for (int w = 0; w < NW; ++w)
@@ -335,7 +483,7 @@ __global__ void __launch_bounds__((64 * paged_waves<T, D, E4M3>()), 1) paged_spl
         if (whole) store_four<T>(out, ch, x, f);
         else store_four<float>(out, ch, x, f);
       }
-      if (wave == 0 && h == 0) {
+      if (wave == 0 && wv.first()) {
         if (!whole) a.part_sums[slot] = make_float2(top, total);
         else if (a.lse) a.lse[int64_t(qh) * a.n_q + seq.q0 + qi] = total == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(total)) * (1.f / LOG2E);
       }
@@ -346,7 +494,7 @@ __global__ void __launch_bounds__((64 * paged_waves<T, D, E4M3>()), 1) paged_spl
   }
 }
 
-// Joins the parts of an item: four rows a work-group, a thread takes four channels of a row and every so-manieth part; items in the order of blocks of 32 rows, as packed
+// Joins the parts of an item: four rows a work-group, a thread takes four channels of a row and every so-manieth part; items in the order of blocks of rows, as packed
 // sequences have them, and key heads.  Bound by a chain of trips to memory: lengths, the parts, the row.
 template <typename T, int D>
 __global__ void __launch_bounds__(256) paged_join_kernel(PagedArgs a, int row_groups) {
@@ -365,7 +513,7 @@ __global__ void __launch_bounds__(256) paged_join_kernel(PagedArgs a, int row_gr
   bool mine = false;
   for (int i = 0; i < deal.each && s < a.packed; ++i, ++s) {
     if (deal.each > 1) seq = PagedSeq(a, s);
-    blk = slot - int(uint32_t(seq.q0 * a.group) / 32) - s;
+    blk = slot - int(uint32_t(seq.q0 * a.group) >> a.row_bits) - s;
     mine = blk >= 0 && blk < seq.blocks;
     if (mine) break;
     base += seq.work(a);
@@ -383,11 +531,11 @@ __global__ void __launch_bounds__(256) paged_join_kernel(PagedArgs a, int row_gr
   __syncthreads();
   seq = PagedSeq(a, s_item[0], s_item[0] + s_item[1], s_item[2]);
   base = s_item[3];
-  blk = s_item[4];
+  const int first = s_item[4] << a.row_bits;
   const int g0 = base / deal.per, g1 = (base + seq.units - 1) / deal.per;
   if (g0 == g1 || g0 < 0 || g1 >= GROUPS) return;    // one work-group had it whole; (past the runs: where starts fall so far that 31 bits do not count all)
-  for (int n = (blockIdx.x - id * row_groups) * RB + in; blk * 32 + n - in < min_of(blk * 32 + 32, seq.n * a.group); n += row_groups * RB) {
-    const int r = min_of(blk * 32 + n, seq.n * a.group - 1), row = r - blk * 32;
+  for (int n = (blockIdx.x - id * row_groups) * RB + in; first + n - in < min_of(first + (1 << a.row_bits), seq.n * a.group); n += row_groups * RB) {
+    const int r = min_of(first + n, seq.n * a.group - 1), row = r - first;
     float top = -INFINITY, total = 0.f, x[4] = {};
     for (int g = g0 + set; g <= g1; g += U * SETS) {
       float2 ml[U];
@@ -395,7 +543,7 @@ __global__ void __launch_bounds__(256) paged_join_kernel(PagedArgs a, int row_gr
 #pragma unroll
       for (int u = 0; u < U; ++u) {                    // behind the last part that once more, with a weight of zero
         const int w = min_of(g + u * SETS, g1);
-        const int64_t i = (int64_t(w) * 2 + (w == g0 && base != w * deal.per)) * 32 + row;
+        const int64_t i = ((int64_t(w) * 2 + (w == g0 && base != w * deal.per)) << a.row_bits) + row;
         ml[u] = a.part_sums[i];
         y[u] = reinterpret_cast<const float4*>(a.part + i * D)[ch];
       }
@@ -422,7 +570,7 @@ __global__ void __launch_bounds__(256) paged_join_kernel(PagedArgs a, int row_gr
     s_x[set][in][ch] = make_float4(x[0], x[1], x[2], x[3]);
     if (ch == 0) s_ml[set][in] = make_float2(top, total);
     __syncthreads();
-    if (set == 0 && blk * 32 + n < seq.n * a.group) {
+    if (set == 0 && first + n < seq.n * a.group) {
 #pragma unroll
       for (int i = 1; i < SETS; ++i) top = fmaxf(top, s_ml[i][in].x);
       const float ref = top == -INFINITY ? 0.f : top;
@@ -513,7 +661,10 @@ int dfs_paged_attn_fwd(const dfs_paged* w, int dtype, const dfs_view* q, const d
   a.part = static_cast<float*>(ws);
   a.part_sums = reinterpret_cast<float2*>(static_cast<char*>(ws) + part_bytes(w));
   // work is counted in 31 bits
-  const int64_t items = (int64_t(a.group) * a.n_q / 32 + w->seqs) * w->heads_kv, pieces = a.n_k / 32 + 2;
+  // 16 rows where the sequences have no more on average: half of the matrix instructions and of the weights (48 streams of 4 heads a key head: XXX us)
+  const int64_t mean = (int64_t(a.group) * a.n_q + w->seqs - 1) / w->seqs;
+  a.row_bits = mean <= 16 && dtype == DFS_BF16 ? 4 : 5;
+  const int64_t items = ((int64_t(a.group) * a.n_q >> a.row_bits) + w->seqs) * w->heads_kv, pieces = a.n_k / 32 + 2;
   const bool bytes = pages->dtype == DFS_E4M3;
   const int row_bytes = w->d * (bytes ? 1 : elem_size(dtype));
   a.unit = 1024 / row_bytes < 8 ? 1024 / row_bytes : 8;                  // a piece for each wave
@@ -525,16 +676,20 @@ int dfs_paged_attn_fwd(const dfs_paged* w, int dtype, const dfs_view* q, const d
   if (whole) a.unit = 64;
   const hipStream_t st = as_stream(stream);
   // work-groups of an item's join, four rows a turn, by the rows that a sequence has on average
-  const int64_t mean = (int64_t(a.group) * a.n_q + w->seqs - 1) / w->seqs;
-  const int row_groups = mean < 32 ? int(mean + 3) / 4 : 8;
+  const int row_groups = mean < 1 << a.row_bits ? int(mean + 3) / 4 : 1 << a.row_bits >> 2;
   const unsigned joins = unsigned(items * row_groups);
   auto run = [&](auto t, auto d, auto b) {
     using T = decltype(t);
     constexpr int D = decltype(d)::value;
     constexpr bool E4M3 = decltype(b)::value;
     constexpr int NT = 64 * paged_waves<T, D, E4M3>();
-    if (a.pages.bits == 4) paged_split_kernel<T, D, E4M3, true><<<GROUPS, NT, 0, st>>>(a);
-    else paged_split_kernel<T, D, E4M3, false><<<GROUPS, NT, 0, st>>>(a);
+    auto of = [&](auto rows) {
+      if (a.pages.bits == 4) paged_split_kernel<decltype(rows)::value, T, D, E4M3, true><<<GROUPS, NT, 0, st>>>(a);
+      else paged_split_kernel<decltype(rows)::value, T, D, E4M3, false><<<GROUPS, NT, 0, st>>>(a);
+    };
+    if constexpr (sizeof(T) == 2)
+      if (a.row_bits == 4) return of(std::integral_constant<int, 16>{});
+    of(std::integral_constant<int, 32>{});
   };
   auto join = [&](auto t, auto d) { paged_join_kernel<decltype(t), decltype(d)::value><<<joins, 256, 0, st>>>(a, row_groups); };
   auto by_dim = [&](auto f) { w->d == 64 ? f(std::integral_constant<int, 64>{}) : f(std::integral_constant<int, 128>{}); };
