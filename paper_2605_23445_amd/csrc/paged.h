@@ -41,6 +41,7 @@ template <bool E4M3> struct Entries {
         const int64_t at = int64_t(id) * a.pages.heads_kv + kvh;
         ks = a.pages.k_scale[at];
         vs = a.pages.v_scale[at];
+        asm volatile("" : "+v"(ks), "+v"(vs));       // waited for here, or the compiler does it wherever they are used, and for all loads
       }
     }
     return i - first;

@@ -115,14 +115,17 @@ template <int D> struct ByteFeed {
       put_at[j] = uint32_t(row[j] * KTile::RB) + (uint32_t(2 * c) ^ uint32_t(KTile::swizzle(row[j]))) * 16;
     }
   }
-  static __device__ __forceinline__ u32x4 load(uint64_t at, uint32_t bytes, uint32_t off) {
+  static __device__ __forceinline__ u32x4 load(uint64_t at_, int rows, const View& view, uint32_t off) {
+    // (without these the descriptor is taken for one that differs from lane to lane, and the load becomes a loop)
+    const uint64_t at = uint64_t(uint32_t(__builtin_amdgcn_readfirstlane(int(at_ >> 32)))) << 32 | uint32_t(__builtin_amdgcn_readfirstlane(int(uint32_t(at_))));
+    const uint32_t bytes = uint32_t(__builtin_amdgcn_readfirstlane(rows)) * uint32_t(view.row);
     return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(__builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(at), 0, bytes, 0x00020000), off, 0, 0));
   }
   __device__ __forceinline__ void ask_keys(const Span& span, int t) {
 #pragma unroll
     for (int j = 0; j < SHARES; ++j) {
       place[j].find(a, entries, span, kvh, t, (j * NW + wave) * 4 / CH);
-      k[j] = load(place[j].k, uint32_t(place[j].rows) * uint32_t(a.pages.k.row), k_off[j]);
+      k[j] = load(place[j].k, place[j].rows, a.pages.k, k_off[j]);
       k_scale[j] = entries.of(entries.ks, place[j].lane);
       next_scale[j] = place[j].rows > 0 ? entries.of(entries.vs, place[j].lane) : 1.f;
     }
@@ -138,7 +141,7 @@ template <int D> struct ByteFeed {
         const int first = (j * NW + wave) * 4 / CH * 16;
         if (first >= unseen.from && first + 16 <= unseen.to) v_scale[j] = 1.f;
       }
-      v[j] = load(place[j].v, uint32_t(place[j].rows) * uint32_t(a.pages.v.row), off);
+      v[j] = load(place[j].v, place[j].rows, a.pages.v, off);
     }
   }
   // Half `h` of a thread's chunk to a tile.

@@ -308,6 +308,10 @@ __global__ void __launch_bounds__(256, 2) window_pipe_kernel(Args a) {
     all_weights(s0, w0, sum);
     settle(s0, w0, sum);
   }
+  if constexpr (!Feed::STRAIGHT) {                   // the queries are waited for here, or the compiler does it in every tile and for all loads
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) asm volatile("" : "+v"(qf[s]));
+  }
   // Tile t's values and tile t + 1's keys: s1 holds the logits of tile t's second half, w0 the weights of its first.
   for (int t = 0; t + 1 < n_tiles; ++t) {
     if constexpr (Feed::STRAIGHT) wait_loads();      // this wave's parts of K(t + 1) and V(t) are there
