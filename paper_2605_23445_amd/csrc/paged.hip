@@ -32,11 +32,23 @@ struct PagedSeq {
   __device__ __forceinline__ int work(const PagedArgs& a) const { return blocks * units * a.heads_kv; }
 };
 
-// Units of all sequences in front of each, as a work-group's threads work them out: thread t adds up `each` sequences from t * each on.
+// Units of all sequences in front of each, as a work-group's threads work them out: thread t adds up `each` sequences from t * each on; with up to 64, lane t of every wave
+// has sequence t.
 template <int NT> struct Deal {
   int each, mine, before, total, per;                // a thread's sum, the sum in front of it, all, and a work-group's share
   PagedSeq last;                                     // a thread's last sequence, which is its only one where there are up to NT
   __device__ __forceinline__ Deal(const PagedArgs& a, int (&sums)[NT / 64]) {
+    if (a.packed <= 64) {                            // every wave by itself: no barrier
+      const int s = threadIdx.x & 63;
+      each = 1;
+      last = PagedSeq(a, min_of(s, a.packed - 1));
+      mine = s < a.packed ? last.work(a) : 0;
+      const int upto = wave_sums(mine);
+      before = upto - mine;
+      total = __builtin_amdgcn_readlane(upto, 63);
+      per = max_of((total + GROUPS - 1) / GROUPS, a.least);
+      return;
+    }
     each = (a.packed + NT - 1) / NT;
     mine = 0;
     for (int i = 0, s = threadIdx.x * each; i < each && s < a.packed; ++i, ++s) {
@@ -320,29 +332,43 @@ __global__ void __launch_bounds__((64 * paged_waves<T, D, E4M3>()), 1) paged_spl
   int at = blockIdx.x * deal.per;
   const int end = min_of(deal.total, at + deal.per), start = at;
   if (at >= end) return;
-  if (threadIdx.x == 0) s_first[0] = a.packed;       // nobody's: where starts fall so far that the units of all pass 31 bits
-  __syncthreads();
-  if (deal.before <= at && at < deal.before + deal.mine) {
-    int s = threadIdx.x * deal.each, off = at - deal.before;
-    PagedSeq x = deal.last;
-    if (deal.each > 1)
-      for (; s < a.packed; ++s) {
-        x = PagedSeq(a, s);
-        const int w = x.work(a);
-        if (off < w) break;
-        off -= w;
-      }
-    s_first[0] = s;
-    s_first[1] = off;
-    s_first[2] = x.q0;
-    s_first[3] = x.n;
-    s_first[4] = x.k;
+  int s = a.packed, off = 0;                         // nobody's: where starts fall so far that the units of all pass 31 bits
+  PagedSeq seq;
+  const bool holds = deal.before <= at && at < deal.before + deal.mine;
+  if (a.packed <= 64) {
+    const uint64_t who = __builtin_amdgcn_ballot_w64(holds);
+    if (who) {
+      s = __builtin_ctzll(who);
+      off = at - __builtin_amdgcn_readlane(deal.before, s);
+      const int q0 = __builtin_amdgcn_readlane(deal.last.q0, s);
+      seq = PagedSeq(a, q0, q0 + __builtin_amdgcn_readlane(deal.last.n, s), __builtin_amdgcn_readlane(deal.last.k, s));
+    }
+  } else {
+    if (threadIdx.x == 0) s_first[0] = a.packed;
+    __syncthreads();
+    if (holds) {
+      int i = threadIdx.x * deal.each, rest = at - deal.before;
+      PagedSeq x = deal.last;
+      if (deal.each > 1)
+        for (; i < a.packed; ++i) {
+          x = PagedSeq(a, i);
+          const int w = x.work(a);
+          if (rest < w) break;
+          rest -= w;
+        }
+      s_first[0] = i;
+      s_first[1] = rest;
+      s_first[2] = x.q0;
+      s_first[3] = x.n;
+      s_first[4] = x.k;
+    }
+    __syncthreads();
+    auto first = [&](int i) { return __builtin_amdgcn_readfirstlane(s_first[i]); };
+    s = first(0);
+    off = first(1);
+    seq = PagedSeq(a, first(2), first(2) + first(3), first(4));
   }
-  __syncthreads();
-  auto first = [&](int i) { return __builtin_amdgcn_readfirstlane(s_first[i]); };
-  int s = first(0), off = first(1);
   if (s >= a.packed) return;
-  PagedSeq seq(a, first(2), first(2) + first(3), first(4));
 
   uint32_t k_off[LOADS], v_off[LOADS];
 #pragma unroll
@@ -505,33 +531,47 @@ __global__ void __launch_bounds__(256) paged_join_kernel(PagedArgs a, int row_gr
   const int id = blockIdx.x / row_groups, in = threadIdx.x / TR % RB, set = threadIdx.x / TR / RB, ch = threadIdx.x % TR;
   const int slot = id / a.heads_kv, kvh = id - slot * a.heads_kv;
   const Deal<256> deal(a, s_sums);
-  if (threadIdx.x == 0) s_owner = -1;
-  __syncthreads();
-  // The sequence that this block is of, and the units in front of its item: some thread has it.
-  int s = threadIdx.x * deal.each, base = deal.before, blk = 0;
-  PagedSeq seq = deal.last;
-  bool mine = false;
-  for (int i = 0; i < deal.each && s < a.packed; ++i, ++s) {
-    if (deal.each > 1) seq = PagedSeq(a, s);
-    blk = slot - int(uint32_t(seq.q0 * a.group) >> a.row_bits) - s;
-    mine = blk >= 0 && blk < seq.blocks;
-    if (mine) break;
-    base += seq.work(a);
+  // The sequence that this block is of, and the units in front of its item.
+  int base = 0, blk = 0;
+  PagedSeq seq;
+  if (a.packed <= 64) {
+    const int lane = threadIdx.x & 63, mine = slot - int(uint32_t(deal.last.q0 * a.group) >> a.row_bits) - lane;
+    const uint64_t who = __builtin_amdgcn_ballot_w64(lane < a.packed && mine >= 0 && mine < deal.last.blocks);
+    if (!who) return;
+    const int s = __builtin_ctzll(who), q0 = __builtin_amdgcn_readlane(deal.last.q0, s);     // (one of them where starts fall)
+    seq = PagedSeq(a, q0, q0 + __builtin_amdgcn_readlane(deal.last.n, s), __builtin_amdgcn_readlane(deal.last.k, s));
+    blk = __builtin_amdgcn_readlane(mine, s);
+    base = __builtin_amdgcn_readlane(deal.before, s) + (blk * a.heads_kv + kvh) * seq.units;
+  } else {
+    if (threadIdx.x == 0) s_owner = -1;
+    __syncthreads();
+    int s = threadIdx.x * deal.each;
+    bool mine = false;
+    base = deal.before;
+    seq = deal.last;
+    for (int i = 0; i < deal.each && s < a.packed; ++i, ++s) {
+      if (deal.each > 1) seq = PagedSeq(a, s);
+      blk = slot - int(uint32_t(seq.q0 * a.group) >> a.row_bits) - s;
+      mine = blk >= 0 && blk < seq.blocks;
+      if (mine) break;
+      base += seq.work(a);
+    }
+    if (mine) s_owner = threadIdx.x;
+    __syncthreads();
+    if (s_owner < 0) return;
+    if (s_owner == int(threadIdx.x)) {               // one thread's numbers, also where starts fall and several have some
+      s_item[0] = seq.q0;
+      s_item[1] = seq.n;
+      s_item[2] = seq.k;
+      s_item[3] = base + (blk * a.heads_kv + kvh) * seq.units;
+      s_item[4] = blk;
+    }
+    __syncthreads();
+    seq = PagedSeq(a, s_item[0], s_item[0] + s_item[1], s_item[2]);
+    base = s_item[3];
+    blk = s_item[4];
   }
-  if (mine) s_owner = threadIdx.x;
-  __syncthreads();
-  if (s_owner < 0) return;
-  if (s_owner == int(threadIdx.x)) {                 // one thread's numbers, also where starts fall and several have some
-    s_item[0] = seq.q0;
-    s_item[1] = seq.n;
-    s_item[2] = seq.k;
-    s_item[3] = base + (blk * a.heads_kv + kvh) * seq.units;
-    s_item[4] = blk;
-  }
-  __syncthreads();
-  seq = PagedSeq(a, s_item[0], s_item[0] + s_item[1], s_item[2]);
-  base = s_item[3];
-  const int first = s_item[4] << a.row_bits;
+  const int first = blk << a.row_bits;
   const int g0 = base / deal.per, g1 = (base + seq.units - 1) / deal.per;
   if (g0 == g1 || g0 < 0 || g1 >= GROUPS) return;    // one work-group had it whole; (past the runs: where starts fall so far that 31 bits do not count all)
   for (int n = (blockIdx.x - id * row_groups) * RB + in; first + n - in < min_of(first + (1 << a.row_bits), seq.n * a.group); n += row_groups * RB) {

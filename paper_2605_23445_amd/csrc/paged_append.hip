@@ -56,7 +56,7 @@ template <class Tok> __device__ __forceinline__ void set_turn(const AppendArgs& 
 
 // Norm and turn of a chunk of a row.
 template <typename T, int D, bool PAIRS>
-__device__ __forceinline__ void norm_and_turn(const AppendArgs& a, const Turn<T, D, PAIRS>& t, const float (&w)[Chunk<T>::N], float (&x)[Chunk<T>::N]) {
+__device__ __forceinline__ void norm_and_turn(const AppendArgs& a, const Turn<T, D, PAIRS, true>& t, const float (&w)[Chunk<T>::N], float (&x)[Chunk<T>::N]) {
   constexpr int N = Chunk<T>::N;
   if (a.norm) {
     float sq = 0.f;
@@ -72,7 +72,7 @@ __device__ __forceinline__ void norm_and_turn(const AppendArgs& a, const Turn<T,
 // Rows of tokens, those of all heads in turn: queries and, where they are stored as they are (KV), keys and values.
 template <typename T, int D, bool PAIRS, bool KV>
 __device__ __forceinline__ void append_tokens(const AppendArgs& a, int id) {
-  using Tok = Turn<T, D, PAIRS>;
+  using Tok = Turn<T, D, PAIRS, true>;
   constexpr int N = Tok::N, L = Tok::L, U = 2;
   const int lane = threadIdx.x & 63, y = id / a.q_groups, x = id - y * a.q_groups, t = x * (256 / L) + threadIdx.x / L;
   const int row = min_of(t, a.tokens - 1), c16 = lane % L * 16, h0 = y * a.per, h1 = min_of(h0 + a.per, a.heads + (KV ? 2 * a.heads_kv : 0));
@@ -213,7 +213,7 @@ template <int D> __device__ __forceinline__ void shrink(const View& v, int page,
 // Rows in 8 bits; PASSES of 256 / L rows are a page.
 template <int D, bool PAIRS, int PASSES>
 __device__ __forceinline__ void append_bytes(const AppendArgs& a, int id) {
-  using Tok = Turn<uint16_t, D, PAIRS>;
+  using Tok = Turn<uint16_t, D, PAIRS, true>;
   constexpr int N = Tok::N, L = Tok::L, R = 256 / L;
   __shared__ float most[2][4];
   const Fresh f(a, id);

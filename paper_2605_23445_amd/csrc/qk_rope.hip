@@ -13,7 +13,7 @@
 
 namespace dfs {
 
-struct RopeArgs : Turns {
+struct RopeRows {
   View in[3], out[3];                                // q, k, v; backward: rows of q and k
   View grad[3];                                      // backward: gradients of the results
   const int32_t* positions;
@@ -25,6 +25,7 @@ struct RopeArgs : Turns {
   int32_t copy_v;
   float* part;                                       // backward: sums of g x r of each work-group [groups][2][d]
 };
+struct RopeArgs : RopeRows, Turns {};
 
 // What a lane keeps of its token: where the token is, and its turn.
 template <typename T, int D, bool PAIRS> struct Token : Turn<T, D, PAIRS> {

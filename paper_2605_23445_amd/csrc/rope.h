@@ -60,8 +60,9 @@ template <int L> __device__ __forceinline__ float row_sum(float x) {
   return x;
 }
 
-// The turn of a token at position (p0, p1, p2): a lane keeps the cosines and sines of its channels.
-template <typename T, int D, bool PAIRS> struct Turn {
+// The turn of a token at position (p0, p1, p2): a lane keeps the cosines and sines of its channels.  SHARE: the two lanes of a pair's channels work out half of their angles
+// each and exchange them, which is less work and a longer way.
+template <typename T, int D, bool PAIRS, bool SHARE = false> struct Turn {
   static constexpr int N = Chunk<T>::N, L = D / N, C = PAIRS ? N / 2 : N;
   int c;
   int partner;                                       // halves: the lane that holds the other channels of this one's pairs
@@ -82,17 +83,25 @@ template <typename T, int D, bool PAIRS> struct Turn {
       const int half = (axis == 0 ? a.rot[0] : axis == 1 ? a.rot[1] : a.rot[2]) / 2, first = (ch - begin) < half;
       const bool turned = ch < end2;
       if (turned) partner = first ? lane + half / N : lane - half / N;
-      // the two lanes of a pair's channels work out half of their angles each and exchange them
-      const int mine = first ? 0 : C / 2, base = begin / 2 + (ch - begin) - (first ? 0 : half) + mine;
+      const int base = begin / 2 + (ch - begin) - (first ? 0 : half);
+      if constexpr (SHARE) {
+        const int mine = first ? 0 : C / 2;
 #pragma unroll
-      for (int i = 0; i < C / 2; ++i) {
-        float c0, s0;
-        turn(axis == 0 ? p0 : axis == 1 ? p1 : p2, turned ? a.freq[base + i] : 0, c0, s0);
-        const float c1 = __shfl(c0, partner), s1 = __shfl(s0, partner);
-        cs[i] = first ? c0 : c1;
-        cs[i + C / 2] = first ? c1 : c0;
-        sn[i] = first ? -s0 : s1;
-        sn[i + C / 2] = first ? -s1 : s0;
+        for (int i = 0; i < C / 2; ++i) {
+          float c0, s0;
+          turn(axis == 0 ? p0 : axis == 1 ? p1 : p2, turned ? a.freq[base + mine + i] : 0, c0, s0);
+          const float c1 = __shfl(c0, partner), s1 = __shfl(s0, partner);
+          cs[i] = first ? c0 : c1;
+          cs[i + C / 2] = first ? c1 : c0;
+          sn[i] = first ? -s0 : s1;
+          sn[i + C / 2] = first ? -s1 : s0;
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < C; ++i) {
+          turn(axis == 0 ? p0 : axis == 1 ? p1 : p2, turned ? a.freq[base + i] : 0, cs[i], sn[i]);
+          if (first) sn[i] = -sn[i];
+        }
       }
     }
   }
