@@ -53,7 +53,7 @@ template <bool E4M3> struct Entries {
   static __device__ __forceinline__ float of(float x, int lane) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), lane)); }
 };
 
-// Whether the rows are so many that blocks of 128 of them, each over all its keys, fill the chip, and the launch of these.
+// Whether the rows are so many that blocks of 128 of them, each over all its keys, are the faster way, and the launch of these.
 bool paged_is_long(const dfs_paged* w);
 int run_paged_long(const PagedArgs& a, int d, int dtype, bool bytes, hipStream_t st);
 

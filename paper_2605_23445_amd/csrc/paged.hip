@@ -710,10 +710,12 @@ int dfs_paged_attn_fwd(const dfs_paged* w, int dtype, const dfs_view* q, const d
   a.unit = 1024 / row_bytes < 8 ? 1024 / row_bytes : 8;                  // a piece for each wave
   while (items * ((pieces + a.unit - 1) / a.unit) >= int64_t(1) << 31) a.unit *= 2;
   a.least = 1;
-  // Where no row sees more than 64 pieces an item is one unit: no parts, no second launch.
+  // Where no row sees many pieces an item is one unit: no parts, no second launch (us, whole against parts; one token of two streams x 2 key heads, d = 128, e4m3, 8 waves:
+  // 1 024 keys 9.8 / 10.9, 2 048 12.9 / 10.8; bf16, 4 waves: 512 keys 10.0 / 10.4, 1 024 13.0 / 10.5; of 16 streams x 8, which fill the chip by themselves: e4m3
+  // 2 048 keys 16.8 / 20.9, bf16 23.9 / 25.4).
   const int64_t reach = a.left == NO_LIMIT ? pieces : (int64_t(a.left) + a.n_q) / 32 + 2 + (a.sinks + 31) / 32, longest = reach < pieces ? reach : pieces;
-  const bool whole = longest <= 64;
-  if (whole) a.unit = 64;
+  const bool whole = longest <= (int64_t(w->seqs) * w->heads_kv >= 128 ? 72 : 5 * a.unit + 1);
+  if (whole) a.unit = int(longest);
   const hipStream_t st = as_stream(stream);
   // work-groups of an item's join, four rows a turn, by the rows that a sequence has on average
   const int row_groups = mean < 1 << a.row_bits ? int(mean + 3) / 4 : 1 << a.row_bits >> 2;

@@ -35,16 +35,16 @@ CASES = {
     "long_small_pages": (4, 1, 64, 16, [1, 2, 1], [3000, 1500, 40], -1, 0, 0, 0),
     "wide_group": (24, 1, 128, 64, [3, 9], [100, 300], -1, 0, 0, 0),
     # enough blocks of 128 rows: the kernel of long calls
-    "blocks": (16, 16, 128, 64, [500, 129, 1], [500, 700, 300], -1, 0, 0, 0),
+    "blocks": (32, 32, 128, 64, [500, 129, 1], [500, 700, 300], -1, 0, 0, 0),
     "blocks_group": (32, 8, 128, 128, [300, 130, 257], [300, 1000, 511], -1, 0, 3, 2),
     "blocks_d64": (32, 16, 64, 32, [400, 1, 333], [600, 64, 333], -1, 0, 0, 0),
-    "blocks_small_pages": (32, 16, 64, 16, [250, 130, 128], [250, 463, 777], -1, 0, 0, 0),
-    "blocks_small_pages_d128": (20, 20, 128, 16, [300, 150], [399, 150], -1, 0, 0, 1),
+    "blocks_small_pages": (36, 18, 64, 16, [250, 130, 128], [250, 463, 777], -1, 0, 0, 0),
+    "blocks_small_pages_d128": (40, 20, 128, 16, [300, 150], [399, 150], -1, 0, 0, 1),
     "blocks_window": (32, 8, 128, 64, [300, 260, 90], [300, 1200, 600], 130, 0, 0, 0),
-    "blocks_window_and_first_keys": (24, 12, 64, 32, [300, 260, 90], [300, 900, 600], 77, 40, 0, 0),
+    "blocks_window_and_first_keys": (26, 13, 64, 32, [300, 260, 90], [300, 900, 600], 77, 40, 0, 0),
     "blocks_many": (16, 8, 128, 32, [(29 * i) % 70 for i in range(70)], [(29 * i) % 70 + 3 * i for i in range(70)], -1, 0, 0, 0),
-    "blocks_long_small_pages": (32, 32, 64, 16, [130, 260], [2600, 1800], -1, 0, 0, 0),
-    "blocks_long_small_pages_window": (32, 16, 128, 16, [130, 260], [2600, 1800], 1500, 33, 0, 0),
+    "blocks_long_small_pages": (44, 44, 64, 16, [130, 260], [2600, 1800], -1, 0, 0, 0),
+    "blocks_long_small_pages_window": (44, 22, 128, 16, [130, 260], [2600, 1800], 1500, 33, 0, 0),
     "blocks_more_queries_than_keys": (64, 64, 64, 16, [140, 130], [70, 3], -1, 0, 0, 0),
 }
 
@@ -127,6 +127,7 @@ def _check(w, dtype, q, p, q_lens, k_lens, front, table, scale, o, lse, mark=7.0
 def test_against_the_oracle(name, kind):
     w, dtype, q, p, q_start, k_len, q_lens, k_lens, front, table = _make(name, kind)
     scale = 1 / np.sqrt(w.d)
+    assert (P.dfs_paged_workspace_bytes(w, W.DT[dtype][0], p) == 0) == name.startswith("blocks")           # which of the two ways it goes
     o, lse = _run(w, dtype, q, p, q_start, k_len, scale)
     _check(w, dtype, q, p, q_lens, k_lens, front, table, scale, o, lse)
     again, _ = _run(w, dtype, q, p, q_start, k_len, scale, lse=False)
