@@ -51,6 +51,7 @@ struct WindowArgs {
   Div by_blocks, by_kv, by_group, by_splits;         // by_splits: by the work-groups that share a block
   int32_t first_tiles, first_splits;                 // backward: tiles of 32 first keys, and work-groups that share one's queries
   int32_t key_splits, row_splits;                    // backward: work-groups that share a block of keys, a block of rows
+  int32_t query_groups;                              // backward, packed: groups of waves that share a block of keys' queries, 1 or 2
   int32_t key_tiles;                                 // backward: tiles of 32 keys of a key head of which parts are kept
   int32_t splits;                                    // forward: work-groups that share the keys of 32 rows
   float scale;

@@ -406,9 +406,8 @@ template <int N> __device__ __forceinline__ void load_sums(const float2* from, i
 // term each: dk and dv are 2.35e-3 from 64 bits in 2-norm where rounding the results alone costs 1.65e-3, and a second term would be half of this kernel's products
 // again.  In fp32 one work-group a CU, whose 263 registers at d = 64 are seven more than two allow (4 000 tokens x 16 heads: 741 us, 54 %; d = 128: 1 490, 52 %).
 //
-// QG: groups of four waves that take the tiles of queries in turn, each with tiles of its own; what they find is added up in the end.  Two for packed sequences in bf16: the
-// blocks of the first keys of long sequences, which under a causal mask have several times the work of others, are done in half the time, and the CU has as many
-// waves as with two work-groups of one.
+// QG: groups of four waves that take the tiles of queries in turn, each with tiles of its own; what they find is added up in the end.  Two halve the time of the longest block,
+// and a CU has as many waves as with two work-groups of one group.
 template <typename T, int D, bool PACKED, int QG>
 __global__ void __launch_bounds__(256 * QG, sizeof(T) == 2 ? 2 / QG : 1) window_dkv_kernel(WindowArgs a) {
   constexpr bool BF16 = sizeof(T) == 2, V_LDS = BF16;
@@ -807,8 +806,11 @@ static int launch(const char* call, const WindowArgs& args, hipStream_t st) {
   if (a.n_k == 0) return DFS_OK;
   a.by_splits = Div(uint32_t(a.key_splits));
   a.set_blocks(blocks_of<PACKED>(a, a.n_k) * a.key_splits);
-  constexpr int QG = PACKED && sizeof(T) == 2 ? 2 : 1;
-  window_dkv_kernel<T, D, PACKED, QG><<<unsigned(a.blocks * seqs), 256 * QG, 0, st>>>(a);
+  bool two = false;
+  if constexpr (PACKED && sizeof(T) == 2) two = a.query_groups == 2;
+  if constexpr (PACKED && sizeof(T) == 2)
+    if (two) window_dkv_kernel<T, D, PACKED, 2><<<unsigned(a.blocks * seqs), 512, 0, st>>>(a);
+  if (!two) window_dkv_kernel<T, D, PACKED, 1><<<unsigned(a.blocks * seqs), 256, 0, st>>>(a);
   if (int rc = launch_status(call)) return rc;
   if constexpr (!PACKED)
     if (a.first_tiles > 0) {
