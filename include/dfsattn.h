@@ -443,7 +443,7 @@ size_t dfs_packed_workspace_bytes(const dfs_packed* w, int dtype, int backward);
 typedef struct {
   dfs_view k, v;                  /* [pages, heads_kv, page, d]: `batch` is from one page to the next; rows lie 2^24 bytes apart at most */
   float *k_scale, *v_scale;       /* DFS_E4M3: [pages, heads_kv], dense; else NULL */
-  const int32_t* table;           /* [seqs, table_row], dense.  An entry that no token of its sequence is on is not read; one outside [0, pages) is no page */
+  const int32_t* table;           /* [seqs, table_row], dense.  An entry that no token of its sequence is on may hold anything; one outside [0, pages) is no page */
   int32_t pages, page, table_row; /* page 16, 32, 64 or 128 rows; table_row x page at most 2^28, pages x heads_kv below 2^31 */
   int32_t dtype;
 } dfs_pages;
@@ -457,7 +457,7 @@ typedef struct {
  *   positions  NULL (axes 1): a token's place in its sequence turns it; or [tokens x axes] int32
  *   norm  0: no norm (w_q and w_k are NULL then);  w_q, w_k [d] fp32 or NULL (ones)
  * Tokens at places below 0, or on no page, go into no page; rows outside the sequences are left as they are, in q_out and in the pages.  A page that new tokens go to
- * belongs to one sequence alone.
+ * stands in the table once, at one sequence; pages that are only read may be shared.
  * DFS_E4M3: the scale of a page and key head is the smallest power of two c, 2^-120 at least, by which the largest of the page's values is 448 c at most, or, with rows from
  * before the call, their scale if that is larger.  Values are normed and turned in fp32 and rounded once; where a scale grows the rows from before are rounded anew, which
  * moves only what falls below the type's smallest value.  An infinite value is stored as NaN; NaN and infinities do not count for the scale.

@@ -57,7 +57,7 @@ template <typename T, int D> struct PageFeed {
   __device__ __forceinline__ u32x4 desc(int j, uint64_t from, const View& v) const {
     const uint32_t front = uint32_t(16 * group(j)) * uint32_t(v.row);     // offsets count from the tile's first row
     const uint64_t at = from - front;
-    const uint32_t bytes = place[j].rows > 0 ? front + uint32_t(place[j].rows) * uint32_t(v.row) : 0;
+    const uint32_t bytes = place[j].rows > 0 ? front + uint32_t(place[j].rows - 1) * uint32_t(v.row) + KTile::RB : 0;
     return u32x4{uint32_t(__builtin_amdgcn_readfirstlane(uint32_t(at))), uint32_t(__builtin_amdgcn_readfirstlane(uint32_t(at >> 32))) & 0xFFFFu,
                  uint32_t(__builtin_amdgcn_readfirstlane(bytes)), 0x00020000u};
   }
@@ -118,7 +118,8 @@ template <int D> struct ByteFeed {
   static __device__ __forceinline__ u32x4 load(uint64_t at_, int rows, const View& view, uint32_t off) {
     // (without these the descriptor is taken for one that differs from lane to lane, and the load becomes a loop)
     const uint64_t at = uint64_t(uint32_t(__builtin_amdgcn_readfirstlane(int(at_ >> 32)))) << 32 | uint32_t(__builtin_amdgcn_readfirstlane(int(uint32_t(at_))));
-    const uint32_t bytes = uint32_t(__builtin_amdgcn_readfirstlane(rows)) * uint32_t(view.row);
+    const int n = __builtin_amdgcn_readfirstlane(rows);
+    const uint32_t bytes = n > 0 ? uint32_t(n - 1) * uint32_t(view.row) + D : 0;
     return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(__builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(at), 0, bytes, 0x00020000), off, 0, 0));
   }
   __device__ __forceinline__ void ask_keys(const Span& span, int t) {

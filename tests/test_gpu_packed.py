@@ -213,6 +213,26 @@ def test_captured_and_replayed():
     assert all(torch.equal(a, b) for a, b in zip(out[0], again))
 
 
+@pytest.mark.parametrize("name", ["causal_d64", "later_pieces"])
+def test_gradients_against_differences(name):
+    """fp32: the change of <o, do> along a direction, by differences.  A difference of step e is off by e^2 of a third derivative and by what o is off by, over e; both stay below
+    2e-3 of the sum of sizes at e = 2^-6, as o is good to 1e-6 and a logit moves by less than a tenth."""
+    w, q, k, v, d_o, q_start, k_start, q_lens, k_lens, front = _make(name, "f32", 7)
+    _, _, dq, dk, dv = _run(w, "f32", q, k, v, d_o, q_start, k_start, 0.1)
+    n, m = slice(front, front + sum(q_lens)), slice(front, front + sum(k_lens))
+    gen = torch.Generator(device="cuda").manual_seed(8)
+
+    def f(*x):
+        o = torch.zeros_like(q)
+        P.dfs_packed_attn_fwd(w, P.DFS_F32, *x, q_start, k_start, 0.1, o, None, _ws(w, "f32", False))
+        return (o[:, n].double() * d_o[:, n].double()).sum()
+    for i, (x, grad, rows) in enumerate(((q, dq, n), (k, dk, m), (v, dv, m))):
+        step = torch.randn(x.shape, generator=gen, device="cuda").sign() * 2.0 ** -6
+        up, down = ([y + s * step if j == i else y for j, y in enumerate((q, k, v))] for s in (1, -1))
+        terms = grad[:, rows].double() * step[:, rows].double()
+        assert abs((f(*up) - f(*down)) / 2 - terms.sum()) <= 2e-3 * terms.abs().sum()
+
+
 def test_no_rows():
     e = lambda h, n: torch.empty(h, n, 64, device="cuda")  # noqa: E731
     start = torch.zeros(3, dtype=torch.int32, device="cuda")

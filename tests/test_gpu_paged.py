@@ -146,6 +146,19 @@ def test_token_major_pages(name, kind):
 
 
 @pytest.mark.parametrize("kind", list(KINDS))
+@pytest.mark.parametrize("name", ["one_token_each", "pieces_d64", "blocks", "blocks_d64", "blocks_small_pages"])
+def test_repeated_rows(name, kind):
+    """Pages of one row, and of one key head, by strides of zero."""
+    w, dtype, q, p, q_start, k_len, q_lens, k_lens, front, table = _make(name, kind, 9)
+    scales = [None if x is None else x[:, :1].repeat(1, w.heads_kv) for x in (p.k_scale, p.v_scale)]
+    part = [p.k[:, :1, :1].expand_as(p.k), p.v[:, :1].expand_as(p.v)]
+    got = _run(w, dtype, q, P.Pages(*part, p.table, *scales), q_start, k_len, 0.1)
+    whole = [x.float().contiguous().to(x.dtype) for x in part]
+    want = _run(w, dtype, q, P.Pages(*whole, p.table, *scales), q_start, k_len, 0.1)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+@pytest.mark.parametrize("kind", list(KINDS))
 @pytest.mark.parametrize("name", ["one_token_each", "window_and_first_keys", "many_first_keys", "first_keys_reach_the_window", "pieces_with_window", "blocks_window",
                                   "blocks_window_and_first_keys", "blocks_small_pages"])
 def test_what_nothing_sees_may_hold_anything(name, kind):
@@ -195,6 +208,19 @@ def test_starts_lengths_and_tables_that_break_the_format(name, kind):
         P.dfs_paged_attn_fwd(w, W.DT[dtype][0], q, p, falling.int(), k_len, 0.1, around[0, 1:-1], None, _ws(w, dtype, p))
         torch.cuda.synchronize()
         assert (around[1] == 7).all() and (around[0, 0] == 7).all() and (around[0, -1] == 7).all()
+
+
+@pytest.mark.parametrize("kind", list(KINDS))
+@pytest.mark.parametrize("name", ["one_token_each", "blocks_group"])
+def test_sequences_that_share_pages(name, kind):
+    """A page that several sequences have, at different places: a common beginning."""
+    w, dtype, q, p, q_start, k_len, q_lens, k_lens, front, table = _make(name, kind, 10)
+    shared = table.copy()
+    shared[1:, 0] = np.where(np.asarray(k_lens)[1:] > 0, table[0, 0], table[1:, 0])
+    shared[0, 1] = table[0, 0]
+    t = torch.from_numpy(shared).cuda()
+    o, lse = _run(w, dtype, q, P.Pages(p.k, p.v, t, p.k_scale, p.v_scale), q_start, k_len, 0.1)
+    _check(w, dtype, q, p, q_lens, k_lens, front, shared, 0.1, o, lse)
 
 
 def test_pages_past_32_bits():
@@ -282,6 +308,29 @@ def test_captured_and_replayed():
         assert torch.equal(o, want[0]) and torch.equal(lse, want[1])
         a = slice(other[8], other[8] + n)
         assert torch.equal(o2[:, a], want_other[0][:, a]) and torch.equal(lse2[:, a], want_other[1][:, a])
+
+
+def test_on_another_stream():
+    """Appending and attending on a stream of their own, behind work that makes their inputs there."""
+    w, dtype, q, p, q_start, k_len, q_lens, k_lens, front, table = _make("few_tokens_each", "e4m3", 11)
+    g = P.QkGeom(w.seqs, w.n_q, w.heads, w.heads_kv, w.d, 0, 1, w.d, 0, 0, 1e4, 1e-5)
+    k, v = (torch.randn(w.heads_kv, w.n_q, w.d, device="cuda").bfloat16() for _ in range(2))
+
+    def step(p_):
+        rows, o = torch.empty_like(q), torch.zeros_like(q)
+        P.dfs_paged_append(g, P.DFS_BF16, q * 2, k, v, q_start, k_len, None, None, None, rows, p_)
+        P.dfs_paged_attn_fwd(w, P.DFS_BF16, rows, p_, q_start, k_len, 0.1, o, None, _ws(w, dtype, p_))
+        return o
+    copy = lambda: P.Pages(p.k.clone(), p.v.clone(), p.table, p.k_scale.clone(), p.v_scale.clone())  # noqa: E731
+    a, b = copy(), copy()
+    want = step(a)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(1000000)
+        got = step(b)
+    side.synchronize()
+    assert torch.equal(got, want) and torch.equal(a.k.view(torch.uint8), b.k.view(torch.uint8)) and torch.equal(a.k_scale, b.k_scale)
 
 
 def test_no_rows():
