@@ -5,8 +5,9 @@
  * paper's Algorithm 1 states it: a 3D Hilbert-curve token reorder, hierarchical block
  * scoring, top-k / adaptive block-mask selection, block-sparse attention over the
  * reordered sequence, and the inverse reorder.  In front of it stand the norms and position
- * rotation of queries and keys, beside it attention over a window and a few first keys, both
- * with their backward passes.
+ * rotation of queries and keys, beside it attention over a window and a few first keys and
+ * within packed sequences, all with their backward passes, and a cache of keys and values in
+ * pages, which is appended to and attended over.
  *
  * Conventions shared by every entry point
  *   - Structs (`g` and its like) are HOST memory.  Every other pointer is DEVICE memory owned by the caller;

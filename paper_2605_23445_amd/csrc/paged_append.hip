@@ -4,7 +4,9 @@
 // are worked on page by page: a work-group takes the new rows of one page and key head.  In 8 bits (e4m3, largest value 448) a page's rows share one power of two c,
 // the smallest with which the largest of them is at most 448 c: it is known when all of a page's new rows are, which therefore stay in registers, and
 // where there are rows from before it is not less than it was; if it grows they are divided by the quotient, which is exact but for what falls below e4m3's smallest.
-// Memory bound, the smallest calls by their chain of loads (starts, lengths and rows, table, scale).
+// Bound by memory: 16 384 tokens of five prompts, 32 + 2 x 8 heads, d = 128, into e4m3 pages of 64 rows: 91 us, 4.05 TB/s (69 where the inputs are in the memory-side cache; a plain
+// copy: 4.9); 5 130 x 3 x 12, d = 64, into bf16 pages of 16: 12 us, 3.9 TB/s.  The smallest calls are bound by the launch and a chain of loads (starts, lengths and rows, table,
+// scale): one token of 32 sequences 6.3 us.
 #include <float.h>
 
 #include "pages.h"
