@@ -704,7 +704,6 @@ int dfs_paged_attn_fwd(const dfs_paged* w, int dtype, const dfs_view* q, const d
   a.scale = scale;
   a.part = static_cast<float*>(ws);
   a.part_sums = reinterpret_cast<float2*>(static_cast<char*>(ws) + part_bytes(w));
-  // work is counted in 31 bits
   // 16 rows where the sequences have no more on average: half of the matrix instructions and of the weights (one token over 80 900 keys, 4 heads a key head, 45 -> 43 us, 16 streams
   // with a window of 1 024 keys 11.5 -> 10.5)
   const int64_t mean = (int64_t(a.group) * a.n_q + w->seqs - 1) / w->seqs;
@@ -713,7 +712,7 @@ int dfs_paged_attn_fwd(const dfs_paged* w, int dtype, const dfs_view* q, const d
   const bool bytes = pages->dtype == DFS_E4M3;
   const int row_bytes = w->d * (bytes ? 1 : elem_size(dtype));
   a.unit = 1024 / row_bytes < 8 ? 1024 / row_bytes : 8;                  // a piece for each wave
-  while (items * ((pieces + a.unit - 1) / a.unit) >= int64_t(1) << 31) a.unit *= 2;
+  while (items * ((pieces + a.unit - 1) / a.unit) >= int64_t(1) << 30) a.unit *= 2;          // units are counted in 31 bits, and the last work-group's run may end behind them
   a.least = 1;
   // Where no row sees many pieces an item is one unit: no parts, no second launch (us, whole against parts; one token of two streams x 2 key heads, d = 128, e4m3, 8 waves:
   // 1 024 keys 9.8 / 10.9, 2 048 12.9 / 10.8; bf16, 4 waves: 512 keys 10.0 / 10.4, 1 024 13.0 / 10.5; of 16 streams x 8, which fill the chip by themselves: e4m3

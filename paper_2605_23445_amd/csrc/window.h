@@ -202,7 +202,8 @@ template <int KIND> struct Seq {
       const int mine = min_of(lane, a.packed - 1), from = start_of(start, mine, most), to = start_of(start, mine + 1, most);
       const int n = lane < a.packed && to > from ? int(uint32_t((to - from) * per + U - 1) / U) : 0;
       // a sequence's blocks have the numbers base .. base + n - 1; those of the largest number come first
-      const int base = KEYS ? 0 : int(int64_t(max_of(0, keys_of(a, mine) - (to - from))) * per / U);
+      const int64_t ahead = KEYS ? 0 : int64_t(max_of(0, keys_of(a, mine) - (to - from))) * per / U;
+      const int base = ahead < 1 << 29 ? int(ahead) : 1 << 29;             // only an order: beyond this all are long, and sums of numbers keep to 31 bits
       int lo = 0, hi = 1;                            // the blocks number lo and more are more than i, those number hi and more are not
       r.real = wave_sum(n) > i;
       if (!r.real) return r;

@@ -180,6 +180,19 @@ def test_offsets_past_32_bits():
     assert all(torch.equal(a, b) for a, b in zip(got, want))
 
 
+def test_most_keys():
+    """2^28 keys, all the same row, with 1 500 heads a key head: a row that sees itself alone gives its value."""
+    n, heads, kv, d = 1 << 28, 10500, 7, 64
+    w = P.Packed(1, heads, kv, d, 3, n, 0, 0)
+    gen = torch.Generator(device="cuda").manual_seed(12)
+    q, k, v = (torch.randn(h, m, d, generator=gen, device="cuda").bfloat16() for h, m in ((heads, 3), (kv, 1), (kv, 1)))
+    q_start, k_start = (torch.tensor([0, x], dtype=torch.int32, device="cuda") for x in (3, n))
+    assert P.dfs_packed_workspace_bytes(w, P.DFS_BF16, False) == 0
+    o = torch.zeros_like(q)
+    P.dfs_packed_attn_fwd(w, P.DFS_BF16, q, k.expand(kv, n, d), v.expand(kv, n, d), q_start, k_start, 0.1, o)
+    assert torch.equal(o, v.expand(kv, 3, d).repeat_interleave(heads // kv, 0))
+
+
 def test_captured_and_replayed():
     """Forward and backward in a graph, replayed with other lengths in the same start array, and a second graph with a workspace of its own."""
     w, q, k, v, d_o, q_start, _, q_lens, k_lens, front = _make("blocks_causal", "bf16", 6)

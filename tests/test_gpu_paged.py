@@ -32,6 +32,10 @@ CASES = {
     "pieces_d64": (4, 4, 64, 16, [130, 64, 3], [130, 500, 777], -1, 0, 0, 4),
     "pieces_with_window": (8, 2, 64, 32, [150, 90, 31], [150, 400, 300], 70, 10, 0, 0),
     "many_streams": (4, 2, 64, 16, [i % 2 for i in range(300)], [(7 * i) % 90 + 1 for i in range(300)], -1, 0, 1, 0),
+    # one long list of keys, so that items come in parts: more sequences than a wave's lanes, and than a work-group's threads
+    "many_streams_one_long": (4, 2, 128, 64, [1 + i % 3 % 2 for i in range(90)], [(11 * i) % 200 + 2 for i in range(70)] + [2900] + [65] * 19, -1, 0, 2, 1),
+    "more_streams_one_long": (2, 1, 64, 16, [(i + 1) % 4 // 3 + (i == 333) for i in range(700)], [(5 * i) % 50 + (3000 if i == 333 else 0) for i in range(700)], -1, 0, 0, 0),
+    "more_streams_with_window": (4, 1, 128, 32, [1] * 650, [(37 * i) % 3300 + 1 for i in range(650)], 2500, 40, 0, 0),
     "long_small_pages": (4, 1, 64, 16, [1, 2, 1], [3000, 1500, 40], -1, 0, 0, 0),
     "wide_group": (24, 1, 128, 64, [3, 9], [100, 300], -1, 0, 0, 0),
     # enough blocks of 128 rows: the kernel of long calls
@@ -331,6 +335,21 @@ def test_on_another_stream():
         got = step(b)
     side.synchronize()
     assert torch.equal(got, want) and torch.equal(a.k.view(torch.uint8), b.k.view(torch.uint8)) and torch.equal(a.k_scale, b.k_scale)
+
+
+@pytest.mark.parametrize("n_q", [1, 6])
+def test_most_keys(n_q):
+    """2^28 keys with 1 500 heads a key head, few rows and blocks of them: a row that sees itself alone gives its value."""
+    w, n = P.Paged(1, 3000, 2, 64, n_q, 0, 0), 1 << 28
+    gen = torch.Generator(device="cuda").manual_seed(12)
+    k, v = (torch.randn(1, 2, 128, 64, generator=gen, device="cuda").bfloat16() for _ in range(2))
+    p = P.Pages(k, v, torch.zeros(1, n // 128, dtype=torch.int32, device="cuda"))
+    assert (P.dfs_paged_workspace_bytes(w, P.DFS_BF16, p) == 0) == (n_q == 6)
+    q = torch.randn(3000, n_q, 64, generator=gen, device="cuda").bfloat16()
+    start, length = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in ([0, n_q], [n - 20]))
+    o, _ = _run(w, "bf16", q, p, start, length, 0.1)
+    rows = (n - 20 - n_q + torch.arange(n_q, device="cuda")) % 128
+    assert torch.equal(o, v[0][:, rows].repeat_interleave(1500, 0))
 
 
 def test_no_rows():
