@@ -70,12 +70,13 @@ template <int NT> struct Deal {
 };
 
 // Tiles of 32 rows of a page's elements in LDS, chunks of 16 bytes swapped within a row so that what is read at once lies in different banks.
-template <typename T, int D, bool E4M3> struct PageTile {
+template <typename T, int D, bool E4M3, int ROWS = 32> struct PageTile {
   static constexpr int RB = E4M3 ? D : D * int(sizeof(T)), CH = RB / 16, BYTES = 32 * RB, LOADS = BYTES / 1024;
   using Rows = Tile<T, D, 32, 1, false>;
   using Columns = Tile<T, D, 32, 1, true>;
   template <bool COLUMNS> static __device__ __forceinline__ int swizzle(int row) {
     if constexpr (E4M3) return row * RB / 256 % CH;
+    else if constexpr (COLUMNS && ROWS == 16 && sizeof(T) == 4) return row / 4 % 4 * 4;      // four rows 4 apart are read at once, 16 channels each
     else return COLUMNS ? Columns::swizzle(row) : Rows::swizzle(row);
   }
   // Byte offset of this lane's chunk of load j of 16 rows.
@@ -192,18 +193,19 @@ template <typename T, int D, bool E4M3, int H> struct Wave32 {
   __device__ __forceinline__ bool first() const { return h == 0; }
 };
 
-template <int D, bool E4M3, int H> struct Wave16 {
-  using PT = PageTile<uint16_t, D, E4M3>;
-  static constexpr int ROWS = 16, STEPS = D / 32, REGS = D / 4;
+template <typename T, int D, bool E4M3, int H> struct Wave16 {
+  using PT = PageTile<T, D, E4M3, 16>;
+  using Frag = typename Mat<T>::Frag;
+  static constexpr int ROWS = 16, STEPS = D * int(sizeof(T)) / 64, REGS = D / 4;
   int lane, n, g;
-  bf16x8 qf[STEPS];
+  Frag qf[STEPS];
   f32x4 acc[D / 16], x[2];
-  u32x4 w;
+  u32x4 w;                                           // weights in bf16; in fp32 they serve as they are
   float m, l;
   __device__ __forceinline__ Wave16(int lane_) : lane(lane_), n(lane_ & 15), g(lane_ >> 4) {}
   __device__ __forceinline__ void start(const char* q) {
 #pragma unroll
-    for (int st = 0; st < STEPS; ++st) qf[st] = *reinterpret_cast<const bf16x8*>(q + (E4M3 ? (st / 2 * 4 + g) * 2 + st % 2 : 4 * st + g) * 16);
+    for (int st = 0; st < STEPS; ++st) qf[st] = *reinterpret_cast<const Frag*>(q + (E4M3 ? (st / 2 * 4 + g) * 2 + st % 2 : 4 * st + g) * 16);
 #pragma unroll
     for (int c = 0; c < D / 16; ++c) acc[c] = f32x4{0.f, 0.f, 0.f, 0.f};
     m = -INFINITY;
@@ -214,28 +216,41 @@ template <int D, bool E4M3, int H> struct Wave16 {
     for (int st = 0; st < STEPS; ++st) asm volatile("" : "+v"(qf[st]));
   }
   __device__ __forceinline__ void keys(uint32_t buf, const float (&scale)[H]) {
-    constexpr int READS = E4M3 ? D / 64 : STEPS;
-    u32x4 raw[2][READS];
-#pragma unroll
-    for (int half = 0; half < 2; ++half)
-#pragma unroll
-      for (int st = 0; st < READS; ++st) {
-        const int row = 16 * half + n;
-        raw[half][st] = *reinterpret_cast<LDS_PTR(const u32x4)>(buf + uint32_t(row * PT::RB + ((4 * st + g) ^ PT::template swizzle<false>(row)) * 16));
-      }
     x[0] = x[1] = f32x4{0.f, 0.f, 0.f, 0.f};
+    auto chunk = [&](int half, int st) {
+      const int row = 16 * half + n;
+      return *reinterpret_cast<LDS_PTR(const u32x4)>(buf + uint32_t(row * PT::RB + ((4 * st + g) ^ PT::template swizzle<false>(row)) * 16));
+    };
+    if constexpr (sizeof(T) == 4) {
 #pragma unroll
-    for (int st = 0; st < READS; ++st)
+      for (int st = 0; st < STEPS; ++st) {
+        const f32x4 k0 = __builtin_bit_cast(f32x4, chunk(0, st)), k1 = __builtin_bit_cast(f32x4, chunk(1, st));
 #pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        const u32x4 r = raw[half][st];
-        if constexpr (E4M3) {
-          x[half] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(eight(r[0], r[1], scale[half < H ? half : 0]), qf[2 * st], x[half], 0, 0, 0);
-          x[half] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(eight(r[2], r[3], scale[half < H ? half : 0]), qf[2 * st + 1], x[half], 0, 0, 0);
-        } else {
-          x[half] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, r), qf[st], x[half], 0, 0, 0);
+        for (int i = 0; i < 4; ++i) {
+          x[0] = __builtin_amdgcn_mfma_f32_16x16x4f32(k0[i], qf[st][i], x[0], 0, 0, 0);
+          x[1] = __builtin_amdgcn_mfma_f32_16x16x4f32(k1[i], qf[st][i], x[1], 0, 0, 0);
         }
       }
+    } else {
+      constexpr int READS = E4M3 ? D / 64 : STEPS;
+      u32x4 raw[2][READS];
+#pragma unroll
+      for (int half = 0; half < 2; ++half)
+#pragma unroll
+        for (int st = 0; st < READS; ++st) raw[half][st] = chunk(half, st);
+#pragma unroll
+      for (int st = 0; st < READS; ++st)
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          const u32x4 r = raw[half][st];
+          if constexpr (E4M3) {
+            x[half] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(eight(r[0], r[1], scale[half < H ? half : 0]), qf[2 * st], x[half], 0, 0, 0);
+            x[half] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(eight(r[2], r[3], scale[half < H ? half : 0]), qf[2 * st + 1], x[half], 0, 0, 0);
+          } else {
+            x[half] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, r), qf[st], x[half], 0, 0, 0);
+          }
+        }
+    }
   }
   static __device__ __forceinline__ float across(float v, bool add) {    // largest or sum over the four lanes of a row
     const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -273,14 +288,27 @@ template <int D, bool E4M3, int H> struct Wave16 {
       for (int i = 0; i < 4; ++i) {
         x[half][i] = __builtin_amdgcn_exp2f(fmaf(x[half][i], c2, -ref));
         l += x[half][i];
-        if (i % 2) {
+        if (sizeof(T) == 2 && i % 2) {
           const bf16x2 pair = {(__bf16)x[half][i - 1], (__bf16)x[half][i]};
           w[2 * half + i / 2] = __builtin_bit_cast(uint32_t, pair);
         }
       }
   }
   __device__ __forceinline__ void values(uint32_t buf, const float (&scale)[H]) {
-    if constexpr (E4M3) {
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int half = 0; half < 2; ++half)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int row = 16 * half + 4 * g + i;
+          const uint32_t from = buf + uint32_t(row * PT::RB), sw = uint32_t(PT::template swizzle<true>(row));
+#pragma unroll
+          for (int c = 0; c < D / 16; ++c) {
+            const float v = *reinterpret_cast<LDS_PTR(const float)>(from + ((uint32_t(4 * c + n / 4)) ^ sw) * 16 + uint32_t(n % 4) * 4);
+            acc[c] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, x[half][i], acc[c], 0, 0, 0);
+          }
+        }
+    } else if constexpr (E4M3) {
       const int i = (lane & 15) >> 1, row = 4 * g + i + (i < 4 ? 0 : 12);                    // keys 4 g .. 4 g + 3 of both halves
       i32x2 raw[D / 16];
 #pragma unroll
@@ -311,7 +339,7 @@ template <int D, bool E4M3, int H> struct Wave16 {
 };
 
 template <int ROWS, typename T, int D, bool E4M3, int H> struct WaveOf { using type = Wave32<T, D, E4M3, H>; };
-template <typename T, int D, bool E4M3, int H> struct WaveOf<16, T, D, E4M3, H> { using type = Wave16<D, E4M3, H>; };
+template <typename T, int D, bool E4M3, int H> struct WaveOf<16, T, D, E4M3, H> { using type = Wave16<T, D, E4M3, H>; };
 
 // Bound by memory and by what stands around it: 48 sequences of up to 16 384 keys, 8 key heads, d = 128, e4m3: 201 us of 217, 6.0 TB/s (as fast without the arithmetic; bare loads of
 // this shape: 6.9); one sequence of 80 900 keys: 30 of 42, 5.5 TB/s.  The rest is the join and the way from one launch to the next.  16 sequences that see 1 024 keys each of
@@ -320,7 +348,7 @@ template <int ROWS, typename T, int D, bool E4M3, bool SMALL>
 __global__ void __launch_bounds__((64 * paged_waves<T, D, E4M3>()), 1) paged_split_kernel(PagedArgs a) {
   constexpr int NW = paged_waves<T, D, E4M3>(), NT = 64 * NW, H = SMALL ? 2 : 1, RPH = 32 / H;        // H: pages of a piece
   using Wave = typename WaveOf<ROWS, T, D, E4M3, H>::type;
-  using PT = PageTile<T, D, E4M3>;
+  using PT = typename Wave::PT;
   constexpr int LOADS = PT::LOADS, BYTES = PT::BYTES, REGS = Wave::REGS;
   static_assert(REGS * 64 * 4 <= 4 * BYTES, "a wave's sums fit where its tiles were");
   __shared__ __attribute__((aligned(1024))) char tiles[NW * 4 * BYTES];
@@ -705,9 +733,9 @@ int dfs_paged_attn_fwd(const dfs_paged* w, int dtype, const dfs_view* q, const d
   a.part = static_cast<float*>(ws);
   a.part_sums = reinterpret_cast<float2*>(static_cast<char*>(ws) + part_bytes(w));
   // 16 rows where the sequences have no more on average: half of the matrix instructions and of the weights (one token over 80 900 keys, 4 heads a key head, 45 -> 43 us, 16 streams
-  // with a window of 1 024 keys 11.5 -> 10.5)
+  // with a window of 1 024 keys 11.5 -> 10.5; fp32, d = 128, 48 streams x 8 key heads over up to 4 000 keys 457 -> 296, 8 x 8 over up to 207 31.6 -> 21.6)
   const int64_t mean = (int64_t(a.group) * a.n_q + w->seqs - 1) / w->seqs;
-  a.row_bits = mean <= 16 && dtype == DFS_BF16 ? 4 : 5;
+  a.row_bits = mean <= 16 ? 4 : 5;
   const int64_t items = ((int64_t(a.group) * a.n_q >> a.row_bits) + w->seqs) * w->heads_kv, pieces = a.n_k / 32 + 2;
   const bool bytes = pages->dtype == DFS_E4M3;
   const int row_bytes = w->d * (bytes ? 1 : elem_size(dtype));
@@ -716,9 +744,11 @@ int dfs_paged_attn_fwd(const dfs_paged* w, int dtype, const dfs_view* q, const d
   a.least = 1;
   // Where no row sees many pieces an item is one unit: no parts, no second launch (us, whole against parts; one token of two streams x 2 key heads, d = 128, e4m3, 8 waves:
   // 1 024 keys 9.8 / 10.9, 2 048 12.9 / 10.8; bf16, 4 waves: 512 keys 10.0 / 10.4, 1 024 13.0 / 10.5; of 16 streams x 8, which fill the chip by themselves: e4m3
-  // 2 048 keys 16.8 / 20.9, bf16 23.9 / 25.4).
+  // 2 048 keys 16.8 / 20.9, bf16 23.9 / 25.4.  fp32, where the matrix instructions of a piece take 2 us: 8 streams x 8, d = 128, 2 waves: 64 keys 10.1 / 12.1, 130 14.4 / 13.6;
+  // d = 64, 4 waves: 250 keys 9.5 / 11.1, 500 13.1 / 11.4, 16 x 8 1 000 keys 22.1 / 22.2, 2 000 36.2 / 28.8).
   const int64_t reach = a.left == NO_LIMIT ? pieces : (int64_t(a.left) + a.n_q) / 32 + 2 + (a.sinks + 31) / 32, longest = reach < pieces ? reach : pieces;
-  const bool whole = longest <= (int64_t(w->seqs) * w->heads_kv >= 128 ? 72 : 5 * a.unit + 1);
+  const bool fills = int64_t(w->seqs) * w->heads_kv >= 128;
+  const bool whole = longest <= (dtype == DFS_F32 ? (fills && w->d == 64 ? 8 : 3) * a.unit : fills ? 72 : 5 * a.unit + 1);
   if (whole) a.unit = int(longest);
   const hipStream_t st = as_stream(stream);
   // work-groups of an item's join, four rows a turn, by the rows that a sequence has on average
@@ -733,8 +763,7 @@ int dfs_paged_attn_fwd(const dfs_paged* w, int dtype, const dfs_view* q, const d
       if (a.pages.bits == 4) paged_split_kernel<decltype(rows)::value, T, D, E4M3, true><<<GROUPS, NT, 0, st>>>(a);
       else paged_split_kernel<decltype(rows)::value, T, D, E4M3, false><<<GROUPS, NT, 0, st>>>(a);
     };
-    if constexpr (sizeof(T) == 2)
-      if (a.row_bits == 4) return of(std::integral_constant<int, 16>{});
+    if (a.row_bits == 4) return of(std::integral_constant<int, 16>{});
     of(std::integral_constant<int, 32>{});
   };
   auto join = [&](auto t, auto d) { paged_join_kernel<decltype(t), decltype(d)::value><<<joins, 256, 0, st>>>(a, row_groups); };

@@ -18,6 +18,7 @@ CASES = {
     "one_token": (1, 1, 128, 16, [1], [1], -1, 0, 0, 0),
     "one_token_each": (8, 2, 128, 64, [1, 1, 1, 1, 1, 1], [300, 1, 64, 65, 31, 1000], -1, 0, 0, 0),
     "one_token_each_d64": (16, 4, 64, 16, [1, 1, 1, 0, 1], [300, 17, 16, 70, 1000], -1, 0, 0, 0),
+    "one_token_each_small_pages": (12, 2, 128, 16, [1, 1, 2, 1, 1], [300, 16, 65, 900, 31], -1, 0, 1, 1),
     "long_stream": (8, 2, 128, 128, [1], [5000], -1, 0, 0, 0),
     "long_and_short": (4, 1, 128, 32, [1, 1, 1], [4000, 3, 900], -1, 0, 0, 0),
     "window": (8, 2, 128, 64, [1, 1, 1, 1], [700, 40, 129, 64], 100, 0, 0, 0),
