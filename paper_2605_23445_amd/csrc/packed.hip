@@ -35,18 +35,24 @@ static int64_t likely(int64_t n, const dfs_packed* w) {
 
 // As for sequences of one length: work-groups share the queries of a block of keys, or the keys of a block of rows, where these are few.
 struct PackedBwd { size_t keys, rows, total; int key_splits, row_splits, query_groups; int64_t key_tiles; };
-static PackedBwd bwd_layout(const dfs_packed* w) {
+static PackedBwd bwd_layout(const dfs_packed* w, int dtype) {
   PackedBwd L;
   const int64_t group = w->heads / w->heads_kv, rows = group * w->n_q, part = 64 * w->d * sizeof(float);
   const int64_t reach = w->left < 0 || w->right < 0 ? int64_t(1) << 40 : int64_t(w->left) + w->right + 128;
   const int64_t key_blocks = (w->n_k / 128 + w->seqs) * int64_t(w->heads_kv), row_blocks = (rows / 128 + w->seqs) * int64_t(w->heads_kv);
   const int64_t q = likely(w->n_q, w), k = likely(w->n_k, w);
-  // twice as many as where all blocks have the same work: under a causal mask half of them have little (1 000 fp32 tokens of three sequences x 12 heads of 4: 122 -> 106 us)
-  L.key_splits = share(key_blocks, ((reach < q ? reach : q) + 31) / 32 * group, 512);
+  // Twice as many as where all blocks have the same work: under a causal mask half of them have little (1 000 fp32 tokens of three sequences x 12 heads of 4: 122 -> 106 us).  For the same
+  // reason up to 340 blocks of keys, a little more than run at once, are shared by three (us, 1 / 3 work-groups: 4 000 causal tokens of three x 32 heads of 8, d = 128, 272 blocks, 360 / 298,
+  // fp32 3 833 / 2 520; 9 000 of six x 32 of 4, d = 64, 304, 480 / 397; 5 000 of two that see all of theirs, 328, 1 284 / 1 154), and in fp32, where a CU has one work-group, up to 512
+  // by two (2 000 of five x 24, d = 64, 480 blocks: bf16 70 / 80, fp32 342 / 323; 6 000 of four x 32 of 8 with a window of 300, 400: 152 / 156, 1 017 / 888).  In bf16 a block has to have the
+  // work for it: 96 tiles of 32 queries (3 000 of two x 12 with a window of 200, 10 tiles, 90 / 106; 3 000 of eight x 16 of 8, 48, 63 / 64; 2 500 of four x 24 of 8, 117, 131 / 122).
+  const int64_t tiles = ((reach < q ? reach : q) + 31) / 32 * group;
+  const int64_t even = dtype == DFS_F32 ? (key_blocks <= 340 ? 3 : key_blocks <= 512 ? 2 : 1) : key_blocks <= 340 && tiles >= 96 ? 3 : 1;
+  L.key_splits = share(key_blocks, tiles, even * key_blocks > 512 ? even * key_blocks : 512);
   L.row_splits = share(row_blocks, ((reach < k ? reach : k) + 63) / 64, 512);
   // Under a causal mask the blocks of the first keys have several times the work of others; where all blocks run at once, or nearly so, the longest one is what the call waits for (us, two
-  // groups of waves against one, d = 128: 4 500 tokens of five texts x 32 heads of 8, 320 blocks, 301 / 333; 12 000, 800, 1 356 / 1 385; 16 000, 1 040, 2 335 / 2 239; 9 000
-  // tokens of two x 12 that see all of theirs 1 560 / 1 470).
+  // groups of waves against one, d = 128, 32 heads of 8: 12 000 tokens of five texts, 800 blocks, 1 356 / 1 385; 16 000, 1 040, 2 335 / 2 239; 9 000 tokens of two x 12 that see all of
+  // theirs 1 560 / 1 470).
   L.query_groups = w->left < 0 && w->right >= 0 && L.key_splits == 1 && key_blocks <= 900 ? 2 : 1;
   L.key_tiles = L.key_splits > 1 ? (int64_t(w->n_k) / 128 + w->seqs) * 4 : 0;
   L.keys = align256(size_t(w->heads) * w->n_q * sizeof(float2));
@@ -124,7 +130,7 @@ extern "C" {
 
 size_t dfs_packed_workspace_bytes(const dfs_packed* w, int dtype, int backward) {
   if (check_packed("dfs_packed_workspace_bytes", w, dtype) != DFS_OK) return 0;
-  return backward ? bwd_layout(w).total : fwd_layout(w, dtype).total;
+  return backward ? bwd_layout(w, dtype).total : fwd_layout(w, dtype).total;
 }
 
 int dfs_packed_attn_fwd(const dfs_packed* w, int dtype, const dfs_view* q, const dfs_view* k, const dfs_view* v, const int32_t* q_start,
@@ -182,7 +188,7 @@ int dfs_packed_attn_bwd(const dfs_packed* w, int dtype, const dfs_view* q, const
   if ((rc = check_view(call, "dv", dv, dtype, 1, w->heads_kv, w->n_k, w->d, true, &a.dv))) return rc;
   if ((rc = check_tiles(call, "q", a.q)) || (rc = check_tiles(call, "d_o", a.d_o))) return rc;
   if (!lse && w->seqs && w->n_q) return fail(DFS_EINVAL, "%s: lse is NULL", call);
-  const PackedBwd L = bwd_layout(w);
+  const PackedBwd L = bwd_layout(w, dtype);
   if ((rc = check_scratch(call, L.total, ws, ws_bytes))) return rc;
   if (w->seqs == 0) return DFS_OK;
   if ((rc = check_apart(call, {{"dq", &a.dq}, {"dk", &a.dk}, {"dv", &a.dv}}, {{"q", &a.q}, {"k", &a.k}, {"v", &a.v}, {"o", &a.o}, {"d_o", &a.d_o}}))) return rc;

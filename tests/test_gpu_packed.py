@@ -39,6 +39,7 @@ CASES = {
     "blocks_many": (24, 12, 64, [(37 * i) % 90 for i in range(80)], None, -1, 0, 0, 0),
     "blocks_64_sequences": (16, 8, 128, [(29 * i) % 70 for i in range(64)], None, -1, 0, 0, 0),
     "blocks_two_groups_of_waves": (40, 40, 128, [333, 130, 200, 31], None, -1, 0, 0, 0),
+    "blocks_shared_by_three": (192, 32, 64, [250, 300], None, -1, 0, 1, 0),
     "blocks_9_key_heads": (18, 9, 128, [260, 700, 130], None, -1, 0, 0, 0),
     "blocks_more_queries_than_keys": (64, 64, 64, [140, 130], [70, 3], -1, 0, 0, 0),
 }
