@@ -54,7 +54,7 @@ template <bool E4M3> struct Entries {
 };
 
 // Whether the rows are so many that blocks of 128 of them, each over all its keys, are the faster way, and the launch of these.
-bool paged_is_long(const dfs_paged* w);
+bool paged_is_long(const dfs_paged* w, int dtype);
 int run_paged_long(const PagedArgs& a, int d, int dtype, bool bytes, hipStream_t st);
 
 }  // namespace dfs

@@ -692,7 +692,7 @@ size_t dfs_paged_workspace_bytes(const dfs_paged* w, int dtype, const dfs_pages*
   const char* call = "dfs_paged_workspace_bytes";
   PageArgs p;
   if (check_paged(call, w, dtype) != DFS_OK || check_pages(call, pages, dtype, w->seqs, w->heads_kv, w->d, false, &p) != DFS_OK) return 0;
-  if (w->seqs == 0 || w->n_q == 0 || paged_is_long(w)) return 0;
+  if (w->seqs == 0 || w->n_q == 0 || paged_is_long(w, dtype)) return 0;
   return part_bytes(w) + size_t(GROUPS) * 2 * 32 * sizeof(float2);
 }
 
@@ -709,7 +709,7 @@ int dfs_paged_attn_fwd(const dfs_paged* w, int dtype, const dfs_view* q, const d
   if ((rc = check_view(call, "o", o, dtype, 1, w->heads, w->n_q, w->d, true, &a.o))) return rc;
   if ((rc = check_pages(call, pages, dtype, w->seqs, w->heads_kv, w->d, false, &a.pages))) return rc;
   if (w->seqs == 0 || w->n_q == 0) return DFS_OK;
-  const size_t need = paged_is_long(w) ? 0 : part_bytes(w) + size_t(GROUPS) * 2 * 32 * sizeof(float2);
+  const size_t need = paged_is_long(w, dtype) ? 0 : part_bytes(w) + size_t(GROUPS) * 2 * 32 * sizeof(float2);
   if (need && (!ws || (uintptr_t(ws) & 255) || ws_bytes < need))
     return fail(DFS_EWORKSPACE, "%s: workspace of %zu bytes needed (256-byte aligned), got %zu", call, need, ws_bytes);
   if ((rc = check_apart(call, {{"o", &a.o}}, {{"q", &a.q}, {"pages.k", &a.pages.k}, {"pages.v", &a.pages.v}}))) return rc;
@@ -768,7 +768,7 @@ int dfs_paged_attn_fwd(const dfs_paged* w, int dtype, const dfs_view* q, const d
   };
   auto join = [&](auto t, auto d) { paged_join_kernel<decltype(t), decltype(d)::value><<<joins, 256, 0, st>>>(a, row_groups); };
   auto by_dim = [&](auto f) { w->d == 64 ? f(std::integral_constant<int, 64>{}) : f(std::integral_constant<int, 128>{}); };
-  if (paged_is_long(w)) return run_paged_long(a, w->d, dtype, bytes, st);
+  if (paged_is_long(w, dtype)) return run_paged_long(a, w->d, dtype, bytes, st);
   by_dim([&](auto d) {
     if (dtype == DFS_F32) run(float{}, d, std::false_type{});
     else if (bytes) run(uint16_t{}, d, std::true_type{});

@@ -173,8 +173,9 @@ template <int D> struct ByteFeed {
 
 // Blocks of 128 rows, if they were all full, need to be 128 (us, blocks of 128 against keys dealt out; e4m3, d = 128, 8 key heads of 4: 200 tokens of two prompts over 4 000 keys, 50 blocks,
 // 77 / 38; 500, 125, 81 / 70; 256 of sixteen, 64, 86 / 51; bf16, 8 of 8: 256 of 32, 128, 120 / 138; d = 64, 4 of 4: 600 of four over 3 000 keys, 75, 44 / 34;
-// 1 600 over 1 000, 200, 28 / 40).
-bool paged_is_long(const dfs_paged* w) { return int64_t(w->heads) * w->n_q >= 128 * 128; }
+// 1 600 over 1 000, 200, 28 / 40; fp32, d = 128, 32 of 8: 600 of four over 2 600, 150, 400 / 461), in fp32 at d = 64, where the others leave fewer rows empty, 256 (600 of four over 2 600, 150,
+// 206 / 124; 5 000 of one x 8, 312, 533 / 529; 2 000 of four over 1 500, 500, 223 / 302).
+bool paged_is_long(const dfs_paged* w, int dtype) { return int64_t(w->heads) * w->n_q >= (w->d == 64 && dtype == DFS_F32 ? 256 * 128 : 128 * 128); }
 
 int run_paged_long(const PagedArgs& args, int d, int dtype, bool bytes, hipStream_t st) {
   PagedArgs a = args;

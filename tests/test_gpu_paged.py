@@ -50,6 +50,8 @@ CASES = {
     "blocks_many": (16, 8, 128, 32, [(29 * i) % 70 for i in range(70)], [(29 * i) % 70 + 3 * i for i in range(70)], -1, 0, 0, 0),
     "blocks_long_small_pages": (44, 44, 64, 16, [130, 260], [2600, 1800], -1, 0, 0, 0),
     "blocks_long_small_pages_window": (44, 22, 128, 16, [130, 260], [2600, 1800], 1500, 33, 0, 0),
+    "blocks_more": (64, 32, 64, 32, [300, 1, 290], [300, 90, 700], -1, 0, 0, 0),
+    "blocks_more_small_pages_window": (80, 40, 64, 16, [330, 200], [330, 650], 150, 10, 0, 0),
     "blocks_more_queries_than_keys": (64, 64, 64, 16, [140, 130], [70, 3], -1, 0, 0, 0),
 }
 
@@ -132,7 +134,8 @@ def _check(w, dtype, q, p, q_lens, k_lens, front, table, scale, o, lse, mark=7.0
 def test_against_the_oracle(name, kind):
     w, dtype, q, p, q_start, k_len, q_lens, k_lens, front, table = _make(name, kind)
     scale = 1 / np.sqrt(w.d)
-    assert (P.dfs_paged_workspace_bytes(w, W.DT[dtype][0], p) == 0) == name.startswith("blocks")           # which of the two ways it goes
+    blocks = name.startswith("blocks") and not (kind == "f32" and w.d == 64 and w.heads * w.n_q < 256 * 128)
+    assert (P.dfs_paged_workspace_bytes(w, W.DT[dtype][0], p) == 0) == blocks          # which of the two ways it goes
     o, lse = _run(w, dtype, q, p, q_start, k_len, scale)
     _check(w, dtype, q, p, q_lens, k_lens, front, table, scale, o, lse)
     again, _ = _run(w, dtype, q, p, q_start, k_len, scale, lse=False)
