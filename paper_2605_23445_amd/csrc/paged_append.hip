@@ -1,12 +1,12 @@
 // New tokens on their way into a cache in pages: queries and keys normed and turned by their position, keys and values put into the pages of their sequence.
 //
 // The arithmetic of a row is that of qk_rope.hip.  Queries are worked on as there: a lane owns 16 bytes of a row at one token and walks over heads.  Keys and values
-// are worked on page by page: a work-group takes the new rows of one page and key head.  In 8 bits (e4m3, largest value 448) a page's rows share one power of two c,
+// are worked on page by page: a work-group takes the new rows of one page and key head, or, where they are few, a wave.  In 8 bits (e4m3, largest value 448) a page's rows share one power of two c,
 // the smallest with which the largest of them is at most 448 c: it is known when all of a page's new rows are, which therefore stay in registers, and
 // where there are rows from before it is not less than it was; if it grows they are divided by the quotient, which is exact but for what falls below e4m3's smallest.
 // Bound by memory: 16 384 tokens of five prompts, 32 + 2 x 8 heads, d = 128, into e4m3 pages of 64 rows: 91 us, 4.05 TB/s (69 where the inputs are in the memory-side cache; a plain
 // copy: 4.9); 5 130 x 3 x 12, d = 64, into bf16 pages of 16: 12 us, 3.9 TB/s.  The smallest calls are bound by the launch and a chain of loads (starts, lengths and rows, table,
-// scale): one token of 32 sequences 6.3 us.
+// scale): one token of 32 sequences 6.2 us, of 128 7.4, of 512 18.5 (15.5 with seven waves a SIMD in place of the four that a whole page's rows in registers leave).
 #include <float.h>
 
 #include "pages.h"
@@ -21,6 +21,7 @@ struct AppendArgs : Turns {
   const int32_t *q_start, *k_len, *positions;
   const float* w[2];
   int32_t seqs, tokens, heads, heads_kv, norm;
+  int32_t fours;                                     // work-groups of four pages
   int32_t q_groups, per;                             // work-groups of all tokens; heads that one walks over
   uint32_t page_share;                               // work-groups of pages in 8 bits out of all, in 2^-32, rounded up
 };
@@ -198,9 +199,9 @@ __device__ __forceinline__ uint32_t four_bytes(float a, float b, float c, float 
   return uint32_t(__builtin_amdgcn_cvt_pk_fp8_f32(c, d, __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false), true));
 }
 
-// Rows [0, n) of a page in 8 bits, times f.
-template <int D> __device__ __forceinline__ void shrink(const View& v, int page, int kvh, int n, float f) {
-  for (int i = threadIdx.x; i < n * (D / 16); i += 256) {
+// Rows [0, n) of a page in 8 bits, times f, by `threads` of which this is number t.
+template <int D> __device__ __forceinline__ void shrink(const View& v, int page, int kvh, int n, float f, int t, int threads) {
+  for (int i = t; i < n * (D / 16); i += threads) {
     u32x4* p = reinterpret_cast<u32x4*>(v.at(page, kvh, i / (D / 16)) + i % (D / 16) * 16);
     u32x4 x = *p;
 #pragma unroll
@@ -264,7 +265,7 @@ __device__ __forceinline__ void append_bytes(const AppendArgs& a, int id) {
     float scale = __uint_as_float(uint32_t(e) << 23);
     if (f.r0 > 0) {
       if (was[x] >= scale) scale = was[x];
-      else shrink<D>(x ? a.pages.v : a.pages.k, f.page, f.kvh, f.r0, was[x] / scale);
+      else shrink<D>(x ? a.pages.v : a.pages.k, f.page, f.kvh, f.r0, was[x] / scale, threadIdx.x, 256);
     }
     back[x] = 1.f / scale;
     if (threadIdx.x == 0) (x ? a.pages.v_scale : a.pages.k_scale)[scale_at] = scale;
@@ -286,14 +287,80 @@ __device__ __forceinline__ void append_bytes(const AppendArgs& a, int id) {
   }
 }
 
-// PASSES 0: pages of T.  The work-groups of pages, which compute more, are spread evenly among those of tokens, which move more.
-template <typename T, int D, bool PAIRS, int PASSES>
+// The same by a wave, where a page's new rows are as many as a wave has at once; false: they are more, and nothing is done.
+template <int D, bool PAIRS> __device__ __forceinline__ bool append_few_bytes(const AppendArgs& a, int id) {
+  using Tok = Turn<uint16_t, D, PAIRS, true>;
+  constexpr int N = Tok::N, L = Tok::L, R = 64 / L;
+  const Fresh f(a, id);
+  if (!f.real) return true;
+  if (f.r1 - f.r0 > R) return false;
+  const int lane = threadIdx.x & 63, c = lane % L, r = f.r0 + lane / L, at = min_of(r, f.r1 - 1);        // past the last row that once more
+  float w[N], y[N], z[N], top[2] = {};
+  const u32x4 raw = load_chunk<false>(a.in[1].at(0, f.kvh, f.row0 + at) + c * 16), v = load_chunk<false>(a.in[2].at(0, f.kvh, f.row0 + at) + c * 16);
+  weights<N>(a.w[1], c, w);
+  if (f.page < 0) return true;
+  const int scale_at = f.page * a.heads_kv + f.kvh;
+  const float was[2] = {a.pages.k_scale[scale_at], a.pages.v_scale[scale_at]};
+  Tok tok;
+  set_turn(a, tok, lane, f.row0 + at, f.p0 + at);
+  Chunk<uint16_t>::open(raw, y);
+  norm_and_turn<uint16_t, D, PAIRS>(a, tok, w, y);
+  Chunk<uint16_t>::open(v, z);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    top[0] = fmaxf(top[0], size_of(y[i]));
+    top[1] = fmaxf(top[1], size_of(z[i]));
+  }
+  float back[2];                                     // 1 / c
+#pragma unroll
+  for (int x = 0; x < 2; ++x) {
+#pragma unroll
+    for (int m = 1; m < 64; m *= 2) top[x] = fmaxf(top[x], __shfl_xor(top[x], m));
+    float scale = __uint_as_float(uint32_t(scale_exponent(top[x])) << 23);
+    if (f.r0 > 0) {
+      if (was[x] >= scale) scale = was[x];
+      else shrink<D>(x ? a.pages.v : a.pages.k, f.page, f.kvh, f.r0, was[x] / scale, lane, 64);
+    }
+    back[x] = 1.f / scale;
+    if (lane == 0) (x ? a.pages.v_scale : a.pages.k_scale)[scale_at] = scale;
+  }
+  if (r >= f.r1) return true;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    y[i] *= back[0];
+    z[i] *= back[1];
+  }
+  *reinterpret_cast<uint2*>(a.pages.k.at(f.page, f.kvh, r) + c * 8) = make_uint2(four_bytes(y[0], y[1], y[2], y[3]), four_bytes(y[4], y[5], y[6], y[7]));
+  *reinterpret_cast<uint2*>(a.pages.v.at(f.page, f.kvh, r) + c * 8) = make_uint2(four_bytes(z[0], z[1], z[2], z[3]), four_bytes(z[4], z[5], z[6], z[7]));
+  return true;
+}
+
+// Four pages to a work-group, a wave for each; those with more rows one after the other by all of it.  The four are far apart, so that a prompt's pages among single tokens are
+// many work-groups'.  (Past the last page there is no sequence's.)
+template <int D, bool PAIRS, int PASSES>
+__device__ __forceinline__ void append_four(const AppendArgs& a, int id) {
+  __shared__ int more[4];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const bool done = append_few_bytes<D, PAIRS>(a, wave * a.fours + id);
+  more[wave] = 0;
+  if (!done) more[wave] = 1;
+  __syncthreads();
+  for (int i = 0; i < 4; ++i)
+    if (__builtin_amdgcn_readfirstlane(more[i])) {
+      append_bytes<D, PAIRS, PASSES>(a, i * a.fours + id);
+      __syncthreads();                               // what its waves told one another has been read
+    }
+}
+
+// PASSES 0: pages of T; FOURS: in 8 bits, few new rows each.  The work-groups of pages, which compute more, are spread evenly among those of tokens, which move more.
+template <typename T, int D, bool PAIRS, int PASSES, bool FOURS>
 __global__ void __launch_bounds__(256) paged_append_kernel(AppendArgs a) {
   const int id = blockIdx.x;
   if constexpr (PASSES > 0) {
     const int pages = int(__umulhi(uint32_t(id), a.page_share));         // of the work-groups in front of this one
-    if (int(__umulhi(uint32_t(id) + 1, a.page_share)) > pages) append_bytes<D, PAIRS, PASSES>(a, pages);
-    else append_tokens<T, D, PAIRS, false>(a, id - pages);
+    if (int(__umulhi(uint32_t(id) + 1, a.page_share)) <= pages) append_tokens<T, D, PAIRS, false>(a, id - pages);
+    else if constexpr (FOURS) append_four<D, PAIRS, PASSES>(a, pages);
+    else append_bytes<D, PAIRS, PASSES>(a, pages);
   } else {
     append_tokens<T, D, PAIRS, true>(a, id);
   }
@@ -356,13 +423,24 @@ int dfs_paged_append(const dfs_qk_geom* g, int dtype, const dfs_view* q, const d
   if (y > all) y = all;
   a.per = int((all + y - 1) / y);
   a.q_groups = int((n * L + 255) / 256);
-  const int64_t page_blocks = bytes && a.pages.row ? slots * g->heads_kv : 0, blocks = int64_t(a.q_groups) * ((all + a.per - 1) / a.per) + page_blocks;
+  // A wave for a page where a sequence has no more rows on average than a wave has at once, else a work-group (us, wave against work-group, 8 key heads, d = 128, pages of 64 rows: one token
+  // of 32 streams 6.2 / 6.7, of 128 7.4 / 12.3, of 512 18.5 / 35.8; four of 128 11.3 / 15.9, eight 29.4 / 19.5; d = 64, eight of 128 10.8 / 13.5, sixteen 27.2 / 17.5; one token of 127 and a
+  // piece of 380 19.1 / 19.6).
+  const bool few = bytes && n <= int64_t(g->batch) * (64 / L);
+  const int64_t all_pages = bytes && a.pages.row ? slots * g->heads_kv : 0, page_blocks = few ? (all_pages + 3) / 4 : all_pages;
+  a.fours = int(page_blocks);
+  const int64_t blocks = int64_t(a.q_groups) * ((all + a.per - 1) / a.per) + page_blocks;
   if (blocks >= 1 << 24) return fail(DFS_ESHAPE, "%s: tokens=%d x heads=%d too large", call, g->tokens, g->heads);
   a.page_share = uint32_t(((uint64_t(page_blocks) << 32) + blocks - 1) / blocks);
   const int passes = !bytes ? 0 : pages->page * L / 256 > 1 ? pages->page * L / 256 : 1;
   const hipStream_t st = as_stream(stream);
   auto run = [&](auto t, auto d, auto p, auto s) {
-    paged_append_kernel<decltype(t), decltype(d)::value, decltype(p)::value, decltype(s)::value><<<unsigned(blocks), 256, 0, st>>>(a);
+    using T = decltype(t);
+    constexpr int D = decltype(d)::value, PASSES = decltype(s)::value;
+    constexpr bool PAIRS = decltype(p)::value;
+    if constexpr (PASSES > 0)
+      if (few) return paged_append_kernel<T, D, PAIRS, PASSES, true><<<unsigned(blocks), 256, 0, st>>>(a);
+    paged_append_kernel<T, D, PAIRS, PASSES, false><<<unsigned(blocks), 256, 0, st>>>(a);
   };
   auto by_passes = [&](auto t, auto d, auto p) {
     if (!passes) run(t, d, p, std::integral_constant<int, 0>{});

@@ -26,6 +26,9 @@ CASES = {
     "large_pages_d64": (4, 2, 64, 128, False, (32,), False, False, [(300, 100), (128, 128), (129, 127)]),
     "pages_of_32": (3, 3, 128, 32, True, (44, 42, 42), True, True, [(50, 10), (100, 0)]),
     "many_streams": (4, 2, 64, 16, False, (64,), True, False, [(i % 3, (5 * i) % 47) for i in range(150)]),
+    # few tokens a sequence but for some, whose pages get many rows
+    "few_but_two": (4, 2, 128, 64, False, (128,), True, False, [(1, 7 * i) for i in range(60)] + [(100, 30), (0, 3), (64, 0)]),
+    "few_but_one": (3, 3, 64, 128, True, (16, 24, 24), True, True, [(i % 4, 97 + i) for i in range(40)] + [(90, 60)]),
     "many_heads": (41, 9, 64, 64, False, (64,), True, False, [(70, 3), (9, 60)]),
 }
 
