@@ -70,6 +70,8 @@ static PackedFwd fwd_layout(const dfs_packed* w, int dtype) {
   // 96, 29.4 / 29.1; 1 000 of four x 16 heads of 4, 140, 12.2 / 16.8; d = 64: 1 770 of three x 9 of 3, 132, 15.1 / 11.0; 1 500 x 16, 192, 24.0 / 24.4; 2 000 of
   // six x 12, 252, 11.9 / 15.2; fp32, d = 64: 2 000 x 16 of 4, 252, 181 / 142; 1 000 of four x 32 of 8, 280, 43 / 49).
   if (rows > 32 && (rows / 128 + some_seqs) * w->heads_kv > (w->d == 128 ? 96 : dtype == DFS_F32 ? 256 : 192)) return L;
+  // Sequences without rows have room for a block as well: so many of them that blocks of 32 rows pass a grid's 2^32 threads leave those of 128, which the checks have counted.
+  if (L.blocks >= 1 << 24) return L;
   const int waves = dtype == DFS_F32 && w->d == 128 ? 2 : 4;
   int64_t keys = likely(w->n_k, w);
   const int64_t reach = int64_t(w->left) + w->right + 32 / group + 1;

@@ -194,6 +194,20 @@ def test_most_keys():
     assert torch.equal(o, v.expand(kv, 3, d).repeat_interleave(heads // kv, 0))
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_most_sequences(dtype):
+    """As many sequences as there may be, two of which have rows: blocks of 32 rows, one for each sequence at least, would pass a grid's 2^32 threads."""
+    seqs, n, d, at = (1 << 24) - 2, [24, 40], 64, [5, (1 << 24) - 9]
+    w = P.Packed(seqs, 1, 1, d, sum(n), sum(n), -1, 0)
+    gen = torch.Generator(device="cuda").manual_seed(13)
+    q, k, v, d_o = (torch.randn(1, sum(n), d, generator=gen, device="cuda").to(DT[dtype][1]) for _ in range(4))
+    start = torch.zeros(seqs + 1, dtype=torch.int32, device="cuda")
+    for a, m in zip(at, n):
+        start[a + 1:] += m
+    got = _run(w, dtype, q, k, v, d_o, start, None, 0.125)
+    _check(w, dtype, q, k, v, d_o, n, n, 0, 0.125, got)
+
+
 def test_captured_and_replayed():
     """Forward and backward in a graph, replayed with other lengths in the same start array, and a second graph with a workspace of its own."""
     w, q, k, v, d_o, q_start, _, q_lens, k_lens, front = _make("blocks_causal", "bf16", 6)
