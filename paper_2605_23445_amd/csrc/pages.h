@@ -34,6 +34,10 @@ inline int check_pages(const char* call, const dfs_pages* p, int dtype, int seqs
   if (some && !p->table) return fail(DFS_EINVAL, "%s: table is NULL", call);
   if (bytes ? some && (!p->k_scale || !p->v_scale) : p->k_scale || p->v_scale)
     return fail(DFS_EINVAL, "%s: pages have scales if they are of DFS_E4M3, and only then", call);
+  if (bytes && some && output) {                     // both are written, each by the values of its own
+    const uintptr_t x = uintptr_t(p->k_scale), y = uintptr_t(p->v_scale);
+    if ((x < y ? y - x : x - y) / sizeof(float) < uint64_t(p->pages) * heads_kv) return fail(DFS_EINVAL, "%s: k_scale and v_scale share memory", call);
+  }
   int rc;
   if ((rc = check_view(call, "pages.k", &p->k, p->dtype, p->pages, heads_kv, p->page, d, output, &a->k))) return rc;
   if ((rc = check_view(call, "pages.v", &p->v, p->dtype, p->pages, heads_kv, p->page, d, output, &a->v))) return rc;

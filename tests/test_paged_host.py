@@ -65,6 +65,13 @@ def test_append_arguments(kw, code):
     assert _append(**kw) == code and lib.dfs_last_error()
 
 
+def test_scales_that_share_memory():
+    """They are written by the append, each by its own values; reading may take one for both."""
+    for at in (AT * 12, AT * 12 + 4, AT * 12 + 4 * (40 * 2 - 1), AT * 12 - 4):
+        assert _append(pages=_pages(v_scale=at)) == -1 and b"share memory" in lib.dfs_last_error()
+        assert _read(pages=_pages(v_scale=at), ws=None) == -4                # refused for the workspace alone
+
+
 @pytest.mark.parametrize("geom,code", [
     ("none", -1), (dict(seqs=-1), -2), (dict(seqs=1 << 20), -2), (dict(n_q=-1), -2), (dict(n_q=(1 << 28) + 1), -2), (dict(heads=0), -2), (dict(heads=65536), -2), (dict(heads_kv=3), -2),
     (dict(heads_kv=0), -2), (dict(d=80), -2), (dict(sinks=-1), -2), (dict(n_q=1 << 28), -2)])
