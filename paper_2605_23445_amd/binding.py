@@ -625,19 +625,22 @@ _CACHE_TYPES = {torch.float32: DFS_F32, torch.bfloat16: DFS_BF16, torch.float8_e
 
 
 def _pages(p: Pages | None, seqs: int, heads_kv: int, d: int):
-    """dfs_pages of a cache (None -> NULL)."""
-    if p is None:
+    """dfs_pages of a cache (None -> NULL).  What is missing of one has no memory, which the library says."""
+    some = None if p is None else p.v if p.k is None else p.k
+    if some is None:
         return None
-    if p.k.dtype not in _CACHE_TYPES:
-        raise ValueError(f"pages.k must be float32, bfloat16 or float8_e4m3fn, got {p.k.dtype}")
-    if p.k.dim() != 4:
-        raise ValueError(f"pages.k must be [pages, heads_kv, page, d], got {list(p.k.shape)}")
-    if p.table.dim() != 2 or p.table.shape[0] != seqs:
+    name = "pages.v" if p.k is None else "pages.k"
+    if some.dtype not in _CACHE_TYPES:
+        raise ValueError(f"{name} must be float32, bfloat16 or float8_e4m3fn, got {some.dtype}")
+    if some.dim() != 4:
+        raise ValueError(f"{name} must be [pages, heads_kv, page, d], got {list(some.shape)}")
+    if p.table is not None and (p.table.dim() != 2 or p.table.shape[0] != seqs):
         raise ValueError(f"pages.table must be [{seqs}, entries], got {list(p.table.shape)}")
-    code, n, page = _CACHE_TYPES[p.k.dtype], p.k.shape[0], p.k.shape[2]
-    return _PagesC(_view(p.k, code, n, heads_kv, page, d, "pages.k"), _view(p.v, code, n, heads_kv, page, d, "pages.v"),
+    code, n, page, row = _CACHE_TYPES[some.dtype], some.shape[0], some.shape[2], 1 if p.table is None else p.table.shape[1]
+    view = lambda t, t_name: _View() if t is None else _view(t, code, n, heads_kv, page, d, t_name)  # noqa: E731
+    return _PagesC(view(p.k, "pages.k"), view(p.v, "pages.v"),
                    _flat(p.k_scale, torch.float32, n * heads_kv, "pages.k_scale"), _flat(p.v_scale, torch.float32, n * heads_kv, "pages.v_scale"),
-                   _flat(p.table, torch.int32, 0, "pages.table"), n, page, p.table.shape[1], code)
+                   _flat(p.table, torch.int32, 0, "pages.table"), n, page, row, code)
 
 
 def dfs_paged_append(g: QkGeom, dtype: int, q, k, v, q_start, k_len, positions, w_q, w_k, q_out, pages: Pages, norm: bool = True):

@@ -291,3 +291,22 @@ def test_refusals_of_the_binding():
         with pytest.raises(P.DfsError):
             P.dfs_paged_append(*args)
     assert not out.any() and _same(before, p)
+
+
+@pytest.mark.parametrize("kind", list(KINDS))
+def test_pages_without_a_part(kind):
+    """A cache that lacks its keys, its values or its table: the library's error, as for a call without a cache."""
+    g, code, q, k, v, q_start, k_len, pos, w, p, norm, lens, front, table = _make("later_pieces", kind)
+    out, before = torch.zeros(g.heads, g.tokens, g.d, dtype=q.dtype, device="cuda"), _copy(p)
+    read = P.Paged(g.batch, g.heads, g.heads_kv, g.d, g.tokens, -1, 0)
+    for part in ("k", "v", "table", "k v"):
+        bad = P.Pages(**dict(dict(k=p.k, v=p.v, table=p.table, k_scale=p.k_scale, v_scale=p.v_scale), **{x: None for x in part.split()}))
+        with pytest.raises(P.DfsError, match="pages" if part != "table" else "table"):
+            P.dfs_paged_append(g, code, q, k, v, q_start, k_len, pos, w[0], w[1], out, bad, norm)
+        with pytest.raises(P.DfsError, match="pages" if part != "table" else "table"):
+            P.dfs_paged_attn_fwd(read, code, q, bad, q_start, k_len, 0.1, out, None, torch.empty(1 << 25, dtype=torch.uint8, device="cuda"))
+        assert P.dfs_paged_workspace_bytes(read, code, bad) == 0
+    if kind == "e4m3":
+        with pytest.raises(P.DfsError, match="share memory"):
+            P.dfs_paged_append(g, code, q, k, v, q_start, k_len, pos, w[0], w[1], out, P.Pages(p.k, p.v, p.table, p.k_scale, p.k_scale), norm)
+    assert not out.any() and _same(before, p)

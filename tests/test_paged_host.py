@@ -2,6 +2,7 @@
 import ctypes as C
 
 import pytest
+import torch
 
 P = pytest.importorskip("paper_2605_23445_amd")
 from paper_2605_23445_amd import binding as B  # noqa: E402
@@ -103,3 +104,10 @@ def test_nothing_to_do():
     assert _append(geom=dict(batch=0)) == 0
     assert _read(geom=dict(n_q=0), q=none, o=none, ws=None) == 0
     assert _read(geom=dict(seqs=0), q_start=None, k_len=None, ws=None) == 0
+
+
+def test_a_cache_without_pages():
+    """What the binding makes of parts that are None, without a GPU: nothing of its own goes wrong."""
+    assert B._pages(None, 3, 2, 128) is None and B._pages(P.Pages(None, None, None), 3, 2, 128) is None
+    with pytest.raises(ValueError, match="pages.v must be"):
+        B._pages(P.Pages(None, torch.zeros(4, 2, 16, 128, dtype=torch.float16), None), 3, 2, 128)
