@@ -461,7 +461,8 @@ typedef struct {
  * stands in the table once, at one sequence; pages that are only read may be shared.
  * DFS_E4M3: the scale of a page and key head is the smallest power of two c, 2^-120 at least, by which the largest of the page's values is 448 c at most, or, with rows from
  * before the call, their scale if that is larger; k_scale and v_scale share no memory.  Values are normed and turned in fp32 and rounded once; where a scale grows the rows from before are rounded anew, which
- * moves only what falls below the type's smallest value.  An infinite value is stored as NaN; NaN and infinities do not count for the scale.
+ * moves only what falls below the type's smallest value.  Rows from before whose scale is NaN or infinite become NaN.  An infinite value is stored as NaN; NaN and infinities
+ * do not count for the scale.
  */
 int dfs_paged_append(const dfs_qk_geom* g, int dtype, const dfs_view* q, const dfs_view* k, const dfs_view* v, const int32_t* q_start, const int32_t* k_len,
                      const int32_t* positions, const float* w_q, const float* w_k, const dfs_view* q_out, const dfs_pages* pages, int norm, void* stream);

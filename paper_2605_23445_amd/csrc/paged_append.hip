@@ -193,6 +193,10 @@ __device__ __forceinline__ int scale_exponent(float m) {
   const uint32_t b = __float_as_uint(m);
   return max_of(int(b >> 23) - 8 + ((b & 0x7FFFFFu) > 0x600000u), 7);
 }
+// The scale of rows from before, as reading takes it: of a number that is no power of two the exponent alone counts.
+__device__ __forceinline__ float scale_of(float was) { return __uint_as_float(__float_as_uint(was) & 0x7F800000u); }
+// Whether it stays where new rows take `scale`.  One that is not finite does not: its rows become NaN.
+__device__ __forceinline__ bool stays(float was, float scale) { return was >= scale && was <= FLT_MAX; }
 // Infinities and NaN do not count for a scale.
 __device__ __forceinline__ float size_of(float x) { return fabsf(x) <= FLT_MAX ? fabsf(x) : 0.f; }
 __device__ __forceinline__ uint32_t four_bytes(float a, float b, float c, float d) {
@@ -234,7 +238,7 @@ __device__ __forceinline__ void append_bytes(const AppendArgs& a, int id) {
   weights<N>(a.w[1], c, w);
   if (f.page < 0) return;
   const int scale_at = f.page * a.heads_kv + f.kvh;
-  const float was[2] = {a.pages.k_scale[scale_at], a.pages.v_scale[scale_at]};
+  const float was[2] = {scale_of(a.pages.k_scale[scale_at]), scale_of(a.pages.v_scale[scale_at])};
 #pragma unroll
   for (int u = 0; u < PASSES; ++u) {
     if (f.r0 + u * R >= f.r1) continue;
@@ -264,7 +268,7 @@ __device__ __forceinline__ void append_bytes(const AppendArgs& a, int id) {
     const int e = scale_exponent(fmaxf(fmaxf(most[x][0], most[x][1]), fmaxf(most[x][2], most[x][3])));
     float scale = __uint_as_float(uint32_t(e) << 23);
     if (f.r0 > 0) {
-      if (was[x] >= scale) scale = was[x];
+      if (stays(was[x], scale)) scale = was[x];
       else shrink<D>(x ? a.pages.v : a.pages.k, f.page, f.kvh, f.r0, was[x] / scale, threadIdx.x, 256);
     }
     back[x] = 1.f / scale;
@@ -300,7 +304,7 @@ template <int D, bool PAIRS> __device__ __forceinline__ bool append_few_bytes(co
   weights<N>(a.w[1], c, w);
   if (f.page < 0) return true;
   const int scale_at = f.page * a.heads_kv + f.kvh;
-  const float was[2] = {a.pages.k_scale[scale_at], a.pages.v_scale[scale_at]};
+  const float was[2] = {scale_of(a.pages.k_scale[scale_at]), scale_of(a.pages.v_scale[scale_at])};
   Tok tok;
   set_turn(a, tok, lane, f.row0 + at, f.p0 + at);
   Chunk<uint16_t>::open(raw, y);
@@ -318,7 +322,7 @@ template <int D, bool PAIRS> __device__ __forceinline__ bool append_few_bytes(co
     for (int m = 1; m < 64; m *= 2) top[x] = fmaxf(top[x], __shfl_xor(top[x], m));
     float scale = __uint_as_float(uint32_t(scale_exponent(top[x])) << 23);
     if (f.r0 > 0) {
-      if (was[x] >= scale) scale = was[x];
+      if (stays(was[x], scale)) scale = was[x];
       else shrink<D>(x ? a.pages.v : a.pages.k, f.page, f.kvh, f.r0, was[x] / scale, lane, 64);
     }
     back[x] = 1.f / scale;

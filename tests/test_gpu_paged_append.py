@@ -237,6 +237,48 @@ def test_values_that_are_not_finite():
     assert float(p.v_scale) == 2.0 ** 120 and torch.equal(p.v.float()[0, 0, :3], (far[0].float() / 2.0 ** 120).to(torch.float8_e4m3fn).float())
 
 
+@pytest.mark.parametrize("new", [1, 3, 20])                     # a wave's page, at d = 128 a work-group's from five rows on
+@pytest.mark.parametrize("size", [1.0, 2.0 ** 30])            # the rows' scale stays, or grows
+def test_rows_from_before_with_a_scale_of_the_users(size, new):
+    """e4m3: of a scale that is no power of two the exponent alone counts, for attention and for an append behind the rows that have it, whose new rows stand beside them."""
+    g = P.QkGeom(1, new, 1, 1, 128, 0, 1, 128, 0, 0, 1e4, 1e-5)
+    gen = torch.Generator(device="cuda").manual_seed(14)
+    was = torch.randn(2, 1, 1, 32, 128, generator=gen, device="cuda").to(torch.float8_e4m3fn)
+    k, v = (torch.randn(2, 1, new, 128, generator=gen, device="cuda") * size).bfloat16()
+    start, length = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in ([0, new], [7 + new]))
+    table, caches = torch.zeros(1, 1, dtype=torch.int32, device="cuda"), []
+    for scales in ((-3.5, 1.25 * 2.0 ** 9), (2.0, 2.0 ** 9)):
+        p = P.Pages(*was.clone(), table, *(torch.full((1, 1), x, device="cuda") for x in scales))
+        one = torch.tensor([0, 1], dtype=torch.int32, device="cuda")
+        w, o = P.Paged(1, 1, 1, 128, 1, -1, 0), torch.empty(1, 1, 128, dtype=torch.bfloat16, device="cuda")
+        ws = torch.empty(P.dfs_paged_workspace_bytes(w, P.DFS_BF16, p), dtype=torch.uint8, device="cuda")
+        P.dfs_paged_attn_fwd(w, P.DFS_BF16, k[:, :1] / size, p, one, torch.full_like(length, 7), 0.01, o, None, ws)
+        P.dfs_paged_append(g, P.DFS_BF16, k, k, v, start, length, None, None, None, torch.empty_like(k), p, False)
+        caches.append((p, o))
+    (a, o_a), (b, o_b) = caches
+    assert _same(a, b) and torch.equal(o_a, o_b)
+    assert (float(a.k_scale), float(a.v_scale)) == (2.0, 512.0) if size == 1 else min(float(a.k_scale), float(a.v_scale)) > 2.0 ** 20
+
+
+@pytest.mark.parametrize("new", [2, 20])
+def test_rows_from_before_whose_scale_is_not_finite(new):
+    """e4m3: they become NaN, the new ones are as on a page of their own scale."""
+    g = P.QkGeom(1, new, 1, 1, 128, 0, 1, 128, 0, 0, 1e4, 1e-5)
+    gen = torch.Generator(device="cuda").manual_seed(15)
+    k, v = torch.randn(2, 1, new, 128, generator=gen, device="cuda").bfloat16()
+    start, length = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in ([0, new], [7 + new]))
+    caches = []
+    for scales in ((float("nan"), float("inf")), (2.0 ** -110, 2.0 ** -110)):
+        p = P.Pages(*torch.ones(2, 1, 1, 32, 128, device="cuda").to(torch.float8_e4m3fn), torch.zeros(1, 1, dtype=torch.int32, device="cuda"),
+                    *(torch.full((1, 1), x, device="cuda") for x in scales))
+        P.dfs_paged_append(g, P.DFS_BF16, k, k, v, start, length, None, None, None, torch.empty_like(k), p, False)
+        caches.append(p)
+    a, b = caches
+    for x, y in ((a.k, b.k), (a.v, b.v)):
+        assert torch.isnan(x[0, 0, :7].float()).all() and torch.equal(_bits(x[0, 0, 7:]), _bits(y[0, 0, 7:]))
+    assert torch.equal(a.k_scale, b.k_scale) and torch.equal(a.v_scale, b.v_scale)
+
+
 def test_pages_past_32_bits():
     """A page more than 2^32 bytes behind the first."""
     g = P.QkGeom(1, 5, 1, 1, 128, 0, 1, 128, 0, 0, 1e4, 1e-5)
