@@ -397,7 +397,8 @@ __global__ void __launch_bounds__((64 * paged_waves<T, D, E4M3>()), 1) paged_spl
     auto first = [&](int i) { return __builtin_amdgcn_readfirstlane(s_first[i]); };
     s = first(0);
     off = first(1);
-    seq = PagedSeq(a, first(2), first(2) + first(3), first(4));
+    // (where starts fall so far that the units of all pass 31 bits, several threads may have written these: no row outside the tensors comes of it)
+    seq = PagedSeq(a, first(2), first(2) + min_of(first(3), a.n_q - first(2)), first(4));
   }
   if (s >= a.packed) return;
 

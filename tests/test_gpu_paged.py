@@ -218,6 +218,23 @@ def test_starts_lengths_and_tables_that_break_the_format(name, kind):
         assert (around[1] == 7).all() and (around[0, 0] == 7).all() and (around[0, -1] == 7).all()
 
 
+def test_falling_starts_over_long_lists():
+    """Starts that fall so often, over such long lists, that the work of all sequences passes 32 bits and two of them claim the same piece: one of rows 0 .. 1 023, one of 512 .. 1 023.
+    Nothing behind the last row is touched."""
+    n_q, n_k = 1024, 1 << 28
+    start = torch.tensor([0, n_q] * 64 + [512, n_q] * 2, dtype=torch.int32, device="cuda")
+    w = P.Paged(len(start) - 1, 1, 1, 64, n_q, -1, 0)
+    gen = torch.Generator(device="cuda").manual_seed(13)
+    k, v = (torch.randn(1, 1, 128, 64, generator=gen, device="cuda").bfloat16() for _ in range(2))
+    p = P.Pages(k, v, torch.zeros(w.seqs, n_k // 128, dtype=torch.int32, device="cuda"))
+    q, around = torch.randn(1, n_q, 64, generator=gen, device="cuda").bfloat16(), torch.full((4, n_q, 64), 7.0, dtype=torch.bfloat16, device="cuda")
+    sums = torch.full((4 * n_q,), 7.0, device="cuda")
+    P.dfs_paged_attn_fwd(w, P.DFS_BF16, q, p, start, torch.full((w.seqs,), n_k, dtype=torch.int32, device="cuda"), 0.1, around[1:2], sums[n_q:2 * n_q].view(1, n_q), _ws(w, "bf16", p))
+    torch.cuda.synchronize()
+    for x in (around, sums.view(4, n_q)):
+        assert (x[0] == 7).all() and (x[2:] == 7).all()
+
+
 @pytest.mark.parametrize("kind", list(KINDS))
 @pytest.mark.parametrize("name", ["one_token_each", "blocks_group"])
 def test_sequences_that_share_pages(name, kind):
