@@ -10,7 +10,6 @@ typedef int i32x2 __attribute__((ext_vector_type(2)));
 struct PagedArgs : WindowArgs {                      // n_k: what the table has room for
   PageArgs pages;
   int32_t unit;                                      // pieces that are dealt out together
-  int32_t least;                                     // units that a work-group takes at least
   int32_t row_bits;                                  // a block has 1 << row_bits rows
 };
 

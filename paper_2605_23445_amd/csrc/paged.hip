@@ -46,7 +46,7 @@ template <int NT> struct Deal {
       const int upto = wave_sums(mine);
       before = upto - mine;
       total = __builtin_amdgcn_readlane(upto, 63);
-      per = max_of((total + GROUPS - 1) / GROUPS, a.least);
+      per = max_of((total + GROUPS - 1) / GROUPS, 1);
       return;
     }
     each = (a.packed + NT - 1) / NT;
@@ -65,7 +65,7 @@ template <int NT> struct Deal {
       if (w < wave) before += sums[w];
       total += sums[w];
     }
-    per = max_of((total + GROUPS - 1) / GROUPS, a.least);
+    per = max_of((total + GROUPS - 1) / GROUPS, 1);
   }
 };
 
@@ -742,7 +742,6 @@ int dfs_paged_attn_fwd(const dfs_paged* w, int dtype, const dfs_view* q, const d
   const int row_bytes = w->d * (bytes ? 1 : elem_size(dtype));
   a.unit = 1024 / row_bytes < 8 ? 1024 / row_bytes : 8;                  // a piece for each wave
   while (items * ((pieces + a.unit - 1) / a.unit) >= int64_t(1) << 30) a.unit *= 2;          // units are counted in 31 bits, and the last work-group's run may end behind them
-  a.least = 1;
   // Where no row sees many pieces an item is one unit: no parts, no second launch (us, whole against parts; one token of two streams x 2 key heads, d = 128, e4m3, 8 waves:
   // 1 024 keys 9.8 / 10.9, 2 048 12.9 / 10.8; bf16, 4 waves: 512 keys 10.0 / 10.4, 1 024 13.0 / 10.5; of 16 streams x 8, which fill the chip by themselves: e4m3
   // 2 048 keys 16.8 / 20.9, bf16 23.9 / 25.4.  fp32, where the matrix instructions of a piece take 2 us: 8 streams x 8, d = 128, 2 waves: 64 keys 10.1 / 12.1, 130 14.4 / 13.6;

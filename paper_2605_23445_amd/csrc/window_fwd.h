@@ -1,4 +1,5 @@
-// Kernels of attention over a window around each query's position and a few first keys, of sequences of one length (PACKED false) or packed ones.
+// Kernels of attention over a window around each query's position and a few first keys, of sequences of one length, of packed ones, or of
+// packed rows over a cache in pages (KIND).
 //
 // The rows of a work-group are queries of ALL heads that share a key head, query by query (row r is head r % group of query r / group): a tile of
 // keys and values is brought in once for the group, and a block of rows spans fewer positions, so that it meets fewer tiles of which it
