@@ -42,6 +42,7 @@ CASES = {
     "blocks_shared_by_three": (192, 32, 64, [250, 300], None, -1, 0, 1, 0),
     "blocks_9_key_heads": (18, 9, 128, [260, 700, 130], None, -1, 0, 0, 0),
     "blocks_more_queries_than_keys": (64, 64, 64, [140, 130], [70, 3], -1, 0, 0, 0),
+    "blocks_one_token_each": (32, 8, 64, [1 - i % 9 // 8 for i in range(90)], [(37 * i) % 150 for i in range(90)], -1, 0, 0, 1),
 }
 
 
@@ -148,6 +149,37 @@ def test_starts_that_break_the_format(name, dtype):
         P.dfs_packed_attn_fwd(w, DT[dtype][0], q, k, v, falling.int(), None, 0.1, o, None, _ws(w, dtype, False))
         torch.cuda.synchronize()
         assert (room[1] == 7).all() and (room[0, 0] == 7).all() and (room[0, -1] == 7).all()
+
+
+def _guarded(shape, dtype, mark=7.0):
+    """A tensor with as much room of marks in front of it and behind."""
+    n = (int(np.prod(shape)) + 4096) // 256 * 256
+    room = torch.full((2 * n + int(np.prod(shape)),), mark, dtype=dtype, device="cuda")
+    return room[n:-n].view(shape), (room[:n], room[-n:])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("name", ["causal", "causal_d64", "later_pieces", "many_short", "many_short_keys", "blocks_causal", "blocks_many", "blocks_64_sequences", "blocks_shared_by_three",
+                                  "blocks_both_ways_window"])
+def test_starts_that_fall_touch_nothing_outside(name, dtype):
+    """Both passes, with starts of queries, of keys or of both that fall, up to 64 sequences and more: nothing in front of or behind o, log-sum-exp, gradients and workspaces."""
+    w, q, k, v, d_o, q_start, k_start, *_ = _make(name, dtype, 14)
+    code, dt = DT[dtype][:2]
+    own = q_start if k_start is None else k_start
+    odd = torch.arange(w.seqs + 1, device="cuda") % 2 == 1
+    falls = lambda x, n: (x.flip(0), torch.where(odd, -x, x), torch.where(odd, torch.zeros_like(x), torch.full_like(x, n + 9)))  # noqa: E731
+    cases = [(a, None if k_start is None else own) for a in falls(q_start, w.n_q)] + [(q_start, b) for b in falls(own, w.n_k)] + list(zip(falls(q_start, w.n_q), falls(own, w.n_k)))
+    for a, b in cases:
+        if b is None and w.n_k != w.n_q:
+            continue
+        (o, o_room), (dq, dq_room), (dk, dk_room), (dv, dv_room) = (_guarded(x.shape, dt) for x in (q, q, k, v))
+        lse, lse_room = _guarded((w.heads, w.n_q), torch.float32)
+        rooms = [*o_room, *dq_room, *dk_room, *dv_room, *lse_room]
+        ws = [_guarded((P.dfs_packed_workspace_bytes(w, code, back),), torch.uint8, 7) for back in (False, True)]
+        P.dfs_packed_attn_fwd(w, code, q, k, v, a.int(), None if b is None else b.int(), 0.1, o, lse, ws[0][0])
+        P.dfs_packed_attn_bwd(w, code, q, k, v, o, lse, d_o, a.int(), None if b is None else b.int(), 0.1, dq, dk, dv, ws[1][0])
+        torch.cuda.synchronize()
+        assert all((x == 7).all() for x in rooms + [*ws[0][1], *ws[1][1]])
 
 
 def test_same_as_window_attention():

@@ -53,6 +53,9 @@ CASES = {
     "blocks_more": (64, 32, 64, 32, [300, 1, 290], [300, 90, 700], -1, 0, 0, 0),
     "blocks_more_small_pages_window": (80, 40, 64, 16, [330, 200], [330, 650], 150, 10, 0, 0),
     "blocks_more_queries_than_keys": (64, 64, 64, 16, [140, 130], [70, 3], -1, 0, 0, 0),
+    # a decoding step of many streams, whose blocks have few rows each
+    "blocks_one_token_each": (128, 8, 128, 32, [1 - i % 9 // 8 for i in range(150)], [(37 * i) % 200 + 1 for i in range(150)], -1, 0, 1, 0),
+    "blocks_one_token_each_window": (256, 4, 64, 16, [1] * 140, [(53 * i) % 300 + 1 for i in range(140)], 60, 5, 0, 0),
 }
 
 
@@ -403,3 +406,41 @@ def test_refusals_of_the_binding():
         with pytest.raises(P.DfsError):
             P.dfs_paged_attn_fwd(*args)
     assert not o.any() and not lse.any()
+
+
+@pytest.mark.parametrize("cuts", [[150], [90, 60], [140] + [1] * 10], ids=["whole", "two_pieces", "token_by_token"])
+def test_a_prompt_and_its_tokens_in_8_bits(cuts):
+    """Appending and attending, e4m3: each piece against attention in 64 bits over what the pages hold behind its append, whose keys and values are as near to the normed and turned
+    ones (bf16, 2^-8) as 8 bits are: 2^-4 of themselves, and where a scale c has grown half a step of the smallest value at each of the scales on the way, 2^-10 (c + c/2 + ...).
+    Norm and rotation are not the same bits in both calls: each is off by (d + 16) 2^-23 sqrt(2) of a row's largest channel before it is rounded (tests/test_gpu_paged_append.py)."""
+    heads, kv, d, n = 8, 2, 64, 150
+    near = (d + 16) * 2.0 ** -23 * np.sqrt(2) * (1 + 2.0 ** -7)
+    gen = torch.Generator(device="cuda").manual_seed(7)
+    x = torch.randn(n, heads + 2 * kv, d, generator=gen, device="cuda").bfloat16().transpose(0, 1)
+    wq, wk = (1 + 0.2 * torch.randn(d, generator=gen, device="cuda") for _ in range(2))
+    i32 = lambda y: torch.tensor(y, dtype=torch.int32, device="cuda")  # noqa: E731
+    table = np.array([[6, 1, 7, 0, 3, 2]], dtype=np.int32)
+    p = P.Pages(*(torch.zeros(8, kv, 32, d, device="cuda").to(torch.float8_e4m3fn) for _ in range(2)), torch.from_numpy(table).cuda(),
+                *(torch.ones(8, kv, device="cuda") for _ in range(2)))
+    rope = [torch.empty(1, h, n, d, dtype=torch.bfloat16, device="cuda") for h in (heads, kv, kv)]
+    g = P.QkGeom(1, n, heads, kv, d, 0, 1, d, 0, 0, 1e4, 1e-5)
+    P.dfs_qk_norm_rope(g, P.DFS_BF16, x[None, :heads], x[None, heads:heads + kv], x[None, heads + kv:], torch.arange(n, device="cuda", dtype=torch.int32)[:, None], wq, wk, *rope)
+    at = 0
+    for m in cuts:
+        g = P.QkGeom(1, m, heads, kv, d, 0, 1, d, 0, 0, 1e4, 1e-5)
+        part, rows = x[:, at:at + m], torch.empty(heads, m, d, dtype=torch.bfloat16, device="cuda")
+        start, length = i32([0, m]), i32([at + m])
+        P.dfs_paged_append(g, P.DFS_BF16, part[:heads], part[heads:heads + kv], part[heads + kv:], start, length, None, wq, wk, rows, p)
+        want = W._np(rope[0][0, :, at:at + m])
+        assert (np.abs(W._np(rows) - want) <= 2 * (near * np.abs(want).max(-1, keepdims=True) + 2.0 ** -8 * (1 + 2.0 ** -7) * np.abs(want))).all()
+        w = P.Paged(1, heads, kv, d, m, -1, 0)
+        o, lse = _run(w, "bf16", rows, p, start, length, 0.125)
+        at += m
+        _check(w, "bf16", rows, p, [m], [at], 0, table, 0.125, o, lse)
+        with pytest.raises(AssertionError):              # the bounds tell a wrong result
+            _check(w, "bf16", rows, p, [m], [at], 0, table, 0.125, torch.zeros_like(o), lse)
+    of_row = table[0, np.arange(n) // 32]
+    for got, want, scale in zip(_rows(p, table, 0, n), rope[1:], (p.k_scale, p.v_scale)):
+        want, c = W._np(want[0]), W._np(scale)[of_row].T[:, :, None]
+        off = 2 * near * np.abs(want).max(-1, keepdims=True)
+        assert (np.abs(got - want) <= (2.0 ** -4 + 2.0 ** -8 + 2.0 ** -11) * np.abs(want) + (1 + 2.0 ** -4) * off + 2.0 ** -9 * c).all()

@@ -214,6 +214,38 @@ def test_tokens_without_a_place(kind):
         assert torch.equal(_bits(x[int(table[3, 0]), :, 10:]), _bits(y[int(table[3, 0]), :, 10:]))
 
 
+def _guarded(like, mark):
+    """A copy of a tensor with as much room of marks in front of it and behind, as bytes."""
+    bits = _bits(like.contiguous()).flatten()
+    n = (bits.numel() + 4096) // 256 * 256
+    room = torch.full((2 * n + bits.numel(),), mark, dtype=torch.uint8, device="cuda")
+    room[n:-n] = bits
+    return room[n:-n].view(like.dtype).view(like.shape), (room[:n], room[-n:])
+
+
+@pytest.mark.parametrize("kind", list(KINDS))
+@pytest.mark.parametrize("name", ["one_token", "tokens_of_streams", "prompts", "later_pieces", "small_pages", "large_pages", "many_streams", "few_but_two", "few_but_one"])
+def test_starts_that_break_the_format(name, kind):
+    """Starts outside the rows are cut to them; where one falls, nothing in front of or behind the queries' rows, the pages and their scales is touched."""
+    g, code, q, k, v, q_start, k_len, pos, w, p, norm, lens, front, table = _make(name, kind, 5)
+    wide, cut = q_start.clone(), q_start.clone()
+    wide[0], wide[-1], cut[0], cut[-1] = -5, 1 << 30, 0, g.tokens
+    outs, caches = [], []
+    for start in (wide, cut):
+        caches.append(_copy(p))
+        outs.append(torch.full((g.heads, g.tokens, g.d), 9.0, dtype=q.dtype, device="cuda"))
+        P.dfs_paged_append(g, code, q, k, v, start, k_len, pos, w[0], w[1], outs[-1], caches[-1], norm)
+    assert _same(*caches) and torch.equal(*outs) and not (outs[0] == 9).all(-1).any()
+    odd = torch.arange(g.batch + 1, device="cuda") % 2 == 1
+    for start in (q_start.flip(0), torch.where(odd, -q_start, q_start), torch.where(odd, torch.zeros_like(q_start), torch.full_like(q_start, g.tokens + 9))):
+        out, out_room = _guarded(torch.full((g.heads, g.tokens, g.d), 9.0, dtype=q.dtype, device="cuda"), 7)
+        parts = [None if x is None else _guarded(x, 7) for x in (p.k, p.v, p.k_scale, p.v_scale)]
+        here = [None if x is None else x[0] for x in parts]
+        P.dfs_paged_append(g, code, q, k, v, start.int(), k_len, pos, w[0], w[1], out, P.Pages(here[0], here[1], p.table, here[2], here[3]), norm)
+        torch.cuda.synchronize()
+        assert all((x == 7).all() for x in [*out_room] + [y for x in parts if x is not None for y in x[1]])
+
+
 def test_values_that_are_not_finite():
     """e4m3: infinities and NaN are stored as NaN and leave the scale to the others; a page of zeros has the smallest scale."""
     g = P.QkGeom(1, 3, 1, 1, 64, 0, 1, 64, 0, 0, 1e4, 1e-5)
