@@ -341,8 +341,8 @@ template <typename T, int D, bool E4M3, int H> struct Wave16 {
 template <int ROWS, typename T, int D, bool E4M3, int H> struct WaveOf { using type = Wave32<T, D, E4M3, H>; };
 template <typename T, int D, bool E4M3, int H> struct WaveOf<16, T, D, E4M3, H> { using type = Wave16<T, D, E4M3, H>; };
 
-// Bound by memory and by what stands around it: 48 sequences of up to 16 384 keys, 8 key heads, d = 128, e4m3: 201 us of 217, 6.0 TB/s (as fast without the arithmetic; bare loads of
-// this shape: 6.9); one sequence of 80 900 keys: 30 of 42, 5.5 TB/s.  The rest is the join and the way from one launch to the next.  16 sequences that see 1 024 keys each of
+// Bound by memory and by what stands around it: 48 sequences of up to 16 384 keys, 8 key heads, d = 128, e4m3: 209 to 214 us of 218, 5.7 TB/s (as fast without the arithmetic; bare loads of
+// this shape: 6.9); one sequence of 80 900 keys: 31 of 42, 5.4 TB/s.  The rest is the join and the way from one launch to the next.  16 sequences that see 1 024 keys each of
 // bf16 pages of 16 rows, d = 64: 10.3 us, a chain of trips to memory (lengths, table, keys, values) and the waves' join.  Matrix cores busy 7 % of the cycles at most.
 template <int ROWS, typename T, int D, bool E4M3, bool SMALL>
 __global__ void __launch_bounds__((64 * paged_waves<T, D, E4M3>()), 1) paged_split_kernel(PagedArgs a) {

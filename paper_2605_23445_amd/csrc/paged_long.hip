@@ -90,8 +90,8 @@ template <typename T, int D> struct PageFeed {
 };
 
 // Rows in 8 bits: through registers, where they become bf16.  A thread takes 16 bytes of a row.  Bound by the vector port and the matrix cores beside it: 4 096 tokens of four prompts
-// over up to 9 200 keys, 32 heads of 8, d = 128: 536 to 555 us, 860 to 890 TFLOP/s, matrix cores busy 39 % of the cycles.  Making bf16 of the bytes costs 80 of them (467
-// without it, 397 without the loads as well: 1.2 PFLOP/s); blocks of 256 rows, which halve it, take as long, as eight waves then wait for one another.  The writes' bank conflicts
+// over up to 9 200 keys, 32 heads of 8, d = 128: 536 to 574 us as the clock has it (593 to 602 under the profiler, which lowers it), 830 to 890 TFLOP/s, 1.21 million cycles of which the matrix cores
+// are busy 39 %.  Where it took 550, making bf16 of the bytes cost 80 of them (467 without it, 397 without the loads as well: 1.2 PFLOP/s); blocks of 256 rows, which halve it, take as long, as eight waves then wait for one another.  The writes' bank conflicts
 // (an eighth of the LDS's time; none with the halves of every second four lanes swapped, which costs selects) are not what it waits for.
 template <int D> struct ByteFeed {
   static constexpr int STEP = 32, NW = 4;
@@ -174,7 +174,9 @@ template <int D> struct ByteFeed {
 // Blocks of 128 rows, if they were all full, need to be 128 (us, blocks of 128 against keys dealt out; e4m3, d = 128, 8 key heads of 4: 200 tokens of two prompts over 4 000 keys, 50 blocks,
 // 77 / 38; 500, 125, 81 / 70; 256 of sixteen, 64, 86 / 51; bf16, 8 of 8: 256 of 32, 128, 120 / 138; d = 64, 4 of 4: 600 of four over 3 000 keys, 75, 44 / 34;
 // 1 600 over 1 000, 200, 28 / 40; fp32, d = 128, 32 of 8: 600 of four over 2 600, 150, 400 / 461), in fp32 at d = 64, where the others leave fewer rows empty, 256 (600 of four over 2 600, 150,
-// 206 / 124; 5 000 of one x 8, 312, 533 / 529; 2 000 of four over 1 500, 500, 223 / 302).
+// 206 / 124; 5 000 of one x 8, 312, 533 / 529; 2 000 of four over 1 500, 500, 223 / 302).  That the rows lie in many sequences, a few in each, is not looked at: one token of each of 511
+// streams over 1 024 to 8 192 keys, e4m3, 32 heads of 8, takes 853 us, of 512 streams, whose blocks have four rows each, 1 461; and a block's keys are one work-group's, so that a token over
+// 100 000 keys beside a prompt of 2 048 and 126 streams makes a call of 2 408 us, of which the prompt alone takes 56 and the tokens alone 278.
 bool paged_is_long(const dfs_paged* w, int dtype) { return int64_t(w->heads) * w->n_q >= (w->d == 64 && dtype == DFS_F32 ? 256 * 128 : 128 * 128); }
 
 int run_paged_long(const PagedArgs& args, int d, int dtype, bool bytes, hipStream_t st) {
