@@ -4,11 +4,11 @@
 // Bound as these are.  Times of calls differ with the clock that a card grants, cycles do not.  Six causal prompts of 16 384 tokens, 32 heads of 8, d = 128: 402 to 421 us, 0.96 to
 // 1.0 PFLOP/s, 0.77 million cycles of which the matrix cores are busy 52 %; three clips of 24 815 x 30, d = 64, both ways: 1 850 to 1 930 us, 880 to 920 TFLOP/s, 3.5 million, 48 %.
 // Forward and backward of nine causal texts, 8 192 tokens x 32 heads of 8, d = 128: 437 to 471 us, of which under the profiler forward 95 to 99, dq 177 to 184 (39 %), dk and dv 199 to
-// 203 (34 %): blocks meet 1 to 21 tiles of keys, 455 keys a row on average; the search for a block's sequence, the ends of blocks and the diagonal are
-// a part of that.  fp32: 701 tokens
-// of five sequences x 4 heads of 2, d = 64: 11.1 us, a launch and two pieces of keys one after the other; forward and backward of 1 000 tokens of three x 12 of 4: 114 us in five
-// launches.  The forward one, 30 us, has 384 work-groups of 128 KB of LDS, one a CU: two rounds (of the same longest text beside shorter ones, 256 work-groups, 17 us; 384, 26.5).  dq,
-// 39 us, is shared by two only, as a work-group's share is four tiles of keys at least; dk and dv take 36.
+// 203 (34 %): blocks meet 1 to 21 tiles of keys, 455 keys a row on average; the search for a block's sequence, the ends of blocks and the diagonal are a part of that.
+//
+// fp32: 701 tokens of five sequences x 4 heads of 2, d = 64: 11.1 us, a launch and two pieces of keys one after the other; forward and backward of 1 000 tokens of three x 12 of 4: 114
+// us in five launches.  The forward one, 30 us, has 384 work-groups of 128 KB of LDS, one a CU: two rounds (of the same longest text beside shorter ones, 256 work-groups, 17 us; 384,
+// 26.5).  dq, 39 us, is shared by two only, as a work-group's share is four tiles of keys at least; dk and dv take 35.
 #include <math.h>
 
 #include "window_fwd.h"
